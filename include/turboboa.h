@@ -271,6 +271,73 @@ int tboa_dequant_gemv(tboa_ctx* ctx, int d_out, int d_in, int bits, int group, c
                       const float* scales, const float* zeros, const float* x, float* y);
 
 /* ------------------------------------------------------------------------------------------------
+ * Serving with a quantized key/value cache: the setting that tboa_build_hout_q_kv_cache prepares W_Q for.  Forward only; everything is enqueued on the context's stream and nothing
+ * synchronises, so the three calls can be captured into a HIP graph (reserve tboa_kv_cache_attention_workspace_bytes before; a workspace that a captured graph uses is kept until
+ * tboa_destroy even if the context's grows later).  A context's calls and the graphs captured from it share its workspace: they run one after the other, on one stream.
+ *
+ * The cache is one buffer of n_pages pages of tboa_kv_cache_page_bytes(desc) bytes, 16-byte aligned (sizes and offsets of 64 bits).  A page holds page_tokens consecutive tokens of one
+ * sequence for all heads, in this order:
+ *   levels of K  uint8 [n_kv_heads][page_tokens][dp]            dp: head_dim rounded up to 32, 64, 96, 128, 192 or 256 (what is beyond head_dim is neither read as a number nor written)
+ *   levels of V  uint8 [n_kv_heads][page_tokens / 16][dp][16]   the 16 tokens of a channel side by side
+ *   grids of K, then of V  fp32 [n_kv_heads][page_tokens / scale_tokens][2]: scale, zero of a head's block of scale_tokens tokens
+ * and level c stands for scale * (c - zero).  Pages need not be cleared before use: no token beyond a sequence's length is read as a number. */
+typedef struct {
+    int n_kv_heads;     /* 1 .. 65535 */
+    int head_dim;       /* 1 .. 256 */
+    int page_tokens;    /* power of two, 16 .. 1024 */
+    int scale_tokens;   /* power of two, 1 .. page_tokens; 1: a grid per token and head */
+    int64_t n_pages;
+} tboa_kv_cache_desc;
+/* A ragged batch.  Rows starts[b] .. starts[b+1] - 1 of K, V, Q, O are the new tokens of sequence b, which has lens[b] tokens WITH them (they are its last ones); its token at place p is in page
+ * pages[b * pages_per_seq + p / page_tokens].  Any number of new tokens per sequence, 0 included; rows beyond starts[n_seqs] are left alone.  Sequences may share pages that no append
+ * of the same call writes.  What the device arrays hold is not checked on the host.  On the device: rows beyond n_tokens and places beyond the row of pages are left out, a page
+ * outside 0 .. n_pages - 1 takes nothing in and is invisible to attention, and tokens before place 0 (lens[b] smaller than the number of new tokens) get no place and see nothing. */
+typedef struct {
+    int n_seqs, pages_per_seq;
+    int64_t n_tokens;           /* rows of K, V, Q, O: at most 2^24 */
+    const int* starts;          /* device [n_seqs + 1], from 0, not falling */
+    const int* lens;            /* device [n_seqs] */
+    const int* pages;           /* device [n_seqs][pages_per_seq]; pages_per_seq * page_tokens <= 2^30 */
+    int max_new;                /* most new tokens of a sequence, or 0: not known.  Chooses between kernels, never changes what is computed */
+} tboa_kv_batch;
+/* Rotation of the first rot_dim channels of a head vector: pair i, channels (i, rot_dim/2 + i) or with `adjacent` (2i, 2i+1), (a, b) -> (a cos - b sin, b cos + a sin), with
+ * cos = cos_sin[p][i], sin = cos_sin[p][rot_dim/2 + i] for position p.  A position outside the table gives NaN. */
+typedef struct {
+    int rot_dim, adjacent;      /* rot_dim even, 0: no rotation */
+    int64_t n_positions;
+    const float* cos_sin;       /* device [n_positions][rot_dim] */
+} tboa_rotation;
+
+size_t tboa_kv_cache_page_bytes(const tboa_kv_cache_desc* desc);      /* host value, no context needed; 0 for an invalid descriptor */
+
+/* Norms of the query and key vectors of every head, and their rotation, in one pass:  y = x / sqrt(mean(x^2) + eps) * w, rotated.
+ *   Q [n_tokens][n_q_heads * head_dim], K likewise, in `dtype` (TBOA_F32 or TBOA_BF16), rows ldq, ldk elements apart; Q_out, K_out likewise (each may be its input); either side may have no heads
+ *   w_q, w_k  fp32 [head_dim], or NULL: that side is not normalised
+ *   rotation  NULL: none; positions  device [n_tokens] (needed with a rotation)
+ * Sums of squares in fp64, everything else in fp32, one rounding at the end. */
+int tboa_head_norm_rotate(tboa_ctx* ctx, int64_t n_tokens, int head_dim, int dtype, int n_q_heads, const void* Q, int64_t ldq, const float* w_q,
+                          int n_k_heads, const void* K, int64_t ldk, const float* w_k, double eps, const tboa_rotation* rotation, const int* positions,
+                          void* Q_out, int64_t ldq_out, void* K_out, int64_t ldk_out);
+
+/* New keys and values into the cache, the keys rotated on the way (rotation NULL: not; positions NULL: a token's place in its sequence).
+ *   K, V [n_tokens][n_kv_heads * head_dim] in `dtype`, rows ldk, ldv elements apart
+ * Min-Max quantizer of tboa_act_fakequant at 8 bits, per head and block of scale_tokens tokens, decided in fp64 on the unrounded rotated values: with lo, hi the ends of the block's values and 0
+ * (-1, 1 where all are 0), scale = (hi - lo) / 255 rounded to fp32, zero = round(-lo / scale), level = clamp(round(v / scale) + zero, 0, 255).
+ * A block that had tokens before the call keeps its grid while every new value lies at most 9/16 of a step beyond its ends; otherwise lo and hi also take in the ends
+ * -zero * scale and (255 - zero) * scale of the old grid, and the earlier levels are rounded to the new one (half a new step each time; a block that comes whole has none of it).
+ * A NaN or infinity among a block's values makes its scale NaN, and so every value of the block, for good.  Pages that the call writes belong to one sequence each. */
+int tboa_kv_cache_append(tboa_ctx* ctx, const tboa_kv_cache_desc* desc, const tboa_kv_batch* batch, int dtype, const void* K, int64_t ldk,
+                         const void* V, int64_t ldv, const tboa_rotation* rotation, const int* positions, void* cache);
+
+/* O[i, h] = sum_t A[t] v_t, A = softmax over t of scale * q_{i,h} . k_t, with k, v of KV head h / (n_q_heads / n_kv_heads) from the cache, t over the places of row i's sequence up to its own
+ * (and, with window > 0, the last `window` of them, its own included).  Rows that see nothing get 0.
+ *   Q, O [n_tokens][n_q_heads * head_dim] in `dtype`, rows ldq, ldo elements apart; scale 0: 1/sqrt(head_dim).  n_tokens * (n_q_heads / n_kv_heads) <= 2^30
+ * Levels enter the products exactly.  TBOA_BF16: q as it is, probabilities times scale rounded to 11 bits, fp32 sums; TBOA_F32: both as pairs of 11 bits. */
+size_t tboa_kv_cache_attention_workspace_bytes(const tboa_kv_cache_desc* desc, int n_q_heads, int n_seqs, int64_t n_tokens);
+int tboa_kv_cache_attention(tboa_ctx* ctx, const tboa_kv_cache_desc* desc, const tboa_kv_batch* batch, int n_q_heads, int dtype, const void* Q, int64_t ldq,
+                            const void* cache, double scale, int window, void* O, int64_t ldo);
+
+/* ------------------------------------------------------------------------------------------------
  * Building blocks, exported for stage-isolated checks and for roofline measurement.
  */
 

@@ -39,6 +39,19 @@ class LayerDesc(C.Structure):
                 ("max_shrink", C.c_double), ("damp", C.c_double), ("grid_guard", C.c_double)]
 
 
+class KVCacheDesc(C.Structure):
+    _fields_ = [("n_kv_heads", C.c_int), ("head_dim", C.c_int), ("page_tokens", C.c_int), ("scale_tokens", C.c_int), ("n_pages", C.c_int64)]
+
+
+class KVBatchDesc(C.Structure):
+    _fields_ = [("n_seqs", C.c_int), ("pages_per_seq", C.c_int), ("n_tokens", C.c_int64), ("starts", C.c_void_p), ("lens", C.c_void_p), ("pages", C.c_void_p),
+                ("max_new", C.c_int)]
+
+
+class RotationDesc(C.Structure):
+    _fields_ = [("rot_dim", C.c_int), ("adjacent", C.c_int), ("n_positions", C.c_int64), ("cos_sin", C.c_void_p)]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError("libturboboa.so is not built (run `python -c 'import __graft_entry__ as g; g.build()'`): "
@@ -76,6 +89,11 @@ def _load():
         "tboa_pack_codes": ([vp, i32, i32, i32, vp, vp], i32),
         "tboa_dequant_gemv": ([vp, i32, i32, i32, i32, vp, vp, vp, vp, vp], i32),
         "tboa_quantize_layer": ([vp, C.POINTER(LayerDesc)] + [vp] * 8 + [C.POINTER(f64), C.POINTER(f64)], i32),
+        "tboa_kv_cache_page_bytes": ([C.POINTER(KVCacheDesc)], C.c_size_t),
+        "tboa_head_norm_rotate": ([vp, i64, i32, i32, i32, vp, i64, vp, i32, vp, i64, vp, f64, C.POINTER(RotationDesc), vp, vp, i64, vp, i64], i32),
+        "tboa_kv_cache_append": ([vp, C.POINTER(KVCacheDesc), C.POINTER(KVBatchDesc), i32, vp, i64, vp, i64, C.POINTER(RotationDesc), vp, vp], i32),
+        "tboa_kv_cache_attention_workspace_bytes": ([C.POINTER(KVCacheDesc), i32, i32, i64], C.c_size_t),
+        "tboa_kv_cache_attention": ([vp, C.POINTER(KVCacheDesc), C.POINTER(KVBatchDesc), i32, i32, vp, i64, vp, f64, i32, vp, i64], i32),
         "tboa_counter": ([vp, i32], i64),
         "tboa_profile_enable": ([vp, i32], i32),
         "tboa_profile_reset": ([vp], i32),
@@ -108,6 +126,59 @@ def _dev(t, dtype=None):
     if dtype is not None:
         assert t.dtype == dtype, "expected %s, got %s" % (dtype, t.dtype)
     return t
+
+
+def _rows(t, heads, head_dim, dtype):
+    """Row pitch of a tensor [tokens, heads, head_dim] whose rows may be pitched (a view of a wider tensor)."""
+    assert t.is_cuda and t.dtype == dtype and t.dim() == 3 and t.shape[1:] == (heads, head_dim), "expected %s [tokens, %d, %d], got %s %s" % (dtype, heads, head_dim, t.dtype, tuple(t.shape))
+    assert t.stride(2) == 1 or head_dim == 1, "channels of a head must be contiguous"
+    assert t.stride(1) == head_dim or heads == 1, "heads of a token must be contiguous"
+    return t.stride(0) if t.shape[0] > 1 else heads * head_dim
+
+
+class Rotation:
+    """Table of a rotation by position: fp32 [positions, rot_dim], a row holding the cosines and then the sines of its rot_dim / 2 pairs; adjacent: pairs (2i, 2i+1)
+    instead of (i, rot_dim/2 + i)."""
+
+    def __init__(self, cos_sin, adjacent=False):
+        _dev(cos_sin, torch.float32)
+        assert cos_sin.dim() == 2
+        self.cos_sin, self.desc = cos_sin, RotationDesc(cos_sin.shape[1], int(adjacent), cos_sin.shape[0], cos_sin.data_ptr())
+
+
+class KVCache:
+    """A quantized key/value cache: uint8 `data` [n_pages, page_bytes] (see tboa_kv_cache_desc for what a page holds)."""
+
+    def __init__(self, data, n_kv_heads, head_dim, page_tokens=64, scale_tokens=1):
+        self.desc = KVCacheDesc(n_kv_heads, head_dim, page_tokens, scale_tokens, data.shape[0])
+        _dev(data, torch.uint8)
+        assert data.dim() == 2 and data.shape[1] == self.page_bytes(n_kv_heads, head_dim, page_tokens, scale_tokens), "data is %s" % (tuple(data.shape),)
+        self.data = data
+
+    @staticmethod
+    def page_bytes(n_kv_heads, head_dim, page_tokens=64, scale_tokens=1):
+        n = int(_lib.tboa_kv_cache_page_bytes(C.byref(KVCacheDesc(n_kv_heads, head_dim, page_tokens, scale_tokens, 0))))
+        assert n > 0, "no cache has %d heads of %d channels, pages of %d and scales of %d tokens" % (n_kv_heads, head_dim, page_tokens, scale_tokens)
+        return n
+
+    @classmethod
+    def empty(cls, n_pages, n_kv_heads, head_dim, page_tokens=64, scale_tokens=1, device="cuda"):
+        data = torch.empty(n_pages, cls.page_bytes(n_kv_heads, head_dim, page_tokens, scale_tokens), dtype=torch.uint8, device=device)
+        return cls(data, n_kv_heads, head_dim, page_tokens, scale_tokens)
+
+
+class KVBatch:
+    """New tokens of a ragged batch (see tboa_kv_batch): int32 starts [n_seqs + 1], lens [n_seqs], pages [n_seqs, pages_per_seq] on the device.
+    max_new: most new tokens of a sequence where the caller knows it (chooses between kernels only)."""
+
+    def __init__(self, starts, lens, pages, max_new=0):
+        for t in (starts, lens, pages):
+            _dev(t, torch.int32)
+        assert pages.dim() == 2 and lens.shape == (pages.shape[0],) and starts.shape == (pages.shape[0] + 1,), "starts %s, lens %s, pages %s" % tuple(tuple(t.shape) for t in (starts, lens, pages))
+        self.starts, self.lens, self.pages, self.max_new = starts, lens, pages, max_new
+
+    def desc(self, n_tokens):
+        return KVBatchDesc(self.pages.shape[0], self.pages.shape[1], n_tokens, self.starts.data_ptr(), self.lens.data_ptr(), self.pages.data_ptr(), self.max_new)
 
 
 class Context:
@@ -363,6 +434,66 @@ class Context:
         out = torch.empty(*X.shape[:-1], d_out, dtype=X.dtype, device=X.device)
         self._check(_lib.tboa_linear_forward(self._h, X.numel() // d_in, d_in, d_out, _dtype_code(X), _ptr(X), _dtype_code(W), _ptr(W),
                                              _ptr(residual), _ptr(out)))
+        return out
+
+    # ---- serving with a quantized key/value cache
+    def _used(self, *tensors):
+        """Memory of tensors that another stream than the context's allocated is not given away before the context's work is done."""
+        for t in tensors:
+            if t is not None:
+                assert t.device.index == (self.device.index or 0), "a tensor of %s, the context's device is %s" % (t.device, self.device)
+        if torch.cuda.current_stream(self.device) != self._stream:
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(self._stream)
+
+    def head_norm_rotate(self, Q, K=None, wq=None, wk=None, eps=1e-6, rotation=None, positions=None, out_q=None, out_k=None):
+        """Norms of head vectors (wq, wk: fp32 [head_dim] or None, not normalised) and their rotation at int32 positions [tokens]; Q [tokens, heads, head_dim], K likewise or None, rows
+        may be pitched.  Returns (Q', K'); out_q, out_k may be the inputs."""
+        T, Hq, dh = Q.shape
+        ldq, Hk, ldk, ldko = _rows(Q, Hq, dh, Q.dtype), 0, 0, 0
+        out_q = torch.empty(T, Hq, dh, dtype=Q.dtype, device=Q.device) if out_q is None else out_q
+        if K is not None:
+            Hk = K.shape[1]
+            assert K.shape[0] == T, "%d rows of K, %d of Q" % (K.shape[0], T)
+            ldk = _rows(K, Hk, dh, Q.dtype)
+            out_k = torch.empty(T, Hk, dh, dtype=K.dtype, device=K.device) if out_k is None else out_k
+            assert out_k.shape[0] == T
+            ldko = _rows(out_k, Hk, dh, Q.dtype)
+        assert out_q.shape[0] == T
+        for w in (wq, wk):
+            assert w is None or _dev(w, torch.float32).shape == (dh,), "weights of a norm: fp32 [%d]" % dh
+        assert rotation is None or (positions is not None and _dev(positions, torch.int32).shape == (T,)), "positions: int32 [%d]" % T
+        self._used(Q, K, wq, wk, positions, out_q, out_k, rotation and rotation.cos_sin)
+        self._check(_lib.tboa_head_norm_rotate(self._h, T, dh, _dtype_code(Q), Hq, _ptr(Q), ldq, _ptr(wq), Hk, _ptr(K), ldk, _ptr(wk), eps, rotation and C.byref(rotation.desc),
+                                               _ptr(positions), _ptr(out_q), _rows(out_q, Hq, dh, Q.dtype), _ptr(out_k), ldko))
+        return out_q, out_k
+
+    def kv_cache_append(self, cache, batch, K, V, rotation=None, positions=None):
+        """New keys (rotated at their place in the sequence, or at int32 positions [tokens]) and values [tokens, n_kv_heads, head_dim] into the cache."""
+        d, T = cache.desc, K.shape[0]
+        assert V.shape[0] == T, "%d rows of V, %d of K" % (V.shape[0], T)
+        ldk, ldv = _rows(K, d.n_kv_heads, d.head_dim, K.dtype), _rows(V, d.n_kv_heads, d.head_dim, K.dtype)
+        assert positions is None or _dev(positions, torch.int32).shape == (T,), "positions: int32 [%d]" % T
+        self._used(cache.data, K, V, positions, batch.starts, batch.lens, batch.pages, rotation and rotation.cos_sin)
+        self._check(_lib.tboa_kv_cache_append(self._h, C.byref(d), C.byref(batch.desc(T)), _dtype_code(K), _ptr(K), ldk, _ptr(V), ldv, rotation and C.byref(rotation.desc),
+                                              _ptr(positions), _ptr(cache.data)))
+
+    @staticmethod
+    def kv_cache_attention_workspace_bytes(cache, n_q_heads, n_seqs, n_tokens):
+        return int(_lib.tboa_kv_cache_attention_workspace_bytes(C.byref(cache.desc), n_q_heads, n_seqs, n_tokens))
+
+    def kv_cache_attention(self, cache, batch, Q, scale=0.0, window=0, out=None):
+        """Causal attention of the batch's new tokens Q [tokens, n_q_heads, head_dim] over the cache (their own keys and values included: append first).  scale 0: 1/sqrt(head_dim);
+        window > 0: a token sees the last `window` ones.  Rows behind the last sequence are not written."""
+        d, (T, Hq, _) = cache.desc, Q.shape
+        ldq = _rows(Q, Hq, d.head_dim, Q.dtype)
+        if out is None:
+            out = torch.empty(T, Hq, d.head_dim, dtype=Q.dtype, device=Q.device)
+        assert out.shape[0] == T
+        self._used(cache.data, Q, out, batch.starts, batch.lens, batch.pages)
+        self._check(_lib.tboa_kv_cache_attention(self._h, C.byref(d), C.byref(batch.desc(T)), Hq, _dtype_code(Q), _ptr(Q), ldq, _ptr(cache.data), scale, window,
+                                                 _ptr(out), _rows(out, Hq, d.head_dim, Q.dtype)))
         return out
 
     def pack_codes(self, codes, bits):

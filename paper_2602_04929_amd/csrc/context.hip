@@ -11,10 +11,23 @@ int tboa_fail(tboa_ctx* ctx, int code, const char* fmt, ...) {
     return code;
 }
 
+static bool capturing(tboa_ctx* ctx) {
+    hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(ctx->stream, &st) != hipSuccess) { (void)hipGetLastError(); return false; }
+    return st == hipStreamCaptureStatusActive;
+}
+
+int tboa_ws_in_graph(tboa_ctx* ctx) {
+    if (ctx->ws && !ctx->ws_in_graph && capturing(ctx)) ctx->ws_in_graph = true;
+    return 0;
+}
+
 int tboa_ws_reserve(tboa_ctx* ctx, size_t bytes) {
     if (ctx->plan_only) { if (bytes > ctx->plan_bytes) ctx->plan_bytes = bytes; if (bytes > ctx->plan_plain) ctx->plan_plain = bytes; return TB_PLAN_STOP; }
     if (bytes <= ctx->ws_bytes) return 0;
+    if (capturing(ctx)) return tboa_fail(ctx, TBOA_ENOMEM, "workspace of %zu bytes: nothing can be allocated while the stream is captured, reserve it before", bytes);
     TB_HIP(ctx, hipStreamSynchronize(ctx->stream));
+    if (ctx->ws && ctx->ws_in_graph) { ctx->ws_kept.push_back(ctx->ws); ctx->ws = nullptr; ctx->ws_bytes = 0; ctx->ws_in_graph = false; }
     const size_t had = ctx->ws_bytes;
     if (ctx->ws) { TB_HIP(ctx, hipFree(ctx->ws)); ctx->ws = nullptr; ctx->ws_bytes = 0; }
     hipError_t e = hipMalloc(&ctx->ws, bytes);
@@ -147,6 +160,7 @@ extern "C" void tboa_destroy(tboa_ctx* ctx) {
     for (auto& t : ctx->tile_orders) (void)hipFree(t.dev);
     for (auto& t : ctx->tile_schedules) (void)hipFree(t.dev);
     if (ctx->ws) (void)hipFree(ctx->ws);
+    for (void* p : ctx->ws_kept) (void)hipFree(p);
     if (ctx->splitk[0]) (void)hipFree(ctx->splitk[0]);
     if (ctx->d_status) (void)hipFree(ctx->d_status);
     if (ctx->h_status) (void)hipHostFree(ctx->h_status);
