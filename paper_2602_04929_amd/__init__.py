@@ -13,5 +13,7 @@ def __getattr__(name):
     if name in _BINDING_NAMES or name == "binding":
         import importlib
         binding = importlib.import_module(__name__ + ".binding")
-        return binding if name == "binding" else getattr(binding, name)
+        value = binding if name == "binding" else getattr(binding, name)
+        globals()[name] = value      # the next access does not come here
+        return value
     raise AttributeError(name)

@@ -130,10 +130,10 @@ def _dev(t, dtype=None):
 
 def _rows(t, heads, head_dim, dtype):
     """Row pitch of a tensor [tokens, heads, head_dim] whose rows may be pitched (a view of a wider tensor)."""
-    assert t.is_cuda and t.dtype == dtype and t.dim() == 3 and t.shape[1:] == (heads, head_dim), "expected %s [tokens, %d, %d], got %s %s" % (dtype, heads, head_dim, t.dtype, tuple(t.shape))
-    assert t.stride(2) == 1 or head_dim == 1, "channels of a head must be contiguous"
-    assert t.stride(1) == head_dim or heads == 1, "heads of a token must be contiguous"
-    return t.stride(0) if t.shape[0] > 1 else heads * head_dim
+    (n, h, d), (pitch, sh, sd) = t.shape, t.stride()
+    assert t.is_cuda and t.dtype is dtype and h == heads and d == head_dim, "expected %s [tokens, %d, %d], got %s %s" % (dtype, heads, head_dim, t.dtype, tuple(t.shape))
+    assert (sd == 1 or d == 1) and (sh == d or h == 1), "a token's heads and a head's channels must be contiguous"
+    return pitch if n > 1 else h * d
 
 
 class Rotation:
@@ -175,10 +175,13 @@ class KVBatch:
         for t in (starts, lens, pages):
             _dev(t, torch.int32)
         assert pages.dim() == 2 and lens.shape == (pages.shape[0],) and starts.shape == (pages.shape[0] + 1,), "starts %s, lens %s, pages %s" % tuple(tuple(t.shape) for t in (starts, lens, pages))
-        self.starts, self.lens, self.pages, self.max_new = starts, lens, pages, max_new
+        self.starts, self.lens, self.pages = starts, lens, pages
+        self._desc = KVBatchDesc(pages.shape[0], pages.shape[1], 0, starts.data_ptr(), lens.data_ptr(), pages.data_ptr(), max_new)
 
     def desc(self, n_tokens):
-        return KVBatchDesc(self.pages.shape[0], self.pages.shape[1], n_tokens, self.starts.data_ptr(), self.lens.data_ptr(), self.pages.data_ptr(), self.max_new)
+        d = KVBatchDesc.from_buffer_copy(self._desc)
+        d.n_tokens = n_tokens
+        return d
 
 
 class Context:
@@ -188,7 +191,7 @@ class Context:
         dev = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
         self.device = dev
         st = torch.cuda.current_stream(dev) if stream is None else stream
-        self._stream = st
+        self._stream, self._raw_stream = st, st.cuda_stream
         h = C.c_void_p()
         rc = _lib.tboa_create(C.byref(h), dev.index or 0, C.c_void_p(st.cuda_stream))
         if rc != 0:
@@ -439,10 +442,10 @@ class Context:
     # ---- serving with a quantized key/value cache
     def _used(self, *tensors):
         """Memory of tensors that another stream than the context's allocated is not given away before the context's work is done."""
+        here = self.device.index or 0
         for t in tensors:
-            if t is not None:
-                assert t.device.index == (self.device.index or 0), "a tensor of %s, the context's device is %s" % (t.device, self.device)
-        if torch.cuda.current_stream(self.device) != self._stream:
+            assert t is None or t.get_device() == here, "a tensor of %s, the context's device is %s" % (t.device, self.device)
+        if torch._C._cuda_getCurrentRawStream(here) != self._raw_stream:
             for t in tensors:
                 if t is not None:
                     t.record_stream(self._stream)

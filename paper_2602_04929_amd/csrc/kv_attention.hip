@@ -50,34 +50,23 @@ struct AttendArgs {
     const void* Q; long long ldq; void* O; long long ldo;
     const unsigned char* cache;
     float scale2;                 // scale log2 e
-    int rep, window, target;      // target: items that fill the chip
-    long long items;              // room in part and stat
-    float* part; float2* stat;    // per item, head and row: unscaled outputs; maximum, sum
+    int rep, window, vec;         // vec: 16-byte pieces of Q
+    int4* info;                   // per workgroup: the unit that begins in its share and ends in another: workgroups, first row of the sequence, row of the first | rows << 27, head
+    float* part; float2* stat;    // per workgroup two pieces of 16 rows (of a unit that began before its share, of one that begins in it): unscaled outputs; maximum, sum
 };
 
 constexpr float HALF_TOP = 0x1p14f;      // what a probability of 1 with the largest scale becomes as half, at most: parts of 2^-28 of it are still normal numbers
-constexpr int ROWS = 16, TILE = 64;      // rows (query token, head of the group) of an item, tokens a wavefront takes at a time
+constexpr int ROWS = 16, TILE = 64;      // rows (query token, head of the group) of a unit, tokens a wavefront takes at a time
+// workgroups that a compute unit holds at once (registers): the shares that the work is cut into are 256 times as many
+template <int DP> constexpr int resident() { return DP <= 64 ? 3 : DP <= 128 ? 2 : 1; }
 
-// how a sequence is cut: row tiles, tokens that its rows see
+// how a sequence is cut: row tiles, tiles of tokens that its rows see
 __device__ __forceinline__ int row_tiles(const KvSeq& s, int rep) { return (int)(((long long)s.n * rep + ROWS - 1) / ROWS); }
 __device__ __forceinline__ int seen_tiles(const KvSeq& s, const AttendArgs& a) {
     const int end = min(s.len, a.q.room);
-    return s.n == 0 ? 0 : (min(end, a.window ? (int)min((long long)a.window + s.n + TILE, 2147483647LL) : end) + TILE - 1) / TILE;
+    return s.n == 0 ? 0 : max((min(end, a.window ? (int)min((long long)a.window + s.n + TILE, 2147483647LL) : end) + TILE - 1) / TILE, 1);
 }
-// tiles of TILE tokens that an item takes at least, so that all items are about `target`; a multiple of the four wavefronts
-__device__ __forceinline__ int item_tiles(const AttendArgs& a) {
-    const int lane = threadIdx.x & 63;
-    long long total = 0;
-    for (int b = lane; b < a.q.n_seqs; b += 64) {
-        const KvSeq s = kv_sequence(a.q, b);
-        total += (long long)row_tiles(s, a.rep) * seen_tiles(s, a);
-    }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) total += __shfl_xor(total, o, 64);
-    const long long c = (total * a.g.heads + a.target - 1) / a.target;
-    return (int)min(max((c + 3) / 4 * 4, 4LL), 1LL << 26);
-}
-__device__ __forceinline__ int cuts(const KvSeq& s, const AttendArgs& a, int per) { return max((seen_tiles(s, a) + per - 1) / per, 1); }
+__device__ __forceinline__ long long unit_tiles(const KvSeq& s, const AttendArgs& a) { return (long long)row_tiles(s, a.rep) * seen_tiles(s, a) * a.g.heads; }
 
 // tokens that rows r0 .. of a sequence see
 struct Span { int lo, hi; };
@@ -86,284 +75,334 @@ __device__ __forceinline__ Span row_span(const KvSeq& s, const AttendArgs& a, in
     return Span{a.window ? max(p0 - a.window + 1, 0) : 0, max(min(p1 + 1, a.q.room), 0)};
 }
 
-// One workgroup per item (16 rows of a sequence's query tokens and the heads of a KV group, a piece of the tokens they see) and KV head; its four wavefronts take every fourth tile of 64
-// tokens and are joined through LDS at the end.  S^T = K Q^T with tile i's row 4 g + j of the matrix instruction being token 16 g + 4 i + j: lane group g then holds the probabilities of
-// tokens 16 g .. 16 g + 15 for row lane % 16, which are the right operand of O^T += V^T P^T as they stand.
+// Units (16 rows of a sequence's query tokens and the heads of a KV group, all tokens that they see) follow each other as a list of tiles of 64 tokens, and every workgroup takes an equal
+// share of that list, wherever units begin and end; its four wavefronts take every fourth tile and are joined through LDS.  A unit that lies in one share is finished there, pieces of the others go to
+// kv_attend_join_kernel.  S^T = K Q^T with tile i's row 4 g + j of the matrix instruction being token 16 g + 4 i + j: lane group g then holds the probabilities of tokens 16 g .. 16 g + 15
+// for row lane % 16, which are the right operand of O^T += V^T P^T as they stand.  The loads of V's tile are in flight while its scores are formed, those of K's next one while it is multiplied.
 template <typename T, int DP>
-__global__ __launch_bounds__(256) void kv_attend_rows_kernel(AttendArgs a) {
+__global__ __launch_bounds__(256, resident<DP>()) void kv_attend_rows_kernel(AttendArgs a) {
     constexpr int NT = sizeof(T) == 2 ? 1 : 2;      // half terms of queries and probabilities
     constexpr int K64 = DP / 64, K32 = (DP % 64) / 32, KS = DP / 32, CT = DP / 16;
     __shared__ float joined[4][ROWS][DP + 4];
     __shared__ float2 ends[4][ROWS];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, grp = lane >> 4, h = blockIdx.y;
-    const int per = item_tiles(a);
-    int x = blockIdx.x, b;
-    KvSeq s;
-    if (!kv_find(a.q, [&](const KvSeq& e) { return e.n ? (int)min((long long)row_tiles(e, a.rep) * cuts(e, a, per), 1LL << 30) : 0; }, x, b, s)) return;
-    const int n_cuts = cuts(s, a, per), r0 = x / n_cuts * ROWS, cut = x % n_cuts, n_rows = (int)min((long long)ROWS, (long long)s.n * a.rep - r0);
-    const Span span = row_span(s, a, r0, n_rows);
-    int lo, hi;
-    {
-        const int t0 = span.lo / TILE, t1 = (span.hi + TILE - 1) / TILE, each = max((t1 - t0 + n_cuts - 1) / n_cuts, 0);
-        lo = (t0 + cut * each) * TILE; hi = min((t0 + (cut + 1) * each) * TILE, span.hi);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, grp = lane >> 4;
+    KvSeq head{0, 0, 0};
+    long long total = 0;
+    for (int i = lane; i < a.q.n_seqs; i += 64) {
+        const KvSeq e = kv_sequence(a.q, i);
+        if (i < 64) head = e;
+        total += unit_tiles(e, a);
     }
-    // this lane's row
-    const bool row_live = col < n_rows;
-    const int r = r0 + (row_live ? col : 0), pos = row_live ? s.len - s.n + r / a.rep : -1, low = a.window ? pos - a.window + 1 : 0;
-    h8 qh[NT][KS];
-    float unit;
-    {
-        const T* q = (const T*)a.Q + (long long)(s.start + r / a.rep) * a.ldq + (long long)(h * a.rep + r % a.rep) * a.g.dh;
-        float v[KS][8], most = 0.f;
 #pragma unroll
-        for (int k = 0; k < KS; ++k)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int c = k < 2 * K64 ? (k >> 1) * 64 + grp * 16 + (k & 1) * 8 + j : K64 * 64 + grp * 8 + j;
-                v[k][j] = row_live && c < a.g.dh ? to_f32(q[c]) : 0.f;
-                const float m = fabsf(v[k][j]);
-                most = m < __builtin_inff() ? fmaxf(most, m) : most;
-            }
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) most = fmaxf(most, __shfl_xor(most, o, 64));
-        int e = 0;
-        if (most > 0.f) { frexpf(most, &e); e = min(14 - e, 100); }
-        unit = ldexpf(a.scale2, -e);
-#pragma unroll
-        for (int k = 0; k < KS; ++k)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float w = ldexpf(v[k][j], e);
-                const _Float16 hi16 = (_Float16)w;
-                qh[0][k][j] = hi16;
-                if constexpr (NT == 2) qh[1][k][j] = (_Float16)(isfinite(w) ? w - (float)hi16 : 0.f);
-            }
-    }
+    for (int o = 1; o < 64; o <<= 1) total += __shfl_xor(total, o, 64);
+    total = (long long)(unsigned)__builtin_amdgcn_readfirstlane((int)total) | (long long)__builtin_amdgcn_readfirstlane((int)(total >> 32)) << 32;
+    const long long share = max((total + gridDim.x - 1) / gridDim.x, 4LL);      // (four: a tile for each wavefront)
+    long long at = blockIdx.x * share;
+    const long long at_end = min(at + share, total);
+    if (threadIdx.x == 0) a.info[blockIdx.x] = make_int4(0, 0, 0, 0);
+    while (at < at_end) {
+        long long x = at;
+        int b, h, k0, tile;
+        KvSeq s;
+        if (!kv_find(a.q, head, [&](const KvSeq& e) { return unit_tiles(e, a); }, x, b, s)) return;
+        const int tiles = seen_tiles(s, a);
+        if (x >> 31) { k0 = (int)(x % tiles); x /= tiles; h = (int)(x % a.g.heads); tile = (int)(x / a.g.heads); }
+        else { const unsigned u = (unsigned)x / tiles; k0 = (unsigned)x - u * tiles; tile = u / a.g.heads; h = u - tile * a.g.heads; }
+        h = __builtin_amdgcn_readfirstlane(h); k0 = __builtin_amdgcn_readfirstlane(k0); tile = __builtin_amdgcn_readfirstlane(tile);
+        const int k1 = (int)min((long long)tiles, k0 + (at_end - at));      // tiles k0 .. k1 - 1 of the unit
+        const int r0 = tile * ROWS, n_rows = (int)min((long long)ROWS, (long long)s.n * a.rep - r0);
+        const Span span = row_span(s, a, r0, n_rows);
+        const int lo = (span.lo / TILE + k0) * TILE, hi = min((span.lo / TILE + k1) * TILE, span.hi);
+        // this lane's row
+        const bool row_live = col < n_rows;
+        const int r = r0 + (row_live ? col : 0), tok = r / a.rep, pos = row_live ? s.len - s.n + tok : -1, low = a.window ? pos - a.window + 1 : 0;
+        const T* const q = (const T*)a.Q + (long long)(s.start + tok) * a.ldq + (long long)(h * a.rep + r - tok * a.rep) * a.g.dh;
+        const int end = min(s.len, a.q.room);
+        const long long head_levels = (long long)h * DP << a.g.pt_log, head_grids = (long long)h << (a.g.pt_log - a.g.st_log);
+        const int in_page = (1 << a.g.pt_log) - 1;
+        const int* const pages = a.q.pages + (long long)b * a.q.per_seq;
 
-    float m = -__builtin_inff(), l = 0.f, ref = 0x1p-126f;
-    f4 o[CT];
-#pragma unroll
-    for (int c = 0; c < CT; ++c) o[c] = f4{0.f, 0.f, 0.f, 0.f};
-
-    const int end = min(s.len, a.q.room);
-    const long long head_levels = (long long)h * DP << a.g.pt_log, head_grids = (long long)h << (a.g.pt_log - a.g.st_log);
-    const int in_page = (1 << a.g.pt_log) - 1;
-    const int* const pages = a.q.pages + (long long)b * a.q.per_seq;
-    for (int t0 = lo + wave * TILE; t0 < hi; t0 += 4 * TILE) {
-        const int tk = t0 + 16 * (col >> 2), tv = t0 + 16 * grp;      // 16 tokens that this lane takes levels of K, of V from
-        const int pk = pages[min(tk >> a.g.pt_log, a.q.per_seq - 1)], pv = pages[min(tv >> a.g.pt_log, a.q.per_seq - 1)];
-        const bool held = pv >= 0 && pv < a.g.n_pages;
-        const unsigned char* const kp = a.cache + (long long)min(max(pk, 0), (int)a.g.n_pages - 1) * a.g.page_bytes;
-        const unsigned char* const vp = a.cache + (long long)(held ? pv : 0) * a.g.page_bytes;
-        const unsigned char* const kb = kp + head_levels + (long long)((tk & in_page) + (col & 3)) * DP + grp * 16;
-        const unsigned char* const vb = vp + a.g.v_at + head_levels + (long long)(tv & in_page) * DP + col * 16;
+        // page of the 16 tokens that this lane takes levels of K from, of V from
+        auto page_of = [&](int t) { return pages[min(t >> a.g.pt_log, a.q.per_seq - 1)]; };
         u4 kr[4][K64 + (K64 == 0)]; uint2 ks[4];
+        float2 gk, gv;
+        bool held = false;
+        int pk = 0, pv = 0;
+        const unsigned char* vb = a.cache;
+        auto load_k = [&](int t0) {      // and the grids of token t0 + lane
+            const int tk = t0 + 16 * (col >> 2), tv = t0 + 16 * grp, t = t0 + lane;
+            held = pv >= 0 && pv < a.g.n_pages;
+            const unsigned char* const kb = a.cache + (long long)min(max(pk, 0), (int)a.g.n_pages - 1) * a.g.page_bytes + head_levels + (long long)((tk & in_page) + (col & 3)) * DP + grp * 16;
+            const unsigned char* const vp = a.cache + (long long)(held ? pv : 0) * a.g.page_bytes;
+            vb = vp + a.g.v_at + head_levels + (long long)(tv & in_page) * DP + col * 16;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < 4; ++i) {
 #pragma unroll
-            for (int k = 0; k < K64; ++k) kr[i][k] = *(const u4*)(kb + i * 4 * DP + k * 64);
-            if constexpr (K32 != 0) ks[i] = *(const uint2*)(kb + i * 4 * DP + K64 * 64 - grp * 8);
+                for (int k = 0; k < K64; ++k) kr[i][k] = *(const u4*)(kb + i * 4 * DP + k * 64);
+                if constexpr (K32 != 0) ks[i] = *(const uint2*)(kb + i * 4 * DP + K64 * 64 - grp * 8);
+            }
+            gk = make_float2(1.f, 0.f); gv = make_float2(0.f, 0.f);
+            if (held && t < end) {
+                const long long gat = head_grids + ((t & in_page) >> a.g.st_log);
+                gk = ((const float2*)(vp + a.g.kg_at))[gat]; gv = ((const float2*)(vp + a.g.vg_at))[gat];
+            }
+        };
+        int t0 = lo + wave * TILE;
+        int pk_next = 0, pv_next = 0;
+        if (t0 < hi) {
+            pk = page_of(t0 + 16 * (col >> 2)); pv = page_of(t0 + 16 * grp);
+            load_k(t0);
+            pk_next = page_of(t0 + 4 * TILE + 16 * (col >> 2)); pv_next = page_of(t0 + 4 * TILE + 16 * grp);
         }
-        u4 vr[CT];
-#pragma unroll
-        for (int c = 0; c < CT; ++c) vr[c] = *(const u4*)(vb + c * 256);
-        // grids of token t0 + lane
-        const int t = t0 + lane;
-        const bool there = held && t < end;
-        float2 gk = make_float2(1.f, 0.f), gv = make_float2(0.f, 0.f);
-        if (there) {
-            const long long at = head_grids + ((t & in_page) >> a.g.st_log);
-            gk = ((const float2*)(vp + a.g.kg_at))[at]; gv = ((const float2*)(vp + a.g.vg_at))[at];
-        }
-        const float sk = gk.x * unit;
 
-        // scores
-        f4 st[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const _Float16 zo = (_Float16)(-1024.f - __shfl(gk.y, 16 * (col >> 2) + 4 * i + (col & 3), 64));
-            const h2 z = {zo, zo};
-            f4 acc = {0.f, 0.f, 0.f, 0.f};
+        h8 qh[NT][KS];
+        float unit;
+        {
+            float v[KS][8], most = 0.f;
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
-                h8 lv;
-                if (k < 2 * K64) lv = levels8(kr[i][k >> 1][(k & 1) * 2], kr[i][k >> 1][(k & 1) * 2 + 1], z, z, z, z);
-                else lv = levels8(ks[i].x, ks[i].y, z, z, z, z);
+                const int c = k < 2 * K64 ? (k >> 1) * 64 + grp * 16 + (k & 1) * 8 : K64 * 64 + grp * 8;
+                if (a.vec) {
+                    union { u4 u[sizeof(T) / 2]; T e[8]; } in;
 #pragma unroll
-                for (int n = 0; n < NT; ++n) acc = mma16(lv, qh[n][k], acc);
+                    for (int j = 0; j < (int)sizeof(T) / 2; ++j) in.u[j] = row_live && c < a.g.dh ? ((const u4*)(q + c))[j] : u4{0, 0, 0, 0};
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[k][j] = to_f32(in.e[j]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[k][j] = row_live && c + j < a.g.dh ? to_f32(q[c + j]) : 0.f;
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) { const float m = fabsf(v[k][j]); most = m < __builtin_inff() ? fmaxf(most, m) : most; }
             }
-            st[i] = acc;
-        }
-        float p[16];
-        unroll<16>([&](auto I) { constexpr int i = I; p[i] = st[i >> 2][i & 3] * row_lane<i>(sk); });
-        const bool all = t0 + TILE - 1 <= s.len - s.n + r0 / a.rep && t0 + TILE <= end && t0 >= (a.window ? span.lo + (n_rows - 1) / a.rep + 1 : 0) && __all(held);
-        unsigned hidden = 0;
-        if (!all) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int tt = tv + i;
-                if (!(row_live && held && tt < end && tt <= pos && tt >= low)) { hidden |= 1u << i; p[i] = -__builtin_inff(); }
+            for (int o = 1; o < 64; o <<= 1) most = fmaxf(most, __shfl_xor(most, o, 64));
+            const int e = most > 0.f ? min(14 - __builtin_amdgcn_frexp_expf(most), 100) : 0;
+            unit = __builtin_amdgcn_ldexpf(a.scale2, -e);
+#pragma unroll
+            for (int k = 0; k < KS; ++k)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float w = __builtin_amdgcn_ldexpf(v[k][j], e);
+                    const _Float16 hi16 = (_Float16)w;
+                    qh[0][k][j] = hi16;
+                    if constexpr (NT == 2) qh[1][k][j] = (_Float16)(isfinite(w) ? w - (float)hi16 : 0.f);
+                }
+        }
+
+        float m = -__builtin_inff(), l = 0.f, ref = 0x1p-126f;
+        f4 o[CT];
+#pragma unroll
+        for (int c = 0; c < CT; ++c) o[c] = f4{0.f, 0.f, 0.f, 0.f};
+        for (; t0 < hi; t0 += 4 * TILE) {
+            u4 vr[CT];
+#pragma unroll
+            for (int c = 0; c < CT; ++c) vr[c] = *(const u4*)(vb + c * 256);
+            const bool there = held;
+            const float sk = gk.x * unit, zk = -1024.f - gk.y, gvx = gv.x, zv = -1024.f - gv.y;
+            // scores
+            f4 st[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const _Float16 zo = (_Float16)__shfl(zk, 16 * (col >> 2) + 4 * i + (col & 3), 64);
+                const h2 z = {zo, zo};
+                f4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int k = 0; k < KS; ++k) {
+                    h8 lv;
+                    if (k < 2 * K64) lv = levels8(kr[i][k >> 1][(k & 1) * 2], kr[i][k >> 1][(k & 1) * 2 + 1], z, z, z, z);
+                    else lv = levels8(ks[i].x, ks[i].y, z, z, z, z);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) acc = mma16(lv, qh[n][k], acc);
+                }
+                st[i] = acc;
+            }
+            if (t0 + 4 * TILE < hi) {
+                pk = pk_next; pv = pv_next;
+                load_k(t0 + 4 * TILE);
+                pk_next = page_of(t0 + 8 * TILE + 16 * (col >> 2)); pv_next = page_of(t0 + 8 * TILE + 16 * grp);
+            }
+            float p[16];
+            unroll<16>([&](auto I) { constexpr int i = I; p[i] = st[i >> 2][i & 3] * row_lane<i>(sk); });
+            const bool all = t0 + TILE - 1 <= s.len - s.n + r0 / a.rep && t0 + TILE <= end && t0 >= (a.window ? span.lo + (n_rows - 1) / a.rep + 1 : 0) && __all(there);
+            unsigned hidden = 0;
+            if (!all) {
+                const int tv = t0 + 16 * grp;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int tt = tv + i;
+                    if (!(row_live && there && tt < end && tt <= pos && tt >= low)) { hidden |= 1u << i; p[i] = -__builtin_inff(); }
+                }
+            }
+            float top = p[0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) top = fmaxf(top, p[i]);
+            top = fmaxf(top, from_xor<16>(top)); top = fmaxf(top, from_xor<32>(top));
+            const float m_new = fmaxf(m, top), base = m_new == -__builtin_inff() ? 0.f : m_new;
+            float turn = ex2(m - base);
+            m = m_new;
+            l *= turn;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) { p[i] = ex2(p[i] - base); l += p[i]; }
+            float s_top = gvx;
+#pragma unroll
+            for (int k = 1; k < 64; k <<= 1) s_top = fmaxf(s_top, __shfl_xor(s_top, k, 64));
+            if (s_top >= ref && s_top < __builtin_inff()) {
+                const float now = __builtin_amdgcn_ldexpf(1.f, min(__builtin_amdgcn_frexp_expf(s_top), 127));
+                turn *= ref / now; ref = now;
+            }
+            if (__any(turn != 1.f)) {
+#pragma unroll
+                for (int c = 0; c < CT; ++c) o[c] *= turn;
+            }
+            const float sv = gvx * (HALF_TOP / ref);
+            unroll<16>([&](auto I) { constexpr int i = I; p[i] *= row_lane<i>(sv); });
+            if (!all) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) if (hidden >> i & 1) p[i] = 0.f;
+            }
+            h8 ph[NT][2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const _Float16 w = (_Float16)p[8 * k + j];
+                    ph[0][k][j] = w;
+                    if constexpr (NT == 2) ph[1][k][j] = (_Float16)(p[8 * k + j] - (float)w);
+                }
+            // zeros of V's 16 tokens as pairs
+            h2 zo[8];
+            {
+                const unsigned mine = __builtin_bit_cast(unsigned short, (_Float16)zv);
+                const unsigned next = (unsigned)__builtin_amdgcn_mov_dpp((int)mine, 0xB1, 0xf, 0xf, true);      // the neighbour's: quad_perm 1 0 3 2
+                const unsigned pair = mine | next << 16;                                                             // (for even lanes)
+                unroll<8>([&](auto I) { constexpr int i = I; zo[i] = __builtin_bit_cast(h2, row_lane<2 * i>(pair)); });
+            }
+#pragma unroll
+            for (int c = 0; c < CT; ++c) {
+                const h8 v0 = levels8(vr[c][0], vr[c][1], zo[0], zo[1], zo[2], zo[3]), v1 = levels8(vr[c][2], vr[c][3], zo[4], zo[5], zo[6], zo[7]);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) { o[c] = mma16(v0, ph[n][0], o[c]); o[c] = mma16(v1, ph[n][1], o[c]); }
             }
         }
-        float top = p[0];
+        l += from_xor<16>(l); l += from_xor<32>(l);
+        if (l != l) m = fmaxf(m, 0.f);      // scores that are all NaN leave the maximum where it was: the row has seen something
+        if (grp == 0) ends[wave][col] = make_float2(m, l);
+        __syncthreads();
+        float top = ends[0][col].x;
 #pragma unroll
-        for (int i = 1; i < 16; ++i) top = fmaxf(top, p[i]);
-        top = fmaxf(top, from_xor<16>(top)); top = fmaxf(top, from_xor<32>(top));
-        const float m_new = fmaxf(m, top), base = m_new == -__builtin_inff() ? 0.f : m_new;
-        float turn = ex2(m - base);
-        m = m_new;
-        l *= turn;
+        for (int w = 1; w < 4; ++w) top = fmaxf(top, ends[w][col].x);
+        const float f = m == -__builtin_inff() ? 0.f : ex2(m - top) * ref * (1.f / HALF_TOP);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) { p[i] = ex2(p[i] - base); l += p[i]; }
-        float s_top = gv.x;
+        for (int c = 0; c < CT; ++c) *(f4*)&joined[wave][col][c * 16 + grp * 4] = m == -__builtin_inff() ? f4{0.f, 0.f, 0.f, 0.f} : o[c] * f;
+        __syncthreads();
+        const bool whole = k0 == 0 && k1 == tiles;
+        const long long piece = (2LL * blockIdx.x + (k0 == 0)) * ROWS;
+        if (threadIdx.x == 0 && k0 == 0 && !whole) a.info[blockIdx.x] = make_int4((int)((at + tiles - 1) / share) - (int)blockIdx.x + 1, s.start, r0 | (n_rows - 1) << 27, h);
+        for (int i = threadIdx.x; i < n_rows * (DP / 4); i += 256) {
+            const int rr = i / (DP / 4), c = i % (DP / 4) * 4;
+            float tp = ends[0][rr].x, sum = 0.f;
+            f4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int q = 1; q < 64; q <<= 1) s_top = fmaxf(s_top, __shfl_xor(s_top, q, 64));
-        if (s_top >= ref && s_top < __builtin_inff()) {
-            int e;
-            frexpf(s_top, &e);
-            const float now = ldexpf(1.f, min(e, 127));
-            turn *= ref / now; ref = now;
-        }
-        if (__any(turn != 1.f)) {
+            for (int w = 1; w < 4; ++w) tp = fmaxf(tp, ends[w][rr].x);
 #pragma unroll
-            for (int c = 0; c < CT; ++c) o[c] *= turn;
-        }
-        const float sv = gv.x * (HALF_TOP / ref);
-        unroll<16>([&](auto I) { constexpr int i = I; p[i] *= row_lane<i>(sv); });
-        if (!all) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) if (hidden >> i & 1) p[i] = 0.f;
-        }
-        h8 ph[NT][2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const _Float16 w = (_Float16)p[8 * k + j];
-                ph[0][k][j] = w;
-                if constexpr (NT == 2) ph[1][k][j] = (_Float16)(p[8 * k + j] - (float)w);
+            for (int w = 0; w < 4; ++w) {
+                if (ends[w][rr].x != -__builtin_inff()) sum += ends[w][rr].y * ex2(ends[w][rr].x - tp);
+                v += *(const f4*)&joined[w][rr][c];
             }
-        // zeros of V's 16 tokens as pairs
-        h2 zo[8];
-        {
-            const unsigned mine = __builtin_bit_cast(unsigned short, (_Float16)(-1024.f - gv.y));
-            const unsigned next = (unsigned)__builtin_amdgcn_mov_dpp((int)mine, 0xB1, 0xf, 0xf, true);      // the neighbour's: quad_perm 1 0 3 2
-            const unsigned pair = mine | next << 16;                                                             // (for even lanes)
-            unroll<8>([&](auto I) { constexpr int i = I; zo[i] = __builtin_bit_cast(h2, row_lane<2 * i>(pair)); });
+            if (whole) {
+                const int row = r0 + rr, tk = row / a.rep;
+                T* out = (T*)a.O + (long long)(s.start + tk) * a.ldo + (long long)(h * a.rep + row - tk * a.rep) * a.g.dh;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) if (c + j < a.g.dh) out[c + j] = from_f32<T>(sum == 0.f ? 0.f : v[j] / sum);
+            } else {
+                *(f4*)(a.part + (piece + rr) * DP + c) = v;
+                if (c == 0) a.stat[piece + rr] = make_float2(tp, sum);
+            }
         }
-#pragma unroll
-        for (int c = 0; c < CT; ++c) {
-            const h8 v0 = levels8(vr[c][0], vr[c][1], zo[0], zo[1], zo[2], zo[3]), v1 = levels8(vr[c][2], vr[c][3], zo[4], zo[5], zo[6], zo[7]);
-#pragma unroll
-            for (int n = 0; n < NT; ++n) { o[c] = mma16(v0, ph[n][0], o[c]); o[c] = mma16(v1, ph[n][1], o[c]); }
-        }
-    }
-    l += from_xor<16>(l); l += from_xor<32>(l);
-    if (l != l) m = fmaxf(m, 0.f);      // scores that are all NaN leave the maximum where it was: the row has seen something
-    if (grp == 0) ends[wave][col] = make_float2(m, l);
-    __syncthreads();
-    float top = ends[0][col].x;
-#pragma unroll
-    for (int w = 1; w < 4; ++w) top = fmaxf(top, ends[w][col].x);
-    const float f = m == -__builtin_inff() ? 0.f : ex2(m - top) * ref * (1.f / HALF_TOP);
-#pragma unroll
-    for (int c = 0; c < CT; ++c) *(f4*)&joined[wave][col][c * 16 + grp * 4] = m == -__builtin_inff() ? f4{0.f, 0.f, 0.f, 0.f} : o[c] * f;
-    __syncthreads();
-    for (int i = threadIdx.x; i < n_rows * a.g.dh; i += 256) {
-        const int rr = i / a.g.dh, c = i - rr * a.g.dh;
-        float tp = ends[0][rr].x, sum = 0.f, v = 0.f;
-#pragma unroll
-        for (int w = 1; w < 4; ++w) tp = fmaxf(tp, ends[w][rr].x);
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            if (ends[w][rr].x != -__builtin_inff()) sum += ends[w][rr].y * ex2(ends[w][rr].x - tp);
-            v += joined[w][rr][c];
-        }
-        if (n_cuts == 1) {
-            const int row = r0 + rr;
-            T* out = (T*)a.O + (long long)(s.start + row / a.rep) * a.ldo + (long long)(h * a.rep + row % a.rep) * a.g.dh;
-            out[c] = from_f32<T>(sum == 0.f ? 0.f : v / sum);
-        } else {
-            const long long at = ((long long)blockIdx.x * a.g.heads + h) * ROWS + rr;
-            a.part[at * DP + c] = v;
-            if (c == 0) a.stat[at] = make_float2(tp, sum);
-        }
+        at += k1 - k0;
+        if (at < at_end) __syncthreads();      // (what is in LDS has been read)
     }
 }
 
-// Items of a row tile of a sequence that was cut: sum of 2^(max_i - max) O_i over that of the sums.  One workgroup per row tile, KV head and row.
-template <typename T>
+// Rows of a unit that lies in several shares: sum of 2^(max_i - max) O_i over that of the sums, a wavefront per row of the unit that begins in share blockIdx.x.  DP / 4 lanes hold a row;
+// the first pieces are on their way before their weights are known.
+template <typename T, int DP>
 __global__ __launch_bounds__(256) void kv_attend_join_kernel(AttendArgs a) {
-    const int h = blockIdx.y, rr = blockIdx.z, per = item_tiles(a);
-    int x = blockIdx.x, b;
-    KvSeq s;
-    if (!kv_find(a.q, [&](const KvSeq& e) { return row_tiles(e, a.rep); }, x, b, s)) return;
-    const int n_cuts = cuts(s, a, per);
-    if (n_cuts == 1 || x * ROWS + rr >= s.n * a.rep) return;
-    // number of the tile's first item: items of the sequences before, and of the tiles before
-    long long before = 0;
-    for (int i = threadIdx.x & 63; i < b; i += 64) { const KvSeq e = kv_sequence(a.q, i); if (e.n) before += (long long)row_tiles(e, a.rep) * cuts(e, a, per); }
+    constexpr int LANES = DP / 4, GROUPS = 64 / LANES, AHEAD = 8;
+    const int4 info = a.info[blockIdx.x];
+    const int pieces = min(info.x, (int)(gridDim.x - blockIdx.x)), r0 = info.z & ((1 << 27) - 1), n_rows = (int)((unsigned)info.z >> 27) + 1, h = info.w;
+    const int lane = threadIdx.x & 63, rr = blockIdx.y * 4 + (threadIdx.x >> 6), c = lane % LANES, group = lane / LANES;
+    if (pieces < 1 || rr >= n_rows) return;
+    auto place = [&](int i) { return (2LL * (blockIdx.x + i) + (i == 0)) * ROWS + rr; };
+    const float* const part = a.part + 4 * c;
+    f4 v = {0.f, 0.f, 0.f, 0.f};
+    float top = -__builtin_inff(), sum = 0.f;
+    for (int i0 = 0; i0 < pieces; i0 += 64) {
+        const float2 st = i0 + lane < pieces ? a.stat[place(i0 + lane)] : make_float2(-__builtin_inff(), 0.f);
+        const int n = min(pieces - i0, 64);
+        f4 ahead[AHEAD];
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) before += __shfl_xor(before, o, 64);
-    const long long first = before + (long long)x * n_cuts;
-    if (first + n_cuts > a.items) return;      // (starts that do not grow)
-    __shared__ float sums[256], outs[256];
-    float top = -__builtin_inff();
-    for (int i = 0; i < n_cuts; ++i) top = fmaxf(top, a.stat[((first + i) * a.g.heads + h) * ROWS + rr].x);
-    const int row = x * ROWS + rr;
-    T* out = (T*)a.O + (long long)(s.start + row / a.rep) * a.ldo + (long long)(h * a.rep + row % a.rep) * a.g.dh;
-    // 64 channels at a time, four shares of the items
-    const int c0 = threadIdx.x & 63, share = threadIdx.x >> 6;
-    for (int c = c0; c < a.g.dp; c += 64) {
-        float v = 0.f, sum = 0.f;
-        for (int i = share; i < n_cuts; i += 4) {
-            const long long at = ((first + i) * a.g.heads + h) * ROWS + rr;
-            const float2 st = a.stat[at];
-            if (st.x == -__builtin_inff()) continue;
-            const float f = ex2(st.x - top);
-            sum += f * st.y;
-            if (c < a.g.dh) v += f * a.part[at * a.g.dp + c];
+        for (int k = 0; k < AHEAD; ++k) { const int i = group + k * GROUPS; ahead[k] = group < GROUPS && i < n ? *(const f4*)(part + place(i0 + i) * DP) : f4{0.f, 0.f, 0.f, 0.f}; }
+        float now = fmaxf(st.x, top);
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) now = fmaxf(now, __shfl_xor(now, o, 64));
+        const float turn = top == now ? 1.f : ex2(top - now), f = st.x == -__builtin_inff() ? 0.f : ex2(st.x - now);
+        v *= turn; sum = sum * turn + (st.x == -__builtin_inff() ? 0.f : f * st.y);
+        top = now;
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) v += ahead[k] * __shfl(f, min(group + k * GROUPS, 63), 64);
+        for (int k0 = AHEAD * GROUPS; k0 < n; k0 += AHEAD * GROUPS) {
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) { const int i = k0 + group + k * GROUPS; ahead[k] = group < GROUPS && i < n ? *(const f4*)(part + place(i0 + i) * DP) : f4{0.f, 0.f, 0.f, 0.f}; }
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) v += ahead[k] * __shfl(f, min(k0 + group + k * GROUPS, 63), 64);
         }
-        sums[threadIdx.x] = sum; outs[threadIdx.x] = v;
-        __syncthreads();
-        if (share == 0 && c < a.g.dh) {
-            sum = sums[c0] + sums[c0 + 64] + sums[c0 + 128] + sums[c0 + 192];
-            v = outs[c0] + outs[c0 + 64] + outs[c0 + 128] + outs[c0 + 192];
-            out[c] = from_f32<T>(sum == 0.f ? 0.f : v / sum);
-        }
-        __syncthreads();
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o, 64);
+    f4 all = v;
+#pragma unroll
+    for (int g = 1; g < GROUPS; ++g)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) all[j] += __shfl(v[j], min(c + g * LANES, 63), 64);
+    if (group == 0) {
+        const int row = r0 + rr, tk = row / a.rep;
+        T* out = (T*)a.O + (long long)(info.y + tk) * a.ldo + (long long)(h * a.rep + row - tk * a.rep) * a.g.dh;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) if (4 * c + i < a.g.dh) out[4 * c + i] = from_f32<T>(sum == 0.f ? 0.f : all[i] / sum);
     }
 }
 
-// Items that fill the chip: four workgroups of 256 compute units each
-constexpr int TARGET = 1024;
-struct AttendPlan { long long tiles, items; size_t bytes; };
-AttendPlan plan(const KvGeometry& g, int n_seqs, long long n_tokens, int rep) {
-    AttendPlan p;
-    // row tiles of all sequences: at most rows / ROWS and one more per sequence, and no sequence with a token has more than ceil(rep / ROWS) per token
-    p.tiles = std::min(n_tokens * rep / ROWS + std::min<long long>(n_seqs, n_tokens), n_tokens * cdiv64(rep, ROWS));
-    p.items = p.tiles + cdiv64(TARGET, g.heads);
-    Arena ar(nullptr);
-    ar.get<float>((size_t)p.items * g.heads * ROWS * g.dp); ar.get<float2>((size_t)p.items * g.heads * ROWS);
-    p.bytes = ar.off;
-    return p;
+int shares(int dp) { return 256 * (dp == 32 ? resident<32>() : dp == 64 ? resident<64>() : dp <= 128 ? resident<128>() : resident<256>()); }
+size_t room(const KvGeometry& g, AttendArgs* a, void* ws) {
+    const size_t n = (size_t)shares(g.dp);
+    Arena ar(ws);
+    float* part = ar.get<float>(2 * n * ROWS * g.dp);
+    float2* stat = ar.get<float2>(2 * n * ROWS);
+    int4* info = ar.get<int4>(n);
+    if (a) { a->part = part; a->stat = stat; a->info = info; }
+    return ar.off;
 }
 
-template <typename T>
-int attend(tboa_ctx* ctx, const AttendArgs& a, const AttendPlan& p) {
-    const dim3 grid((unsigned)p.items, (unsigned)a.g.heads), block(256);
-    switch (a.g.dp) {
-        case 32: hipLaunchKernelGGL((kv_attend_rows_kernel<T, 32>), grid, block, 0, ctx->stream, a); break;
-        case 64: hipLaunchKernelGGL((kv_attend_rows_kernel<T, 64>), grid, block, 0, ctx->stream, a); break;
-        case 96: hipLaunchKernelGGL((kv_attend_rows_kernel<T, 96>), grid, block, 0, ctx->stream, a); break;
-        case 128: hipLaunchKernelGGL((kv_attend_rows_kernel<T, 128>), grid, block, 0, ctx->stream, a); break;
-        case 192: hipLaunchKernelGGL((kv_attend_rows_kernel<T, 192>), grid, block, 0, ctx->stream, a); break;
-        default: hipLaunchKernelGGL((kv_attend_rows_kernel<T, 256>), grid, block, 0, ctx->stream, a);
-    }
+template <typename T, int DP>
+int attend(tboa_ctx* ctx, const AttendArgs& a) {
+    hipLaunchKernelGGL((kv_attend_rows_kernel<T, DP>), dim3(256 * resident<DP>()), dim3(256), 0, ctx->stream, a);
     TB_KERNEL_CHECK(ctx);
-    hipLaunchKernelGGL((kv_attend_join_kernel<T>), dim3((unsigned)p.tiles, (unsigned)a.g.heads, ROWS), block, 0, ctx->stream, a);
+    hipLaunchKernelGGL((kv_attend_join_kernel<T, DP>), dim3(256 * resident<DP>(), ROWS / 4), dim3(256), 0, ctx->stream, a);
     TB_KERNEL_CHECK(ctx);
     return 0;
+}
+template <typename T>
+int attend(tboa_ctx* ctx, const AttendArgs& a) {
+    switch (a.g.dp) {
+        case 32: return attend<T, 32>(ctx, a);
+        case 64: return attend<T, 64>(ctx, a);
+        case 96: return attend<T, 96>(ctx, a);
+        case 128: return attend<T, 128>(ctx, a);
+        case 192: return attend<T, 192>(ctx, a);
+        default: return attend<T, 256>(ctx, a);
+    }
 }
 
 }  // namespace
@@ -371,7 +410,7 @@ int attend(tboa_ctx* ctx, const AttendArgs& a, const AttendPlan& p) {
 extern "C" size_t tboa_kv_cache_attention_workspace_bytes(const tboa_kv_cache_desc* desc, int n_q_heads, int n_seqs, int64_t n_tokens) {
     KvGeometry g;
     if (!kv_geometry(desc, g) || n_q_heads <= 0 || n_q_heads > 65535 || n_q_heads % g.heads || n_seqs < 0 || n_seqs > 1 << 20 || n_tokens < 0 || n_tokens > 1 << 24) return 0;
-    return n_seqs == 0 || n_tokens == 0 ? 0 : plan(g, n_seqs, n_tokens, n_q_heads / g.heads).bytes;
+    return n_seqs == 0 || n_tokens == 0 ? 0 : room(g, nullptr, nullptr);
 }
 
 extern "C" int tboa_kv_cache_attention(tboa_ctx* ctx, const tboa_kv_cache_desc* desc, const tboa_kv_batch* batch, int n_q_heads, int dtype, const void* Q, int64_t ldq,
@@ -386,20 +425,18 @@ extern "C" int tboa_kv_cache_attention(tboa_ctx* ctx, const tboa_kv_cache_desc* 
     if (batch->pages_per_seq == 0 || g.n_pages == 0) return tboa_fail(ctx, TBOA_EINVAL, "kv_cache_attention: no pages");
     if (!Q || !O) return tboa_fail(ctx, TBOA_EINVAL, "kv_cache_attention: null argument");
     if (ldq < (int64_t)n_q_heads * g.dh || ldo < (int64_t)n_q_heads * g.dh) return tboa_fail(ctx, TBOA_EINVAL, "kv_cache_attention: a row pitch is smaller than its heads");
+    const int rep = n_q_heads / g.heads, size = dtype == TBOA_F32 ? 4 : 2;
+    if (batch->n_tokens * rep >= 1LL << 27) return tboa_fail(ctx, TBOA_EINVAL, "kv_cache_attention: too many rows");
     KvDevice dev(ctx->device);
-    const int rep = n_q_heads / g.heads;
-    const AttendPlan p = plan(g, batch->n_seqs, batch->n_tokens, rep);
-    if (batch->n_tokens * rep > 1LL << 30) return tboa_fail(ctx, TBOA_EINVAL, "kv_cache_attention: too many rows");
-    TB_TRY(tboa_ws_reserve(ctx, p.bytes));
+    TB_TRY(tboa_ws_reserve(ctx, room(g, nullptr, nullptr)));
     TB_TRY(tboa_ws_in_graph(ctx));
     AttendArgs a;
     a.g = g;
     a.q = KvBatch{batch->n_seqs, batch->pages_per_seq, (int)batch->n_tokens, batch->pages_per_seq * desc->page_tokens, batch->starts, batch->lens, batch->pages};
     a.Q = Q; a.ldq = ldq; a.O = O; a.ldo = ldo; a.cache = (const unsigned char*)cache;
     a.scale2 = (float)((scale == 0.0 ? 1.0 / sqrt((double)g.dh) : scale) * 1.4426950408889634);
-    a.rep = rep; a.window = window; a.target = TARGET; a.items = p.items;
-    Arena ar(ctx->ws);
-    a.part = ar.get<float>((size_t)p.items * g.heads * ROWS * g.dp);
-    a.stat = ar.get<float2>((size_t)p.items * g.heads * ROWS);
-    return dtype == TBOA_F32 ? attend<float>(ctx, a, p) : attend<bf16>(ctx, a, p);
+    a.rep = rep; a.window = window;
+    a.vec = g.dh % 8 == 0 && ((uintptr_t)Q & 15) == 0 && ldq * size % 16 == 0;
+    room(g, &a, ctx->ws);
+    return dtype == TBOA_F32 ? attend<float>(ctx, a) : attend<bf16>(ctx, a);
 }

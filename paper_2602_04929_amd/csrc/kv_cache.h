@@ -28,26 +28,29 @@ __device__ __forceinline__ KvSeq kv_sequence(const KvBatch& q, int b) {
     return KvSeq{a, e - a, min(max(q.lens[b], 0), KV_MOST_TOKENS)};
 }
 
+__device__ __forceinline__ KvSeq kv_head(const KvBatch& q) { const int lane = threadIdx.x & 63; return lane < q.n_seqs ? kv_sequence(q, lane) : KvSeq{0, 0, 0}; }
+
 // Item x of a list in which sequence b has count(sequence) items: its sequence, and x becomes the number within it.  Every wavefront finds its own, 64 sequences at a time.
-template <typename Count>
-__device__ __forceinline__ bool kv_find(const KvBatch& q, Count count, int& x, int& b, KvSeq& s) {
+// `head`: sequence threadIdx.x % 64, which the caller may have read already.
+template <typename N, typename Count>
+__device__ __forceinline__ bool kv_find(const KvBatch& q, const KvSeq& head, Count count, N& x, int& b, KvSeq& s) {
     const int lane = threadIdx.x & 63;
     for (int base = 0; base < q.n_seqs; base += 64) {
         KvSeq mine{0, 0, 0};
-        int c = 0;
-        if (base + lane < q.n_seqs) { mine = kv_sequence(q, base + lane); c = count(mine); }
-        int sum = c;
+        N c = 0;
+        if (base + lane < q.n_seqs) { mine = base ? kv_sequence(q, base + lane) : head; c = count(mine); }
+        N sum = c;
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) { const int v = __shfl_up(sum, o, 64); if (lane >= o) sum += v; }
+        for (int o = 1; o < 64; o <<= 1) { const N v = __shfl_up(sum, o, 64); if (lane >= o) sum += v; }
         const unsigned long long past = __ballot(sum > x);
         if (past) {
             const int at = __builtin_ctzll(past);
             b = base + at;
-            x -= __builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(c, at);
+            x -= __shfl(sum - c, at, 64);
             s = KvSeq{__builtin_amdgcn_readlane(mine.start, at), __builtin_amdgcn_readlane(mine.n, at), __builtin_amdgcn_readlane(mine.len, at)};
             return true;
         }
-        x -= __builtin_amdgcn_readlane(sum, 63);
+        x -= __shfl(sum, 63, 64);
     }
     return false;
 }

@@ -202,7 +202,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs<T> a) {
     int x = blockIdx.x, b;
     KvSeq s;
     const int room = a.q.room;
-    if (!kv_find(a.q, [ul, room](const KvSeq& e) {
+    if (!kv_find(a.q, kv_head(a.q), [ul, room](const KvSeq& e) {
             const int p0 = max(e.len - e.n, 0), end = min(e.len, room);
             return end > p0 && e.n > 0 ? ((end - 1) >> ul) - (p0 >> ul) + 1 : 0; }, x, b, s)) return;
     const int first = max(s.len - s.n, 0);                 // first position that gets a token
