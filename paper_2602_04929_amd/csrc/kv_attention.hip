@@ -15,6 +15,7 @@ typedef __hip_bfloat16 bf16;
 typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef float f4 __attribute__((ext_vector_type(4)));
+typedef float f16v __attribute__((ext_vector_type(16)));
 typedef unsigned u4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ float to_f32(float v) { return v; }
@@ -51,7 +52,9 @@ struct AttendArgs {
     const unsigned char* cache;
     float scale2;                 // scale log2 e
     int rep, window, vec;         // vec: 16-byte pieces of Q
+    int few;                      // sequences of more rows are kv_attend_tiles_kernel's
     int4* info;                   // per workgroup: the unit that begins in its share and ends in another: workgroups, first row of the sequence, row of the first | rows << 27, head
+    float* tile_part; float2* tile_stat;      // kv_attend_tiles_kernel: per piece, its rows
     float* part; float2* stat;    // per workgroup two pieces of 16 rows (of a unit that began before its share, of one that begins in it): unscaled outputs; maximum, sum
 };
 
@@ -66,7 +69,7 @@ __device__ __forceinline__ int seen_tiles(const KvSeq& s, const AttendArgs& a) {
     const int end = min(s.len, a.q.room);
     return s.n == 0 ? 0 : max((min(end, a.window ? (int)min((long long)a.window + s.n + TILE, 2147483647LL) : end) + TILE - 1) / TILE, 1);
 }
-__device__ __forceinline__ long long unit_tiles(const KvSeq& s, const AttendArgs& a) { return (long long)row_tiles(s, a.rep) * seen_tiles(s, a) * a.g.heads; }
+__device__ __forceinline__ long long unit_tiles(const KvSeq& s, const AttendArgs& a) { return s.n * a.rep > a.few ? 0 : (long long)row_tiles(s, a.rep) * seen_tiles(s, a) * a.g.heads; }
 
 // tokens that rows r0 .. of a sequence see
 struct Span { int lo, hi; };
@@ -329,7 +332,7 @@ __global__ __launch_bounds__(256, resident<DP>()) void kv_attend_rows_kernel(Att
 // the first pieces are on their way before their weights are known.
 template <typename T, int DP>
 __global__ __launch_bounds__(256) void kv_attend_join_kernel(AttendArgs a) {
-    constexpr int LANES = DP / 4, GROUPS = 64 / LANES, AHEAD = 8;
+    constexpr int LANES = DP / 4, GROUPS = 64 / LANES, AHEAD = 16;
     const int4 info = a.info[blockIdx.x];
     const int pieces = min(info.x, (int)(gridDim.x - blockIdx.x)), r0 = info.z & ((1 << 27) - 1), n_rows = (int)((unsigned)info.z >> 27) + 1, h = info.w;
     const int lane = threadIdx.x & 63, rr = blockIdx.y * 4 + (threadIdx.x >> 6), c = lane % LANES, group = lane / LANES;
@@ -374,34 +377,419 @@ __global__ __launch_bounds__(256) void kv_attend_join_kernel(AttendArgs a) {
     }
 }
 
+// ------------------------------------------------------------------------------------------------ many rows
+// Sequences of many new tokens: bound by the matrix instructions and the exponentials' vector instructions, so what one workgroup reads of the cache serves 32 rows in each of its W wavefronts.
+// A tile of 64 tokens is made into half once, by all of them, and kept in LDS (K by token, V by channel, 16-byte pieces XOR-permuted by row, two tiles of each).  S^T = K Q^T with 32 x 32 x 16
+// instructions: the tokens of a tile's rows are ordered so that a lane's 16 scores are the right operand of O^T += V^T P^T as they stand.  The scores of tile n + 1 are formed in the same run of
+// instructions as the exponentials of tile n, so that matrix and vector units work side by side.
+// A row's maximum is only followed where it has grown by more than GROW powers of two: up to there the probabilities simply exceed 1.
+constexpr float GROW = 4.f, TILE_TOP = 0x1p11f;      // 2^4 2^11 = 2^15, within half
+template <int DP> constexpr int permuted() { return DP % 128 == 0 ? 15 : DP % 64 == 0 ? 7 : 3; }      // bits of a piece's number that K's rows are XORed into
+template <int DP, int W> constexpr int tiles_lds() { return 2 * 2 * TILE * DP * 2; }
+constexpr int TILES_TARGET = 512;                    // workgroups that the units of a call are cut into where they are fewer: two rounds of the chip
+
+struct TilesUnit { int b, h, tile, cut, n_cuts; KvSeq s; };
+template <int RT>
+__device__ __forceinline__ int unit_rows(const KvSeq& s, const AttendArgs& a) { return s.n * a.rep > a.few ? (s.n * a.rep + RT - 1) / RT : 0; }
+// Piece x of the call: units by sequence, the last rows first (they see most), heads side by side (an XCD keeps to few heads: its cache holds them)
+template <int RT>
+__device__ __forceinline__ bool find_unit(const AttendArgs& a, int x, TilesUnit& u) {
+    const int lane = threadIdx.x & 63;
+    KvSeq head{0, 0, 0};
+    int total = 0;
+    for (int i = lane; i < a.q.n_seqs; i += 64) {
+        const KvSeq e = kv_sequence(a.q, i);
+        if (i < 64) head = e;
+        total += unit_rows<RT>(e, a);
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) total += __shfl_xor(total, o, 64);
+    const long long units = (long long)__builtin_amdgcn_readfirstlane(total) * a.g.heads;
+    if (units == 0) return false;
+    const int split = units >= TILES_TARGET ? 1 : (int)(TILES_TARGET / units);
+    if (x >= units * split) return false;
+    u.cut = x % split;
+    const int unit = x / split;
+    u.h = unit % a.g.heads;
+    int at = unit / a.g.heads;
+    if (!kv_find(a.q, head, [&](const KvSeq& e) { return unit_rows<RT>(e, a); }, at, u.b, u.s)) return false;
+    u.tile = __builtin_amdgcn_readfirstlane(unit_rows<RT>(u.s, a) - 1 - at);
+    u.n_cuts = max(min(split, seen_tiles(u.s, a) / 4), 1);
+    return u.cut < u.n_cuts;
+}
+
+__device__ __forceinline__ f16v mma32(h8 a, h8 b, f16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+
+template <int DP, int W, bool WIDE>      // WIDE: pages of 64 tokens and more, a tile lies in one
+__global__ __launch_bounds__(64 * W, 2) void kv_attend_tiles_kernel(AttendArgs a) {
+    constexpr int RT = 32 * W, KS = DP / 16, CT = DP / 32, PIECES = 4 * DP, PP = (PIECES + 64 * W - 1) / (64 * W);      // 16-byte pieces of a tile of K (and of V), per thread
+    constexpr int KROW = DP * 2, VROW = TILE * 2;      // bytes of a row in LDS
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    unsigned char* const kbuf = lds;
+    unsigned char* const vbuf = lds + 2 * TILE * KROW;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, half = lane >> 5, i16 = lane & 15;
+    TilesUnit u;
+    if (!find_unit<RT>(a, blockIdx.x, u)) return;
+    const KvSeq s = u.s;
+    const int h = u.h, r0 = u.tile * RT, n_rows = min(RT, s.n * a.rep - r0);
+    const Span span = row_span(s, a, r0, n_rows);
+    const int end = min(s.len, a.q.room);
+    int lo, hi;      // tokens of this piece: whole tiles, the last one up to hi
+    {
+        const int t0 = span.lo / TILE, t1 = (span.hi + TILE - 1) / TILE, each = max((t1 - t0 + u.n_cuts - 1) / u.n_cuts, 0);
+        lo = (t0 + u.cut * each) * TILE; hi = min((t0 + (u.cut + 1) * each) * TILE, span.hi);
+    }
+    const int n_tiles = __builtin_amdgcn_readfirstlane(max((hi - lo + TILE - 1) / TILE, 0));
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    // this lane's row; the wavefront's rows
+    const int w0 = wave * 32, w_rows = min(max(n_rows - w0, 0), 32);
+    const bool row_live = col < w_rows;
+    const int r = r0 + w0 + (row_live ? col : 0), tok = r / a.rep, pos = row_live ? s.len - s.n + tok : -1, low = a.window ? pos - a.window + 1 : 0;
+    const Span mine = w_rows ? row_span(s, a, r0 + w0, w_rows) : Span{0, 0};
+    const int w_first = s.len - s.n + (r0 + w0) / a.rep, w_low = a.window ? s.len - s.n + (r0 + w0 + max(w_rows, 1) - 1) / a.rep - a.window + 1 : 0;      // places that all its rows see: up to w_first, from w_low on
+
+    const long long head_levels = (long long)h * DP << a.g.pt_log, head_grids = (long long)h << (a.g.pt_log - a.g.st_log);
+    const int in_page = (1 << a.g.pt_log) - 1, st_log = a.g.st_log;
+    const int* const pages = a.q.pages + (long long)u.b * a.q.per_seq;
+    auto page_at = [&](int t) { return pages[min(t >> a.g.pt_log, a.q.per_seq - 1)]; };
+    auto base_of = [&](int pg) { return a.cache + (long long)min(max(pg, 0), (int)a.g.n_pages - 1) * a.g.page_bytes; };
+
+    // raw levels of a tile's K (one ahead of V), zero of a piece's token (K), of token 16 g + lane % 16 (V)
+    u4 kraw[PP], vraw[PP];
+    float kz[PP], vz[PP];
+    auto fetch_k = [&](int t0) {
+        const unsigned char* page = nullptr;
+        if constexpr (WIDE) page = base_of(__builtin_amdgcn_readfirstlane(page_at(t0)));
+#pragma unroll
+        for (int j = 0; j < PP; ++j) {
+            const int i = tid + j * 64 * W, tk = i / (DP / 16), c = i % (DP / 16) * 16;
+            if (PIECES % (64 * W) != 0 && i >= PIECES) break;
+            if constexpr (!WIDE) page = base_of(page_at(t0 + tk));
+            const int o = (t0 + tk) & in_page;
+            kraw[j] = *(const u4*)(page + head_levels + (long long)o * DP + c);
+            kz[j] = t0 + tk < end ? *(const float*)(page + a.g.kg_at + (head_grids + (o >> st_log)) * 8 + 4) : 0.f;
+        }
+    };
+    auto fetch_v = [&](int t0) {
+        const unsigned char* page = nullptr;
+        if constexpr (WIDE) page = base_of(__builtin_amdgcn_readfirstlane(page_at(t0)));
+#pragma unroll
+        for (int j = 0; j < PP; ++j) {
+            const int i = tid + j * 64 * W, g = i / DP, c = i % DP;
+            if (PIECES % (64 * W) != 0 && i >= PIECES) break;
+            if constexpr (!WIDE) page = base_of(page_at(t0 + 16 * g));
+            const int o = (t0 + 16 * g) & in_page;
+            vraw[j] = *(const u4*)(page + a.g.v_at + head_levels + (long long)o * DP + c * 16);
+            vz[j] = t0 + 16 * g + i16 < end ? *(const float*)(page + a.g.vg_at + (head_grids + ((o + i16) >> st_log)) * 8 + 4) : 0.f;
+        }
+    };
+    auto store_k = [&](int buf) {
+#pragma unroll
+        for (int j = 0; j < PP; ++j) {
+            const int i = tid + j * 64 * W, tk = i / (DP / 16), c = i % (DP / 16) * 2;
+            if (PIECES % (64 * W) != 0 && i >= PIECES) break;
+            const _Float16 zo = (_Float16)(-1024.f - kz[j]);
+            const h2 z = {zo, zo};
+            const int row = (tk & ~12) | (tk & 4) << 1 | (tk & 8) >> 1;      // the matrix instruction's row whose result is this token's
+            unsigned char* const p = kbuf + buf * TILE * KROW + row * KROW;
+            constexpr int M = permuted<DP>();
+            *(h8*)(p + (((c & ~M) | ((c ^ row) & M)) << 4)) = levels8(kraw[j][0], kraw[j][1], z, z, z, z);
+            *(h8*)(p + ((((c + 1) & ~M) | (((c + 1) ^ row) & M)) << 4)) = levels8(kraw[j][2], kraw[j][3], z, z, z, z);
+        }
+    };
+    auto store_v = [&](int buf) {
+#pragma unroll
+        for (int j = 0; j < PP; ++j) {
+            const int i = tid + j * 64 * W, g = i / DP, c = i % DP;
+            if (PIECES % (64 * W) != 0 && i >= PIECES) break;
+            h2 zo[8];
+            const unsigned one = __builtin_bit_cast(unsigned short, (_Float16)(-1024.f - vz[j]));
+            const unsigned pair = one | (unsigned)__builtin_amdgcn_mov_dpp((int)one, 0xB1, 0xf, 0xf, true) << 16;
+            unroll<8>([&](auto I) { constexpr int n = I; zo[n] = __builtin_bit_cast(h2, row_lane<2 * n>(pair)); });
+            unsigned char* const p = vbuf + buf * DP * VROW + c * VROW;
+            *(h8*)(p + (((2 * g) ^ (c & 7)) << 4)) = levels8(vraw[j][0], vraw[j][1], zo[0], zo[1], zo[2], zo[3]);
+            *(h8*)(p + (((2 * g + 1) ^ (c & 7)) << 4)) = levels8(vraw[j][2], vraw[j][3], zo[4], zo[5], zo[6], zo[7]);
+        }
+    };
+    // scales of tokens 32 k + 16 (i16 / 8) + 8 half + i16 % 8, k = 0, 1: those of a lane's scores, one in each lane of a row of 16; which groups of 16 tokens there are
+    float gk[2], gv[2];
+    unsigned there = 0;      // bit 2 k + i16 / 8
+    auto fetch_grids = [&](int t0) {
+        const unsigned char* page = nullptr;
+        int pg = 0;
+        if constexpr (WIDE) { pg = __builtin_amdgcn_readfirstlane(page_at(t0)); page = base_of(pg); }
+        there = 0;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int t = t0 + 32 * k + 16 * (i16 >> 3) + 8 * half + (i16 & 7);
+            if constexpr (!WIDE) { pg = page_at(t); page = base_of(pg); }
+            const bool ok = pg >= 0 && pg < a.g.n_pages;
+            const unsigned long long b = __ballot(ok);
+            there |= (unsigned)(b & 1) << 2 * k | (unsigned)(b >> 8 & 1) << (2 * k + 1);
+            gk[k] = 1.f; gv[k] = 0.f;
+            if (ok && t < end) {
+                const long long at = (head_grids + ((t & in_page) >> st_log)) * 8;
+                gk[k] = *(const float*)(page + a.g.kg_at + at); gv[k] = *(const float*)(page + a.g.vg_at + at);
+            }
+        }
+    };
+
+    if (n_tiles) { fetch_k(lo); fetch_v(lo); fetch_grids(lo); }
+    h8 qf[KS];
+    float unit;
+    {
+        const bf16* const q = (const bf16*)a.Q + (long long)(s.start + tok) * a.ldq + (long long)(h * a.rep + r - tok * a.rep) * a.g.dh;
+        float most = 0.f;
+        h8 raw[KS];
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            const int c = k * 16 + half * 8;
+            union { u4 w; bf16 e[8]; h8 v; } in;
+            if (a.vec) in.w = row_live && c < a.g.dh ? *(const u4*)(q + c) : u4{0, 0, 0, 0};
+            else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) in.e[j] = row_live && c + j < a.g.dh ? q[c + j] : from_f32<bf16>(0.f);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) { const float m = fabsf(to_f32(in.e[j])); most = m < __builtin_inff() ? fmaxf(most, m) : most; }
+            raw[k] = in.v;
+        }
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) most = fmaxf(most, __shfl_xor(most, o, 64));
+        const int e = most > 0.f ? min(14 - __builtin_amdgcn_frexp_expf(most), 100) : 0;
+        unit = __builtin_amdgcn_ldexpf(a.scale2, -e);
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            union { bf16 e[8]; h8 v; } in;
+            in.v = raw[k];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) qf[k][j] = (_Float16)__builtin_amdgcn_ldexpf(to_f32(in.e[j]), e);
+        }
+    }
+
+    f16v o[CT], sc[2];
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) o[c][j] = 0.f;
+    float m = -__builtin_inff(), l = 0.f, ref = 0x1p-126f;
+
+    auto scores = [&](int buf, f16v (&out)[2]) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            f16v acc;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) acc[j] = 0.f;
+            const int row = 32 * k + col;
+            const unsigned char* const p = kbuf + buf * TILE * KROW + row * KROW;
+            constexpr int M = permuted<DP>();
+#pragma unroll
+            for (int c = 0; c < KS; ++c) {
+                const int piece = 2 * c + half;
+                acc = mma32(*(const h8*)(p + (((piece & ~M) | ((piece ^ row) & M)) << 4)), qf[c], acc);
+            }
+            out[k] = acc;
+        }
+    };
+
+    if (n_tiles) {
+        store_k(0); store_v(0);
+        if (n_tiles > 1) { fetch_k(lo + TILE); fetch_v(lo + TILE); }
+        __syncthreads();
+        scores(0, sc);
+        if (n_tiles > 1) { store_k(1); if (n_tiles > 2) fetch_k(lo + 2 * TILE); }
+        __syncthreads();
+    }
+    for (int n = 0; n < n_tiles; ++n) {
+        const int t0 = lo + n * TILE;
+        const float sk[2] = {gk[0] * unit, gk[1] * unit}, sv0[2] = {gv[0], gv[1]};
+        const unsigned here = there;
+        if (n + 1 < n_tiles) fetch_grids(t0 + TILE);
+        const bool work = t0 < mine.hi && t0 + TILE > mine.lo && w_rows > 0;      // (the same for the wavefront)
+        f16v next[2];
+        if (n + 1 < n_tiles) scores((n + 1) & 1, next);
+        if (work) {
+            unsigned hidden[2] = {0, 0};
+            unroll<32>([&](auto I) { constexpr int i = I; sc[i >> 4][i & 15] *= row_lane<i & 15>(sk[i >> 4]); });
+            const bool all = t0 + TILE - 1 <= w_first && t0 >= w_low && t0 + TILE <= end && here == 15u;
+            if (!all) {
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int t = t0 + 32 * k + 16 * (i >> 3) + 8 * half + (i & 7);
+                        if (!(row_live && t <= pos && t >= low && t < end && (here >> (2 * k + (i >> 3)) & 1))) { hidden[k] |= 1u << i; sc[k][i] = -__builtin_inff(); }
+                    }
+            }
+            float top = fmaxf(sc[0][0], sc[1][0]);
+#pragma unroll
+            for (int i = 1; i < 16; ++i) top = fmaxf(top, fmaxf(sc[0][i], sc[1][i]));
+            top = fmaxf(top, from_xor<32>(top));
+            float s_top = fmaxf(sv0[0], sv0[1]);
+#pragma unroll
+            for (int k = 1; k < 64; k <<= 1) s_top = fmaxf(s_top, __shfl_xor(s_top, k, 64));
+            const bool scale_grown = s_top >= ref && s_top < __builtin_inff();
+            if (__any(top > m + GROW) || scale_grown) {
+                const float to = top > m + GROW ? top : m;      // (-inf where nothing has been seen)
+                float turn = m == -__builtin_inff() ? 0.f : ex2(m - to);
+                m = to; l *= turn;
+                if (scale_grown) {
+                    const float now = __builtin_amdgcn_ldexpf(1.f, min(__builtin_amdgcn_frexp_expf(s_top), 127));
+                    turn *= ref / now; ref = now;
+                }
+#pragma unroll
+                for (int c = 0; c < CT; ++c) o[c] *= turn;
+            }
+            const float base = m == -__builtin_inff() ? 0.f : m;
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) { sc[k][i] = ex2(sc[k][i] - base); l += sc[k][i]; }
+            const float sv[2] = {sv0[0] * (TILE_TOP / ref), sv0[1] * (TILE_TOP / ref)};
+            unroll<32>([&](auto I) { constexpr int i = I; sc[i >> 4][i & 15] *= row_lane<i & 15>(sv[i >> 4]); });
+            if (!all) {
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) if (hidden[k] >> i & 1) sc[k][i] = 0.f;
+            }
+            const unsigned char* const vp = vbuf + (n & 1) * DP * VROW;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                h8 pf;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) pf[j] = (_Float16)sc[k >> 1][(k & 1) * 8 + j];
+#pragma unroll
+                for (int c = 0; c < CT; ++c) {
+                    const int row = 32 * c + col;
+                    o[c] = mma32(*(const h8*)(vp + row * VROW + (((2 * k + half) ^ (row & 7)) << 4)), pf, o[c]);
+                }
+            }
+        }
+        if (n + 1 < n_tiles) { sc[0] = next[0]; sc[1] = next[1]; }
+        if (n + 2 < n_tiles) { store_k(n & 1); if (n + 3 < n_tiles) fetch_k(t0 + 3 * TILE); }
+        if (n + 1 < n_tiles) { store_v((n + 1) & 1); if (n + 2 < n_tiles) fetch_v(t0 + 2 * TILE); }
+        __syncthreads();
+    }
+    l += from_xor<32>(l);
+    if (l != l) m = fmaxf(m, 0.f);      // scores that are all NaN leave the maximum where it was
+    if (!row_live) return;
+    const float unscale = m == -__builtin_inff() ? 0.f : ref * (1.f / TILE_TOP);
+    if (u.n_cuts == 1) {
+        bf16* const out = (bf16*)a.O + (long long)(s.start + tok) * a.ldo + (long long)(h * a.rep + r - tok * a.rep) * a.g.dh;
+        const float f = l == 0.f ? 0.f : unscale / l;
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int ch = 32 * c + 8 * (i >> 2) + 4 * half + (i & 3);
+                if (ch < a.g.dh) out[ch] = from_f32<bf16>(l == 0.f ? 0.f : o[c][i] * f);
+            }
+    } else {
+        const long long at = (long long)blockIdx.x * RT + w0 + col;
+        if (half == 0) a.tile_stat[at] = make_float2(m, l);
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *(f4*)(a.tile_part + at * DP + 32 * c + 8 * i + 4 * half) = m == -__builtin_inff() ? f4{0.f, 0.f, 0.f, 0.f} : f4{o[c][4 * i], o[c][4 * i + 1], o[c][4 * i + 2], o[c][4 * i + 3]} * unscale;
+    }
+}
+
+// Rows of units that were cut: a wavefront per row, as kv_attend_join_kernel
+template <int DP, int RT>
+__global__ __launch_bounds__(256) void kv_attend_tiles_join_kernel(AttendArgs a) {
+    TilesUnit u;
+    {   // unit blockIdx.x: the piece with cut 0 tells how many there are
+        KvSeq head{0, 0, 0};
+        int total = 0;
+        for (int i = threadIdx.x & 63; i < a.q.n_seqs; i += 64) total += unit_rows<RT>(kv_sequence(a.q, i), a);
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) total += __shfl_xor(total, o, 64);
+        const long long units = (long long)__builtin_amdgcn_readfirstlane(total) * a.g.heads;
+        if (blockIdx.x >= units || units >= TILES_TARGET) return;
+        const int split = (int)(TILES_TARGET / units);
+        if (split < 2 || !find_unit<RT>(a, blockIdx.x * split, u) || u.n_cuts < 2) return;
+        u.cut = blockIdx.x * split;      // (its number)
+    }
+    const int r0 = u.tile * RT, n_rows = min(RT, u.s.n * a.rep - r0), lane = threadIdx.x & 63;
+    for (int rr = blockIdx.y * 4 + (threadIdx.x >> 6); rr < n_rows; rr += 4 * gridDim.y) {
+        float top = -__builtin_inff();
+        for (int i = 0; i < u.n_cuts; ++i) top = fmaxf(top, a.tile_stat[(long long)(u.cut + i) * RT + rr].x);
+        const int row = r0 + rr, tk = row / a.rep;
+        bf16* const out = (bf16*)a.O + (long long)(u.s.start + tk) * a.ldo + (long long)(u.h * a.rep + row - tk * a.rep) * a.g.dh;
+        for (int c = lane; c < a.g.dh; c += 64) {
+            float v = 0.f, sum = 0.f;
+#pragma unroll 4
+            for (int i = 0; i < u.n_cuts; ++i) {
+                const long long at = (long long)(u.cut + i) * RT + rr;
+                const float2 st = a.tile_stat[at];
+                const float f = st.x == -__builtin_inff() ? 0.f : ex2(st.x - top);
+                sum += st.x == -__builtin_inff() ? 0.f : f * st.y;
+                v += f * a.tile_part[at * DP + c];
+            }
+            out[c] = from_f32<bf16>(sum == 0.f ? 0.f : v / sum);
+        }
+    }
+}
+
 int shares(int dp) { return 256 * (dp == 32 ? resident<32>() : dp == 64 ? resident<64>() : dp <= 128 ? resident<128>() : resident<256>()); }
-size_t room(const KvGeometry& g, AttendArgs* a, void* ws) {
-    const size_t n = (size_t)shares(g.dp);
+constexpr int FEW = 32, WAVES = 8;      // rows of a sequence up to which kv_attend_rows_kernel takes it
+// Row tiles of all sequences that kv_attend_tiles_kernel takes: at most one more per sequence than rows / RT, and one per token or more
+long long most_units(const KvGeometry& g, int n_seqs, long long n_tokens, int rep) {
+    const int rt = 32 * WAVES;
+    return std::min(n_tokens * rep / rt + std::min<long long>(n_seqs, n_tokens), n_tokens * cdiv64(rep, rt)) * g.heads;
+}
+size_t room(const KvGeometry& g, bool tiles, long long units, AttendArgs* a, void* ws) {
+    const size_t n = (size_t)shares(g.dp), pieces = tiles ? (size_t)std::min<long long>(TILES_TARGET, std::max<long long>(units, 1) * TILES_TARGET) : 0;
     Arena ar(ws);
     float* part = ar.get<float>(2 * n * ROWS * g.dp);
     float2* stat = ar.get<float2>(2 * n * ROWS);
     int4* info = ar.get<int4>(n);
-    if (a) { a->part = part; a->stat = stat; a->info = info; }
+    float* tile_part = ar.get<float>(pieces * 32 * WAVES * g.dp);
+    float2* tile_stat = ar.get<float2>(pieces * 32 * WAVES);
+    if (a) { a->part = part; a->stat = stat; a->info = info; a->tile_part = tile_part; a->tile_stat = tile_stat; }
     return ar.off;
 }
 
 template <typename T, int DP>
-int attend(tboa_ctx* ctx, const AttendArgs& a) {
+int attend_rows(tboa_ctx* ctx, const AttendArgs& a) {
     hipLaunchKernelGGL((kv_attend_rows_kernel<T, DP>), dim3(256 * resident<DP>()), dim3(256), 0, ctx->stream, a);
     TB_KERNEL_CHECK(ctx);
     hipLaunchKernelGGL((kv_attend_join_kernel<T, DP>), dim3(256 * resident<DP>(), ROWS / 4), dim3(256), 0, ctx->stream, a);
     TB_KERNEL_CHECK(ctx);
     return 0;
 }
+template <int DP>
+int attend_tiles(tboa_ctx* ctx, const AttendArgs& a, long long units) {
+    constexpr int LDS = tiles_lds<DP, WAVES>();
+    const dim3 grid((unsigned)std::max<long long>(units, TILES_TARGET)), block(64 * WAVES);
+    if (a.g.pt_log >= 6) {
+        TB_HIP(ctx, hipFuncSetAttribute((const void*)kv_attend_tiles_kernel<DP, WAVES, true>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
+        hipLaunchKernelGGL((kv_attend_tiles_kernel<DP, WAVES, true>), grid, block, LDS, ctx->stream, a);
+    } else {
+        TB_HIP(ctx, hipFuncSetAttribute((const void*)kv_attend_tiles_kernel<DP, WAVES, false>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
+        hipLaunchKernelGGL((kv_attend_tiles_kernel<DP, WAVES, false>), grid, block, LDS, ctx->stream, a);
+    }
+    TB_KERNEL_CHECK(ctx);
+    hipLaunchKernelGGL((kv_attend_tiles_join_kernel<DP, 32 * WAVES>), dim3((unsigned)std::min<long long>(units, TILES_TARGET / 2), 8), dim3(256), 0, ctx->stream, a);
+    TB_KERNEL_CHECK(ctx);
+    return 0;
+}
+template <typename T, int DP>
+int attend(tboa_ctx* ctx, const AttendArgs& a, bool rows, long long units) {
+    if constexpr (sizeof(T) == 2) { if (units) TB_TRY(attend_tiles<DP>(ctx, a, units)); }
+    return rows ? attend_rows<T, DP>(ctx, a) : 0;
+}
 template <typename T>
-int attend(tboa_ctx* ctx, const AttendArgs& a) {
+int attend(tboa_ctx* ctx, const AttendArgs& a, bool rows, long long units) {
     switch (a.g.dp) {
-        case 32: return attend<T, 32>(ctx, a);
-        case 64: return attend<T, 64>(ctx, a);
-        case 96: return attend<T, 96>(ctx, a);
-        case 128: return attend<T, 128>(ctx, a);
-        case 192: return attend<T, 192>(ctx, a);
-        default: return attend<T, 256>(ctx, a);
+        case 32: return attend<T, 32>(ctx, a, rows, units);
+        case 64: return attend<T, 64>(ctx, a, rows, units);
+        case 96: return attend<T, 96>(ctx, a, rows, units);
+        case 128: return attend<T, 128>(ctx, a, rows, units);
+        case 192: return attend<T, 192>(ctx, a, rows, units);
+        default: return attend<T, 256>(ctx, a, rows, units);
     }
 }
 
@@ -410,7 +798,7 @@ int attend(tboa_ctx* ctx, const AttendArgs& a) {
 extern "C" size_t tboa_kv_cache_attention_workspace_bytes(const tboa_kv_cache_desc* desc, int n_q_heads, int n_seqs, int64_t n_tokens) {
     KvGeometry g;
     if (!kv_geometry(desc, g) || n_q_heads <= 0 || n_q_heads > 65535 || n_q_heads % g.heads || n_seqs < 0 || n_seqs > 1 << 20 || n_tokens < 0 || n_tokens > 1 << 24) return 0;
-    return n_seqs == 0 || n_tokens == 0 ? 0 : room(g, nullptr, nullptr);
+    return n_seqs == 0 || n_tokens == 0 ? 0 : room(g, n_tokens * (n_q_heads / g.heads) > FEW, most_units(g, n_seqs, n_tokens, n_q_heads / g.heads), nullptr, nullptr);
 }
 
 extern "C" int tboa_kv_cache_attention(tboa_ctx* ctx, const tboa_kv_cache_desc* desc, const tboa_kv_batch* batch, int n_q_heads, int dtype, const void* Q, int64_t ldq,
@@ -428,7 +816,12 @@ extern "C" int tboa_kv_cache_attention(tboa_ctx* ctx, const tboa_kv_cache_desc* 
     const int rep = n_q_heads / g.heads, size = dtype == TBOA_F32 ? 4 : 2;
     if (batch->n_tokens * rep >= 1LL << 27) return tboa_fail(ctx, TBOA_EINVAL, "kv_cache_attention: too many rows");
     KvDevice dev(ctx->device);
-    TB_TRY(tboa_ws_reserve(ctx, room(g, nullptr, nullptr)));
+    // sequences of more than FEW rows go to the tiles' kernel (16-bit inputs), the others to the rows'; what the caller says of the batch may spare one of the two launches
+    const long long most = batch->max_new > 0 ? std::min<long long>(batch->max_new, batch->n_tokens) : batch->n_tokens;
+    const bool tiles = dtype == TBOA_BF16 && most * rep > FEW, rows = !tiles || batch->n_seqs > 1 || batch->n_tokens * rep <= FEW;
+    const long long units = tiles ? most_units(g, batch->n_seqs, batch->n_tokens, rep) : 0;
+    if (units > 2147483647LL) return tboa_fail(ctx, TBOA_EINVAL, "kv_cache_attention: too many rows");
+    TB_TRY(tboa_ws_reserve(ctx, room(g, tiles, units, nullptr, nullptr)));
     TB_TRY(tboa_ws_in_graph(ctx));
     AttendArgs a;
     a.g = g;
@@ -437,6 +830,7 @@ extern "C" int tboa_kv_cache_attention(tboa_ctx* ctx, const tboa_kv_cache_desc* 
     a.scale2 = (float)((scale == 0.0 ? 1.0 / sqrt((double)g.dh) : scale) * 1.4426950408889634);
     a.rep = rep; a.window = window;
     a.vec = g.dh % 8 == 0 && ((uintptr_t)Q & 15) == 0 && ldq * size % 16 == 0;
-    room(g, &a, ctx->ws);
-    return dtype == TBOA_F32 ? attend<float>(ctx, a) : attend<bf16>(ctx, a);
+    a.few = !tiles ? 1 << 30 : rows ? FEW : 0;
+    room(g, tiles, units, &a, ctx->ws);
+    return dtype == TBOA_F32 ? attend<float>(ctx, a, rows, units) : attend<bf16>(ctx, a, rows, units);
 }
