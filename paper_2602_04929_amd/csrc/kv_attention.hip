@@ -378,14 +378,16 @@ __global__ __launch_bounds__(256) void kv_attend_join_kernel(AttendArgs a) {
 }
 
 // ------------------------------------------------------------------------------------------------ many rows
-// Sequences of many new tokens: bound by the matrix instructions and the exponentials' vector instructions, so what one workgroup reads of the cache serves 32 rows in each of its W wavefronts.
+// Sequences of many new tokens: bound by the matrix instructions and the softmax's vector instructions, so what one workgroup reads of the cache serves 32 rows in each of its W wavefronts.
 // A tile of 64 tokens is made into half once, by all of them, and kept in LDS (K by token, V by channel, 16-byte pieces XOR-permuted by row, two tiles of each).  S^T = K Q^T with 32 x 32 x 16
-// instructions: the tokens of a tile's rows are ordered so that a lane's 16 scores are the right operand of O^T += V^T P^T as they stand.  The scores of tile n + 1 are formed in the same run of
-// instructions as the exponentials of tile n, so that matrix and vector units work side by side.
+// instructions: the tokens of a tile's rows are ordered so that a lane's 32 scores, as half, are the right operand of O^T += V^T P^T as they stand.
+// A wavefront alternates between a run of matrix instructions, scores of tile n and products with V of tile n - 1, and a run of vector instructions, the softmax of tile n and its part in making
+// the next tile.  Runs end at a barrier; of the two wavefronts of a SIMD one is a run behind the other, so that one multiplies while the other exponentiates.
 // A row's maximum is only followed where it has grown by more than GROW powers of two: up to there the probabilities simply exceed 1.
 constexpr float GROW = 4.f, TILE_TOP = 0x1p11f;      // 2^4 2^11 = 2^15, within half
+template <int DP> constexpr int waves() { return DP <= 128 ? 8 : 4; }      // (wider heads need twice the registers)
 template <int DP> constexpr int permuted() { return DP % 128 == 0 ? 15 : DP % 64 == 0 ? 7 : 3; }      // bits of a piece's number that K's rows are XORed into
-template <int DP, int W> constexpr int tiles_lds() { return 2 * 2 * TILE * DP * 2; }
+template <int DP> constexpr int tiles_lds() { return 2 * 2 * TILE * DP * 2; }
 constexpr int TILES_TARGET = 512;                    // workgroups that the units of a call are cut into where they are fewer: two rounds of the chip
 
 struct TilesUnit { int b, h, tile, cut, n_cuts; KvSeq s; };
@@ -420,14 +422,37 @@ __device__ __forceinline__ bool find_unit(const AttendArgs& a, int x, TilesUnit&
 
 __device__ __forceinline__ f16v mma32(h8 a, h8 b, f16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 
-template <int DP, int W, bool WIDE>      // WIDE: pages of 64 tokens and more, a tile lies in one
-__global__ __launch_bounds__(64 * W, 2) void kv_attend_tiles_kernel(AttendArgs a) {
-    constexpr int RT = 32 * W, KS = DP / 16, CT = DP / 32, PIECES = 4 * DP, PP = (PIECES + 64 * W - 1) / (64 * W);      // 16-byte pieces of a tile of K (and of V), per thread
-    constexpr int KROW = DP * 2, VROW = TILE * 2;      // bytes of a row in LDS
+__device__ __forceinline__ float across_halves(float v) {      // maximum of lanes l and l ^ 32
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ void run_ends() {      // everything before it is before, what was written to LDS is there
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+#ifndef AHEAD_
+#define AHEAD_ 6
+#endif
+// N matrix instructions with an LDS operand each: the operands' loads AHEAD of them, no more (the registers would not hold them)
+template <int N, int AHEAD>
+__device__ __forceinline__ void operands_ahead() {
+    __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+#pragma unroll
+    for (int i = 0; i < N - AHEAD; ++i) { __builtin_amdgcn_sched_group_barrier(0x8, 1, 0); __builtin_amdgcn_sched_group_barrier(0x100, 1, 0); }
+    __builtin_amdgcn_sched_group_barrier(0x8, AHEAD, 0);
+}
+
+template <int DP, bool WIDE>      // WIDE: pages of 64 tokens and more, a tile lies in one
+__global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_tiles_kernel(AttendArgs a) {
+    constexpr int W = waves<DP>(), RT = 32 * W, KS = DP / 16, CT = DP / 32, PIECES = 4 * DP, PP = (PIECES + 64 * W - 1) / (64 * W);      // 16-byte pieces of a tile of K (and of V), per thread
+    constexpr bool EVEN = PIECES % (64 * W) == 0;
+    constexpr int KROW = DP * 2, VROW = TILE * 2, AHEAD = AHEAD_;      // bytes of a row in LDS; operands on their way
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     unsigned char* const kbuf = lds;
     unsigned char* const vbuf = lds + 2 * TILE * KROW;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, half = lane >> 5, i16 = lane & 15;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5, i16 = lane & 15;
     TilesUnit u;
     if (!find_unit<RT>(a, blockIdx.x, u)) return;
     const KvSeq s = u.s;
@@ -445,41 +470,48 @@ __global__ __launch_bounds__(64 * W, 2) void kv_attend_tiles_kernel(AttendArgs a
     const int w0 = wave * 32, w_rows = min(max(n_rows - w0, 0), 32);
     const bool row_live = col < w_rows;
     const int r = r0 + w0 + (row_live ? col : 0), tok = r / a.rep, pos = row_live ? s.len - s.n + tok : -1, low = a.window ? pos - a.window + 1 : 0;
-    const Span mine = w_rows ? row_span(s, a, r0 + w0, w_rows) : Span{0, 0};
-    const int w_first = s.len - s.n + (r0 + w0) / a.rep, w_low = a.window ? s.len - s.n + (r0 + w0 + max(w_rows, 1) - 1) / a.rep - a.window + 1 : 0;      // places that all its rows see: up to w_first, from w_low on
+    // tiles that the wavefront's rows see anything of, and places that all of them see
+    int see0 = 0, see1 = 0, all0 = 0, all1 = -1;
+    if (w_rows) {
+        const Span mine = row_span(s, a, r0 + w0, w_rows);
+        see0 = max(mine.lo - lo, 0) / TILE; see1 = min((mine.hi - lo + TILE - 1) / TILE, n_tiles);
+        all0 = a.window ? s.len - s.n + (r0 + w0 + w_rows - 1) / a.rep - a.window + 1 : 0; all1 = min(s.len - s.n + (r0 + w0) / a.rep, end - 1);
+        if (w_rows < 32) all1 = -1;
+    }
+    see0 = __builtin_amdgcn_readfirstlane(see0); see1 = __builtin_amdgcn_readfirstlane(see1); all0 = __builtin_amdgcn_readfirstlane(all0); all1 = __builtin_amdgcn_readfirstlane(all1);
 
     const long long head_levels = (long long)h * DP << a.g.pt_log, head_grids = (long long)h << (a.g.pt_log - a.g.st_log);
     const int in_page = (1 << a.g.pt_log) - 1, st_log = a.g.st_log;
     const int* const pages = a.q.pages + (long long)u.b * a.q.per_seq;
-    auto page_at = [&](int t) { return pages[min(t >> a.g.pt_log, a.q.per_seq - 1)]; };
+    // pages of tile n: that of its 16 tokens lane % 4 (a vector load in either case: a scalar one would share its counter with LDS)
+    auto pages_of = [&](int n) { return pages[min((lo + n * TILE + 16 * (lane & 3)) >> a.g.pt_log, a.q.per_seq - 1)]; };
+    auto page_in = [&](int ids, int group) { return WIDE ? __builtin_amdgcn_readfirstlane(ids) : __shfl(ids, group, 64); };
     auto base_of = [&](int pg) { return a.cache + (long long)min(max(pg, 0), (int)a.g.n_pages - 1) * a.g.page_bytes; };
 
-    // raw levels of a tile's K (one ahead of V), zero of a piece's token (K), of token 16 g + lane % 16 (V)
+    // raw levels of K of one tile and V of the one before it, zero of a piece's token (K), of token 16 g + lane % 16 (V)
     u4 kraw[PP], vraw[PP];
     float kz[PP], vz[PP];
-    auto fetch_k = [&](int t0) {
-        const unsigned char* page = nullptr;
-        if constexpr (WIDE) page = base_of(__builtin_amdgcn_readfirstlane(page_at(t0)));
+    auto fetch_k = [&](int n, int ids) {
+        const int t0 = lo + n * TILE;
 #pragma unroll
         for (int j = 0; j < PP; ++j) {
             const int i = tid + j * 64 * W, tk = i / (DP / 16), c = i % (DP / 16) * 16;
-            if (PIECES % (64 * W) != 0 && i >= PIECES) break;
-            if constexpr (!WIDE) page = base_of(page_at(t0 + tk));
+            if (!EVEN && i >= PIECES) break;
+            const unsigned char* const page = base_of(page_in(ids, tk >> 4));
             const int o = (t0 + tk) & in_page;
-            kraw[j] = *(const u4*)(page + head_levels + (long long)o * DP + c);
+            kraw[j] = *(const u4*)(page + head_levels + (long long)(o * DP + c));
             kz[j] = t0 + tk < end ? *(const float*)(page + a.g.kg_at + (head_grids + (o >> st_log)) * 8 + 4) : 0.f;
         }
     };
-    auto fetch_v = [&](int t0) {
-        const unsigned char* page = nullptr;
-        if constexpr (WIDE) page = base_of(__builtin_amdgcn_readfirstlane(page_at(t0)));
+    auto fetch_v = [&](int n, int ids) {
+        const int t0 = lo + n * TILE;
 #pragma unroll
         for (int j = 0; j < PP; ++j) {
             const int i = tid + j * 64 * W, g = i / DP, c = i % DP;
-            if (PIECES % (64 * W) != 0 && i >= PIECES) break;
-            if constexpr (!WIDE) page = base_of(page_at(t0 + 16 * g));
+            if (!EVEN && i >= PIECES) break;
+            const unsigned char* const page = base_of(page_in(ids, g));
             const int o = (t0 + 16 * g) & in_page;
-            vraw[j] = *(const u4*)(page + a.g.v_at + head_levels + (long long)o * DP + c * 16);
+            vraw[j] = *(const u4*)(page + a.g.v_at + head_levels + (long long)(o * DP + c * 16));
             vz[j] = t0 + 16 * g + i16 < end ? *(const float*)(page + a.g.vg_at + (head_grids + ((o + i16) >> st_log)) * 8 + 4) : 0.f;
         }
     };
@@ -487,7 +519,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv_attend_tiles_kernel(AttendArgs a
 #pragma unroll
         for (int j = 0; j < PP; ++j) {
             const int i = tid + j * 64 * W, tk = i / (DP / 16), c = i % (DP / 16) * 2;
-            if (PIECES % (64 * W) != 0 && i >= PIECES) break;
+            if (!EVEN && i >= PIECES) break;
             const _Float16 zo = (_Float16)(-1024.f - kz[j]);
             const h2 z = {zo, zo};
             const int row = (tk & ~12) | (tk & 4) << 1 | (tk & 8) >> 1;      // the matrix instruction's row whose result is this token's
@@ -501,7 +533,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv_attend_tiles_kernel(AttendArgs a
 #pragma unroll
         for (int j = 0; j < PP; ++j) {
             const int i = tid + j * 64 * W, g = i / DP, c = i % DP;
-            if (PIECES % (64 * W) != 0 && i >= PIECES) break;
+            if (!EVEN && i >= PIECES) break;
             h2 zo[8];
             const unsigned one = __builtin_bit_cast(unsigned short, (_Float16)(-1024.f - vz[j]));
             const unsigned pair = one | (unsigned)__builtin_amdgcn_mov_dpp((int)one, 0xB1, 0xf, 0xf, true) << 16;
@@ -514,18 +546,16 @@ __global__ __launch_bounds__(64 * W, 2) void kv_attend_tiles_kernel(AttendArgs a
     // scales of tokens 32 k + 16 (i16 / 8) + 8 half + i16 % 8, k = 0, 1: those of a lane's scores, one in each lane of a row of 16; which groups of 16 tokens there are
     float gk[2], gv[2];
     unsigned there = 0;      // bit 2 k + i16 / 8
-    auto fetch_grids = [&](int t0) {
-        const unsigned char* page = nullptr;
-        int pg = 0;
-        if constexpr (WIDE) { pg = __builtin_amdgcn_readfirstlane(page_at(t0)); page = base_of(pg); }
+    auto fetch_grids = [&](int n, int ids) {
+        const int t0 = lo + n * TILE;
         there = 0;
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            const int t = t0 + 32 * k + 16 * (i16 >> 3) + 8 * half + (i16 & 7);
-            if constexpr (!WIDE) { pg = page_at(t); page = base_of(pg); }
+            const int t = t0 + 32 * k + 16 * (i16 >> 3) + 8 * half + (i16 & 7), pg = page_in(ids, 2 * k + (i16 >> 3));
             const bool ok = pg >= 0 && pg < a.g.n_pages;
-            const unsigned long long b = __ballot(ok);
-            there |= (unsigned)(b & 1) << 2 * k | (unsigned)(b >> 8 & 1) << (2 * k + 1);
+            const unsigned char* const page = base_of(pg);
+            if constexpr (WIDE) there |= ok ? 3u << 2 * k : 0u;
+            else { const unsigned long long b = __ballot(ok); there |= (unsigned)(b & 1) << 2 * k | (unsigned)(b >> 8 & 1) << (2 * k + 1); }
             gk[k] = 1.f; gv[k] = 0.f;
             if (ok && t < end) {
                 const long long at = (head_grids + ((t & in_page) >> st_log)) * 8;
@@ -534,13 +564,23 @@ __global__ __launch_bounds__(64 * W, 2) void kv_attend_tiles_kernel(AttendArgs a
         }
     };
 
-    if (n_tiles) { fetch_k(lo); fetch_v(lo); fetch_grids(lo); }
+    // Slot n of LDS, buffer n & 1: K of tile n and V of tile n - 1.  Run n of matrix instructions reads it: the first four wavefronts in the 2 n-th stretch between barriers, the others (`later`)
+    // in the next one; its buffer is written in the two stretches before, by the later ones first.
+    const int later = __builtin_amdgcn_readfirstlane(W > 4 ? wave >> 2 : 0);
+    int ids0 = 0, ids1 = 0, ids2 = 0, ids3 = 0;      // pages of tiles n + 1 .. n + 4
+    if (n_tiles) {
+        const int first = pages_of(0);
+        ids0 = pages_of(1); ids1 = pages_of(2); ids2 = pages_of(3);
+        fetch_k(0, first); fetch_grids(0, first);
+        store_k(0);
+        fetch_v(0, first);
+        if (n_tiles > 1) fetch_k(1, ids0);
+    }
     h8 qf[KS];
     float unit;
     {
         const bf16* const q = (const bf16*)a.Q + (long long)(s.start + tok) * a.ldq + (long long)(h * a.rep + r - tok * a.rep) * a.g.dh;
         float most = 0.f;
-        h8 raw[KS];
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
             const int c = k * 16 + half * 8;
@@ -552,7 +592,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv_attend_tiles_kernel(AttendArgs a
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) { const float m = fabsf(to_f32(in.e[j])); most = m < __builtin_inff() ? fmaxf(most, m) : most; }
-            raw[k] = in.v;
+            qf[k] = in.v;
         }
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) most = fmaxf(most, __shfl_xor(most, o, 64));
@@ -561,81 +601,80 @@ __global__ __launch_bounds__(64 * W, 2) void kv_attend_tiles_kernel(AttendArgs a
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
             union { bf16 e[8]; h8 v; } in;
-            in.v = raw[k];
+            in.v = qf[k];
 #pragma unroll
             for (int j = 0; j < 8; ++j) qf[k][j] = (_Float16)__builtin_amdgcn_ldexpf(to_f32(in.e[j]), e);
         }
     }
-
     f16v o[CT], sc[2];
 #pragma unroll
     for (int c = 0; c < CT; ++c)
 #pragma unroll
         for (int j = 0; j < 16; ++j) o[c][j] = 0.f;
-    float m = -__builtin_inff(), l = 0.f, ref = 0x1p-126f;
-
-    auto scores = [&](int buf, f16v (&out)[2]) {
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            f16v acc;
-#pragma unroll
-            for (int j = 0; j < 16; ++j) acc[j] = 0.f;
-            const int row = 32 * k + col;
-            const unsigned char* const p = kbuf + buf * TILE * KROW + row * KROW;
-            constexpr int M = permuted<DP>();
-#pragma unroll
-            for (int c = 0; c < KS; ++c) {
-                const int piece = 2 * c + half;
-                acc = mma32(*(const h8*)(p + (((piece & ~M) | ((piece ^ row) & M)) << 4)), qf[c], acc);
-            }
-            out[k] = acc;
-        }
+    h8 pf[4];
+    float m = -__builtin_inff(), l = 0.f, ref = 0x1p-126f, unref = TILE_TOP * 0x1p126f;      // unref = TILE_TOP / ref
+    // operands in LDS
+    constexpr int M = permuted<DP>();
+    auto k_piece = [&](int buf, int k, int c) {
+        const int row = 32 * k + col, piece = 2 * c + half;
+        return *(const h8*)(kbuf + buf * TILE * KROW + row * KROW + (((piece & ~M) | ((piece ^ col) & M)) << 4));
     };
-
-    if (n_tiles) {
-        store_k(0); store_v(0);
-        if (n_tiles > 1) { fetch_k(lo + TILE); fetch_v(lo + TILE); }
-        __syncthreads();
-        scores(0, sc);
-        if (n_tiles > 1) { store_k(1); if (n_tiles > 2) fetch_k(lo + 2 * TILE); }
-        __syncthreads();
+    auto v_piece = [&](int buf, int k, int c) { return *(const h8*)(vbuf + buf * DP * VROW + (32 * c + col) * VROW + (((2 * k + half) ^ (col & 7)) << 4)); };
+    run_ends();
+    if (later) {
+        if (n_tiles > 0) { store_v(1); if (n_tiles > 1) { store_k(1); fetch_v(1, ids0); } if (n_tiles > 2) fetch_k(2, ids1); }
+        run_ends();
     }
-    for (int n = 0; n < n_tiles; ++n) {
+    for (int n = 0; n <= n_tiles && n_tiles; ++n) {
+        const int buf = n & 1;
+        const bool qk = n >= see0 && n < see1, pv = n - 1 >= see0 && n - 1 < see1;
+        if (qk) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) sc[k][j] = 0.f;
+#pragma unroll
+            for (int i = 0; i < 2 * KS; ++i) sc[i & 1] = mma32(k_piece(buf, i & 1, i >> 1), qf[i >> 1], sc[i & 1]);
+            operands_ahead<2 * KS, (AHEAD < 2 * KS ? AHEAD : 2 * KS)>();
+        }
+        if (pv) {
+#pragma unroll
+            for (int i = 0; i < 4 * CT; ++i) o[i % CT] = mma32(v_piece(buf, i / CT, i % CT), pf[i / CT], o[i % CT]);
+            operands_ahead<4 * CT, (AHEAD < 4 * CT ? AHEAD : 4 * CT)>();
+        }
+        run_ends();
         const int t0 = lo + n * TILE;
-        const float sk[2] = {gk[0] * unit, gk[1] * unit}, sv0[2] = {gv[0], gv[1]};
-        const unsigned here = there;
-        if (n + 1 < n_tiles) fetch_grids(t0 + TILE);
-        const bool work = t0 < mine.hi && t0 + TILE > mine.lo && w_rows > 0;      // (the same for the wavefront)
-        f16v next[2];
-        if (n + 1 < n_tiles) scores((n + 1) & 1, next);
-        if (work) {
-            unsigned hidden[2] = {0, 0};
+        if (qk) {
+            const float sk[2] = {gk[0] * unit, gk[1] * unit};
+            const bool all = t0 >= all0 && t0 + TILE - 1 <= all1 && there == 15u;
             unroll<32>([&](auto I) { constexpr int i = I; sc[i >> 4][i & 15] *= row_lane<i & 15>(sk[i >> 4]); });
-            const bool all = t0 + TILE - 1 <= w_first && t0 >= w_low && t0 + TILE <= end && here == 15u;
+            // places 32 k + 16 (i / 8) + i % 8 from first_seen on, seen of them, are seen by this row
+            const int first_seen = low - t0 - 8 * half;
+            const unsigned seen = (unsigned)max(min(pos, end - 1) - low + 1, 0);
+            const unsigned gone = ~there;
             if (!all) {
 #pragma unroll
                 for (int k = 0; k < 2; ++k)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int t = t0 + 32 * k + 16 * (i >> 3) + 8 * half + (i & 7);
-                        if (!(row_live && t <= pos && t >= low && t < end && (here >> (2 * k + (i >> 3)) & 1))) { hidden[k] |= 1u << i; sc[k][i] = -__builtin_inff(); }
-                    }
+                    for (int i = 0; i < 16; ++i)
+                        if ((unsigned)(32 * k + 16 * (i >> 3) + (i & 7) - first_seen) >= seen || (gone >> (2 * k + (i >> 3)) & 1)) sc[k][i] = -__builtin_inff();
             }
             float top = fmaxf(sc[0][0], sc[1][0]);
 #pragma unroll
             for (int i = 1; i < 16; ++i) top = fmaxf(top, fmaxf(sc[0][i], sc[1][i]));
-            top = fmaxf(top, from_xor<32>(top));
-            float s_top = fmaxf(sv0[0], sv0[1]);
-#pragma unroll
-            for (int k = 1; k < 64; k <<= 1) s_top = fmaxf(s_top, __shfl_xor(s_top, k, 64));
-            const bool scale_grown = s_top >= ref && s_top < __builtin_inff();
-            if (__any(top > m + GROW) || scale_grown) {
+            top = across_halves(top);
+            const float s_most = fmaxf(gv[0], gv[1]);
+            if (__any(top > m + GROW) || __any(s_most >= ref)) {
                 const float to = top > m + GROW ? top : m;      // (-inf where nothing has been seen)
                 float turn = m == -__builtin_inff() ? 0.f : ex2(m - to);
                 m = to; l *= turn;
-                if (scale_grown) {
-                    const float now = __builtin_amdgcn_ldexpf(1.f, min(__builtin_amdgcn_frexp_expf(s_top), 127));
-                    turn *= ref / now; ref = now;
+                float s_top = s_most;
+#pragma unroll
+                for (int k = 1; k < 64; k <<= 1) s_top = fmaxf(s_top, __shfl_xor(s_top, k, 64));
+                if (s_top >= ref && s_top < __builtin_inff()) {
+                    const int e = min(__builtin_amdgcn_frexp_expf(s_top), 127);
+                    const float now = __builtin_amdgcn_ldexpf(1.f, e);
+                    turn *= ref / now; ref = now; unref = __builtin_amdgcn_ldexpf(TILE_TOP, -e);
                 }
 #pragma unroll
                 for (int c = 0; c < CT; ++c) o[c] *= turn;
@@ -645,32 +684,33 @@ __global__ __launch_bounds__(64 * W, 2) void kv_attend_tiles_kernel(AttendArgs a
             for (int k = 0; k < 2; ++k)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) { sc[k][i] = ex2(sc[k][i] - base); l += sc[k][i]; }
-            const float sv[2] = {sv0[0] * (TILE_TOP / ref), sv0[1] * (TILE_TOP / ref)};
+            const float sv[2] = {gv[0] * unref, gv[1] * unref};
             unroll<32>([&](auto I) { constexpr int i = I; sc[i >> 4][i & 15] *= row_lane<i & 15>(sv[i >> 4]); });
             if (!all) {
 #pragma unroll
                 for (int k = 0; k < 2; ++k)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) if (hidden[k] >> i & 1) sc[k][i] = 0.f;
+                    for (int i = 0; i < 16; ++i)
+                        if ((unsigned)(32 * k + 16 * (i >> 3) + (i & 7) - first_seen) >= seen || (gone >> (2 * k + (i >> 3)) & 1)) sc[k][i] = 0.f;      // (whatever its scale is)
             }
-            const unsigned char* const vp = vbuf + (n & 1) * DP * VROW;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                h8 pf;
+            for (int k = 0; k < 4; ++k)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) pf[j] = (_Float16)sc[k >> 1][(k & 1) * 8 + j];
-#pragma unroll
-                for (int c = 0; c < CT; ++c) {
-                    const int row = 32 * c + col;
-                    o[c] = mma32(*(const h8*)(vp + row * VROW + (((2 * k + half) ^ (row & 7)) << 4)), pf, o[c]);
-                }
-            }
+                for (int j = 0; j < 8; ++j) pf[k][j] = (_Float16)sc[k >> 1][(k & 1) * 8 + j];
         }
-        if (n + 1 < n_tiles) { sc[0] = next[0]; sc[1] = next[1]; }
-        if (n + 2 < n_tiles) { store_k(n & 1); if (n + 3 < n_tiles) fetch_k(t0 + 3 * TILE); }
-        if (n + 1 < n_tiles) { store_v((n + 1) & 1); if (n + 2 < n_tiles) fetch_v(t0 + 2 * TILE); }
-        __syncthreads();
+        // this wavefront's part of slot n + 1 (of n + 2 where it is a run behind), and its loads for the one after
+        const int slot = n + 1 + later;
+        ids3 = pages_of(n + 4);
+        if (slot <= n_tiles) {
+            store_v(slot & 1);
+            if (slot < n_tiles) { store_k(slot & 1); fetch_v(slot, later ? ids1 : ids0); }
+            if (slot + 1 < n_tiles) fetch_k(slot + 1, later ? ids2 : ids1);
+        }
+        if (n + 1 < n_tiles) fetch_grids(n + 1, ids0);
+        ids0 = ids1; ids1 = ids2; ids2 = ids3;
+        run_ends();
     }
+    if (W > 4 && !later) run_ends();      // as many as the others
     l += from_xor<32>(l);
     if (l != l) m = fmaxf(m, 0.f);      // scores that are all NaN leave the maximum where it was
     if (!row_live) return;
@@ -734,10 +774,11 @@ __global__ __launch_bounds__(256) void kv_attend_tiles_join_kernel(AttendArgs a)
 }
 
 int shares(int dp) { return 256 * (dp == 32 ? resident<32>() : dp == 64 ? resident<64>() : dp <= 128 ? resident<128>() : resident<256>()); }
-constexpr int FEW = 32, WAVES = 8;      // rows of a sequence up to which kv_attend_rows_kernel takes it
+constexpr int FEW = 32;      // rows of a sequence up to which kv_attend_rows_kernel takes it
+int unit_rows_of(int dp) { return 32 * (dp <= 128 ? waves<128>() : waves<256>()); }
 // Row tiles of all sequences that kv_attend_tiles_kernel takes: at most one more per sequence than rows / RT, and one per token or more
 long long most_units(const KvGeometry& g, int n_seqs, long long n_tokens, int rep) {
-    const int rt = 32 * WAVES;
+    const int rt = unit_rows_of(g.dp);
     return std::min(n_tokens * rep / rt + std::min<long long>(n_seqs, n_tokens), n_tokens * cdiv64(rep, rt)) * g.heads;
 }
 size_t room(const KvGeometry& g, bool tiles, long long units, AttendArgs* a, void* ws) {
@@ -746,8 +787,8 @@ size_t room(const KvGeometry& g, bool tiles, long long units, AttendArgs* a, voi
     float* part = ar.get<float>(2 * n * ROWS * g.dp);
     float2* stat = ar.get<float2>(2 * n * ROWS);
     int4* info = ar.get<int4>(n);
-    float* tile_part = ar.get<float>(pieces * 32 * WAVES * g.dp);
-    float2* tile_stat = ar.get<float2>(pieces * 32 * WAVES);
+    float* tile_part = ar.get<float>(pieces * unit_rows_of(g.dp) * g.dp);
+    float2* tile_stat = ar.get<float2>(pieces * unit_rows_of(g.dp));
     if (a) { a->part = part; a->stat = stat; a->info = info; a->tile_part = tile_part; a->tile_stat = tile_stat; }
     return ar.off;
 }
@@ -762,17 +803,17 @@ int attend_rows(tboa_ctx* ctx, const AttendArgs& a) {
 }
 template <int DP>
 int attend_tiles(tboa_ctx* ctx, const AttendArgs& a, long long units) {
-    constexpr int LDS = tiles_lds<DP, WAVES>();
-    const dim3 grid((unsigned)std::max<long long>(units, TILES_TARGET)), block(64 * WAVES);
+    constexpr int LDS = tiles_lds<DP>();
+    const dim3 grid((unsigned)std::max<long long>(units, TILES_TARGET)), block(64 * waves<DP>());
     if (a.g.pt_log >= 6) {
-        TB_HIP(ctx, hipFuncSetAttribute((const void*)kv_attend_tiles_kernel<DP, WAVES, true>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
-        hipLaunchKernelGGL((kv_attend_tiles_kernel<DP, WAVES, true>), grid, block, LDS, ctx->stream, a);
+        TB_HIP(ctx, hipFuncSetAttribute((const void*)kv_attend_tiles_kernel<DP, true>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
+        hipLaunchKernelGGL((kv_attend_tiles_kernel<DP, true>), grid, block, LDS, ctx->stream, a);
     } else {
-        TB_HIP(ctx, hipFuncSetAttribute((const void*)kv_attend_tiles_kernel<DP, WAVES, false>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
-        hipLaunchKernelGGL((kv_attend_tiles_kernel<DP, WAVES, false>), grid, block, LDS, ctx->stream, a);
+        TB_HIP(ctx, hipFuncSetAttribute((const void*)kv_attend_tiles_kernel<DP, false>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
+        hipLaunchKernelGGL((kv_attend_tiles_kernel<DP, false>), grid, block, LDS, ctx->stream, a);
     }
     TB_KERNEL_CHECK(ctx);
-    hipLaunchKernelGGL((kv_attend_tiles_join_kernel<DP, 32 * WAVES>), dim3((unsigned)std::min<long long>(units, TILES_TARGET / 2), 8), dim3(256), 0, ctx->stream, a);
+    hipLaunchKernelGGL((kv_attend_tiles_join_kernel<DP, 32 * waves<DP>()>), dim3((unsigned)std::min<long long>(units, TILES_TARGET / 2), 8), dim3(256), 0, ctx->stream, a);
     TB_KERNEL_CHECK(ctx);
     return 0;
 }
