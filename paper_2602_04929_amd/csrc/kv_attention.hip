@@ -383,8 +383,9 @@ __global__ __launch_bounds__(256) void kv_attend_join_kernel(AttendArgs a) {
 // instructions: the tokens of a tile's rows are ordered so that a lane's 32 scores, as half, are the right operand of O^T += V^T P^T as they stand.
 // A wavefront alternates between a run of matrix instructions, scores of tile n and products with V of tile n - 1, and a run of vector instructions, the softmax of tile n and its part in making
 // the next tile.  Runs end at a barrier; of the two wavefronts of a SIMD one is a run behind the other, so that one multiplies while the other exponentiates.
-// A row's maximum is only followed where it has grown by more than GROW powers of two: up to there the probabilities simply exceed 1.
-constexpr float GROW = 4.f, TILE_TOP = 0x1p11f;      // 2^4 2^11 = 2^15, within half
+// A row's maximum is only followed where it has to be: as long as the sum of a lane's 32 probabilities stays below MOST, so does each of them, and they simply exceed 1 (MOST TILE_TOP = 2^15 is
+// within half); no maximum is formed then.
+constexpr float MOST = 0x1p7f, TILE_TOP = 0x1p8f;
 template <int DP> constexpr int waves() { return DP <= 128 ? 8 : 4; }      // (wider heads need twice the registers)
 template <int DP> constexpr int permuted() { return DP % 128 == 0 ? 15 : DP % 64 == 0 ? 7 : 3; }      // bits of a piece's number that K's rows are XORed into
 template <int DP> constexpr int tiles_lds() { return 2 * 2 * TILE * DP * 2; }
@@ -491,28 +492,42 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
     // raw levels of K of one tile and V of the one before it, zero of a piece's token (K), of token 16 g + lane % 16 (V)
     u4 kraw[PP], vraw[PP];
     float kz[PP], vz[PP];
+    // where tile n's levels and grids of this head begin, in a page that holds all of it
+    auto levels_at = [&](int n, int ids) { return base_of(page_in(ids, 0)) + head_levels + (((lo + n * TILE) & in_page) * DP); };
+    auto grids_at = [&](int n, int ids) { return base_of(page_in(ids, 0)) + a.g.kg_at + (head_grids + (((lo + n * TILE) & in_page) >> st_log)) * 8; };
+    const unsigned k_to_v = (unsigned)(a.g.vg_at - a.g.kg_at);
     auto fetch_k = [&](int n, int ids) {
         const int t0 = lo + n * TILE;
 #pragma unroll
         for (int j = 0; j < PP; ++j) {
-            const int i = tid + j * 64 * W, tk = i / (DP / 16), c = i % (DP / 16) * 16;
+            const unsigned i = tid + j * 64 * W, tk = i / (DP / 16);
             if (!EVEN && i >= PIECES) break;
-            const unsigned char* const page = base_of(page_in(ids, tk >> 4));
-            const int o = (t0 + tk) & in_page;
-            kraw[j] = *(const u4*)(page + head_levels + (long long)(o * DP + c));
-            kz[j] = t0 + tk < end ? *(const float*)(page + a.g.kg_at + (head_grids + (o >> st_log)) * 8 + 4) : 0.f;
+            if constexpr (WIDE) {
+                kraw[j] = *(const u4*)(levels_at(n, ids) + i * 16);
+                kz[j] = *(const float*)(grids_at(n, ids) + ((tk >> st_log) * 8 + 4));
+            } else {
+                const unsigned char* const page = base_of(page_in(ids, tk >> 4));
+                const int o = (t0 + (int)tk) & in_page;
+                kraw[j] = *(const u4*)(page + head_levels + (o * DP + i % (DP / 16) * 16));
+                kz[j] = *(const float*)(page + a.g.kg_at + (head_grids + (o >> st_log)) * 8 + 4);
+            }
         }
     };
     auto fetch_v = [&](int n, int ids) {
         const int t0 = lo + n * TILE;
 #pragma unroll
         for (int j = 0; j < PP; ++j) {
-            const int i = tid + j * 64 * W, g = i / DP, c = i % DP;
+            const unsigned i = tid + j * 64 * W, g = i / DP;
             if (!EVEN && i >= PIECES) break;
-            const unsigned char* const page = base_of(page_in(ids, g));
-            const int o = (t0 + 16 * g) & in_page;
-            vraw[j] = *(const u4*)(page + a.g.v_at + head_levels + (long long)(o * DP + c * 16));
-            vz[j] = t0 + 16 * g + i16 < end ? *(const float*)(page + a.g.vg_at + (head_grids + ((o + i16) >> st_log)) * 8 + 4) : 0.f;
+            if constexpr (WIDE) {
+                vraw[j] = *(const u4*)(levels_at(n, ids) + a.g.v_at + i * 16);
+                vz[j] = *(const float*)(grids_at(n, ids) + k_to_v + (((16 * g + i16) >> st_log) * 8 + 4));
+            } else {
+                const unsigned char* const page = base_of(page_in(ids, g));
+                const int o = (t0 + 16 * (int)g) & in_page;
+                vraw[j] = *(const u4*)(page + a.g.v_at + head_levels + (o * DP + i % DP * 16));
+                vz[j] = *(const float*)(page + a.g.vg_at + (head_grids + ((o + i16) >> st_log)) * 8 + 4);
+            }
         }
     };
     auto store_k = [&](int buf) {
@@ -535,7 +550,7 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
             const int i = tid + j * 64 * W, g = i / DP, c = i % DP;
             if (!EVEN && i >= PIECES) break;
             h2 zo[8];
-            const unsigned one = __builtin_bit_cast(unsigned short, (_Float16)(-1024.f - vz[j]));
+            const unsigned one = __builtin_bit_cast(unsigned short, (_Float16)(-1024.f - fminf(fmaxf(vz[j], 0.f), 255.f)));      // (what is behind the last token may be anything)
             const unsigned pair = one | (unsigned)__builtin_amdgcn_mov_dpp((int)one, 0xB1, 0xf, 0xf, true) << 16;
             unroll<8>([&](auto I) { constexpr int n = I; zo[n] = __builtin_bit_cast(h2, row_lane<2 * n>(pair)); });
             unsigned char* const p = vbuf + buf * DP * VROW + c * VROW;
@@ -551,16 +566,23 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
         there = 0;
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            const int t = t0 + 32 * k + 16 * (i16 >> 3) + 8 * half + (i16 & 7), pg = page_in(ids, 2 * k + (i16 >> 3));
-            const bool ok = pg >= 0 && pg < a.g.n_pages;
-            const unsigned char* const page = base_of(pg);
-            if constexpr (WIDE) there |= ok ? 3u << 2 * k : 0u;
-            else { const unsigned long long b = __ballot(ok); there |= (unsigned)(b & 1) << 2 * k | (unsigned)(b >> 8 & 1) << (2 * k + 1); }
-            gk[k] = 1.f; gv[k] = 0.f;
-            if (ok && t < end) {
-                const long long at = (head_grids + ((t & in_page) >> st_log)) * 8;
-                gk[k] = *(const float*)(page + a.g.kg_at + at); gv[k] = *(const float*)(page + a.g.vg_at + at);
+            const unsigned at = 32 * k + 16 * (i16 >> 3) + 8 * half + (i16 & 7);
+            if constexpr (WIDE) {
+                const int pg = page_in(ids, 0);
+                there |= pg >= 0 && pg < a.g.n_pages ? 3u << 2 * k : 0u;
+                const unsigned char* const g = grids_at(n, ids);
+                gk[k] = *(const float*)(g + (at >> st_log) * 8); gv[k] = *(const float*)(g + k_to_v + (at >> st_log) * 8);
+            } else {
+                const int pg = page_in(ids, 2 * k + (i16 >> 3)), o = (t0 + (int)at) & in_page;
+                const unsigned long long b = __ballot(pg >= 0 && pg < a.g.n_pages);
+                there |= (unsigned)(b & 1) << 2 * k | (unsigned)(b >> 8 & 1) << (2 * k + 1);
+                const unsigned char* const g = base_of(pg) + a.g.kg_at + (head_grids + (o >> st_log)) * 8;
+                gk[k] = *(const float*)g; gv[k] = *(const float*)(g + k_to_v);
             }
+        }
+        if (t0 + TILE > end || there != 15u) {      // what is not there counts for no scale
+#pragma unroll
+            for (int k = 0; k < 2; ++k) if (t0 + 32 * k + 16 * (i16 >> 3) + 8 * half + (i16 & 7) >= end || !(there >> (2 * k + (i16 >> 3)) & 1)) { gk[k] = 1.f; gv[k] = 0.f; }
         }
     };
 
@@ -646,29 +668,24 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
         const int t0 = lo + n * TILE;
         if (qk) {
             const float sk[2] = {gk[0] * unit, gk[1] * unit};
-            const bool all = t0 >= all0 && t0 + TILE - 1 <= all1 && there == 15u;
-            unroll<32>([&](auto I) { constexpr int i = I; sc[i >> 4][i & 15] *= row_lane<i & 15>(sk[i >> 4]); });
-            // places 32 k + 16 (i / 8) + i % 8 from first_seen on, seen of them, are seen by this row
-            const int first_seen = low - t0 - 8 * half;
-            const unsigned seen = (unsigned)max(min(pos, end - 1) - low + 1, 0);
-            const unsigned gone = ~there;
-            if (!all) {
-#pragma unroll
-                for (int k = 0; k < 2; ++k)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if ((unsigned)(32 * k + 16 * (i >> 3) + (i & 7) - first_seen) >= seen || (gone >> (2 * k + (i >> 3)) & 1)) sc[k][i] = -__builtin_inff();
-            }
-            float top = fmaxf(sc[0][0], sc[1][0]);
-#pragma unroll
-            for (int i = 1; i < 16; ++i) top = fmaxf(top, fmaxf(sc[0][i], sc[1][i]));
-            top = across_halves(top);
+            float p[32], part[4] = {0.f, 0.f, 0.f, 0.f};
+            unroll<32>([&](auto I) { constexpr int i = I; sc[i >> 4][i & 15] *= row_lane<i & 15>(sk[i >> 4]); p[i] = ex2(sc[i >> 4][i & 15] - m); part[i & 3] += p[i]; });
+            float sum = (part[0] + part[1]) + (part[2] + part[3]);
             const float s_most = fmaxf(gv[0], gv[1]);
-            if (__any(top > m + GROW) || __any(s_most >= ref)) {
-                const float to = top > m + GROW ? top : m;      // (-inf where nothing has been seen)
-                float turn = m == -__builtin_inff() ? 0.f : ex2(m - to);
+            const bool all = t0 >= all0 && t0 + TILE - 1 <= all1 && there == 15u;
+            if (!all || __any(sum > MOST || s_most >= ref)) {
+                // places 32 k + 16 (i / 8) + i % 8 from first_seen on, seen of them, are seen by this row
+                const int first_seen = low - t0 - 8 * half;
+                const unsigned seen = (unsigned)max(min(pos, end - 1) - low + 1, 0), gone = ~there;
+                float top = -__builtin_inff();
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    if ((unsigned)(32 * (i >> 4) + 16 * (i >> 3 & 1) + (i & 7) - first_seen) >= seen || (gone >> (i >> 3) & 1)) sc[i >> 4][i & 15] = -__builtin_inff();
+                    top = fmaxf(top, sc[i >> 4][i & 15]);
+                }
+                const float to = fmaxf(m, across_halves(top));      // (-inf where nothing has been seen)
+                float turn = m == -__builtin_inff() ? 0.f : ex2(m - to), s_top = s_most;
                 m = to; l *= turn;
-                float s_top = s_most;
 #pragma unroll
                 for (int k = 1; k < 64; k <<= 1) s_top = fmaxf(s_top, __shfl_xor(s_top, k, 64));
                 if (s_top >= ref && s_top < __builtin_inff()) {
@@ -678,25 +695,25 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
                 }
 #pragma unroll
                 for (int c = 0; c < CT; ++c) o[c] *= turn;
+                const float base = m == -__builtin_inff() ? 0.f : m;
+                sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < 32; ++i) { p[i] = ex2(sc[i >> 4][i & 15] - base); sum += p[i]; }
             }
-            const float base = m == -__builtin_inff() ? 0.f : m;
-#pragma unroll
-            for (int k = 0; k < 2; ++k)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) { sc[k][i] = ex2(sc[k][i] - base); l += sc[k][i]; }
+            l += sum;
             const float sv[2] = {gv[0] * unref, gv[1] * unref};
-            unroll<32>([&](auto I) { constexpr int i = I; sc[i >> 4][i & 15] *= row_lane<i & 15>(sv[i >> 4]); });
+            unroll<32>([&](auto I) { constexpr int i = I; p[i] *= row_lane<i & 15>(sv[i >> 4]); });
             if (!all) {
+                const int first_seen = low - t0 - 8 * half;
+                const unsigned seen = (unsigned)max(min(pos, end - 1) - low + 1, 0), gone = ~there;
 #pragma unroll
-                for (int k = 0; k < 2; ++k)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if ((unsigned)(32 * k + 16 * (i >> 3) + (i & 7) - first_seen) >= seen || (gone >> (2 * k + (i >> 3)) & 1)) sc[k][i] = 0.f;      // (whatever its scale is)
+                for (int i = 0; i < 32; ++i)
+                    if ((unsigned)(32 * (i >> 4) + 16 * (i >> 3 & 1) + (i & 7) - first_seen) >= seen || (gone >> (i >> 3) & 1)) p[i] = 0.f;      // (whatever its scale is)
             }
 #pragma unroll
             for (int k = 0; k < 4; ++k)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) pf[k][j] = (_Float16)sc[k >> 1][(k & 1) * 8 + j];
+                for (int j = 0; j < 8; ++j) pf[k][j] = (_Float16)p[8 * k + j];
         }
         // this wavefront's part of slot n + 1 (of n + 2 where it is a run behind), and its loads for the one after
         const int slot = n + 1 + later;
