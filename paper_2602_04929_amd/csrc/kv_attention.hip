@@ -484,49 +484,56 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
     const long long head_levels = (long long)h * DP << a.g.pt_log, head_grids = (long long)h << (a.g.pt_log - a.g.st_log);
     const int in_page = (1 << a.g.pt_log) - 1, st_log = a.g.st_log;
     const int* const pages = a.q.pages + (long long)u.b * a.q.per_seq;
-    // pages of tile n: that of its 16 tokens lane % 4 (a vector load in either case: a scalar one would share its counter with LDS)
+    // pages of tile n: that of its 16 tokens lane % 4 (a vector load in either case: a scalar one would share its counter with LDS).  Place: where the tile's levels and grids lie, from
+    // the head's in the cache's first page on, or the pages where they are several.
     auto pages_of = [&](int n) { return pages[min((lo + n * TILE + 16 * (lane & 3)) >> a.g.pt_log, a.q.per_seq - 1)]; };
-    auto page_in = [&](int ids, int group) { return WIDE ? __builtin_amdgcn_readfirstlane(ids) : __shfl(ids, group, 64); };
-    auto base_of = [&](int pg) { return a.cache + (long long)min(max(pg, 0), (int)a.g.n_pages - 1) * a.g.page_bytes; };
+    auto page_offset = [&](int pg) { return (long long)min(max(pg, 0), (int)a.g.n_pages - 1) * a.g.page_bytes; };
+    struct Place { int ids; bool held; long long lev, grid; };
+    auto place_of = [&](int n, int ids) {
+        Place p{ids, false, 0, 0};
+        if constexpr (WIDE) {
+            const int pg = __builtin_amdgcn_readfirstlane(ids), o = (lo + n * TILE) & in_page;
+            p.held = pg >= 0 && pg < (int)a.g.n_pages;
+            const long long at = page_offset(pg);
+            p.lev = at + o * DP; p.grid = at + (o >> st_log) * 8;
+        }
+        return p;
+    };
+    const unsigned char* const k_levels = a.cache + head_levels, * const v_levels = k_levels + a.g.v_at;
+    const unsigned char* const k_grids = a.cache + a.g.kg_at + head_grids * 8, * const v_grids = a.cache + a.g.vg_at + head_grids * 8;
 
     // raw levels of K of one tile and V of the one before it, zero of a piece's token (K), of token 16 g + lane % 16 (V)
     u4 kraw[PP], vraw[PP];
     float kz[PP], vz[PP];
-    // where tile n's levels and grids of this head begin, in a page that holds all of it
-    auto levels_at = [&](int n, int ids) { return base_of(page_in(ids, 0)) + head_levels + (((lo + n * TILE) & in_page) * DP); };
-    auto grids_at = [&](int n, int ids) { return base_of(page_in(ids, 0)) + a.g.kg_at + (head_grids + (((lo + n * TILE) & in_page) >> st_log)) * 8; };
-    const unsigned k_to_v = (unsigned)(a.g.vg_at - a.g.kg_at);
-    auto fetch_k = [&](int n, int ids) {
-        const int t0 = lo + n * TILE;
+    auto fetch_k = [&](int n, const Place& at) {
 #pragma unroll
         for (int j = 0; j < PP; ++j) {
             const unsigned i = tid + j * 64 * W, tk = i / (DP / 16);
             if (!EVEN && i >= PIECES) break;
             if constexpr (WIDE) {
-                kraw[j] = *(const u4*)(levels_at(n, ids) + i * 16);
-                kz[j] = *(const float*)(grids_at(n, ids) + ((tk >> st_log) * 8 + 4));
+                kraw[j] = *(const u4*)(k_levels + at.lev + i * 16);
+                kz[j] = *(const float*)(k_grids + at.grid + ((tk >> st_log) * 8 + 4));
             } else {
-                const unsigned char* const page = base_of(page_in(ids, tk >> 4));
-                const int o = (t0 + (int)tk) & in_page;
-                kraw[j] = *(const u4*)(page + head_levels + (o * DP + i % (DP / 16) * 16));
-                kz[j] = *(const float*)(page + a.g.kg_at + (head_grids + (o >> st_log)) * 8 + 4);
+                const long long page = page_offset(__shfl(at.ids, tk >> 4, 64));
+                const int o = (lo + n * TILE + (int)tk) & in_page;
+                kraw[j] = *(const u4*)(k_levels + page + (o * DP + i % (DP / 16) * 16));
+                kz[j] = *(const float*)(k_grids + page + ((o >> st_log) * 8 + 4));
             }
         }
     };
-    auto fetch_v = [&](int n, int ids) {
-        const int t0 = lo + n * TILE;
+    auto fetch_v = [&](int n, const Place& at) {
 #pragma unroll
         for (int j = 0; j < PP; ++j) {
             const unsigned i = tid + j * 64 * W, g = i / DP;
             if (!EVEN && i >= PIECES) break;
             if constexpr (WIDE) {
-                vraw[j] = *(const u4*)(levels_at(n, ids) + a.g.v_at + i * 16);
-                vz[j] = *(const float*)(grids_at(n, ids) + k_to_v + (((16 * g + i16) >> st_log) * 8 + 4));
+                vraw[j] = *(const u4*)(v_levels + at.lev + i * 16);
+                vz[j] = *(const float*)(v_grids + at.grid + (((16 * g + i16) >> st_log) * 8 + 4));
             } else {
-                const unsigned char* const page = base_of(page_in(ids, g));
-                const int o = (t0 + 16 * (int)g) & in_page;
-                vraw[j] = *(const u4*)(page + a.g.v_at + head_levels + (o * DP + i % DP * 16));
-                vz[j] = *(const float*)(page + a.g.vg_at + (head_grids + ((o + i16) >> st_log)) * 8 + 4);
+                const long long page = page_offset(__shfl(at.ids, g, 64));
+                const int o = (lo + n * TILE + 16 * (int)g) & in_page;
+                vraw[j] = *(const u4*)(v_levels + page + (o * DP + i % DP * 16));
+                vz[j] = *(const float*)(v_grids + page + (((o + i16) >> st_log) * 8 + 4));
             }
         }
     };
@@ -561,42 +568,34 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
     // scales of tokens 32 k + 16 (i16 / 8) + 8 half + i16 % 8, k = 0, 1: those of a lane's scores, one in each lane of a row of 16; which groups of 16 tokens there are
     float gk[2], gv[2];
     unsigned there = 0;      // bit 2 k + i16 / 8
-    auto fetch_grids = [&](int n, int ids) {
+    auto fetch_grids = [&](int n, const Place& at) {
         const int t0 = lo + n * TILE;
-        there = 0;
+        there = WIDE && at.held ? 15u : 0u;
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            const unsigned at = 32 * k + 16 * (i16 >> 3) + 8 * half + (i16 & 7);
-            if constexpr (WIDE) {
-                const int pg = page_in(ids, 0);
-                there |= pg >= 0 && pg < a.g.n_pages ? 3u << 2 * k : 0u;
-                const unsigned char* const g = grids_at(n, ids);
-                gk[k] = *(const float*)(g + (at >> st_log) * 8); gv[k] = *(const float*)(g + k_to_v + (at >> st_log) * 8);
-            } else {
-                const int pg = page_in(ids, 2 * k + (i16 >> 3)), o = (t0 + (int)at) & in_page;
-                const unsigned long long b = __ballot(pg >= 0 && pg < a.g.n_pages);
+            const unsigned in = 32 * k + 16 * (i16 >> 3) + 8 * half + (i16 & 7);
+            if constexpr (WIDE) { gk[k] = *(const float*)(k_grids + at.grid + (in >> st_log) * 8); gv[k] = *(const float*)(v_grids + at.grid + (in >> st_log) * 8); }
+            else {
+                const int pg = __shfl(at.ids, 2 * k + (i16 >> 3), 64), o = (t0 + (int)in) & in_page;
+                const unsigned long long b = __ballot(pg >= 0 && pg < (int)a.g.n_pages);
                 there |= (unsigned)(b & 1) << 2 * k | (unsigned)(b >> 8 & 1) << (2 * k + 1);
-                const unsigned char* const g = base_of(pg) + a.g.kg_at + (head_grids + (o >> st_log)) * 8;
-                gk[k] = *(const float*)g; gv[k] = *(const float*)(g + k_to_v);
+                const long long page = page_offset(pg) + (o >> st_log) * 8;
+                gk[k] = *(const float*)(k_grids + page); gv[k] = *(const float*)(v_grids + page);
             }
-        }
-        if (t0 + TILE > end || there != 15u) {      // what is not there counts for no scale
-#pragma unroll
-            for (int k = 0; k < 2; ++k) if (t0 + 32 * k + 16 * (i16 >> 3) + 8 * half + (i16 & 7) >= end || !(there >> (2 * k + (i16 >> 3)) & 1)) { gk[k] = 1.f; gv[k] = 0.f; }
         }
     };
 
     // Slot n of LDS, buffer n & 1: K of tile n and V of tile n - 1.  Run n of matrix instructions reads it: the first four wavefronts in the 2 n-th stretch between barriers, the others (`later`)
     // in the next one; its buffer is written in the two stretches before, by the later ones first.
     const int later = __builtin_amdgcn_readfirstlane(W > 4 ? wave >> 2 : 0);
-    int ids0 = 0, ids1 = 0, ids2 = 0, ids3 = 0;      // pages of tiles n + 1 .. n + 4
+    Place here{}, next{}, second{};      // of tiles n, n + 1, n + 2
+    int ids = 0;                         // pages of tile n + 3
     if (n_tiles) {
-        const int first = pages_of(0);
-        ids0 = pages_of(1); ids1 = pages_of(2); ids2 = pages_of(3);
-        fetch_k(0, first); fetch_grids(0, first);
+        here = place_of(0, pages_of(0)); next = place_of(1, pages_of(1)); second = place_of(2, pages_of(2));
+        ids = pages_of(3);
+        fetch_k(0, here);
         store_k(0);
-        fetch_v(0, first);
-        if (n_tiles > 1) fetch_k(1, ids0);
+        if (later) { fetch_v(0, here); if (n_tiles > 1) fetch_k(1, next); }
     }
     h8 qf[KS];
     float unit;
@@ -644,10 +643,17 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
     auto v_piece = [&](int buf, int k, int c) { return *(const h8*)(vbuf + buf * DP * VROW + (32 * c + col) * VROW + (((2 * k + half) ^ (col & 7)) << 4)); };
     run_ends();
     if (later) {
-        if (n_tiles > 0) { store_v(1); if (n_tiles > 1) { store_k(1); fetch_v(1, ids0); } if (n_tiles > 2) fetch_k(2, ids1); }
+        if (n_tiles > 0) store_v(1);
+        if (n_tiles > 1) store_k(1);
         run_ends();
     }
     for (int n = 0; n <= n_tiles && n_tiles; ++n) {
+        // what this wavefront adds to slot n + 1, to slot n + 2 where it is a run behind
+        const int slot = n + 1 + later;
+        if (n < n_tiles) fetch_grids(n, here);
+        if (slot <= n_tiles) fetch_v(slot - 1, later ? next : here);
+        if (slot < n_tiles) fetch_k(slot, later ? second : next);
+        const int ids_after = pages_of(n + 4);
         const int buf = n & 1;
         const bool qk = n >= see0 && n < see1, pv = n - 1 >= see0 && n - 1 < see1;
         if (qk) {
@@ -667,6 +673,10 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
         run_ends();
         const int t0 = lo + n * TILE;
         if (qk) {
+            if (t0 + TILE > end || there != 15u) {      // what is not there counts for no scale
+#pragma unroll
+                for (int k = 0; k < 2; ++k) if (t0 + 32 * k + 16 * (i16 >> 3) + 8 * half + (i16 & 7) >= end || !(there >> (2 * k + (i16 >> 3)) & 1)) { gk[k] = 1.f; gv[k] = 0.f; }
+            }
             const float sk[2] = {gk[0] * unit, gk[1] * unit};
             float p[32], part[4] = {0.f, 0.f, 0.f, 0.f};
             unroll<32>([&](auto I) { constexpr int i = I; sc[i >> 4][i & 15] *= row_lane<i & 15>(sk[i >> 4]); p[i] = ex2(sc[i >> 4][i & 15] - m); part[i & 3] += p[i]; });
@@ -715,16 +725,9 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
 #pragma unroll
                 for (int j = 0; j < 8; ++j) pf[k][j] = (_Float16)p[8 * k + j];
         }
-        // this wavefront's part of slot n + 1 (of n + 2 where it is a run behind), and its loads for the one after
-        const int slot = n + 1 + later;
-        ids3 = pages_of(n + 4);
-        if (slot <= n_tiles) {
-            store_v(slot & 1);
-            if (slot < n_tiles) { store_k(slot & 1); fetch_v(slot, later ? ids1 : ids0); }
-            if (slot + 1 < n_tiles) fetch_k(slot + 1, later ? ids2 : ids1);
-        }
-        if (n + 1 < n_tiles) fetch_grids(n + 1, ids0);
-        ids0 = ids1; ids1 = ids2; ids2 = ids3;
+        if (slot <= n_tiles) store_v(slot & 1);
+        if (slot < n_tiles) store_k(slot & 1);
+        here = next; next = second; second = place_of(n + 3, ids); ids = ids_after;
         run_ends();
     }
     if (W > 4 && !later) run_ends();      // as many as the others
