@@ -2,6 +2,7 @@
 #include "kv_cache.h"
 #include <math.h>
 #include <algorithm>
+#include <type_traits>
 
 namespace {
 
@@ -162,7 +163,7 @@ struct AppendArgs {
     KvGeometry g; KvBatch q;
     const T* x[2]; long long ld[2];      // K, V
     Rotation rot; const int* positions;
-    unsigned char* cache; int unit_log;
+    unsigned char* cache; int unit_log; bool vec[2];      // vec: every lane's channels are whole aligned words
 };
 
 // Scale and zero of a block from the ends of its new values and, where it has earlier tokens, from the stored grid; everything in fp64 on what is stored in fp32
@@ -182,147 +183,263 @@ __device__ __forceinline__ Grid block_grid(double lo, double hi, bool bad, bool 
     r.z = rint(-lo / r.s);
     return r;
 }
-__device__ __forceinline__ unsigned char level_of(double v, double s, double inv, double z) {
-    const double t = v * inv;
-    double r = rint(t);
-    if (!(fabs(t - r) < 0.5 - 1e-6)) r = rint(v / s);      // next to a border the quotient itself decides (|t| below 2^10: the product is off by 2^-42 at most)
-    return (unsigned char)fmin(fmax(r + z, 0.0), 255.0);
+template <bool MOST, typename V>
+__device__ __forceinline__ V pick(V a, V b) { return MOST ? fmax(a, b) : fmin(a, b); }
+// 16 values in every lane -> value (lane % 16) over all lanes, in every lane: each step gives half of the values away and keeps the extremes of the other half
+template <bool MOST, typename V>
+__device__ __forceinline__ V extremes(V (&v)[16]) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {      // bit s of the lane chooses among the values' bit s
+        const bool up = lane >> s & 1;
+#pragma unroll
+        for (int i = 0; i < 8 >> s; ++i) {
+            const V keep = up ? v[2 * i + 1] : v[2 * i], give = up ? v[2 * i] : v[2 * i + 1];
+            v[i] = pick<MOST>(keep, __shfl_xor(give, 1 << s, 64));
+        }
+    }
+    V r = v[0];
+    r = pick<MOST>(r, __shfl_xor(r, 16, 64)); r = pick<MOST>(r, __shfl_xor(r, 32, 64));
+    return r;
 }
 
-// One workgroup per unit of max(16, scale_tokens) tokens of a sequence, head, and K or V.  A tile of 16 tokens goes through LDS; 16 lanes per token hold its channels, rotated in fp64
-// (products of 24 bits are exact there), find the ends, and after the block's grid stands turn them into levels.
-template <typename T, int NC>
-__global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs<T> a) {
-    constexpr int DP = 16 * NC;
-    __shared__ float xs[16][DP + 4];
-    __shared__ __align__(16) unsigned char lev[16 * DP];
-    __shared__ double tlo[16], thi[16];
-    __shared__ int tbad[16];
-    const int h = blockIdx.y, kv = blockIdx.z, ul = a.unit_log;
+__device__ __forceinline__ float lane_float(float v, int lane) { return __uint_as_float((unsigned)__builtin_amdgcn_readlane((int)__float_as_uint(v), lane)); }
+
+template <int CPL, typename T>
+__device__ __forceinline__ void load_row(const T* p, bool vec, int n, float (&o)[CPL]) {      // n: channels that there are
+    if (vec && n == CPL) {
+        if constexpr (sizeof(T) == 2 && CPL == 2) { const unsigned w = *(const unsigned*)p; o[0] = __uint_as_float(w << 16); o[1] = __uint_as_float(w & 0xffff0000u); return; }
+        if constexpr (sizeof(T) == 2 && CPL == 4) { const uint2 w = *(const uint2*)p; o[0] = __uint_as_float(w.x << 16); o[1] = __uint_as_float(w.x & 0xffff0000u); o[2] = __uint_as_float(w.y << 16); o[3] = __uint_as_float(w.y & 0xffff0000u); return; }
+        if constexpr (sizeof(T) == 4 && CPL == 2) { const float2 w = *(const float2*)p; o[0] = w.x; o[1] = w.y; return; }
+        if constexpr (sizeof(T) == 4 && CPL == 4) { const float4 w = *(const float4*)p; o[0] = w.x; o[1] = w.y; o[2] = w.z; o[3] = w.w; return; }
+    }
+#pragma unroll
+    for (int j = 0; j < CPL; ++j) { o[j] = 0.f; if (j < n) o[j] = to_f32(p[j]); }
+}
+
+// What a wavefront does with 16 tokens of a head: lane l holds channels CPL l .. CPL l + CPL - 1 of all of them, so a token's row is one coalesced access, the ends of all tokens come out of one
+// exchange that halves the values at every step, lane t of each row of 16 then makes the grid of token t's block, and what a lane writes are whole pieces (16 bytes of a channel of V) or parts
+// of a row that its neighbours complete.
+// ROT: keys, rotated in fp64 (products of 24 bits are exact there); else the inputs themselves, in fp32.  Levels come from fp32 products, and where such a product lies within 2^-20 of a border from
+// the fp64 quotient.
+template <typename T, int CPL, bool ROT>
+struct AppendTile {
+    typedef typename std::conditional<ROT, double, float>::type V;
+    const AppendArgs<T>& a;
+    int kv, c0, mine, lane;      // channels from c0 on, mine of them
+    bool vec;
+    V v[16][CPL];
+
+    __device__ __forceinline__ AppendTile(const AppendArgs<T>& args, int kv_) : a(args), kv(kv_) {
+        lane = threadIdx.x & 63; c0 = CPL * lane; mine = min(max(a.g.dh - c0, 0), CPL); vec = a.vec[kv];
+    }
+    // row: of the tile's first token; p: its place; fresh: which of the 16 are new (the same for the wavefront)
+    __device__ __forceinline__ void fetch(int row, int p, int h, unsigned fresh) {
+        const long long ld = a.ld[kv];
+        const T* const src = a.x[kv] + (long long)row * ld + (long long)h * a.g.dh;
+        float raw[16][CPL];
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            if (fresh >> r & 1) load_row<CPL>(src + r * ld + c0, vec, mine, raw[r]);
+        const bool adjacent = a.rot.adjacent, in_lane = adjacent && CPL > 1, by_lane = !adjacent && a.rot.dim / 2 % CPL == 0;
+        const int rot = a.rot.dim, half = rot / 2, away = half / CPL;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            if (!(fresh >> r & 1)) {
+#pragma unroll
+                for (int i = 0; i < CPL; ++i) v[r][i] = 0;
+                continue;
+            }
+            if constexpr (!ROT) {
+#pragma unroll
+                for (int i = 0; i < CPL; ++i) v[r][i] = raw[r][i];
+            } else {
+                const long long at = a.positions ? a.positions[row + r] : p + r;
+                const bool known = at >= 0 && at < a.rot.positions;
+                const float* const tab = a.rot.table + (known ? at : 0) * rot;
+                float other[CPL];
+#pragma unroll
+                for (int i = 0; i < CPL; ++i) {
+                    int pair; bool second;
+                    if (in_lane) other[i] = raw[r][i ^ (CPL > 1)];
+                    else if (by_lane) other[i] = __shfl(raw[r][i], (lane < away ? lane + away : lane - away) & 63, 64);      // (beyond rot: not used)
+                    else { other[i] = 0.f; if (c0 + i < rot) other[i] = to_f32(src[r * ld + partner(c0 + i, a.rot, pair, second)]); }
+                }
+#pragma unroll
+                for (int i = 0; i < CPL; ++i) {
+                    const int c = c0 + i;
+                    v[r][i] = (double)raw[r][i];
+                    if (c < rot) {
+                        int pair; bool second;
+                        partner(c, a.rot, pair, second);
+                        const double cs = (double)(known ? tab[pair] : __builtin_nanf("")), sn = (double)(known ? tab[half + pair] : __builtin_nanf(""));
+                        v[r][i] = second ? v[r][i] * cs + (double)other[i] * sn : v[r][i] * cs - (double)other[i] * sn;
+                    }
+                }
+            }
+        }
+    }
+    // ends of token lane % 16, and whether one of its values is no number
+    __device__ __forceinline__ void ends(double& lo, double& hi, bool& bad) {
+        V l[16], u[16];
+        unsigned wrong = 0;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            l[r] = u[r] = 0;
+#pragma unroll
+            for (int i = 0; i < CPL; ++i) { l[r] = pick<false>(l[r], v[r][i]); u[r] = pick<true>(u[r], v[r][i]); if (!isfinite(v[r][i])) wrong |= 1u << r; }
+        }
+        lo = (double)extremes<false>(l); hi = (double)extremes<true>(u);
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) wrong |= (unsigned)__shfl_xor((int)wrong, o, 64);
+        bad = wrong >> (lane & 15) & 1;
+    }
+    // levels of the new tokens and, where g (of token lane % 16's block) has grown, of the tile's first `before` tokens
+    __device__ __forceinline__ void put(unsigned char* tile, unsigned fresh, int before, const Grid& g) {
+        const int dp = a.g.dp, dh = a.g.dh;
+        const unsigned moved = (unsigned)(__ballot(g.grown) & 0xffffu) & ((1u << before) - 1), set = fresh | moved;
+        if (!set) return;
+        const float inv = (float)(1.0 / g.s), z = (float)g.z;
+        unsigned words[CPL][4] = {};      // V: four tokens of a channel each
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            if (!(set >> r & 1)) continue;
+            const float iv = lane_float(inv, r), zr = lane_float(z, r);      // (not a shuffle: lanes may be switched off where it is used)
+            const double s1 = lane_value(g.s, r);
+            unsigned q[CPL];
+            if (fresh >> r & 1) {
+#pragma unroll
+                for (int i = 0; i < CPL; ++i) {
+                    const float x = (float)v[r][i] * iv;
+                    float n = rintf(x);
+                    if (!(fabsf(x - n) < 0.5f - (fabsf(x) * 0x1p-20f + 0x1p-20f))) n = (float)rint((double)v[r][i] / s1);
+                    q[i] = (unsigned)fminf(fmaxf(n + zr, 0.f), 255.f);      // (NaN: 0)
+                }
+            } else {
+                const double s0 = lane_value(g.s0, r), z0 = lane_value(g.z0, r);
+#pragma unroll
+                for (int i = 0; i < CPL; ++i) {
+                    const int c = min(c0 + i, dh - 1);
+                    const double w = ((double)tile[kv ? c * 16 + r : r * dp + c] - z0) * s0;
+                    q[i] = (unsigned)fmin(fmax(rint(w / s1) + (double)zr, 0.0), 255.0);
+                }
+            }
+            if (kv) {
+#pragma unroll
+                for (int i = 0; i < CPL; ++i) words[i][r >> 2] |= q[i] << 8 * (r & 3);
+            } else {
+                unsigned char* const p = tile + r * dp + c0;
+                if constexpr (CPL == 2) { if (mine == 2) { *(unsigned short*)p = (unsigned short)(q[0] | q[1] << 8); continue; } }
+                if constexpr (CPL == 4) { if (mine == 4) { *(unsigned*)p = q[0] | q[1] << 8 | q[2] << 16 | q[3] << 24; continue; } }
+#pragma unroll
+                for (int i = 0; i < CPL; ++i) if (i < mine) p[i] = (unsigned char)q[i];
+            }
+        }
+        if (kv) {
+#pragma unroll
+            for (int i = 0; i < CPL; ++i) {
+                if (i >= mine) continue;
+                unsigned char* const p = tile + (c0 + i) * 16;
+                if (set == 0xffffu) *(uint4*)p = make_uint4(words[i][0], words[i][1], words[i][2], words[i][3]);
+                else {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) if (set >> r & 1) p[r] = (unsigned char)(words[i][r >> 2] >> 8 * (r & 3));
+                }
+            }
+        }
+    }
+};
+
+// A unit of max(16, scale_tokens) tokens of a sequence
+struct Unit {
+    int first, place, end, row0;      // first place that gets a token, the unit's first place and the end of its places; row of place p: row0 + p
+    unsigned char* page;
+    int in_page;
+};
+
+template <typename T, int CPL, bool ROT, bool MANY>
+__device__ __forceinline__ void append_unit(const AppendArgs<T>& a, const Unit& u, int kv) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, st_log = a.g.st_log, st = 1 << st_log, pt = 1 << a.g.pt_log;
+    AppendTile<T, CPL, ROT> t(a, kv);
+    auto fresh_of = [&](int p) {      // of 16 places from p on, those that get a token
+        const int from = max(u.first - p, 0), to = min(max(u.end - p, 0), 16);
+        return from < to ? ((1u << to) - 1) & ~((1u << from) - 1) : 0u;
+    };
+    auto grids_of = [&](int h) { return (float2*)(u.page + (kv ? a.g.vg_at : a.g.kg_at)) + ((long long)h << (a.g.pt_log - st_log)) + (u.in_page >> st_log); };
+    auto levels_of = [&](int h) { return u.page + (kv ? a.g.v_at : 0) + ((long long)h * pt + u.in_page) * a.g.dp; };
+    if constexpr (!MANY) {
+        const unsigned fresh = __builtin_amdgcn_readfirstlane(fresh_of(u.place));
+        const int tok = lane & 15, t_block = tok & ~(st - 1), p_block = u.place + t_block;
+        const bool touched = p_block < u.end && p_block + st > u.first, had = touched && p_block < u.first;
+        const int per = (a.g.heads + (int)gridDim.y * 4 - 1) / ((int)gridDim.y * 4), h0 = ((int)blockIdx.y * 4 + wave) * per, h1 = min(h0 + per, a.g.heads);
+        for (int h = h0; h < h1; ++h) {
+            float2* const grid = grids_of(h) + (tok >> st_log);
+            float2 old = make_float2(0.f, 0.f);
+            if (had) old = *grid;
+            t.fetch(u.row0 + u.place, u.place, h, fresh);
+            double lo, hi;
+            bool bad;
+            t.ends(lo, hi, bad);
+            for (int o = 1; o < st; o <<= 1) { lo = fmin(lo, __shfl_xor(lo, o, 64)); hi = fmax(hi, __shfl_xor(hi, o, 64)); bad |= __shfl_xor((int)bad, o, 64) != 0; }      // (st <= 16: within the row)
+            const Grid g = block_grid(lo, hi, bad, had, old.x, old.y);
+            t.put(levels_of(h), fresh, min(max(u.first - u.place, 0), 16), g);
+            if (touched && lane < 16 && tok == t_block) *grid = make_float2((float)g.s, (float)g.z);
+        }
+    } else {
+        __shared__ double ends[2][4];
+        __shared__ int bads[4];
+        const int h = blockIdx.y, tiles = 1 << (a.unit_log - 4);
+        const bool had = u.place < u.first, once = tiles <= 4;      // once: a tile for each wavefront, whose values stay where they are
+        double lo = 0.0, hi = 0.0;
+        bool bad = false;
+        for (int j = wave; j < tiles; j += 4) {
+            const unsigned fresh = __builtin_amdgcn_readfirstlane(fresh_of(u.place + 16 * j));
+            if (!fresh) continue;
+            t.fetch(u.row0 + u.place + 16 * j, u.place + 16 * j, h, fresh);
+            double l, m;
+            bool w;
+            t.ends(l, m, w);
+#pragma unroll
+            for (int o = 1; o < 16; o <<= 1) { l = fmin(l, __shfl_xor(l, o, 64)); m = fmax(m, __shfl_xor(m, o, 64)); w |= __shfl_xor((int)w, o, 64) != 0; }
+            lo = fmin(lo, l); hi = fmax(hi, m); bad |= w;
+        }
+        if (lane == 0) { ends[0][wave] = lo; ends[1][wave] = hi; bads[wave] = bad; }
+        float2* const grid = grids_of(h);
+        float2 old = make_float2(0.f, 0.f);
+        if (had) old = *grid;
+        __syncthreads();
+        lo = fmin(fmin(ends[0][0], ends[0][1]), fmin(ends[0][2], ends[0][3])); hi = fmax(fmax(ends[1][0], ends[1][1]), fmax(ends[1][2], ends[1][3]));
+        const Grid g = block_grid(lo, hi, bads[0] | bads[1] | bads[2] | bads[3], had, old.x, old.y);
+        if (threadIdx.x == 0) *grid = make_float2((float)g.s, (float)g.z);
+        for (int j = wave; j < tiles; j += 4) {
+            const int p = u.place + 16 * j;
+            const unsigned fresh = __builtin_amdgcn_readfirstlane(fresh_of(p));
+            if (!once && fresh) t.fetch(u.row0 + p, p, h, fresh);
+            t.put(levels_of(h) + (long long)16 * j * a.g.dp, fresh, min(max(u.first - p, 0), 16), g);
+        }
+    }
+}
+
+// One workgroup per unit, and its four wavefronts take heads of K (blockIdx.z 0) or V; where a unit is several tiles of 16 tokens (MANY): per unit and head, and they take its tiles.
+template <typename T, int CPL, bool MANY>
+__global__ __launch_bounds__(256, CPL <= 2 ? 2 : 1) void kv_append_kernel(AppendArgs<T> a) {
+    const int ul = a.unit_log, room = a.q.room;
     int x = blockIdx.x, b;
     KvSeq s;
-    const int room = a.q.room;
     if (!kv_find(a.q, kv_head(a.q), [ul, room](const KvSeq& e) {
             const int p0 = max(e.len - e.n, 0), end = min(e.len, room);
             return end > p0 && e.n > 0 ? ((end - 1) >> ul) - (p0 >> ul) + 1 : 0; }, x, b, s)) return;
-    const int first = max(s.len - s.n, 0);                 // first position that gets a token
-    const int p_unit = ((first >> ul) + x) << ul;
-    const long long page = a.q.pages[(long long)b * a.q.per_seq + (p_unit >> a.g.pt_log)];
-    if (page < 0 || page >= a.g.n_pages) return;
-    const int row0 = s.start + s.n - s.len;                // row of position p: row0 + p
-    unsigned char* const pg = a.cache + page * a.g.page_bytes;
-    const int pt = 1 << a.g.pt_log, o_unit = p_unit & (pt - 1), st_log = a.g.st_log, st = 1 << st_log, dh = a.g.dh;
-    float2* const grids = (float2*)(pg + (kv ? a.g.vg_at : a.g.kg_at)) + ((long long)h << (a.g.pt_log - st_log));
-    const T* const X = a.x[kv] + (long long)h * dh;
-    const long long ld = a.ld[kv];
-    const int tok = threadIdx.x >> 4, sub = threadIdx.x & 15;
-    const int tiles = 1 << (ul - 4), unit_end = min(p_unit + (1 << ul), min(s.len, room));
-    const int rot = kv ? 0 : a.rot.dim;
-
-    double v[NC];
-    auto fetch = [&](int j) {      // values of tile j's tokens, channels sub + 16 i
-        const int p0 = p_unit + 16 * j;
-        __syncthreads();
-        for (int i = threadIdx.x; i < 16 * dh; i += 256) {
-            const int r = i / dh, c = i - r * dh, p = p0 + r;
-            xs[r][c] = p >= first && p < unit_end ? to_f32(X[(row0 + p) * ld + c]) : 0.f;
-        }
-        __syncthreads();
-        const int p = p0 + tok;
-        const bool is_new = p >= first && p < unit_end;
-        long long at = 0;
-        bool known = true;
-        if (rot && is_new) {
-            at = a.positions ? a.positions[row0 + p] : p;
-            known = at >= 0 && at < a.rot.positions;
-        }
-#pragma unroll
-        for (int i = 0; i < NC; ++i) {
-            const int c = sub + 16 * i;
-            v[i] = 0.0;
-            if (c < dh && is_new) {
-                v[i] = (double)xs[tok][c];
-                if (c < rot) {
-                    int pair; bool second;
-                    const double w = (double)xs[tok][partner(c, a.rot, pair, second)];
-                    const double cs = known ? (double)a.rot.table[at * rot + pair] : __builtin_nan(""), sn = known ? (double)a.rot.table[at * rot + rot / 2 + pair] : __builtin_nan("");
-                    v[i] = second ? v[i] * cs + w * sn : v[i] * cs - w * sn;
-                }
-            }
-        }
-    };
-
-    double lo = 0.0, hi = 0.0;
-    int bad = 0;
-    const int span = min(st, 16), t_first = tok & ~(span - 1);
-    for (int j = 0; j < tiles; ++j) {
-        if (p_unit + 16 * j >= unit_end || p_unit + 16 * j + 16 <= first) continue;
-        fetch(j);
-        double l = 0.0, u = 0.0;
-        bool inf = false;
-#pragma unroll
-        for (int i = 0; i < NC; ++i) { l = fmin(l, v[i]); u = fmax(u, v[i]); inf |= !isfinite(v[i]); }
-#pragma unroll
-        for (int o = 1; o < 16; o <<= 1) { l = fmin(l, __shfl_xor(l, o, 64)); u = fmax(u, __shfl_xor(u, o, 64)); inf |= __shfl_xor((int)inf, o, 64) != 0; }
-        if (sub == 0) { tlo[tok] = l; thi[tok] = u; tbad[tok] = inf; }
-        __syncthreads();
-        for (int i = 0; i < span; ++i) { lo = fmin(lo, tlo[t_first + i]); hi = fmax(hi, thi[t_first + i]); bad |= tbad[t_first + i]; }
-    }
-    // this thread's block: the unit (st >= 16), or its token's within the only tile
-    const int block = (o_unit >> st_log) + (st < 16 ? tok >> st_log : 0);
-    const int p_block = p_unit + (st < 16 ? t_first : 0);
-    const bool touched = p_block < unit_end && p_block + st > first;
-    const bool had = touched && p_block < first;
-    float2 old = make_float2(0.f, 0.f);
-    if (had) old = grids[block];
-    const Grid gr = block_grid(lo, hi, bad != 0, had, old.x, old.y);
-    const double inv = 1.0 / gr.s;
-    __syncthreads();      // every stored grid has been read
-    if (touched && sub == 0 && (st < 16 ? (tok & (st - 1)) == 0 : tok == 0)) grids[block] = make_float2((float)gr.s, (float)gr.z);
-
-    unsigned char* const levels = pg + (kv ? a.g.v_at : 0) + (long long)h * pt * DP + (long long)o_unit * DP;
-    for (int j = 0; j < tiles; ++j) {
-        const int p0 = p_unit + 16 * j;
-        if (p0 >= unit_end) break;
-        if (p0 + 16 <= first && !gr.grown) continue;      // (tiles > 1: one block, the same for all threads)
-        if (tiles > 1) fetch(j);
-        const int p = p0 + tok;
-        unsigned char* const tile = levels + (long long)j * 16 * DP;
-        const bool fresh = p >= first && p < unit_end, moved = p < first && gr.grown;      // a grown block: p lies in it, since it has earlier tokens
-#pragma unroll
-        for (int i = 0; i < NC; ++i) {
-            const int c = sub + 16 * i;
-            unsigned char q = 0;
-            if (fresh) q = level_of(v[i], gr.s, inv, gr.z);
-            else if (moved && c < dh) {
-                const double w = ((double)tile[kv ? c * 16 + tok : tok * DP + c] - gr.z0) * gr.s0;
-                q = (unsigned char)fmin(fmax(rint(w / gr.s) + gr.z, 0.0), 255.0);
-            }
-            lev[kv ? c * 16 + tok : tok * DP + c] = q;
-        }
-        // K rows, V bytes of the tokens that have a new level
-        const bool put = fresh || moved;
-        if (sub == 0) tbad[tok] = put;
-        __syncthreads();
-        if (kv) {
-            int all = 1;
-            for (int i = 0; i < 16; ++i) all &= tbad[i];
-            if (all) {
-                for (int c = threadIdx.x; c < dh; c += 256) *(uint4*)(tile + c * 16) = *(const uint4*)(lev + c * 16);
-            } else {
-                for (int c = threadIdx.x; c < 16 * dh; c += 256) if (tbad[c & 15]) tile[c] = lev[c];
-            }
-        } else {
-            const int whole = dh & ~15;
-            for (int c = 16 * threadIdx.x; c < 16 * DP; c += 16 * 256) if (c % DP < whole && tbad[c / DP]) *(uint4*)(tile + c) = *(const uint4*)(lev + c);
-            if (whole < dh)
-                for (int i = threadIdx.x; i < 16 * (dh - whole); i += 256) {
-                    const int r = i / (dh - whole), c = whole + i % (dh - whole);
-                    if (tbad[r]) tile[r * DP + c] = lev[r * DP + c];
-                }
-        }
-        __syncthreads();
-    }
+    Unit u;
+    u.first = max(s.len - s.n, 0);
+    u.place = __builtin_amdgcn_readfirstlane(((u.first >> ul) + x) << ul);
+    u.end = min(u.place + (1 << ul), min(s.len, room));
+    u.row0 = s.start + s.n - s.len;
+    const int page = a.q.pages[(long long)b * a.q.per_seq + (u.place >> a.g.pt_log)];
+    if (page < 0 || page >= (int)a.g.n_pages) return;
+    u.page = a.cache + (long long)page * a.g.page_bytes;
+    u.in_page = u.place & ((1 << a.g.pt_log) - 1);
+    if (blockIdx.z == 0 && a.rot.dim) append_unit<T, CPL, true, MANY>(a, u, 0);
+    else append_unit<T, CPL, false, MANY>(a, u, blockIdx.z);
 }
 
 template <typename T>
@@ -344,19 +461,24 @@ int head_norm_rotate(tboa_ctx* ctx, long long n_tokens, int dh, int nq, const vo
     return 0;
 }
 
-template <typename T>
+template <typename T, int CPL>
 int append(tboa_ctx* ctx, const AppendArgs<T>& a, long long units) {
-    const dim3 grid((unsigned)units, (unsigned)a.g.heads, 2), block(256);
-    switch (a.g.dp) {
-        case 32: hipLaunchKernelGGL((kv_append_kernel<T, 2>), grid, block, 0, ctx->stream, a); break;
-        case 64: hipLaunchKernelGGL((kv_append_kernel<T, 4>), grid, block, 0, ctx->stream, a); break;
-        case 96: hipLaunchKernelGGL((kv_append_kernel<T, 6>), grid, block, 0, ctx->stream, a); break;
-        case 128: hipLaunchKernelGGL((kv_append_kernel<T, 8>), grid, block, 0, ctx->stream, a); break;
-        case 192: hipLaunchKernelGGL((kv_append_kernel<T, 12>), grid, block, 0, ctx->stream, a); break;
-        default: hipLaunchKernelGGL((kv_append_kernel<T, 16>), grid, block, 0, ctx->stream, a);
+    if (a.unit_log > 4) {
+        hipLaunchKernelGGL((kv_append_kernel<T, CPL, true>), dim3((unsigned)units, (unsigned)a.g.heads, 2), dim3(256), 0, ctx->stream, a);
+    } else {
+        // heads that one wavefront goes through: as few as fill the chip (256 compute units, 16 wavefronts each), for the tile is found and the tables are read once for all of them
+        const long long all = units * a.g.heads * 2;
+        const int per = (int)std::min<long long>(std::max<long long>(all / 4096, 1), 8), groups = (a.g.heads + 4 * per - 1) / (4 * per);
+        hipLaunchKernelGGL((kv_append_kernel<T, CPL, false>), dim3((unsigned)units, (unsigned)groups, 2), dim3(256), 0, ctx->stream, a);
     }
     TB_KERNEL_CHECK(ctx);
     return 0;
+}
+template <typename T>
+int append(tboa_ctx* ctx, AppendArgs<T> a, long long units) {
+    const int cpl = a.g.dh <= 64 ? 1 : a.g.dh <= 128 ? 2 : 4, bytes = cpl * (int)sizeof(T);
+    for (int i = 0; i < 2; ++i) a.vec[i] = a.g.dh % cpl == 0 && ((uintptr_t)a.x[i] % bytes) == 0 && a.ld[i] % cpl == 0;
+    return cpl == 1 ? append<T, 1>(ctx, a, units) : cpl == 2 ? append<T, 2>(ctx, a, units) : append<T, 4>(ctx, a, units);
 }
 
 int check_rotation(tboa_ctx* ctx, const char* who, const tboa_rotation* r, int dh, Rotation& out) {
@@ -435,6 +557,6 @@ extern "C" int tboa_kv_cache_append(tboa_ctx* ctx, const tboa_kv_cache_desc* des
     const long long units = std::min<long long>(batch->n_tokens, (batch->n_tokens >> unit_log) + 2LL * batch->n_seqs);
     const KvBatch q{batch->n_seqs, batch->pages_per_seq, (int)batch->n_tokens, batch->pages_per_seq * desc->page_tokens, batch->starts, batch->lens, batch->pages};
     KvDevice dev(ctx->device);
-    if (dtype == TBOA_F32) return append<float>(ctx, AppendArgs<float>{g, q, {(const float*)K, (const float*)V}, {ldk, ldv}, rot, positions, (unsigned char*)cache, unit_log}, units);
-    return append<bf16>(ctx, AppendArgs<bf16>{g, q, {(const bf16*)K, (const bf16*)V}, {ldk, ldv}, rot, positions, (unsigned char*)cache, unit_log}, units);
+    if (dtype == TBOA_F32) return append<float>(ctx, AppendArgs<float>{g, q, {(const float*)K, (const float*)V}, {ldk, ldv}, rot, positions, (unsigned char*)cache, unit_log, {}}, units);
+    return append<bf16>(ctx, AppendArgs<bf16>{g, q, {(const bf16*)K, (const bf16*)V}, {ldk, ldv}, rot, positions, (unsigned char*)cache, unit_log, {}}, units);
 }
