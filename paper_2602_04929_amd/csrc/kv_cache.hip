@@ -163,7 +163,7 @@ struct AppendArgs {
     KvGeometry g; KvBatch q;
     const T* x[2]; long long ld[2];      // K, V
     Rotation rot; const int* positions;
-    unsigned char* cache; int unit_log; bool vec[2];      // vec: every lane's channels are whole aligned words
+    unsigned char* cache; int unit_log; bool vec[2], vec_table;      // pieces of 8 channels, rows of the table in aligned pieces
 };
 
 // Scale and zero of a block from the ends of its new values and, where it has earlier tokens, from the stored grid; everything in fp64 on what is stored in fp32
@@ -185,167 +185,177 @@ __device__ __forceinline__ Grid block_grid(double lo, double hi, bool bad, bool 
 }
 template <bool MOST, typename V>
 __device__ __forceinline__ V pick(V a, V b) { return MOST ? fmax(a, b) : fmin(a, b); }
-// 16 values in every lane -> value (lane % 16) over all lanes, in every lane: each step gives half of the values away and keeps the extremes of the other half
-template <bool MOST, typename V>
-__device__ __forceinline__ V extremes(V (&v)[16]) {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {      // bit s of the lane chooses among the values' bit s
-        const bool up = lane >> s & 1;
-#pragma unroll
-        for (int i = 0; i < 8 >> s; ++i) {
-            const V keep = up ? v[2 * i + 1] : v[2 * i], give = up ? v[2 * i] : v[2 * i + 1];
-            v[i] = pick<MOST>(keep, __shfl_xor(give, 1 << s, 64));
-        }
-    }
-    V r = v[0];
-    r = pick<MOST>(r, __shfl_xor(r, 16, 64)); r = pick<MOST>(r, __shfl_xor(r, 32, 64));
-    return r;
+template <int CTRL>
+__device__ __forceinline__ double dpp(double v) {
+    const int lo = __builtin_amdgcn_mov_dpp(__double2loint(v), CTRL, 0xf, 0xf, true), hi = __builtin_amdgcn_mov_dpp(__double2hiint(v), CTRL, 0xf, 0xf, true);
+    return __hiloint2double(hi, lo);
+}
+// over the four lanes of a token
+template <bool MOST>
+__device__ __forceinline__ double of_token(double v) {
+    v = pick<MOST>(v, dpp<0xB1>(v));      // quad_perm 1 0 3 2
+    return pick<MOST>(v, dpp<0x4E>(v));      // 2 3 0 1
 }
 
-__device__ __forceinline__ float lane_float(float v, int lane) { return __uint_as_float((unsigned)__builtin_amdgcn_readlane((int)__float_as_uint(v), lane)); }
-
-template <int CPL, typename T>
-__device__ __forceinline__ void load_row(const T* p, bool vec, int n, float (&o)[CPL]) {      // n: channels that there are
-    if (vec && n == CPL) {
-        if constexpr (sizeof(T) == 2 && CPL == 2) { const unsigned w = *(const unsigned*)p; o[0] = __uint_as_float(w << 16); o[1] = __uint_as_float(w & 0xffff0000u); return; }
-        if constexpr (sizeof(T) == 2 && CPL == 4) { const uint2 w = *(const uint2*)p; o[0] = __uint_as_float(w.x << 16); o[1] = __uint_as_float(w.x & 0xffff0000u); o[2] = __uint_as_float(w.y << 16); o[3] = __uint_as_float(w.y & 0xffff0000u); return; }
-        if constexpr (sizeof(T) == 4 && CPL == 2) { const float2 w = *(const float2*)p; o[0] = w.x; o[1] = w.y; return; }
-        if constexpr (sizeof(T) == 4 && CPL == 4) { const float4 w = *(const float4*)p; o[0] = w.x; o[1] = w.y; o[2] = w.z; o[3] = w.w; return; }
-    }
+template <typename T>
+__device__ __forceinline__ void load_piece(const T* p, bool vec, int n, float (&o)[8]) {      // n of 8 channels are there
+    if (vec && n == 8) { load8(p, o); return; }
 #pragma unroll
-    for (int j = 0; j < CPL; ++j) { o[j] = 0.f; if (j < n) o[j] = to_f32(p[j]); }
+    for (int j = 0; j < 8; ++j) { o[j] = 0.f; if (j < n) o[j] = to_f32(p[j]); }
 }
 
-// What a wavefront does with 16 tokens of a head: lane l holds channels CPL l .. CPL l + CPL - 1 of all of them, so a token's row is one coalesced access, the ends of all tokens come out of one
-// exchange that halves the values at every step, lane t of each row of 16 then makes the grid of token t's block, and what a lane writes are whole pieces (16 bytes of a channel of V) or parts
-// of a row that its neighbours complete.
-// ROT: keys, rotated in fp64 (products of 24 bits are exact there); else the inputs themselves, in fp32.  Levels come from fp32 products, and where such a product lies within 2^-20 of a border from
-// the fp64 quotient.
-template <typename T, int CPL, bool ROT>
+// What a wavefront does with 16 tokens of a head.  Four lanes per token, NP pieces of 8 channels in each (piece q + 4 i of a token is lane q's): the ends of a token are found in its lanes, whose
+// grid is then theirs, and a token's levels leave as whole pieces; those of V turn by way of LDS into 16 tokens of a channel.
+// ROT: keys, rotated in fp64 (products of 24 bits are exact there); a piece's partners are read once more.  Else the inputs themselves, in fp32.  Levels come from fp32 products, and a piece with such
+// a product within 2^-21 of a border from the fp64 quotients (three roundings are off by 3 * 2^-24 of it).
+template <typename T, int NP, bool ROT>
 struct AppendTile {
     typedef typename std::conditional<ROT, double, float>::type V;
     const AppendArgs<T>& a;
-    int kv, c0, mine, lane;      // channels from c0 on, mine of them
+    int kv, lane, tok, q;
     bool vec;
-    V v[16][CPL];
+    V v[NP][8];
 
-    __device__ __forceinline__ AppendTile(const AppendArgs<T>& args, int kv_) : a(args), kv(kv_) {
-        lane = threadIdx.x & 63; c0 = CPL * lane; mine = min(max(a.g.dh - c0, 0), CPL); vec = a.vec[kv];
-    }
-    // row: of the tile's first token; p: its place; fresh: which of the 16 are new (the same for the wavefront)
-    __device__ __forceinline__ void fetch(int row, int p, int h, unsigned fresh) {
-        const long long ld = a.ld[kv];
-        const T* const src = a.x[kv] + (long long)row * ld + (long long)h * a.g.dh;
-        float raw[16][CPL];
+    __device__ __forceinline__ AppendTile(const AppendArgs<T>& args, int kv_) : a(args), kv(kv_) { lane = threadIdx.x & 63; tok = lane >> 2; q = lane & 3; vec = a.vec[kv]; }
+    __device__ __forceinline__ int channel(int i) const { return 8 * (q + 4 * i); }
+    // row, p: of the tile's first token, its place; fresh: this lane's token is new
+    __device__ __forceinline__ void fetch(int row, int p, int h, bool fresh) {
+        const int dh = a.g.dh, rot = a.rot.dim, half = rot / 2;
+        const T* const src = a.x[kv] + (long long)(row + tok) * a.ld[kv] + (long long)h * dh;
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-            if (fresh >> r & 1) load_row<CPL>(src + r * ld + c0, vec, mine, raw[r]);
-        const bool adjacent = a.rot.adjacent, in_lane = adjacent && CPL > 1, by_lane = !adjacent && a.rot.dim / 2 % CPL == 0;
-        const int rot = a.rot.dim, half = rot / 2, away = half / CPL;
+        for (int i = 0; i < NP; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            if (!(fresh >> r & 1)) {
+            for (int j = 0; j < 8; ++j) v[i][j] = 0;
+        if (!fresh) return;
+        float raw[NP][8];
 #pragma unroll
-                for (int i = 0; i < CPL; ++i) v[r][i] = 0;
-                continue;
-            }
-            if constexpr (!ROT) {
+        for (int i = 0; i < NP; ++i) load_piece(src + channel(i), vec, min(max(dh - channel(i), 0), 8), raw[i]);
+        if constexpr (!ROT) {
 #pragma unroll
-                for (int i = 0; i < CPL; ++i) v[r][i] = raw[r][i];
-            } else {
-                const long long at = a.positions ? a.positions[row + r] : p + r;
-                const bool known = at >= 0 && at < a.rot.positions;
-                const float* const tab = a.rot.table + (known ? at : 0) * rot;
-                float other[CPL];
+            for (int i = 0; i < NP; ++i)
 #pragma unroll
-                for (int i = 0; i < CPL; ++i) {
-                    int pair; bool second;
-                    if (in_lane) other[i] = raw[r][i ^ (CPL > 1)];
-                    else if (by_lane) other[i] = __shfl(raw[r][i], (lane < away ? lane + away : lane - away) & 63, 64);      // (beyond rot: not used)
-                    else { other[i] = 0.f; if (c0 + i < rot) other[i] = to_f32(src[r * ld + partner(c0 + i, a.rot, pair, second)]); }
+                for (int j = 0; j < 8; ++j) v[i][j] = raw[i][j];
+        } else {
+            const long long at = a.positions ? a.positions[row + tok] : p + tok;
+            const bool known = at >= 0 && at < a.rot.positions, adjacent = a.rot.adjacent;
+            const float* const tab = a.rot.table + (known ? at : 0) * rot;
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                const int c = channel(i);
+                float other[8], cs[8], sn[8];
+                if (c >= rot) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[i][j] = (double)raw[i][j];
+                    continue;
                 }
+                if (adjacent) {
 #pragma unroll
-                for (int i = 0; i < CPL; ++i) {
-                    const int c = c0 + i;
-                    v[r][i] = (double)raw[r][i];
-                    if (c < rot) {
-                        int pair; bool second;
-                        partner(c, a.rot, pair, second);
-                        const double cs = (double)(known ? tab[pair] : __builtin_nanf("")), sn = (double)(known ? tab[half + pair] : __builtin_nanf(""));
-                        v[r][i] = second ? v[r][i] * cs + (double)other[i] * sn : v[r][i] * cs - (double)other[i] * sn;
+                    for (int j = 0; j < 8; ++j) other[j] = raw[i][j ^ 1];
+                    if (a.vec_table) {
+                        const float4 x = *(const float4*)(tab + c / 2), y = *(const float4*)(tab + half + c / 2);
+                        cs[0] = cs[1] = x.x; cs[2] = cs[3] = x.y; cs[4] = cs[5] = x.z; cs[6] = cs[7] = x.w;
+                        sn[0] = -y.x; sn[1] = y.x; sn[2] = -y.y; sn[3] = y.y; sn[4] = -y.z; sn[5] = y.z; sn[6] = -y.w; sn[7] = y.w;
+                    }
+                } else if (a.vec_table && vec) {      // a piece is of one half
+                    const bool second = c >= half;
+                    load8(src + (second ? c - half : c + half), other);
+                    load8(tab + (second ? c - half : c), cs); load8(tab + (second ? c : c + half), sn);
+                    if (!second) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) sn[j] = -sn[j];
                     }
                 }
+                if (!a.vec_table || (!adjacent && !vec)) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        other[j] = cs[j] = sn[j] = 0.f;
+                        if (c + j < rot) {
+                            int pair; bool second;
+                            other[j] = to_f32(src[partner(c + j, a.rot, pair, second)]);
+                            cs[j] = tab[pair]; sn[j] = second ? tab[half + pair] : -tab[half + pair];
+                        } else cs[j] = 1.f;
+                    }
+                }
+                const double lost = known ? 0.0 : __builtin_nan("");
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    v[i][j] = (double)raw[i][j] * (double)cs[j] + (double)other[j] * (double)sn[j];
+                    if (!known && c + j < rot) v[i][j] = lost;
+                }
             }
         }
     }
-    // ends of token lane % 16, and whether one of its values is no number
+    // ends of this lane's token, and whether one of its values is no number
     __device__ __forceinline__ void ends(double& lo, double& hi, bool& bad) {
-        V l[16], u[16];
-        unsigned wrong = 0;
+        V l = 0, u = 0, none = 0;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            l[r] = u[r] = 0;
+        for (int i = 0; i < NP; ++i)
 #pragma unroll
-            for (int i = 0; i < CPL; ++i) { l[r] = pick<false>(l[r], v[r][i]); u[r] = pick<true>(u[r], v[r][i]); if (!isfinite(v[r][i])) wrong |= 1u << r; }
-        }
-        lo = (double)extremes<false>(l); hi = (double)extremes<true>(u);
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) wrong |= (unsigned)__shfl_xor((int)wrong, o, 64);
-        bad = wrong >> (lane & 15) & 1;
+            for (int j = 0; j < 8; ++j) { l = pick<false>(l, v[i][j]); u = pick<true>(u, v[i][j]); none += v[i][j] * 0; }      // (an infinity or NaN leaves NaN)
+        lo = of_token<false>((double)l); hi = of_token<true>((double)u);
+        int wrong = none != 0;
+        wrong |= __builtin_amdgcn_mov_dpp(wrong, 0xB1, 0xf, 0xf, true); wrong |= __builtin_amdgcn_mov_dpp(wrong, 0x4E, 0xf, 0xf, true);
+        bad = wrong;
     }
-    // levels of the new tokens and, where g (of token lane % 16's block) has grown, of the tile's first `before` tokens
-    __device__ __forceinline__ void put(unsigned char* tile, unsigned fresh, int before, const Grid& g) {
+    // levels of the token: new (fresh), or one of the `before` first ones of a block whose grid has grown
+    __device__ __forceinline__ void put(unsigned char* tile, bool fresh, int before, const Grid& g, unsigned char* lds) {
         const int dp = a.g.dp, dh = a.g.dh;
-        const unsigned moved = (unsigned)(__ballot(g.grown) & 0xffffu) & ((1u << before) - 1), set = fresh | moved;
-        if (!set) return;
+        const bool moved = tok < before && g.grown, set = fresh || moved;
+        const unsigned long long sets = __ballot(set);
+        if (!sets) return;
         const float inv = (float)(1.0 / g.s), z = (float)g.z;
-        unsigned words[CPL][4] = {};      // V: four tokens of a channel each
+        unsigned w[NP][2] = {};
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            if (!(set >> r & 1)) continue;
-            const float iv = lane_float(inv, r), zr = lane_float(z, r);      // (not a shuffle: lanes may be switched off where it is used)
-            const double s1 = lane_value(g.s, r);
-            unsigned q[CPL];
-            if (fresh >> r & 1) {
+        for (int i = 0; i < NP; ++i) {
+            const int c = channel(i);
+            float n[8];
+            bool close = false;
 #pragma unroll
-                for (int i = 0; i < CPL; ++i) {
-                    const float x = (float)v[r][i] * iv;
-                    float n = rintf(x);
-                    if (!(fabsf(x - n) < 0.5f - (fabsf(x) * 0x1p-20f + 0x1p-20f))) n = (float)rint((double)v[r][i] / s1);
-                    q[i] = (unsigned)fminf(fmaxf(n + zr, 0.f), 255.f);      // (NaN: 0)
-                }
-            } else {
-                const double s0 = lane_value(g.s0, r), z0 = lane_value(g.z0, r);
+            for (int j = 0; j < 8; ++j) {
+                const float x = (float)v[i][j] * inv;
+                n[j] = rintf(x);
+                close |= !(fabsf(x - n[j]) < fmaf(fabsf(x), -0x1p-21f, 0.5f - 0x1p-21f));
+            }
+            if (close) {
 #pragma unroll
-                for (int i = 0; i < CPL; ++i) {
-                    const int c = min(c0 + i, dh - 1);
-                    const double w = ((double)tile[kv ? c * 16 + r : r * dp + c] - z0) * s0;
-                    q[i] = (unsigned)fmin(fmax(rint(w / s1) + (double)zr, 0.0), 255.0);
+                for (int j = 0; j < 8; ++j) n[j] = (float)rint((double)v[i][j] / g.s);
+            }
+            if (moved) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int ch = min(c + j, dh - 1);
+                    n[j] = (float)(rint(((double)tile[kv ? ch * 16 + tok : tok * dp + ch] - g.z0) * g.s0 / g.s));
                 }
             }
-            if (kv) {
 #pragma unroll
-                for (int i = 0; i < CPL; ++i) words[i][r >> 2] |= q[i] << 8 * (r & 3);
-            } else {
-                unsigned char* const p = tile + r * dp + c0;
-                if constexpr (CPL == 2) { if (mine == 2) { *(unsigned short*)p = (unsigned short)(q[0] | q[1] << 8); continue; } }
-                if constexpr (CPL == 4) { if (mine == 4) { *(unsigned*)p = q[0] | q[1] << 8 | q[2] << 16 | q[3] << 24; continue; } }
-#pragma unroll
-                for (int i = 0; i < CPL; ++i) if (i < mine) p[i] = (unsigned char)q[i];
-            }
+            for (int j = 0; j < 8; ++j) w[i][j >> 2] |= (unsigned)fminf(fmaxf(n[j] + z, 0.f), 255.f) << 8 * (j & 3);      // (NaN: 0)
         }
-        if (kv) {
+        if (!kv) {
+            if (!set) return;
 #pragma unroll
-            for (int i = 0; i < CPL; ++i) {
-                if (i >= mine) continue;
-                unsigned char* const p = tile + (c0 + i) * 16;
-                if (set == 0xffffu) *(uint4*)p = make_uint4(words[i][0], words[i][1], words[i][2], words[i][3]);
+            for (int i = 0; i < NP; ++i) {
+                const int c = channel(i);
+                unsigned char* const p = tile + tok * dp + c;
+                if (c + 8 <= dh) *(uint2*)p = make_uint2(w[i][0], w[i][1]);
                 else {
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) if (set >> r & 1) p[r] = (unsigned char)(words[i][r >> 2] >> 8 * (r & 3));
+                    for (int j = 0; j < 8; ++j) if (c + j < dh) p[j] = (unsigned char)(w[i][j >> 2] >> 8 * (j & 3));
                 }
             }
+        } else if (sets == ~0ull) {
+#pragma unroll
+            for (int i = 0; i < NP; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) lds[(channel(i) + j) * 16 + tok] = (unsigned char)(w[i][j >> 2] >> 8 * (j & 3));
+            __builtin_amdgcn_wave_barrier();      // (its own part of LDS)
+#pragma unroll
+            for (int i = 0; i < (32 * NP + 63) / 64; ++i) { const int c = lane + 64 * i; if (c < dh) *(uint4*)(tile + c * 16) = *(const uint4*)(lds + c * 16); }
+            __builtin_amdgcn_wave_barrier();
+        } else if (set) {
+#pragma unroll
+            for (int i = 0; i < NP; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) if (channel(i) + j < dh) tile[(channel(i) + j) * 16 + tok] = (unsigned char)(w[i][j >> 2] >> 8 * (j & 3));
         }
     }
 };
@@ -357,19 +367,16 @@ struct Unit {
     int in_page;
 };
 
-template <typename T, int CPL, bool ROT, bool MANY>
-__device__ __forceinline__ void append_unit(const AppendArgs<T>& a, const Unit& u, int kv) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, st_log = a.g.st_log, st = 1 << st_log, pt = 1 << a.g.pt_log;
-    AppendTile<T, CPL, ROT> t(a, kv);
-    auto fresh_of = [&](int p) {      // of 16 places from p on, those that get a token
-        const int from = max(u.first - p, 0), to = min(max(u.end - p, 0), 16);
-        return from < to ? ((1u << to) - 1) & ~((1u << from) - 1) : 0u;
-    };
+template <typename T, int NP, bool ROT, bool MANY>
+__device__ __forceinline__ void append_unit(const AppendArgs<T>& a, const Unit& u, int kv, unsigned char* lds) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, st_log = a.g.st_log, st = 1 << st_log, pt = 1 << a.g.pt_log, tok = lane >> 2;
+    AppendTile<T, NP, ROT> t(a, kv);
+    auto is_new = [&](int p) { return p >= u.first && p < u.end; };
     auto grids_of = [&](int h) { return (float2*)(u.page + (kv ? a.g.vg_at : a.g.kg_at)) + ((long long)h << (a.g.pt_log - st_log)) + (u.in_page >> st_log); };
     auto levels_of = [&](int h) { return u.page + (kv ? a.g.v_at : 0) + ((long long)h * pt + u.in_page) * a.g.dp; };
     if constexpr (!MANY) {
-        const unsigned fresh = __builtin_amdgcn_readfirstlane(fresh_of(u.place));
-        const int tok = lane & 15, t_block = tok & ~(st - 1), p_block = u.place + t_block;
+        const bool fresh = is_new(u.place + tok);
+        const int t_block = tok & ~(st - 1), p_block = u.place + t_block;
         const bool touched = p_block < u.end && p_block + st > u.first, had = touched && p_block < u.first;
         const int per = (a.g.heads + (int)gridDim.y * 4 - 1) / ((int)gridDim.y * 4), h0 = ((int)blockIdx.y * 4 + wave) * per, h1 = min(h0 + per, a.g.heads);
         for (int h = h0; h < h1; ++h) {
@@ -380,10 +387,10 @@ __device__ __forceinline__ void append_unit(const AppendArgs<T>& a, const Unit& 
             double lo, hi;
             bool bad;
             t.ends(lo, hi, bad);
-            for (int o = 1; o < st; o <<= 1) { lo = fmin(lo, __shfl_xor(lo, o, 64)); hi = fmax(hi, __shfl_xor(hi, o, 64)); bad |= __shfl_xor((int)bad, o, 64) != 0; }      // (st <= 16: within the row)
+            for (int o = 1; o < st; o <<= 1) { lo = fmin(lo, __shfl_xor(lo, 4 * o, 64)); hi = fmax(hi, __shfl_xor(hi, 4 * o, 64)); bad |= __shfl_xor((int)bad, 4 * o, 64) != 0; }      // (st <= 16)
             const Grid g = block_grid(lo, hi, bad, had, old.x, old.y);
-            t.put(levels_of(h), fresh, min(max(u.first - u.place, 0), 16), g);
-            if (touched && lane < 16 && tok == t_block) *grid = make_float2((float)g.s, (float)g.z);
+            t.put(levels_of(h), fresh, min(max(u.first - u.place, 0), 16), g, lds);
+            if (touched && lane == 4 * t_block) *grid = make_float2((float)g.s, (float)g.z);
         }
     } else {
         __shared__ double ends[2][4];
@@ -393,14 +400,14 @@ __device__ __forceinline__ void append_unit(const AppendArgs<T>& a, const Unit& 
         double lo = 0.0, hi = 0.0;
         bool bad = false;
         for (int j = wave; j < tiles; j += 4) {
-            const unsigned fresh = __builtin_amdgcn_readfirstlane(fresh_of(u.place + 16 * j));
-            if (!fresh) continue;
-            t.fetch(u.row0 + u.place + 16 * j, u.place + 16 * j, h, fresh);
+            const int p = u.place + 16 * j;
+            if (p >= u.end || p + 16 <= u.first) continue;
+            t.fetch(u.row0 + p, p, h, is_new(p + tok));
             double l, m;
             bool w;
             t.ends(l, m, w);
 #pragma unroll
-            for (int o = 1; o < 16; o <<= 1) { l = fmin(l, __shfl_xor(l, o, 64)); m = fmax(m, __shfl_xor(m, o, 64)); w |= __shfl_xor((int)w, o, 64) != 0; }
+            for (int o = 4; o < 64; o <<= 1) { l = fmin(l, __shfl_xor(l, o, 64)); m = fmax(m, __shfl_xor(m, o, 64)); w |= __shfl_xor((int)w, o, 64) != 0; }
             lo = fmin(lo, l); hi = fmax(hi, m); bad |= w;
         }
         if (lane == 0) { ends[0][wave] = lo; ends[1][wave] = hi; bads[wave] = bad; }
@@ -413,16 +420,16 @@ __device__ __forceinline__ void append_unit(const AppendArgs<T>& a, const Unit& 
         if (threadIdx.x == 0) *grid = make_float2((float)g.s, (float)g.z);
         for (int j = wave; j < tiles; j += 4) {
             const int p = u.place + 16 * j;
-            const unsigned fresh = __builtin_amdgcn_readfirstlane(fresh_of(p));
-            if (!once && fresh) t.fetch(u.row0 + p, p, h, fresh);
-            t.put(levels_of(h) + (long long)16 * j * a.g.dp, fresh, min(max(u.first - p, 0), 16), g);
+            if (!once && p < u.end && p + 16 > u.first) t.fetch(u.row0 + p, p, h, is_new(p + tok));
+            t.put(levels_of(h) + (long long)16 * j * a.g.dp, is_new(p + tok), min(max(u.first - p, 0), 16), g, lds);
         }
     }
 }
 
 // One workgroup per unit, and its four wavefronts take heads of K (blockIdx.z 0) or V; where a unit is several tiles of 16 tokens (MANY): per unit and head, and they take its tiles.
-template <typename T, int CPL, bool MANY>
-__global__ __launch_bounds__(256, CPL <= 2 ? 2 : 1) void kv_append_kernel(AppendArgs<T> a) {
+template <typename T, int NP, bool MANY>
+__global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs<T> a) {
+    __shared__ __align__(16) unsigned char turned[4][32 * NP * 16];
     const int ul = a.unit_log, room = a.q.room;
     int x = blockIdx.x, b;
     KvSeq s;
@@ -438,8 +445,9 @@ __global__ __launch_bounds__(256, CPL <= 2 ? 2 : 1) void kv_append_kernel(Append
     if (page < 0 || page >= (int)a.g.n_pages) return;
     u.page = a.cache + (long long)page * a.g.page_bytes;
     u.in_page = u.place & ((1 << a.g.pt_log) - 1);
-    if (blockIdx.z == 0 && a.rot.dim) append_unit<T, CPL, true, MANY>(a, u, 0);
-    else append_unit<T, CPL, false, MANY>(a, u, blockIdx.z);
+    unsigned char* const lds = turned[threadIdx.x >> 6];
+    if (blockIdx.z == 0 && a.rot.dim) append_unit<T, NP, true, MANY>(a, u, 0, lds);
+    else append_unit<T, NP, false, MANY>(a, u, blockIdx.z, lds);
 }
 
 template <typename T>
@@ -461,24 +469,32 @@ int head_norm_rotate(tboa_ctx* ctx, long long n_tokens, int dh, int nq, const vo
     return 0;
 }
 
-template <typename T, int CPL>
+template <typename T, int NP>
 int append(tboa_ctx* ctx, const AppendArgs<T>& a, long long units) {
     if (a.unit_log > 4) {
-        hipLaunchKernelGGL((kv_append_kernel<T, CPL, true>), dim3((unsigned)units, (unsigned)a.g.heads, 2), dim3(256), 0, ctx->stream, a);
+        hipLaunchKernelGGL((kv_append_kernel<T, NP, true>), dim3((unsigned)units, (unsigned)a.g.heads, 2), dim3(256), 0, ctx->stream, a);
     } else {
-        // heads that one wavefront goes through: as few as fill the chip (256 compute units, 16 wavefronts each), for the tile is found and the tables are read once for all of them
+        // heads that one wavefront goes through: as few as fill the chip (256 compute units, 16 wavefronts each), for the tile is found once for all of them
         const long long all = units * a.g.heads * 2;
         const int per = (int)std::min<long long>(std::max<long long>(all / 4096, 1), 8), groups = (a.g.heads + 4 * per - 1) / (4 * per);
-        hipLaunchKernelGGL((kv_append_kernel<T, CPL, false>), dim3((unsigned)units, (unsigned)groups, 2), dim3(256), 0, ctx->stream, a);
+        hipLaunchKernelGGL((kv_append_kernel<T, NP, false>), dim3((unsigned)units, (unsigned)groups, 2), dim3(256), 0, ctx->stream, a);
     }
     TB_KERNEL_CHECK(ctx);
     return 0;
 }
 template <typename T>
 int append(tboa_ctx* ctx, AppendArgs<T> a, long long units) {
-    const int cpl = a.g.dh <= 64 ? 1 : a.g.dh <= 128 ? 2 : 4, bytes = cpl * (int)sizeof(T);
-    for (int i = 0; i < 2; ++i) a.vec[i] = a.g.dh % cpl == 0 && ((uintptr_t)a.x[i] % bytes) == 0 && a.ld[i] % cpl == 0;
-    return cpl == 1 ? append<T, 1>(ctx, a, units) : cpl == 2 ? append<T, 2>(ctx, a, units) : append<T, 4>(ctx, a, units);
+    const int e = 16 / (int)sizeof(T);
+    for (int i = 0; i < 2; ++i) a.vec[i] = a.g.dh % 8 == 0 && ((uintptr_t)a.x[i] & 15) == 0 && a.ld[i] % e == 0;
+    a.vec_table = a.rot.dim % 16 == 0 && ((uintptr_t)a.rot.table & 15) == 0;
+    switch (a.g.dp) {
+        case 32: return append<T, 1>(ctx, a, units);
+        case 64: return append<T, 2>(ctx, a, units);
+        case 96: return append<T, 3>(ctx, a, units);
+        case 128: return append<T, 4>(ctx, a, units);
+        case 192: return append<T, 6>(ctx, a, units);
+        default: return append<T, 8>(ctx, a, units);
+    }
 }
 
 int check_rotation(tboa_ctx* ctx, const char* who, const tboa_rotation* r, int dh, Rotation& out) {
@@ -557,6 +573,6 @@ extern "C" int tboa_kv_cache_append(tboa_ctx* ctx, const tboa_kv_cache_desc* des
     const long long units = std::min<long long>(batch->n_tokens, (batch->n_tokens >> unit_log) + 2LL * batch->n_seqs);
     const KvBatch q{batch->n_seqs, batch->pages_per_seq, (int)batch->n_tokens, batch->pages_per_seq * desc->page_tokens, batch->starts, batch->lens, batch->pages};
     KvDevice dev(ctx->device);
-    if (dtype == TBOA_F32) return append<float>(ctx, AppendArgs<float>{g, q, {(const float*)K, (const float*)V}, {ldk, ldv}, rot, positions, (unsigned char*)cache, unit_log, {}}, units);
-    return append<bf16>(ctx, AppendArgs<bf16>{g, q, {(const bf16*)K, (const bf16*)V}, {ldk, ldv}, rot, positions, (unsigned char*)cache, unit_log, {}}, units);
+    if (dtype == TBOA_F32) return append<float>(ctx, AppendArgs<float>{g, q, {(const float*)K, (const float*)V}, {ldk, ldv}, rot, positions, (unsigned char*)cache, unit_log, {}, false}, units);
+    return append<bf16>(ctx, AppendArgs<bf16>{g, q, {(const bf16*)K, (const bf16*)V}, {ldk, ldv}, rot, positions, (unsigned char*)cache, unit_log, {}, false}, units);
 }
