@@ -282,6 +282,7 @@ struct AppendTile {
                     v[i][j] = (double)raw[i][j] * (double)cs[j] + (double)other[j] * (double)sn[j];
                     if (!known && c + j < rot) v[i][j] = lost;
                 }
+                __builtin_amdgcn_sched_barrier(0);      // a piece at a time: all pieces' operands side by side do not fit in the registers
             }
         }
     }
@@ -428,7 +429,7 @@ __device__ __forceinline__ void append_unit(const AppendArgs<T>& a, const Unit& 
 
 // One workgroup per unit, and its four wavefronts take heads of K (blockIdx.z 0) or V; where a unit is several tiles of 16 tokens (MANY): per unit and head, and they take its tiles.
 template <typename T, int NP, bool MANY>
-__global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs<T> a) {
+__global__ __launch_bounds__(256, NP <= 4 ? 2 : 1) void kv_append_kernel(AppendArgs<T> a) {
     __shared__ __align__(16) unsigned char turned[4][32 * NP * 16];
     const int ul = a.unit_log, room = a.q.room;
     int x = blockIdx.x, b;
