@@ -222,3 +222,22 @@ def quantize_mlp(ctx, mlp, cfg, alpha=0.25, use_R=True, cd_iters=1, adaptive_gri
     out["hessians"] = dict(H_gate_up=H, R_gate_up=R, H_down=Hd, R_down=Rd)
     out["act"], out["act_fp"] = act, act_fp
     return out
+
+
+def serve_attention_block(ctx, weights, X, cache, batch, n_q_heads, rotation=None, positions=None, norm_q=None, norm_k=None, eps=1e-6, scale=0.0, window=0, residual=None):
+    """The attention block with its weights quantized and its keys and values in a quantized cache, for the new tokens X [tokens, d_model] of a ragged batch (prompts, single tokens or both):
+    projections -> norms and rotation -> append -> attention over the cache -> output projection (+ residual).
+
+    weights: dict with Wqkv = [W_Q; W_K; W_V] and Wo, as quantize_attention_block's dequantized matrices; rotation by int32 positions [tokens]; norm_q, norm_k: fp32 [head_dim] weights of the
+    norms of every head's query and key.  Keys without a norm are rotated by the append itself, on unrounded values.  Returns a dict: Y [tokens, d_model], and q, k, v, o on the way
+    (k as it goes to the append)."""
+    Hq, Hkv, dh = n_q_heads, cache.desc.n_kv_heads, cache.desc.head_dim
+    qkv = ctx.linear_forward(X, weights["Wqkv"]).view(X.shape[0], Hq + 2 * Hkv, dh)
+    q, k, v = qkv[:, :Hq], qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:]
+    in_append = rotation is not None and norm_k is None
+    if rotation is not None or norm_q is not None or norm_k is not None:
+        ctx.head_norm_rotate(q, None if in_append else k, norm_q, norm_k, eps, rotation, positions, out_q=q, out_k=None if in_append else k)
+    ctx.kv_cache_append(cache, batch, k, v, *((rotation, positions) if in_append else ()))
+    o = ctx.kv_cache_attention(cache, batch, q, scale=scale, window=window)
+    Y = ctx.linear_forward(o.view(-1, Hq * dh), weights["Wo"], residual=residual)
+    return dict(Y=Y, q=q, k=k, v=v, o=o)
