@@ -1,5 +1,6 @@
 // Context, error reporting, workspace, and small elementwise kernels.
 #include "internal.h"
+#include <new>
 
 int tboa_fail(tboa_ctx* ctx, int code, const char* fmt, ...) {
     if (ctx) {
@@ -27,7 +28,10 @@ int tboa_ws_reserve(tboa_ctx* ctx, size_t bytes) {
     if (bytes <= ctx->ws_bytes) return 0;
     if (capturing(ctx)) return tboa_fail(ctx, TBOA_ENOMEM, "workspace of %zu bytes: nothing can be allocated while the stream is captured, reserve it before", bytes);
     TB_HIP(ctx, hipStreamSynchronize(ctx->stream));
-    if (ctx->ws && ctx->ws_in_graph) { ctx->ws_kept.push_back(ctx->ws); ctx->ws = nullptr; ctx->ws_bytes = 0; ctx->ws_in_graph = false; }
+    if (ctx->ws && ctx->ws_in_graph) {
+        try { ctx->ws_kept.push_back(ctx->ws); } catch (const std::bad_alloc&) { return tboa_fail(ctx, TBOA_ENOMEM, "out of host memory"); }
+        ctx->ws = nullptr; ctx->ws_bytes = 0; ctx->ws_in_graph = false;
+    }
     const size_t had = ctx->ws_bytes;
     if (ctx->ws) { TB_HIP(ctx, hipFree(ctx->ws)); ctx->ws = nullptr; ctx->ws_bytes = 0; }
     hipError_t e = hipMalloc(&ctx->ws, bytes);

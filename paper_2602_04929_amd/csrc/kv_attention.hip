@@ -23,6 +23,7 @@ __device__ __forceinline__ float to_f32(bf16 v) { return __bfloat162float(v); }
 template <typename T> __device__ __forceinline__ T from_f32(float v);
 template <> __device__ __forceinline__ float from_f32<float>(float v) { return v; }
 template <> __device__ __forceinline__ bf16 from_f32<bf16>(float v) { return __float2bfloat16(v); }
+__device__ __forceinline__ f4 by_power(f4 v, int e) { return f4{__builtin_amdgcn_ldexpf(v[0], e), __builtin_amdgcn_ldexpf(v[1], e), __builtin_amdgcn_ldexpf(v[2], e), __builtin_amdgcn_ldexpf(v[3], e)}; }
 __device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
 
 template <int N, int I = 0, typename F>
@@ -58,7 +59,7 @@ struct AttendArgs {
     float* part; float2* stat;    // per workgroup two pieces of 16 rows (of a unit that began before its share, of one that begins in it): unscaled outputs; maximum, sum
 };
 
-constexpr float HALF_TOP = 0x1p14f;      // what a probability of 1 with the largest scale becomes as half, at most: parts of 2^-28 of it are still normal numbers
+constexpr int HALF_TOP = 14;      // a probability of 1 with the largest scale becomes 2^14 as half, at most: parts of 2^-28 of it are still normal numbers
 constexpr int ROWS = 16, TILE = 64;      // rows (query token, head of the group) of a unit, tokens a wavefront takes at a time
 // workgroups that a compute unit holds at once (registers): the shares that the work is cut into are 256 times as many
 template <int DP> constexpr int resident() { return DP <= 64 ? 3 : DP <= 128 ? 2 : 1; }
@@ -258,7 +259,7 @@ __global__ __launch_bounds__(256, resident<DP>()) void kv_attend_rows_kernel(Att
 #pragma unroll
                 for (int c = 0; c < CT; ++c) o[c] *= turn;
             }
-            const float sv = gvx * (HALF_TOP / ref);
+            const float sv = __builtin_amdgcn_ldexpf(gvx, HALF_TOP + 1 - __builtin_amdgcn_frexp_expf(ref));
             unroll<16>([&](auto I) { constexpr int i = I; p[i] *= row_lane<i>(sv); });
             if (!all) {
 #pragma unroll
@@ -295,9 +296,10 @@ __global__ __launch_bounds__(256, resident<DP>()) void kv_attend_rows_kernel(Att
         float top = ends[0][col].x;
 #pragma unroll
         for (int w = 1; w < 4; ++w) top = fmaxf(top, ends[w][col].x);
-        const float f = m == -__builtin_inff() ? 0.f : ex2(m - top) * ref * (1.f / HALF_TOP);
+        const float f = m == -__builtin_inff() ? 0.f : ex2(m - top);
+        const int back = __builtin_amdgcn_frexp_expf(ref) - 1 - HALF_TOP;
 #pragma unroll
-        for (int c = 0; c < CT; ++c) *(f4*)&joined[wave][col][c * 16 + grp * 4] = m == -__builtin_inff() ? f4{0.f, 0.f, 0.f, 0.f} : o[c] * f;
+        for (int c = 0; c < CT; ++c) *(f4*)&joined[wave][col][c * 16 + grp * 4] = m == -__builtin_inff() ? f4{0.f, 0.f, 0.f, 0.f} : by_power(o[c] * f, back);
         __syncthreads();
         const bool whole = k0 == 0 && k1 == tiles;
         const long long piece = (2LL * blockIdx.x + (k0 == 0)) * ROWS;
@@ -383,9 +385,10 @@ __global__ __launch_bounds__(256) void kv_attend_join_kernel(AttendArgs a) {
 // instructions: the tokens of a tile's rows are ordered so that a lane's 32 scores, as half, are the right operand of O^T += V^T P^T as they stand.
 // A wavefront alternates between a run of matrix instructions, scores of tile n and products with V of tile n - 1, and a run of vector instructions, the softmax of tile n and its part in making
 // the next tile.  Runs end at a barrier; of the two wavefronts of a SIMD one is a run behind the other, so that one multiplies while the other exponentiates.
-// A row's maximum is only followed where it has to be: as long as the sum of a lane's 32 probabilities stays below MOST, so does each of them, and they simply exceed 1 (MOST TILE_TOP = 2^15 is
+// A row's maximum is only followed where it has to be: as long as the sum of a lane's 32 probabilities stays below MOST, so does each of them, and they simply exceed 1 (MOST 2^TILE_TOP = 2^15 is
 // within half); no maximum is formed then.
-constexpr float MOST = 0x1p7f, TILE_TOP = 0x1p8f;
+constexpr float MOST = 0x1p7f;
+constexpr int TILE_TOP = 8;      // as HALF_TOP
 template <int DP> constexpr int waves() { return DP <= 128 ? 8 : 4; }      // (wider heads need twice the registers)
 template <int DP> constexpr int permuted() { return DP % 128 == 0 ? 15 : DP % 64 == 0 ? 7 : 3; }      // bits of a piece's number that K's rows are XORed into
 template <int DP> constexpr int tiles_lds() { return 2 * 2 * TILE * DP * 2; }
@@ -433,9 +436,6 @@ __device__ __forceinline__ void run_ends() {      // everything before it is bef
     __builtin_amdgcn_sched_barrier(0);
 }
 
-#ifndef AHEAD_
-#define AHEAD_ 6
-#endif
 // N matrix instructions with an LDS operand each: the operands' loads AHEAD of them, no more (the registers would not hold them)
 template <int N, int AHEAD>
 __device__ __forceinline__ void operands_ahead() {
@@ -449,7 +449,7 @@ template <int DP, bool WIDE>      // WIDE: pages of 64 tokens and more, a tile l
 __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_tiles_kernel(AttendArgs a) {
     constexpr int W = waves<DP>(), RT = 32 * W, KS = DP / 16, CT = DP / 32, PIECES = 4 * DP, PP = (PIECES + 64 * W - 1) / (64 * W);      // 16-byte pieces of a tile of K (and of V), per thread
     constexpr bool EVEN = PIECES % (64 * W) == 0;
-    constexpr int KROW = DP * 2, VROW = TILE * 2, AHEAD = AHEAD_;      // bytes of a row in LDS; operands on their way
+    constexpr int KROW = DP * 2, VROW = TILE * 2, AHEAD = 6;      // bytes of a row in LDS; operands on their way
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     unsigned char* const kbuf = lds;
     unsigned char* const vbuf = lds + 2 * TILE * KROW;
@@ -633,7 +633,8 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
 #pragma unroll
         for (int j = 0; j < 16; ++j) o[c][j] = 0.f;
     h8 pf[4];
-    float m = -__builtin_inff(), l = 0.f, ref = 0x1p-126f, unref = TILE_TOP * 0x1p126f;      // unref = TILE_TOP / ref
+    float m = -__builtin_inff(), l = 0.f, ref = 0x1p-126f;
+    int up = TILE_TOP + 126;      // 2^up ref = 2^TILE_TOP
     // operands in LDS
     constexpr int M = permuted<DP>();
     auto k_piece = [&](int buf, int k, int c) {
@@ -701,7 +702,7 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
                 if (s_top >= ref && s_top < __builtin_inff()) {
                     const int e = min(__builtin_amdgcn_frexp_expf(s_top), 127);
                     const float now = __builtin_amdgcn_ldexpf(1.f, e);
-                    turn *= ref / now; ref = now; unref = __builtin_amdgcn_ldexpf(TILE_TOP, -e);
+                    turn *= ref / now; ref = now; up = TILE_TOP - e;
                 }
 #pragma unroll
                 for (int c = 0; c < CT; ++c) o[c] *= turn;
@@ -711,7 +712,7 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
                 for (int i = 0; i < 32; ++i) { p[i] = ex2(sc[i >> 4][i & 15] - base); sum += p[i]; }
             }
             l += sum;
-            const float sv[2] = {gv[0] * unref, gv[1] * unref};
+            const float sv[2] = {__builtin_amdgcn_ldexpf(gv[0], up), __builtin_amdgcn_ldexpf(gv[1], up)};
             unroll<32>([&](auto I) { constexpr int i = I; p[i] *= row_lane<i & 15>(sv[i >> 4]); });
             if (!all) {
                 const int first_seen = low - t0 - 8 * half;
@@ -734,16 +735,16 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
     l += from_xor<32>(l);
     if (l != l) m = fmaxf(m, 0.f);      // scores that are all NaN leave the maximum where it was
     if (!row_live) return;
-    const float unscale = m == -__builtin_inff() ? 0.f : ref * (1.f / TILE_TOP);
+    const bool none = m == -__builtin_inff();
     if (u.n_cuts == 1) {
         bf16* const out = (bf16*)a.O + (long long)(s.start + tok) * a.ldo + (long long)(h * a.rep + r - tok * a.rep) * a.g.dh;
-        const float f = l == 0.f ? 0.f : unscale / l;
+        const float f = none || l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
         for (int c = 0; c < CT; ++c)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const int ch = 32 * c + 8 * (i >> 2) + 4 * half + (i & 3);
-                if (ch < a.g.dh) out[ch] = from_f32<bf16>(l == 0.f ? 0.f : o[c][i] * f);
+                if (ch < a.g.dh) out[ch] = from_f32<bf16>(none || l == 0.f ? 0.f : __builtin_amdgcn_ldexpf(o[c][i] * f, -up));
             }
     } else {
         const long long at = (long long)blockIdx.x * RT + w0 + col;
@@ -752,7 +753,7 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
         for (int c = 0; c < CT; ++c)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                *(f4*)(a.tile_part + at * DP + 32 * c + 8 * i + 4 * half) = m == -__builtin_inff() ? f4{0.f, 0.f, 0.f, 0.f} : f4{o[c][4 * i], o[c][4 * i + 1], o[c][4 * i + 2], o[c][4 * i + 3]} * unscale;
+                *(f4*)(a.tile_part + at * DP + 32 * c + 8 * i + 4 * half) = none ? f4{0.f, 0.f, 0.f, 0.f} : by_power(f4{o[c][4 * i], o[c][4 * i + 1], o[c][4 * i + 2], o[c][4 * i + 3]}, -up);
     }
 }
 
@@ -889,7 +890,7 @@ extern "C" int tboa_kv_cache_attention(tboa_ctx* ctx, const tboa_kv_cache_desc* 
     a.q = KvBatch{batch->n_seqs, batch->pages_per_seq, (int)batch->n_tokens, batch->pages_per_seq * desc->page_tokens, batch->starts, batch->lens, batch->pages};
     a.Q = Q; a.ldq = ldq; a.O = O; a.ldo = ldo; a.cache = (const unsigned char*)cache;
     a.scale2 = (float)((scale == 0.0 ? 1.0 / sqrt((double)g.dh) : scale) * 1.4426950408889634);
-    a.rep = rep; a.window = window;
+    a.rep = rep; a.window = window < KV_MOST_TOKENS ? window : 0;      // (no sequence is longer)
     a.vec = g.dh % 8 == 0 && ((uintptr_t)Q & 15) == 0 && ldq * size % 16 == 0;
     a.few = !tiles ? 1 << 30 : rows ? FEW : 0;
     room(g, tiles, units, &a, ctx->ws);
