@@ -163,7 +163,7 @@ struct AppendArgs {
     KvGeometry g; KvBatch q;
     const T* x[2]; long long ld[2];      // K, V
     Rotation rot; const int* positions;
-    unsigned char* cache; int unit_log; bool vec[2], vec_table;      // pieces of 8 channels, rows of the table in aligned pieces
+    unsigned char* cache; int unit_log, per; bool vec[2], vec_table;      // pieces of 8 channels, rows of the table in aligned pieces
 };
 
 // Scale and zero of a block from the ends of its new values and, where it has earlier tokens, from the stored grid; everything in fp64 on what is stored in fp32
@@ -190,11 +190,14 @@ __device__ __forceinline__ double dpp(double v) {
     const int lo = __builtin_amdgcn_mov_dpp(__double2loint(v), CTRL, 0xf, 0xf, true), hi = __builtin_amdgcn_mov_dpp(__double2hiint(v), CTRL, 0xf, 0xf, true);
     return __hiloint2double(hi, lo);
 }
-// over the four lanes of a token
-template <bool MOST>
+// over the LPT lanes of a token
+template <int LPT, bool MOST>
 __device__ __forceinline__ double of_token(double v) {
     v = pick<MOST>(v, dpp<0xB1>(v));      // quad_perm 1 0 3 2
-    return pick<MOST>(v, dpp<0x4E>(v));      // 2 3 0 1
+    v = pick<MOST>(v, dpp<0x4E>(v));      // 2 3 0 1
+    if constexpr (LPT > 4) v = pick<MOST>(v, dpp<0x141>(v));      // the other four of eight
+    if constexpr (LPT > 8) v = pick<MOST>(v, dpp<0x140>(v));      // the other eight of sixteen
+    return v;
 }
 
 template <typename T>
@@ -204,20 +207,24 @@ __device__ __forceinline__ void load_piece(const T* p, bool vec, int n, float (&
     for (int j = 0; j < 8; ++j) { o[j] = 0.f; if (j < n) o[j] = to_f32(p[j]); }
 }
 
-// What a wavefront does with 16 tokens of a head.  Four lanes per token, NP pieces of 8 channels in each (piece q + 4 i of a token is lane q's): the ends of a token are found in its lanes, whose
-// grid is then theirs, and a token's levels leave as whole pieces; those of V turn by way of LDS into 16 tokens of a channel.
+// What a wavefront does with TOKENS tokens of a head.  LPT lanes per token, NP pieces of 8 channels in each (piece q + LPT i of a token is lane q's): the ends of a token are found in its lanes,
+// whose grid is then theirs, and a token's levels leave as whole pieces; those of V turn by way of LDS into the tokens of a channel.
+// Bound by its instructions, not by its bytes (prompts of four sequences, 32 heads of 128: 147 MB would take 31 us): a key's value costs about ten operations in fp64, which is what the grid is
+// decided in, and 18 in fp32.  As many lanes per token as it has pieces, up to 16: four with up to eight pieces each took 14.5 us instead of 4.8 for a token of each of 64 sequences, 50 instead
+// of 42 for four prompts of 2000 (8 heads, a grid per token) and spilled registers.
 // ROT: keys, rotated in fp64 (products of 24 bits are exact there); a piece's partners are read once more.  Else the inputs themselves, in fp32.  Levels come from fp32 products, and a piece with such
 // a product within 2^-21 of a border from the fp64 quotients (three roundings are off by 3 * 2^-24 of it).
-template <typename T, int NP, bool ROT>
+template <typename T, int LPT, int NP, bool ROT>
 struct AppendTile {
+    static constexpr int TOKENS = 64 / LPT;
     typedef typename std::conditional<ROT, double, float>::type V;
     const AppendArgs<T>& a;
     int kv, lane, tok, q;
     bool vec;
     V v[NP][8];
 
-    __device__ __forceinline__ AppendTile(const AppendArgs<T>& args, int kv_) : a(args), kv(kv_) { lane = threadIdx.x & 63; tok = lane >> 2; q = lane & 3; vec = a.vec[kv]; }
-    __device__ __forceinline__ int channel(int i) const { return 8 * (q + 4 * i); }
+    __device__ __forceinline__ AppendTile(const AppendArgs<T>& args, int kv_) : a(args), kv(kv_) { lane = threadIdx.x & 63; tok = lane / LPT; q = lane % LPT; vec = a.vec[kv]; }
+    __device__ __forceinline__ int channel(int i) const { return 8 * (q + LPT * i); }
     // row, p: of the tile's first token, its place; fresh: this lane's token is new
     __device__ __forceinline__ void fetch(int row, int p, int h, bool fresh) {
         const int dh = a.g.dh, rot = a.rot.dim, half = rot / 2;
@@ -279,7 +286,7 @@ struct AppendTile {
                 const double lost = known ? 0.0 : __builtin_nan("");
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    v[i][j] = (double)raw[i][j] * (double)cs[j] + (double)other[j] * (double)sn[j];
+                    v[i][j] = fma((double)raw[i][j], (double)cs[j], (double)other[j] * (double)sn[j]);      // (the product is exact)
                     if (!known && c + j < rot) v[i][j] = lost;
                 }
                 __builtin_amdgcn_sched_barrier(0);      // a piece at a time: all pieces' operands side by side do not fit in the registers
@@ -292,10 +299,12 @@ struct AppendTile {
 #pragma unroll
         for (int i = 0; i < NP; ++i)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) { l = pick<false>(l, v[i][j]); u = pick<true>(u, v[i][j]); none += v[i][j] * 0; }      // (an infinity or NaN leaves NaN)
-        lo = of_token<false>((double)l); hi = of_token<true>((double)u);
+            for (int j = 0; j < 8; ++j) { l = pick<false>(l, v[i][j]); u = pick<true>(u, v[i][j]); none = fma(v[i][j], (V)0, none); }      // (an infinity or NaN leaves NaN)
+        lo = of_token<LPT, false>((double)l); hi = of_token<LPT, true>((double)u);
         int wrong = none != 0;
         wrong |= __builtin_amdgcn_mov_dpp(wrong, 0xB1, 0xf, 0xf, true); wrong |= __builtin_amdgcn_mov_dpp(wrong, 0x4E, 0xf, 0xf, true);
+        if constexpr (LPT > 4) wrong |= __builtin_amdgcn_mov_dpp(wrong, 0x141, 0xf, 0xf, true);
+        if constexpr (LPT > 8) wrong |= __builtin_amdgcn_mov_dpp(wrong, 0x140, 0xf, 0xf, true);
         bad = wrong;
     }
     // levels of the token: new (fresh), or one of the `before` first ones of a block whose grid has grown
@@ -344,13 +353,14 @@ struct AppendTile {
                 }
             }
         } else if (sets == ~0ull) {
+            typedef unsigned Column __attribute__((ext_vector_type(TOKENS / 4)));
 #pragma unroll
             for (int i = 0; i < NP; ++i)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) lds[(channel(i) + j) * 16 + tok] = (unsigned char)(w[i][j >> 2] >> 8 * (j & 3));
+                for (int j = 0; j < 8; ++j) lds[(channel(i) + j) * TOKENS + tok] = (unsigned char)(w[i][j >> 2] >> 8 * (j & 3));
             __builtin_amdgcn_wave_barrier();      // (its own part of LDS)
 #pragma unroll
-            for (int i = 0; i < (32 * NP + 63) / 64; ++i) { const int c = lane + 64 * i; if (c < dh) *(uint4*)(tile + c * 16) = *(const uint4*)(lds + c * 16); }
+            for (int i = 0; i < (8 * LPT * NP + 63) / 64; ++i) { const int c = lane + 64 * i; if (c < dh) *(Column*)(tile + c * 16) = *(const Column*)(lds + c * TOKENS); }
             __builtin_amdgcn_wave_barrier();
         } else if (set) {
 #pragma unroll
@@ -361,76 +371,106 @@ struct AppendTile {
     }
 };
 
-// A unit of max(16, scale_tokens) tokens of a sequence
+// A unit of max(TOKENS, scale_tokens) tokens of a sequence
+constexpr int MOST_WAVES = 8;      // of a workgroup
 struct Unit {
     int first, place, end, row0;      // first place that gets a token, the unit's first place and the end of its places; row of place p: row0 + p
     unsigned char* page;
     int in_page;
 };
 
-template <typename T, int NP, bool ROT, bool MANY>
+template <typename T, int LPT, int NP, bool ROT, int FORM>
 __device__ __forceinline__ void append_unit(const AppendArgs<T>& a, const Unit& u, int kv, unsigned char* lds) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, st_log = a.g.st_log, st = 1 << st_log, pt = 1 << a.g.pt_log, tok = lane >> 2;
-    AppendTile<T, NP, ROT> t(a, kv);
+    typedef AppendTile<T, LPT, NP, ROT> Tile;
+    constexpr int TOKENS = Tile::TOKENS;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, st_log = a.g.st_log, st = 1 << st_log, pt = 1 << a.g.pt_log, tok = lane / LPT;
     auto is_new = [&](int p) { return p >= u.first && p < u.end; };
     auto grids_of = [&](int h) { return (float2*)(u.page + (kv ? a.g.vg_at : a.g.kg_at)) + ((long long)h << (a.g.pt_log - st_log)) + (u.in_page >> st_log); };
-    auto levels_of = [&](int h) { return u.page + (kv ? a.g.v_at : 0) + ((long long)h * pt + u.in_page) * a.g.dp; };
-    if constexpr (!MANY) {
-        const bool fresh = is_new(u.place + tok);
-        const int t_block = tok & ~(st - 1), p_block = u.place + t_block;
+    auto levels_of = [&](int h, int j) {      // of the unit's tile j
+        const int at = u.in_page + TOKENS * j;
+        return kv ? u.page + a.g.v_at + ((long long)h * pt + (at & ~15)) * a.g.dp + (at & 15) : u.page + ((long long)h * pt + at) * a.g.dp;
+    };
+    if constexpr (FORM > 0) {
+        const int t_block = FORM == 1 ? tok & ~(st - 1) : 0, p_block = u.place + t_block, tiles = FORM == 1 ? 1 : (1 << a.unit_log) / TOKENS;
         const bool touched = p_block < u.end && p_block + st > u.first, had = touched && p_block < u.first;
-        const int per = (a.g.heads + (int)gridDim.y * 4 - 1) / ((int)gridDim.y * 4), h0 = ((int)blockIdx.y * 4 + wave) * per, h1 = min(h0 + per, a.g.heads);
+        const int h0 = ((int)blockIdx.y * 4 + wave) * a.per, h1 = min(h0 + a.per, a.g.heads);
         for (int h = h0; h < h1; ++h) {
-            float2* const grid = grids_of(h) + (tok >> st_log);
+            float2* const grid = grids_of(h) + (FORM == 1 ? tok >> st_log : 0);
             float2 old = make_float2(0.f, 0.f);
             if (had) old = *grid;
-            t.fetch(u.row0 + u.place, u.place, h, fresh);
-            double lo, hi;
-            bool bad;
-            t.ends(lo, hi, bad);
-            for (int o = 1; o < st; o <<= 1) { lo = fmin(lo, __shfl_xor(lo, 4 * o, 64)); hi = fmax(hi, __shfl_xor(hi, 4 * o, 64)); bad |= __shfl_xor((int)bad, 4 * o, 64) != 0; }      // (st <= 16)
+            Tile t[4] = {Tile(a, kv), Tile(a, kv), Tile(a, kv), Tile(a, kv)};
+            double lo = 0.0, hi = 0.0;
+            bool bad = false;
+#pragma unroll
+            for (int k = 0; k < FORM; ++k) {
+                const int p = u.place + TOKENS * k;
+                if (FORM > 1 && (k >= tiles || p >= u.end || p + TOKENS <= u.first)) continue;
+                t[k].fetch(u.row0 + p, p, h, is_new(p + tok));
+                double l, m;
+                bool w;
+                t[k].ends(l, m, w);
+                lo = fmin(lo, l); hi = fmax(hi, m); bad |= w;
+            }
+            for (int o = LPT; o < (FORM == 1 ? LPT << st_log : 64); o <<= 1) { lo = fmin(lo, __shfl_xor(lo, o, 64)); hi = fmax(hi, __shfl_xor(hi, o, 64)); bad |= __shfl_xor((int)bad, o, 64) != 0; }
             const Grid g = block_grid(lo, hi, bad, had, old.x, old.y);
-            t.put(levels_of(h), fresh, min(max(u.first - u.place, 0), 16), g, lds);
-            if (touched && lane == 4 * t_block) *grid = make_float2((float)g.s, (float)g.z);
+#pragma unroll
+            for (int k = 0; k < FORM; ++k) {
+                const int p = u.place + TOKENS * k;
+                if (FORM > 1 && k >= tiles) continue;
+                t[k].put(levels_of(h, k), is_new(p + tok), min(max(u.first - p, 0), TOKENS), g, lds);
+            }
+            if (touched && lane == LPT * t_block) *grid = make_float2((float)g.s, (float)g.z);
         }
     } else {
-        __shared__ double ends[2][4];
-        __shared__ int bads[4];
-        const int h = blockIdx.y, tiles = 1 << (a.unit_log - 4);
-        const bool had = u.place < u.first, once = tiles <= 4;      // once: a tile for each wavefront, whose values stay where they are
-        double lo = 0.0, hi = 0.0;
-        bool bad = false;
-        for (int j = wave; j < tiles; j += 4) {
-            const int p = u.place + 16 * j;
-            if (p >= u.end || p + 16 <= u.first) continue;
-            t.fetch(u.row0 + p, p, h, is_new(p + tok));
-            double l, m;
-            bool w;
-            t.ends(l, m, w);
+        __shared__ double ends[2][2][MOST_WAVES];
+        __shared__ int bads[2][MOST_WAVES];
+        constexpr int KEPT = NP == 1 ? 2 : 1;      // tiles that a wavefront keeps the values of
+        const int tiles = (1 << a.unit_log) / TOKENS, waves = blockDim.x >> 6, h0 = (int)blockIdx.y * a.per, h1 = min(h0 + a.per, a.g.heads);
+        const bool had = u.place < u.first, once = tiles <= KEPT * waves;
+        auto some_new = [&](int p) { return p < u.end && p + TOKENS > u.first; };
+        for (int h = h0; h < h1; ++h) {
+            Tile t[2] = {Tile(a, kv), Tile(a, kv)};
+            double lo = 0.0, hi = 0.0;
+            bool bad = false;
+            for (int j0 = wave; j0 < tiles; j0 += KEPT * waves)
 #pragma unroll
-            for (int o = 4; o < 64; o <<= 1) { l = fmin(l, __shfl_xor(l, o, 64)); m = fmax(m, __shfl_xor(m, o, 64)); w |= __shfl_xor((int)w, o, 64) != 0; }
-            lo = fmin(lo, l); hi = fmax(hi, m); bad |= w;
-        }
-        if (lane == 0) { ends[0][wave] = lo; ends[1][wave] = hi; bads[wave] = bad; }
-        float2* const grid = grids_of(h);
-        float2 old = make_float2(0.f, 0.f);
-        if (had) old = *grid;
-        __syncthreads();
-        lo = fmin(fmin(ends[0][0], ends[0][1]), fmin(ends[0][2], ends[0][3])); hi = fmax(fmax(ends[1][0], ends[1][1]), fmax(ends[1][2], ends[1][3]));
-        const Grid g = block_grid(lo, hi, bads[0] | bads[1] | bads[2] | bads[3], had, old.x, old.y);
-        if (threadIdx.x == 0) *grid = make_float2((float)g.s, (float)g.z);
-        for (int j = wave; j < tiles; j += 4) {
-            const int p = u.place + 16 * j;
-            if (!once && p < u.end && p + 16 > u.first) t.fetch(u.row0 + p, p, h, is_new(p + tok));
-            t.put(levels_of(h) + (long long)16 * j * a.g.dp, is_new(p + tok), min(max(u.first - p, 0), 16), g, lds);
+                for (int k = 0; k < KEPT; ++k) {
+                    const int j = j0 + k * waves, p = u.place + TOKENS * j;
+                    if (j >= tiles || !some_new(p)) continue;
+                    t[k].fetch(u.row0 + p, p, h, is_new(p + tok));
+                    double l, m;
+                    bool w;
+                    t[k].ends(l, m, w);
+                    lo = fmin(lo, l); hi = fmax(hi, m); bad |= w;
+                }
+#pragma unroll
+            for (int o = LPT; o < 64; o <<= 1) { lo = fmin(lo, __shfl_xor(lo, o, 64)); hi = fmax(hi, __shfl_xor(hi, o, 64)); bad |= __shfl_xor((int)bad, o, 64) != 0; }
+            const int turn = h & 1;      // (what the head before this one left is still read)
+            if (lane == 0) { ends[turn][0][wave] = lo; ends[turn][1][wave] = hi; bads[turn][wave] = bad; }
+            float2* const grid = grids_of(h);
+            float2 old = make_float2(0.f, 0.f);
+            if (had) old = *grid;
+            __syncthreads();
+            for (int w = 0; w < waves; ++w) { lo = fmin(lo, ends[turn][0][w]); hi = fmax(hi, ends[turn][1][w]); bad |= bads[turn][w] != 0; }
+            const Grid g = block_grid(lo, hi, bad, had, old.x, old.y);
+            if (threadIdx.x == 0) *grid = make_float2((float)g.s, (float)g.z);
+            for (int j0 = wave; j0 < tiles; j0 += KEPT * waves)
+#pragma unroll
+                for (int k = 0; k < KEPT; ++k) {
+                    const int j = j0 + k * waves, p = u.place + TOKENS * j;
+                    if (j >= tiles) continue;
+                    if (!once && some_new(p)) t[k].fetch(u.row0 + p, p, h, is_new(p + tok));
+                    t[k].put(levels_of(h, j), is_new(p + tok), min(max(u.first - p, 0), TOKENS), g, lds);
+                }
         }
     }
 }
 
-// One workgroup per unit, and its four wavefronts take heads of K (blockIdx.z 0) or V; where a unit is several tiles of 16 tokens (MANY): per unit and head, and they take its tiles.
-template <typename T, int NP, bool MANY>
-__global__ __launch_bounds__(256, NP <= 4 ? 2 : 1) void kv_append_kernel(AppendArgs<T> a) {
-    __shared__ __align__(16) unsigned char turned[4][32 * NP * 16];
+// One workgroup per unit and group of heads, K (blockIdx.z 0) or V.  FORM 1: a unit is one tile, of one or more blocks; 4: one block of at most four tiles.  In both, each of the four wavefronts
+// has `per` heads of its own.  FORM 0: one block of more tiles, which all wavefronts share for the same `per` heads.
+template <typename T, int LPT, int NP, int FORM>
+__global__ __launch_bounds__(FORM ? 256 : 64 * MOST_WAVES, 2) void kv_append_kernel(AppendArgs<T> a) {
+    __shared__ __align__(16) unsigned char turned[FORM ? 4 : MOST_WAVES][8 * LPT * NP * (64 / LPT)];
     const int ul = a.unit_log, room = a.q.room;
     int x = blockIdx.x, b;
     KvSeq s;
@@ -447,8 +487,8 @@ __global__ __launch_bounds__(256, NP <= 4 ? 2 : 1) void kv_append_kernel(AppendA
     u.page = a.cache + (long long)page * a.g.page_bytes;
     u.in_page = u.place & ((1 << a.g.pt_log) - 1);
     unsigned char* const lds = turned[threadIdx.x >> 6];
-    if (blockIdx.z == 0 && a.rot.dim) append_unit<T, NP, true, MANY>(a, u, 0, lds);
-    else append_unit<T, NP, false, MANY>(a, u, blockIdx.z, lds);
+    if (blockIdx.z == 0 && a.rot.dim) append_unit<T, LPT, NP, true, FORM>(a, u, 0, lds);
+    else append_unit<T, LPT, NP, false, FORM>(a, u, blockIdx.z, lds);
 }
 
 template <typename T>
@@ -470,31 +510,41 @@ int head_norm_rotate(tboa_ctx* ctx, long long n_tokens, int dh, int nq, const vo
     return 0;
 }
 
-template <typename T, int NP>
-int append(tboa_ctx* ctx, const AppendArgs<T>& a, long long units) {
-    if (a.unit_log > 4) {
-        hipLaunchKernelGGL((kv_append_kernel<T, NP, true>), dim3((unsigned)units, (unsigned)a.g.heads, 2), dim3(256), 0, ctx->stream, a);
-    } else {
-        // heads that one wavefront goes through: as few as fill the chip (256 compute units, 16 wavefronts each), for the tile is found once for all of them
-        const long long all = units * a.g.heads * 2;
-        const int per = (int)std::min<long long>(std::max<long long>(all / 4096, 1), 8), groups = (a.g.heads + 4 * per - 1) / (4 * per);
-        hipLaunchKernelGGL((kv_append_kernel<T, NP, false>), dim3((unsigned)units, (unsigned)groups, 2), dim3(256), 0, ctx->stream, a);
-    }
+template <typename T, int LPT, int NP>
+int append(tboa_ctx* ctx, AppendArgs<T> a) {
+    int tile_log = 0;
+    while (LPT << tile_log < 64) ++tile_log;
+    a.unit_log = std::max(tile_log, a.g.st_log);
+    const int tiles = 1 << (a.unit_log - tile_log), waves = tiles <= (NP == 1 ? 4 : 1) ? 1 : std::min(tiles, MOST_WAVES);
+    const long long units = std::min<long long>(a.q.n_tokens, (a.q.n_tokens >> a.unit_log) + 2LL * a.q.n_seqs);
+    // heads that one wavefront, or a workgroup of several tiles, goes through: as few as fill the chip (256 compute units, 16 wavefronts each), for the tile is found once for all of them
+    const int most = (int)std::min<long long>(std::max<long long>(units * a.g.heads * 2 * waves / 4096, 1), 8) * (waves > 1 ? 1 : 4);      // of a workgroup
+    const unsigned groups = (unsigned)((a.g.heads + most - 1) / most);
+    a.per = (a.g.heads + (int)groups - 1) / (int)groups;
+    if (waves == 1) a.per = (a.per + 3) / 4;
+    if (waves > 1) hipLaunchKernelGGL((kv_append_kernel<T, LPT, NP, 0>), dim3((unsigned)units, groups, 2), dim3(64 * waves), 0, ctx->stream, a);
+    else if (tiles == 1) hipLaunchKernelGGL((kv_append_kernel<T, LPT, NP, 1>), dim3((unsigned)units, groups, 2), dim3(256), 0, ctx->stream, a);
+    else if constexpr (NP == 1) hipLaunchKernelGGL((kv_append_kernel<T, LPT, NP, 4>), dim3((unsigned)units, groups, 2), dim3(256), 0, ctx->stream, a);
     TB_KERNEL_CHECK(ctx);
     return 0;
 }
+template <typename T, int DP>
+int append(tboa_ctx* ctx, const AppendArgs<T>& a) {
+    constexpr int LANES = DP <= 32 ? 4 : DP <= 64 ? 8 : 16;
+    return append<T, LANES, (DP / 8 + LANES - 1) / LANES>(ctx, a);
+}
 template <typename T>
-int append(tboa_ctx* ctx, AppendArgs<T> a, long long units) {
+int append(tboa_ctx* ctx, AppendArgs<T> a) {
     const int e = 16 / (int)sizeof(T);
     for (int i = 0; i < 2; ++i) a.vec[i] = a.g.dh % 8 == 0 && ((uintptr_t)a.x[i] & 15) == 0 && a.ld[i] % e == 0;
     a.vec_table = a.rot.dim % 16 == 0 && ((uintptr_t)a.rot.table & 15) == 0;
     switch (a.g.dp) {
-        case 32: return append<T, 1>(ctx, a, units);
-        case 64: return append<T, 2>(ctx, a, units);
-        case 96: return append<T, 3>(ctx, a, units);
-        case 128: return append<T, 4>(ctx, a, units);
-        case 192: return append<T, 6>(ctx, a, units);
-        default: return append<T, 8>(ctx, a, units);
+        case 32: return append<T, 32>(ctx, a);
+        case 64: return append<T, 64>(ctx, a);
+        case 96: return append<T, 96>(ctx, a);
+        case 128: return append<T, 128>(ctx, a);
+        case 192: return append<T, 192>(ctx, a);
+        default: return append<T, 256>(ctx, a);
     }
 }
 
@@ -570,10 +620,8 @@ extern "C" int tboa_kv_cache_append(tboa_ctx* ctx, const tboa_kv_cache_desc* des
     if (batch->n_seqs == 0 || batch->n_tokens == 0 || batch->pages_per_seq == 0 || g.n_pages == 0) return 0;
     if (!K || !V) return tboa_fail(ctx, TBOA_EINVAL, "kv_cache_append: null argument");
     if (ldk < (int64_t)g.heads * g.dh || ldv < (int64_t)g.heads * g.dh) return tboa_fail(ctx, TBOA_EINVAL, "kv_cache_append: a row pitch is smaller than its heads");
-    const int unit_log = std::max(4, g.st_log);
-    const long long units = std::min<long long>(batch->n_tokens, (batch->n_tokens >> unit_log) + 2LL * batch->n_seqs);
     const KvBatch q{batch->n_seqs, batch->pages_per_seq, (int)batch->n_tokens, batch->pages_per_seq * desc->page_tokens, batch->starts, batch->lens, batch->pages};
     KvDevice dev(ctx->device);
-    if (dtype == TBOA_F32) return append<float>(ctx, AppendArgs<float>{g, q, {(const float*)K, (const float*)V}, {ldk, ldv}, rot, positions, (unsigned char*)cache, unit_log, {}, false}, units);
-    return append<bf16>(ctx, AppendArgs<bf16>{g, q, {(const bf16*)K, (const bf16*)V}, {ldk, ldv}, rot, positions, (unsigned char*)cache, unit_log, {}, false}, units);
+    if (dtype == TBOA_F32) return append<float>(ctx, AppendArgs<float>{g, q, {(const float*)K, (const float*)V}, {ldk, ldv}, rot, positions, (unsigned char*)cache, 0, 0, {}, false});
+    return append<bf16>(ctx, AppendArgs<bf16>{g, q, {(const bf16*)K, (const bf16*)V}, {ldk, ldv}, rot, positions, (unsigned char*)cache, 0, 0, {}, false});
 }

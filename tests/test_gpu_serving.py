@@ -218,6 +218,29 @@ def test_scales_of_any_size(ctx, lib, dtype, new, kind):
     check(got, cache, starts, lens, pages, q, 1 / 8, 0, dtype)
 
 
+@pytest.mark.parametrize("heads,dh,st,new", [(9, 64, 1, 4101), (33, 64, 16, 2050), (13, 128, 16, 2050), (33, 128, 64, 1030), (18, 256, 64, 1030), (34, 32, 8, 2050)])
+def test_prompts_that_fill_the_chip(ctx, lib, heads, dh, st, new):
+    """So many blocks that a wavefront goes through several heads, whose number is no multiple of anything; the prompt begins inside a block whose grid has to grow."""
+    had = st // 2
+    total, pages = layout([had + new], 64, 6)
+    cache = lib.KVCache(torch.zeros(total, lib.KVCache.page_bytes(heads, dh, 64, st), dtype=torch.uint8, device="cuda"), heads, dh, 64, st)
+    want = ref.Cache(cache.data.cpu().numpy(), heads, dh, 64, st)
+    g = torch.Generator().manual_seed(heads)
+    tab = table(had + new, dh)
+    for size, a, e in ((0.1, 0, had), (1.0, had, had + new)):
+        if a == e:
+            continue
+        k, v = ((size * torch.randn(e - a, heads, dh, generator=g)).bfloat16() for _ in "kv")
+        ctx.kv_cache_append(cache, lib.KVBatch(i32([0, e - a]), i32([e]), i32(pages)), k.cuda(), v.cuda(), rotation=lib.Rotation(tab.cuda()))
+        torch.cuda.synchronize()
+        x = f64(k).reshape(e - a, heads, 2, dh // 2)
+        c, s = (np.asarray(tab[a:e], np.float64).reshape(e - a, 1, 2, dh // 2)[:, :, i] for i in range(2))
+        turned = np.stack([x[:, :, 0] * c - x[:, :, 1] * s, x[:, :, 1] * c + x[:, :, 0] * s], 2).reshape(e - a, heads, dh)
+        ref.append(want, [0, e - a], [e], pages, turned, f64(v), e - a)
+        got = cache.data.cpu().numpy()
+        assert np.array_equal(got, want.data), np.argwhere(got != want.data)[:5]
+
+
 def test_refusals_of_the_append(ctx, lib):
     cache = lib.KVCache.empty(3, 2, 64, 16, 1)
     x = torch.zeros(2, 2, 64, device="cuda")
