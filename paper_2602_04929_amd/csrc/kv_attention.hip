@@ -53,11 +53,30 @@ struct AttendArgs {
     const unsigned char* cache;
     float scale2;                 // scale log2 e
     int rep, window, vec;         // vec: 16-byte pieces of Q
+    int out_piece;                // elements of O that may be written together: 8, 4 or 1
     int few;                      // sequences of more rows are kv_attend_tiles_kernel's
     int4* info;                   // per workgroup: the unit that begins in its share and ends in another: workgroups, first row of the sequence, row of the first | rows << 27, head
     float* tile_part; float2* tile_stat;      // kv_attend_tiles_kernel: per piece, its rows
     float* part; float2* stat;    // per workgroup two pieces of 16 rows (of a unit that began before its share, of one that begins in it): unscaled outputs; maximum, sum
 };
+
+// channels c .. c + 3 of a row of the outputs
+__device__ __forceinline__ void store4(float* out, int c, const AttendArgs& a, f4 v) {
+    if (a.out_piece >= 4) { if (c < a.g.dh) *(f4*)(out + c) = v; return; }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) if (c + j < a.g.dh) out[c + j] = v[j];
+}
+__device__ __forceinline__ uint2 pack4(f4 v) {
+    union { bf16 e[4]; uint2 u; } p;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) p.e[j] = from_f32<bf16>(v[j]);
+    return p.u;
+}
+__device__ __forceinline__ void store4(bf16* out, int c, const AttendArgs& a, f4 v) {
+    if (a.out_piece >= 4) { if (c < a.g.dh) *(uint2*)(out + c) = pack4(v); return; }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) if (c + j < a.g.dh) out[c + j] = from_f32<bf16>(v[j]);
+}
 
 constexpr int HALF_TOP = 14;      // a probability of 1 with the largest scale becomes 2^14 as half, at most: parts of 2^-28 of it are still normal numbers
 constexpr int ROWS = 16, TILE = 64;      // rows (query token, head of the group) of a unit, tokens a wavefront takes at a time
@@ -318,8 +337,7 @@ __global__ __launch_bounds__(256, resident<DP>()) void kv_attend_rows_kernel(Att
             if (whole) {
                 const int row = r0 + rr, tk = row / a.rep;
                 T* out = (T*)a.O + (long long)(s.start + tk) * a.ldo + (long long)(h * a.rep + row - tk * a.rep) * a.g.dh;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) if (c + j < a.g.dh) out[c + j] = from_f32<T>(sum == 0.f ? 0.f : v[j] / sum);
+                store4(out, c, a, sum == 0.f ? f4{0.f, 0.f, 0.f, 0.f} : v / sum);
             } else {
                 *(f4*)(a.part + (piece + rr) * DP + c) = v;
                 if (c == 0) a.stat[piece + rr] = make_float2(tp, sum);
@@ -374,8 +392,7 @@ __global__ __launch_bounds__(256) void kv_attend_join_kernel(AttendArgs a) {
     if (group == 0) {
         const int row = r0 + rr, tk = row / a.rep;
         T* out = (T*)a.O + (long long)(info.y + tk) * a.ldo + (long long)(h * a.rep + row - tk * a.rep) * a.g.dh;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) if (4 * c + i < a.g.dh) out[4 * c + i] = from_f32<T>(sum == 0.f ? 0.f : all[i] / sum);
+        store4(out, 4 * c, a, sum == 0.f ? f4{0.f, 0.f, 0.f, 0.f} : all / sum);
     }
 }
 
@@ -734,19 +751,32 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
     if (W > 4 && !later) run_ends();      // as many as the others
     l += from_xor<32>(l);
     if (l != l) m = fmaxf(m, 0.f);      // scores that are all NaN leave the maximum where it was
-    if (!row_live) return;
     const bool none = m == -__builtin_inff();
     if (u.n_cuts == 1) {
         bf16* const out = (bf16*)a.O + (long long)(s.start + tok) * a.ldo + (long long)(h * a.rep + r - tok * a.rep) * a.g.dh;
         const float f = none || l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
-        for (int c = 0; c < CT; ++c)
+        for (int c = 0; c < CT; ++c) {
+            f4 v[4];      // channels 32 c + 8 g + 4 half ..
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int ch = 32 * c + 8 * (i >> 2) + 4 * half + (i & 3);
-                if (ch < a.g.dh) out[ch] = from_f32<bf16>(none || l == 0.f ? 0.f : __builtin_amdgcn_ldexpf(o[c][i] * f, -up));
+            for (int g = 0; g < 4; ++g)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[g][k] = none || l == 0.f ? 0.f : __builtin_amdgcn_ldexpf(o[c][4 * g + k] * f, -up);
+            if (a.out_piece == 8) {      // the two halves of the wavefront exchange theirs for whole 16-byte pieces
+#pragma unroll
+                for (int g = 0; g < 4; g += 2) {
+                    const uint2 x = pack4(v[g]), y = pack4(v[g + 1]);
+                    const auto p = __builtin_amdgcn_permlane32_swap(x.x, y.x, false, false), q = __builtin_amdgcn_permlane32_swap(x.y, y.y, false, false);
+                    const int ch = 32 * c + 8 * (g + half);
+                    if (row_live && ch < a.g.dh) *(uint4*)(out + ch) = make_uint4(p[0], q[0], p[1], q[1]);
+                }
+            } else if (row_live) {
+#pragma unroll
+                for (int g = 0; g < 4; ++g) store4(out, 32 * c + 8 * g + 4 * half, a, v[g]);
             }
+        }
     } else {
+        if (!row_live) return;
         const long long at = (long long)blockIdx.x * RT + w0 + col;
         if (half == 0) a.tile_stat[at] = make_float2(m, l);
 #pragma unroll
@@ -797,6 +827,14 @@ __global__ __launch_bounds__(256) void kv_attend_tiles_join_kernel(AttendArgs a)
 int shares(int dp) { return 256 * (dp == 32 ? resident<32>() : dp == 64 ? resident<64>() : dp <= 128 ? resident<128>() : resident<256>()); }
 constexpr int FEW = 32;      // rows of a sequence up to which kv_attend_rows_kernel takes it
 int unit_rows_of(int dp) { return 32 * (dp <= 128 ? waves<128>() : waves<256>()); }
+// Calls whose units of 16 rows, by what the host knows, are few and short: the rows' kernel alone.  Two units (or a few of three) per workgroup of it are done before a tiles' workgroup has gone through the
+// serial part of its first one: 256 new tokens of one sequence (64 query heads of 128, 8 KV heads, 1024 units) 25 us, not 46; 64 behind 4000 others 45, not 110; 512 (2048 units) 54 and 72,
+// but 16 sequences of 250 (8192) 158 and 62.  Long ones have to read the cache for every 16 rows instead of 256: 256 new tokens behind 4000 others (68000 tiles of all units) 107 and 109,
+// behind 31000 others 635 and 334.
+bool is_small(const KvGeometry& g, const tboa_kv_batch& b, int rep, int window) {
+    const long long room = ((long long)b.pages_per_seq << g.pt_log) + TILE, units = (b.n_tokens * rep / ROWS + std::min<long long>(b.n_seqs, b.n_tokens)) * g.heads;
+    return units <= 9 * shares(g.dp) / 4 && units * ((window ? std::min<long long>(room, (long long)window + b.n_tokens + 2 * TILE) : room) / TILE) <= 65536;
+}
 // Row tiles of all sequences that kv_attend_tiles_kernel takes: at most one more per sequence than rows / RT, and one per token or more
 long long most_units(const KvGeometry& g, int n_seqs, long long n_tokens, int rep) {
     const int rt = unit_rows_of(g.dp);
@@ -880,7 +918,8 @@ extern "C" int tboa_kv_cache_attention(tboa_ctx* ctx, const tboa_kv_cache_desc* 
     KvDevice dev(ctx->device);
     // sequences of more than FEW rows go to the tiles' kernel (16-bit inputs), the others to the rows'; what the caller says of the batch may spare one of the two launches
     const long long most = batch->max_new > 0 ? std::min<long long>(batch->max_new, batch->n_tokens) : batch->n_tokens;
-    const bool tiles = dtype == TBOA_BF16 && most * rep > FEW, rows = !tiles || batch->n_seqs > 1 || batch->n_tokens * rep <= FEW;
+    const bool tiles = dtype == TBOA_BF16 && most * rep > FEW && !is_small(g, *batch, rep, window);
+    const bool rows = !tiles || batch->n_seqs > 1 || batch->n_tokens * rep <= FEW;
     const long long units = tiles ? most_units(g, batch->n_seqs, batch->n_tokens, rep) : 0;
     if (units > 2147483647LL) return tboa_fail(ctx, TBOA_EINVAL, "kv_cache_attention: too many rows");
     TB_TRY(tboa_ws_reserve(ctx, room(g, tiles, units, nullptr, nullptr)));
@@ -892,6 +931,7 @@ extern "C" int tboa_kv_cache_attention(tboa_ctx* ctx, const tboa_kv_cache_desc* 
     a.scale2 = (float)((scale == 0.0 ? 1.0 / sqrt((double)g.dh) : scale) * 1.4426950408889634);
     a.rep = rep; a.window = window < KV_MOST_TOKENS ? window : 0;      // (no sequence is longer)
     a.vec = g.dh % 8 == 0 && ((uintptr_t)Q & 15) == 0 && ldq * size % 16 == 0;
+    a.out_piece = g.dh % 8 == 0 && ldo % 8 == 0 && ((uintptr_t)O & 15) == 0 ? 8 : g.dh % 4 == 0 && ldo % 4 == 0 && ((uintptr_t)O & (4 * size - 1)) == 0 ? 4 : 1;
     a.few = !tiles ? 1 << 30 : rows ? FEW : 0;
     room(g, tiles, units, &a, ctx->ws);
     return dtype == TBOA_F32 ? attend<float>(ctx, a, rows, units) : attend<bf16>(ctx, a, rows, units);

@@ -6,6 +6,7 @@ import torch
 
 from paper_2602_04929_amd import pipeline, synth
 from tests import serving_ref as ref
+from tests import test_gpu_kv_cache_attention as attention
 from tests.test_gpu_head_norm_rotate import close, table
 from tests.test_gpu_kv_cache_append import i32, layout
 from tests.test_gpu_kv_cache_attention import case, check
@@ -198,6 +199,59 @@ def test_windows_longer_than_any_sequence(ctx, lib, dtype, new):
     for window in (1 << 30, (1 << 31) - 1, (1 << 30) - 1, 3):
         assert torch.equal(ctx.kv_cache_attention(dev, batch, q, window=window), base), window
     check(base, cache, starts, lens, pages, q, 1 / 8, 0, dtype)
+
+
+@pytest.fixture
+def wide_tables(monkeypatch):
+    """Rows of pages for 2^22 tokens, of which the sequences have few: by what the host knows these are long calls, and prompts of 16-bit inputs take the kernel for many rows."""
+    def wide(lens, pt, seed, *args):
+        total, pages = layout(lens, pt, seed, *args)
+        return total, np.pad(pages, ((0, 0), (0, (1 << 22) // pt - pages.shape[1])), constant_values=-1)
+    monkeypatch.setattr(attention, "layout", wide)
+
+
+@pytest.mark.parametrize("shape", [s for s in attention.SHAPES if max(s[3]) * s[1] > 32 and not s[5]], ids=lambda s: "-".join(str(x).replace(" ", "") for x in s))
+def test_few_rows_in_wide_tables(ctx, lib, wide_tables, shape):
+    attention.test_ragged_batches(ctx, lib, torch.bfloat16, shape)
+
+
+def test_special_cases_in_wide_tables(ctx, lib, wide_tables):
+    attention.test_values_that_are_special(ctx, lib, torch.bfloat16, 50)
+    for kind in ("nothing", "least", "small", "mixed", "late"):
+        test_scales_of_any_size(ctx, lib, torch.bfloat16, 50, kind)
+    test_windows_longer_than_any_sequence(ctx, lib, torch.bfloat16, [50, 3, 1])
+
+
+@pytest.mark.parametrize("pt", [16, 64])
+def test_holes_in_wide_tables(ctx, lib, wide_tables, pt):
+    """Pages outside the cache, the first and the last one of a sequence among them, and one sequence that has none."""
+    new, lens = [40, 33, 70, 20], [300, 290, 80, 64]
+    starts, pages, cache, dev, q = case(lib, 2, 2, 64, new, lens, pt, 1, torch.bfloat16, 22)
+    pages[0, 1], pages[1, 0], pages[1, 289 // pt], pages[2, :] = -1, len(cache.data), 1 << 30, -7
+    got = ctx.kv_cache_attention(dev, lib.KVBatch(i32(starts), i32(lens), i32(pages)), q)
+    torch.cuda.synchronize()
+    check(got, cache, starts, lens, pages, q, 1 / 8, 0, torch.bfloat16)
+    assert (got[starts[2]:starts[3]] == 0).all()
+
+
+@pytest.mark.parametrize("heads,rep,dh,window,pt,st", [(12, 8, 128, 100, 64, 1), (6, 8, 256, 33, 16, 16), (20, 8, 64, 1, 128, 4), (13, 8, 90, 257, 32, 32), (25, 6, 32, 64, 64, 1)])
+def test_windows_of_many_rows(ctx, lib, heads, rep, dh, window, pt, st):
+    """Windows that cut tiles at their lower end, so many rows that the kernel for many takes them."""
+    new, lens = [200, 90, 3], [400, 91, 500]
+    starts, pages, cache, dev, q = case(lib, heads, rep, dh, new, lens, pt, st, torch.bfloat16, 13, spare_rows=2)
+    batch = lib.KVBatch(i32(starts), i32(lens), i32(pages))
+    out = torch.full_like(q, 7)
+    ctx.kv_cache_attention(dev, batch, q, window=window, out=out)
+    torch.cuda.synchronize()
+    check(out, cache, starts, lens, pages, q, 1 / np.sqrt(dh), window, torch.bfloat16)
+    assert (out[starts[-1]:] == 7).all()
+    # outputs that are not aligned to 16 bytes, or to 8: the same values
+    for shift in (4, 1):
+        odd = torch.full((q.numel() + 8,), 7, dtype=q.dtype, device="cuda")
+        view = odd[shift:shift + q.numel()].view(q.shape)
+        ctx.kv_cache_attention(dev, batch, q, window=window, out=view)
+        torch.cuda.synchronize()
+        assert torch.equal(view, out) and (odd[:shift] == 7).all() and (odd[shift + q.numel():] == 7).all()
 
 
 @pytest.mark.parametrize("new", [1, 50])
