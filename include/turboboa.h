@@ -280,7 +280,7 @@ int tboa_dequant_gemv(tboa_ctx* ctx, int d_out, int d_in, int bits, int group, c
  *   levels of K  uint8 [n_kv_heads][page_tokens][dp]            dp: head_dim rounded up to 32, 64, 96, 128, 192 or 256 (what is beyond head_dim is neither read as a number nor written)
  *   levels of V  uint8 [n_kv_heads][page_tokens / 16][dp][16]   the 16 tokens of a channel side by side
  *   grids of K, then of V  fp32 [n_kv_heads][page_tokens / scale_tokens][2]: scale, zero of a head's block of scale_tokens tokens
- * and level c stands for scale * (c - zero).  Pages need not be cleared before use: no token beyond a sequence's length is read as a number. */
+ * and level c stands for scale * (c - zero), scale not negative, zero a whole number of 0 .. 255.  Pages need not be cleared before use: no token beyond a sequence's length is read as a number. */
 typedef struct {
     int n_kv_heads;     /* 1 .. 65535 */
     int head_dim;       /* 1 .. 256 */
@@ -311,7 +311,7 @@ typedef struct {
 size_t tboa_kv_cache_page_bytes(const tboa_kv_cache_desc* desc);      /* host value, no context needed; 0 for an invalid descriptor */
 
 /* Norms of the query and key vectors of every head, and their rotation, in one pass:  y = x / sqrt(mean(x^2) + eps) * w, rotated.
- *   Q [n_tokens][n_q_heads * head_dim], K likewise, in `dtype` (TBOA_F32 or TBOA_BF16), rows ldq, ldk elements apart; Q_out, K_out likewise (each may be its input); either side may have no heads
+ *   Q [n_tokens][n_q_heads * head_dim], K likewise, in `dtype` (TBOA_F32 or TBOA_BF16), rows ldq, ldk elements apart; Q_out, K_out likewise (each may be its input, with the same pitch, and overlaps nothing else); either side may have no heads
  *   w_q, w_k  fp32 [head_dim], or NULL: that side is not normalised
  *   rotation  NULL: none; positions  device [n_tokens] (needed with a rotation)
  * Sums of squares in fp64, everything else in fp32, one rounding at the end. */
@@ -332,7 +332,7 @@ int tboa_kv_cache_append(tboa_ctx* ctx, const tboa_kv_cache_desc* desc, const tb
 /* O[i, h] = sum_t A[t] v_t, A = softmax over t of scale * q_{i,h} . k_t, with k, v of KV head h / (n_q_heads / n_kv_heads) from the cache, t over the places of row i's sequence up to its own
  * (and, with window > 0, the last `window` of them, its own included).  Rows that see nothing get 0.
  *   Q, O [n_tokens][n_q_heads * head_dim] in `dtype`, rows ldq, ldo elements apart; scale 0: 1/sqrt(head_dim).  n_tokens * (n_q_heads / n_kv_heads) < 2^27
- * Levels enter the products exactly.  TBOA_BF16: q as it is, probabilities times scale rounded to 11 bits, fp32 sums; TBOA_F32: both as pairs of 11 bits. */
+ * O overlaps neither Q nor the cache.  Levels enter the products exactly.  TBOA_BF16: q as it is, probabilities times scale rounded to 11 bits, fp32 sums; TBOA_F32: both as pairs of 11 bits. */
 size_t tboa_kv_cache_attention_workspace_bytes(const tboa_kv_cache_desc* desc, int n_q_heads, int n_seqs, int64_t n_tokens);
 int tboa_kv_cache_attention(tboa_ctx* ctx, const tboa_kv_cache_desc* desc, const tboa_kv_batch* batch, int n_q_heads, int dtype, const void* Q, int64_t ldq,
                             const void* cache, double scale, int window, void* O, int64_t ldo);
