@@ -7,6 +7,7 @@ library raises: there is no fallback path.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 
 import torch
@@ -156,6 +157,7 @@ class KVCache:
         self.data = data
 
     @staticmethod
+    @functools.lru_cache(maxsize=64)
     def page_bytes(n_kv_heads, head_dim, page_tokens=64, scale_tokens=1):
         n = int(_lib.tboa_kv_cache_page_bytes(C.byref(KVCacheDesc(n_kv_heads, head_dim, page_tokens, scale_tokens, 0))))
         assert n > 0, "no cache has %d heads of %d channels, pages of %d and scales of %d tokens" % (n_kv_heads, head_dim, page_tokens, scale_tokens)

@@ -112,15 +112,18 @@ __global__ __launch_bounds__(256, resident<DP>()) void kv_attend_rows_kernel(Att
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, grp = lane >> 4;
     KvSeq head{0, 0, 0};
     long long total = 0;
+    int longest = 1;      // tiles of a unit, up to four
     for (int i = lane; i < a.q.n_seqs; i += 64) {
         const KvSeq e = kv_sequence(a.q, i);
         if (i < 64) head = e;
-        total += unit_tiles(e, a);
+        const long long mine = unit_tiles(e, a);
+        total += mine;
+        if (mine) longest = max(longest, min(seen_tiles(e, a), 4));
     }
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) total += __shfl_xor(total, o, 64);
     total = (long long)(unsigned)__builtin_amdgcn_readfirstlane((int)total) | (long long)__builtin_amdgcn_readfirstlane((int)(total >> 32)) << 32;
-    const long long share = max((total + gridDim.x - 1) / gridDim.x, 4LL);      // (four: a tile for each wavefront)
+    const long long share = max((total + gridDim.x - 1) / gridDim.x, 1LL + (__any(longest > 1) != 0) + (__any(longest > 2) != 0) + (__any(longest > 3) != 0));      // (four: a tile for each wavefront)
     long long at = blockIdx.x * share;
     const long long at_end = min(at + share, total);
     if (threadIdx.x == 0) a.info[blockIdx.x] = make_int4(0, 0, 0, 0);
@@ -411,7 +414,8 @@ constexpr int TILE_TOP = 8;      // as HALF_TOP
 template <int DP> constexpr int waves() { return DP <= 128 ? 8 : 4; }      // (wider heads need twice the registers)
 template <int DP> constexpr int permuted() { return DP % 128 == 0 ? 15 : DP % 64 == 0 ? 7 : 3; }      // bits of a piece's number that K's rows are XORed into
 template <int DP> constexpr int tiles_lds() { return 2 * 2 * TILE * DP * 2; }
-constexpr int TILES_TARGET = 512;                    // workgroups that the units of a call are cut into where they are fewer: two rounds of the chip
+constexpr int TILES_TARGET = 256;                    // pieces that the units of a call are cut into where they are fewer: one for each compute unit, which holds one workgroup at a time (512: 79 us for 1000 tokens
+                                                     // of 64 / 8 heads, not 50)
 
 struct TilesUnit { int b, h, tile, cut, n_cuts; KvSeq s; };
 template <int RT>
@@ -789,9 +793,10 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
     }
 }
 
-// Rows of units that were cut: a wavefront per row, as kv_attend_join_kernel
+// Rows of units that were cut: DP / 4 lanes per row, as kv_attend_join_kernel
 template <int DP, int RT>
 __global__ __launch_bounds__(256) void kv_attend_tiles_join_kernel(AttendArgs a) {
+    constexpr int LANES = DP / 4, GROUPS = 64 / LANES;
     TilesUnit u;
     {   // unit blockIdx.x: the piece with cut 0 tells how many there are
         KvSeq head{0, 0, 0};
@@ -805,37 +810,38 @@ __global__ __launch_bounds__(256) void kv_attend_tiles_join_kernel(AttendArgs a)
         if (split < 2 || !find_unit<RT>(a, blockIdx.x * split, u) || u.n_cuts < 2) return;
         u.cut = blockIdx.x * split;      // (its number)
     }
-    const int r0 = u.tile * RT, n_rows = min(RT, u.s.n * a.rep - r0), lane = threadIdx.x & 63;
-    for (int rr = blockIdx.y * 4 + (threadIdx.x >> 6); rr < n_rows; rr += 4 * gridDim.y) {
-        float top = -__builtin_inff();
+    const int r0 = u.tile * RT, n_rows = min(RT, u.s.n * a.rep - r0), lane = threadIdx.x & 63, c = 4 * (lane % LANES), group = lane / LANES;
+    if (group >= GROUPS || c >= a.g.dh) return;
+    for (int rr = (blockIdx.y * 4 + (threadIdx.x >> 6)) * GROUPS + group; rr < n_rows; rr += 4 * gridDim.y * GROUPS) {
+        float top = -__builtin_inff(), sum = 0.f;
+#pragma unroll 4
         for (int i = 0; i < u.n_cuts; ++i) top = fmaxf(top, a.tile_stat[(long long)(u.cut + i) * RT + rr].x);
+        f4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int i = 0; i < u.n_cuts; ++i) {
+            const long long at = (long long)(u.cut + i) * RT + rr;
+            const float2 st = a.tile_stat[at];
+            const float f = st.x == -__builtin_inff() ? 0.f : ex2(st.x - top);
+            sum += st.x == -__builtin_inff() ? 0.f : f * st.y;
+            v += f * *(const f4*)(a.tile_part + at * DP + c);
+        }
         const int row = r0 + rr, tk = row / a.rep;
         bf16* const out = (bf16*)a.O + (long long)(u.s.start + tk) * a.ldo + (long long)(u.h * a.rep + row - tk * a.rep) * a.g.dh;
-        for (int c = lane; c < a.g.dh; c += 64) {
-            float v = 0.f, sum = 0.f;
-#pragma unroll 4
-            for (int i = 0; i < u.n_cuts; ++i) {
-                const long long at = (long long)(u.cut + i) * RT + rr;
-                const float2 st = a.tile_stat[at];
-                const float f = st.x == -__builtin_inff() ? 0.f : ex2(st.x - top);
-                sum += st.x == -__builtin_inff() ? 0.f : f * st.y;
-                v += f * a.tile_part[at * DP + c];
-            }
-            out[c] = from_f32<bf16>(sum == 0.f ? 0.f : v / sum);
-        }
+        store4(out, c, a, sum == 0.f ? f4{0.f, 0.f, 0.f, 0.f} : v / sum);
     }
 }
 
 int shares(int dp) { return 256 * (dp == 32 ? resident<32>() : dp == 64 ? resident<64>() : dp <= 128 ? resident<128>() : resident<256>()); }
-constexpr int FEW = 32;      // rows of a sequence up to which kv_attend_rows_kernel takes it
+// Rows of a sequence up to which kv_attend_rows_kernel takes it (32 sequences behind 2000 others): 32 rows 155 us, not 247 (32 heads); 64 rows 270 and 267, or 67 and 70 (64 / 8 heads);
+// 128 rows 125 and 74.
+constexpr int FEW = 32;
 int unit_rows_of(int dp) { return 32 * (dp <= 128 ? waves<128>() : waves<256>()); }
-// Calls whose units of 16 rows, by what the host knows, are few and short: the rows' kernel alone.  Two units (or a few of three) per workgroup of it are done before a tiles' workgroup has gone through the
-// serial part of its first one: 256 new tokens of one sequence (64 query heads of 128, 8 KV heads, 1024 units) 25 us, not 46; 64 behind 4000 others 45, not 110; 512 (2048 units) 54 and 72,
-// but 16 sequences of 250 (8192) 158 and 62.  Long ones have to read the cache for every 16 rows instead of 256: 256 new tokens behind 4000 others (68000 tiles of all units) 107 and 109,
-// behind 31000 others 635 and 334.
+// Calls whose units of 16 rows, by what the host knows, are few and short: the rows' kernel alone.  Two units (or a few of three) per workgroup of it are done before a tiles' workgroup has gone
+// through the serial part of its first one: 36 new tokens behind 1093 others of six sequences (32 heads of 128, 576 units, 10000 tiles in all) 47 us, not 64; 256 new tokens of one (64 / 8 heads, 1024
+// units) 25, not 30; 64 behind 4000 others (256 units, 16000 tiles) 43 and 39, 16 behind 31000 (64 units, 31000 tiles) 96 and 52; 16 sequences of 250 (8192 units) 158 and 62.
 bool is_small(const KvGeometry& g, const tboa_kv_batch& b, int rep, int window) {
     const long long room = ((long long)b.pages_per_seq << g.pt_log) + TILE, units = (b.n_tokens * rep / ROWS + std::min<long long>(b.n_seqs, b.n_tokens)) * g.heads;
-    return units <= 9 * shares(g.dp) / 4 && units * ((window ? std::min<long long>(room, (long long)window + b.n_tokens + 2 * TILE) : room) / TILE) <= 65536;
+    return units <= 9 * shares(g.dp) / 4 && units * ((window ? std::min<long long>(room, (long long)window + b.n_tokens + 2 * TILE) : room) / TILE) <= 16384;
 }
 // Row tiles of all sequences that kv_attend_tiles_kernel takes: at most one more per sequence than rows / RT, and one per token or more
 long long most_units(const KvGeometry& g, int n_seqs, long long n_tokens, int rep) {
@@ -866,6 +872,7 @@ template <int DP>
 int attend_tiles(tboa_ctx* ctx, const AttendArgs& a, long long units) {
     constexpr int LDS = tiles_lds<DP>();
     const dim3 grid((unsigned)std::max<long long>(units, TILES_TARGET)), block(64 * waves<DP>());
+    const unsigned cut = (unsigned)std::min<long long>(units, TILES_TARGET / 2);      // units that may be cut
     if (a.g.pt_log >= 6) {
         TB_HIP(ctx, hipFuncSetAttribute((const void*)kv_attend_tiles_kernel<DP, true>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
         hipLaunchKernelGGL((kv_attend_tiles_kernel<DP, true>), grid, block, LDS, ctx->stream, a);
@@ -874,7 +881,7 @@ int attend_tiles(tboa_ctx* ctx, const AttendArgs& a, long long units) {
         hipLaunchKernelGGL((kv_attend_tiles_kernel<DP, false>), grid, block, LDS, ctx->stream, a);
     }
     TB_KERNEL_CHECK(ctx);
-    hipLaunchKernelGGL((kv_attend_tiles_join_kernel<DP, 32 * waves<DP>()>), dim3((unsigned)std::min<long long>(units, TILES_TARGET / 2), 8), dim3(256), 0, ctx->stream, a);
+    hipLaunchKernelGGL((kv_attend_tiles_join_kernel<DP, 32 * waves<DP>()>), dim3(cut, (unsigned)std::min<long long>(std::max(2048u / cut, 1u), 8 * waves<DP>())), dim3(256), 0, ctx->stream, a);
     TB_KERNEL_CHECK(ctx);
     return 0;
 }
