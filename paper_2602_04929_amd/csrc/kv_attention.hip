@@ -17,6 +17,9 @@ typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef float f16v __attribute__((ext_vector_type(16)));
 typedef unsigned u4 __attribute__((ext_vector_type(4)));
+typedef unsigned u2 __attribute__((ext_vector_type(2)));
+template <typename T> struct Four { typedef u4 type; };      // four elements
+template <> struct Four<bf16> { typedef u2 type; };
 
 __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(bf16 v) { return __bfloat162float(v); }
@@ -52,8 +55,8 @@ struct AttendArgs {
     const void* Q; long long ldq; void* O; long long ldo;
     const unsigned char* cache;
     float scale2;                 // scale log2 e
-    int rep, window, vec;         // vec: 16-byte pieces of Q
-    int out_piece;                // elements of O that may be written together: 8, 4 or 1
+    int rep, window;
+    int vec, out_piece;           // elements of Q that may be read together, 8, 4 or 0 (one by one); of O that may be written together: 8, 4 or 1
     int few;                      // sequences of more rows are kv_attend_tiles_kernel's
     int4* info;                   // per workgroup: the unit that begins in its share and ends in another: workgroups, first row of the sequence, row of the first | rows << 27, head
     float* tile_part; float2* tile_stat;      // kv_attend_tiles_kernel: per piece, its rows
@@ -189,7 +192,13 @@ __global__ __launch_bounds__(256, resident<DP>()) void kv_attend_rows_kernel(Att
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
                 const int c = k < 2 * K64 ? (k >> 1) * 64 + grp * 16 + (k & 1) * 8 : K64 * 64 + grp * 8;
-                if (a.vec) {
+                if (a.vec == 4) {
+                    union { typename Four<T>::type u[2]; T e[8]; } in;
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) in.u[j] = row_live && c + 4 * j < a.g.dh ? *(const typename Four<T>::type*)(q + c + 4 * j) : typename Four<T>::type{};
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[k][j] = to_f32(in.e[j]);
+                } else if (a.vec) {
                     union { u4 u[sizeof(T) / 2]; T e[8]; } in;
 #pragma unroll
                     for (int j = 0; j < (int)sizeof(T) / 2; ++j) in.u[j] = row_live && c < a.g.dh ? ((const u4*)(q + c))[j] : u4{0, 0, 0, 0};
@@ -628,8 +637,12 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
             const int c = k * 16 + half * 8;
-            union { u4 w; bf16 e[8]; h8 v; } in;
-            if (a.vec) in.w = row_live && c < a.g.dh ? *(const u4*)(q + c) : u4{0, 0, 0, 0};
+            union { u4 w; u2 f[2]; bf16 e[8]; h8 v; } in;
+            if (a.vec == 8) in.w = row_live && c < a.g.dh ? *(const u4*)(q + c) : u4{0, 0, 0, 0};
+            else if (a.vec) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j) in.f[j] = row_live && c + 4 * j < a.g.dh ? *(const u2*)(q + c + 4 * j) : u2{0, 0};
+            }
             else {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) in.e[j] = row_live && c + j < a.g.dh ? q[c + j] : from_f32<bf16>(0.f);
@@ -939,7 +952,7 @@ extern "C" int tboa_kv_cache_attention(tboa_ctx* ctx, const tboa_kv_cache_desc* 
     a.Q = Q; a.ldq = ldq; a.O = O; a.ldo = ldo; a.cache = (const unsigned char*)cache;
     a.scale2 = (float)((scale == 0.0 ? 1.0 / sqrt((double)g.dh) : scale) * 1.4426950408889634);
     a.rep = rep; a.window = window < KV_MOST_TOKENS ? window : 0;      // (no sequence is longer)
-    a.vec = g.dh % 8 == 0 && ((uintptr_t)Q & 15) == 0 && ldq * size % 16 == 0;
+    a.vec = g.dh % 8 == 0 && ((uintptr_t)Q & 15) == 0 && ldq * size % 16 == 0 ? 8 : g.dh % 4 == 0 && ldq % 4 == 0 && ((uintptr_t)Q & (4 * size - 1)) == 0 ? 4 : 0;
     a.out_piece = g.dh % 8 == 0 && ldo % 8 == 0 && ((uintptr_t)O & 15) == 0 ? 8 : g.dh % 4 == 0 && ldo % 4 == 0 && ((uintptr_t)O & (4 * size - 1)) == 0 ? 4 : 1;
     a.few = !tiles ? 1 << 30 : rows ? FEW : 0;
     room(g, tiles, units, &a, ctx->ws);
