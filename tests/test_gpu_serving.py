@@ -245,13 +245,33 @@ def test_windows_of_many_rows(ctx, lib, heads, rep, dh, window, pt, st):
     torch.cuda.synchronize()
     check(out, cache, starts, lens, pages, q, 1 / np.sqrt(dh), window, torch.bfloat16)
     assert (out[starts[-1]:] == 7).all()
-    # outputs that are not aligned to 16 bytes, or to 8: the same values
+    shifted(ctx, dev, batch, q, out, window=window)
+
+
+def shifted(ctx, cache, batch, q, out, **kw):
+    """Queries and outputs that are not aligned to 16 bytes, or to 8: the same values."""
     for shift in (4, 1):
-        odd = torch.full((q.numel() + 8,), 7, dtype=q.dtype, device="cuda")
-        view = odd[shift:shift + q.numel()].view(q.shape)
-        ctx.kv_cache_attention(dev, batch, q, window=window, out=view)
-        torch.cuda.synchronize()
-        assert torch.equal(view, out) and (odd[:shift] == 7).all() and (odd[shift + q.numel():] == 7).all()
+        odd, moved = (torch.full((q.numel() + 8,), 7, dtype=q.dtype, device="cuda") for _ in "oq")
+        view, query = (x[shift:shift + q.numel()].view(q.shape) for x in (odd, moved))
+        query.copy_(q)
+        for a in (q, query):
+            view.fill_(7)
+            ctx.kv_cache_attention(cache, batch, a, out=view, **kw)
+            torch.cuda.synchronize()
+            assert torch.equal(view, out) and (odd[:shift] == 7).all() and (odd[shift + q.numel():] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("dh", [128, 100, 33])
+def test_unaligned_rows(ctx, lib, dtype, dh):
+    new, lens = [3, 1, 0, 9], [200, 90, 4, 2000]
+    starts, pages, cache, dev, q = case(lib, 2, 2, dh, new, lens, 16, 4, dtype, 14, spare_rows=1)
+    batch = lib.KVBatch(i32(starts), i32(lens), i32(pages))
+    out = torch.full_like(q, 7)
+    ctx.kv_cache_attention(dev, batch, q, out=out)
+    torch.cuda.synchronize()
+    check(out, cache, starts, lens, pages, q, 1 / np.sqrt(dh), 0, dtype)
+    shifted(ctx, dev, batch, q, out)
 
 
 @pytest.mark.parametrize("new", [1, 50])
