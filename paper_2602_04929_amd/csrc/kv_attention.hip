@@ -3,8 +3,9 @@
 // One pass over the cache with the running maximum and sum of the softmax.  Levels minus their zero are whole numbers up to 255 and so exact in half; they are made in registers from the
 // cache's bytes (a byte beside 0x64 is 1024 + level as half; one packed addition takes 1024 + zero away), and the scales multiply scores and probabilities:
 //     x[t] = (scale s^K_t log2 e) q.(c^K_t - z^K_t),   p = 2^(x - max),   O += (p s^V_t 2^14 / ref) (c^V_t - z^V_t),   ref: a power of two above the scales seen so far
-// Queries become half times a power of two that brings the largest of a tile to 2^13 .. 2^14 (bf16 queries stay exact down to 2^-31 of it); p s 2^14 / ref is rounded to half:
-// 2^-11 of it at most, an eighth of an output's rounding to bf16.  fp32 queries and probabilities are split into two half terms (2^-22 of them at most).
+// Queries become half times a power of two that brings the largest of a tile to 2^13 .. 2^14 (bf16 queries stay exact down to 2^-31 of it); fp32 queries are split into two half
+// terms (2^-22 of them at most), and so is p s 2^14 / ref; but one half (2^-11 of it at most, an eighth of an output's rounding to bf16) in the kernel for many rows, whose matrix instructions
+// are its time: two would cost it a third (two prompts of 2048 tokens behind 4096 take 614 us, not 461), where single tokens wait for the cache's bytes (78.1 us, not 77.1; 70.1, not 69.0 for one long sequence).
 #include "kv_cache.h"
 #include <math.h>
 #include <algorithm>
@@ -108,7 +109,7 @@ __device__ __forceinline__ Span row_span(const KvSeq& s, const AttendArgs& a, in
 // Bound by the cache's bytes: 32 sequences of 1000 to 8000 tokens, 64 / 8 heads of 128 (319 MB): 67 us and 5 us for the pieces, 4.4 TB/s; one of 131000 tokens (285 MB): 50 + 9 us.
 template <typename T, int DP>
 __global__ __launch_bounds__(256, resident<DP>()) void kv_attend_rows_kernel(AttendArgs a) {
-    constexpr int NT = sizeof(T) == 2 ? 1 : 2;      // half terms of queries and probabilities
+    constexpr int NT = sizeof(T) == 2 ? 1 : 2, PT = 2;      // half terms of queries, of probabilities
     constexpr int K64 = DP / 64, K32 = (DP % 64) / 32, KS = DP / 32, CT = DP / 16;
     __shared__ float joined[4][ROWS][DP + 4];
     __shared__ float2 ends[4][ROWS];
@@ -297,14 +298,14 @@ __global__ __launch_bounds__(256, resident<DP>()) void kv_attend_rows_kernel(Att
 #pragma unroll
                 for (int i = 0; i < 16; ++i) if (hidden >> i & 1) p[i] = 0.f;
             }
-            h8 ph[NT][2];
+            h8 ph[PT][2];
 #pragma unroll
             for (int k = 0; k < 2; ++k)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     const _Float16 w = (_Float16)p[8 * k + j];
                     ph[0][k][j] = w;
-                    if constexpr (NT == 2) ph[1][k][j] = (_Float16)(p[8 * k + j] - (float)w);
+                    ph[1][k][j] = (_Float16)(p[8 * k + j] - (float)w);
                 }
             // zeros of V's 16 tokens as pairs
             h2 zo[8];
@@ -318,7 +319,7 @@ __global__ __launch_bounds__(256, resident<DP>()) void kv_attend_rows_kernel(Att
             for (int c = 0; c < CT; ++c) {
                 const h8 v0 = levels8(vr[c][0], vr[c][1], zo[0], zo[1], zo[2], zo[3]), v1 = levels8(vr[c][2], vr[c][3], zo[4], zo[5], zo[6], zo[7]);
 #pragma unroll
-                for (int n = 0; n < NT; ++n) { o[c] = mma16(v0, ph[n][0], o[c]); o[c] = mma16(v1, ph[n][1], o[c]); }
+                for (int n = 0; n < PT; ++n) { o[c] = mma16(v0, ph[n][0], o[c]); o[c] = mma16(v1, ph[n][1], o[c]); }
             }
         }
         l += from_xor<16>(l); l += from_xor<32>(l);
