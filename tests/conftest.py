@@ -1,3 +1,4 @@
+import gc
 import os
 import sys
 
@@ -19,4 +20,15 @@ def lib():
     if not torch.cuda.is_available():
         pytest.skip("no GPU")
     import paper_2602_04929_amd as tb
+    gc.collect()
+    gc.freeze()      # what the imports made is not looked through again after every test
     return tb
+
+
+@pytest.fixture(autouse=True)
+def collected(request):
+    """A test that keeps an exception (`pytest.raises(...) as e`) leaves its frame in a cycle, with the graphs that it captured.  They go here: a collection in the middle of a later test's capture would
+    destroy them there, where the device cannot be synchronised, and a destructor that fails ends the process."""
+    yield
+    if request.node.get_closest_marker("gpu"):
+        gc.collect()
