@@ -4,8 +4,9 @@
 // cache's bytes (a byte beside 0x64 is 1024 + level as half; one packed addition takes 1024 + zero away), and the scales multiply scores and probabilities:
 //     x[t] = (scale s^K_t log2 e) q.(c^K_t - z^K_t),   p = 2^(x - max),   O += (p s^V_t 2^14 / ref) (c^V_t - z^V_t),   ref: a power of two above the scales seen so far
 // Queries become half times a power of two that brings the largest of a tile to 2^13 .. 2^14 (bf16 queries stay exact down to 2^-31 of it); fp32 queries are split into two half
-// terms (2^-22 of them at most), and so is p s 2^14 / ref; but one half (2^-11 of it at most, an eighth of an output's rounding to bf16) in the kernel for many rows, whose matrix instructions
-// are its time: two would cost it a third (two prompts of 2048 tokens behind 4096 take 614 us, not 461), where single tokens wait for the cache's bytes (78.1 us, not 77.1; 70.1, not 69.0 for one long sequence).
+// terms (2^-22 of them at most), and so is p s 2^14 / ref; but one half (2^-11 of it at most, an eighth of an output's rounding to bf16) for bf16 queries of sequences of more than FEW rows, in
+// either kernel, so that a row's bits do not hang on which one takes it: two prompts of 2048 tokens behind 4096, whose time is matrix instructions, would take 614 us, not 461.  Single tokens
+// wait for the cache's bytes and pay one per cent for the second half (32 sequences 78.1 us, not 77.1; one of 131000 tokens 70.1, not 69.0).
 #include "kv_cache.h"
 #include <math.h>
 #include <algorithm>
@@ -87,6 +88,10 @@ constexpr int ROWS = 16, TILE = 64;      // rows (query token, head of the group
 // workgroups that a compute unit holds at once (registers): the shares that the work is cut into are 256 times as many
 template <int DP> constexpr int resident() { return DP <= 64 ? 3 : DP <= 128 ? 2 : 1; }
 
+// Rows of a sequence up to which kv_attend_rows_kernel takes it in any call (32 sequences behind 2000 others): 32 rows 155 us, not 247 (32 heads); 64 rows 270 and 267, or 67 and 70
+// (64 / 8 heads); 128 rows 125 and 74.
+constexpr int FEW = 32;
+
 // how a sequence is cut: row tiles, tiles of tokens that its rows see
 __device__ __forceinline__ int row_tiles(const KvSeq& s, int rep) { return (int)(((long long)s.n * rep + ROWS - 1) / ROWS); }
 __device__ __forceinline__ int seen_tiles(const KvSeq& s, const AttendArgs& a) {
@@ -109,7 +114,7 @@ __device__ __forceinline__ Span row_span(const KvSeq& s, const AttendArgs& a, in
 // Bound by the cache's bytes: 32 sequences of 1000 to 8000 tokens, 64 / 8 heads of 128 (319 MB): 67 us and 5 us for the pieces, 4.4 TB/s; one of 131000 tokens (285 MB): 50 + 9 us.
 template <typename T, int DP>
 __global__ __launch_bounds__(256, resident<DP>()) void kv_attend_rows_kernel(AttendArgs a) {
-    constexpr int NT = sizeof(T) == 2 ? 1 : 2, PT = 2;      // half terms of queries, of probabilities
+    constexpr int NT = sizeof(T) == 2 ? 1 : 2;      // half terms of queries
     constexpr int K64 = DP / 64, K32 = (DP % 64) / 32, KS = DP / 32, CT = DP / 16;
     __shared__ float joined[4][ROWS][DP + 4];
     __shared__ float2 ends[4][ROWS];
@@ -140,6 +145,7 @@ __global__ __launch_bounds__(256, resident<DP>()) void kv_attend_rows_kernel(Att
         if (x >> 31) { k0 = (int)(x % tiles); x /= tiles; h = (int)(x % a.g.heads); tile = (int)(x / a.g.heads); }
         else { const unsigned u = (unsigned)x / tiles; k0 = (unsigned)x - u * tiles; tile = u / a.g.heads; h = u - tile * a.g.heads; }
         h = __builtin_amdgcn_readfirstlane(h); k0 = __builtin_amdgcn_readfirstlane(k0); tile = __builtin_amdgcn_readfirstlane(tile);
+        const bool two = NT == 2 || s.n * a.rep <= FEW;      // half terms of probabilities
         const int k1 = (int)min((long long)tiles, k0 + (at_end - at));      // tiles k0 .. k1 - 1 of the unit
         const int r0 = tile * ROWS, n_rows = (int)min((long long)ROWS, (long long)s.n * a.rep - r0);
         const Span span = row_span(s, a, r0, n_rows);
@@ -298,7 +304,7 @@ __global__ __launch_bounds__(256, resident<DP>()) void kv_attend_rows_kernel(Att
 #pragma unroll
                 for (int i = 0; i < 16; ++i) if (hidden >> i & 1) p[i] = 0.f;
             }
-            h8 ph[PT][2];
+            h8 ph[2][2];
 #pragma unroll
             for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -318,8 +324,8 @@ __global__ __launch_bounds__(256, resident<DP>()) void kv_attend_rows_kernel(Att
 #pragma unroll
             for (int c = 0; c < CT; ++c) {
                 const h8 v0 = levels8(vr[c][0], vr[c][1], zo[0], zo[1], zo[2], zo[3]), v1 = levels8(vr[c][2], vr[c][3], zo[4], zo[5], zo[6], zo[7]);
-#pragma unroll
-                for (int n = 0; n < PT; ++n) { o[c] = mma16(v0, ph[n][0], o[c]); o[c] = mma16(v1, ph[n][1], o[c]); }
+                o[c] = mma16(v0, ph[0][0], o[c]); o[c] = mma16(v1, ph[0][1], o[c]);
+                if (two) { o[c] = mma16(v0, ph[1][0], o[c]); o[c] = mma16(v1, ph[1][1], o[c]); }
             }
         }
         l += from_xor<16>(l); l += from_xor<32>(l);
@@ -846,9 +852,6 @@ __global__ __launch_bounds__(256) void kv_attend_tiles_join_kernel(AttendArgs a)
 }
 
 int shares(int dp) { return 256 * (dp == 32 ? resident<32>() : dp == 64 ? resident<64>() : dp <= 128 ? resident<128>() : resident<256>()); }
-// Rows of a sequence up to which kv_attend_rows_kernel takes it (32 sequences behind 2000 others): 32 rows 155 us, not 247 (32 heads); 64 rows 270 and 267, or 67 and 70 (64 / 8 heads);
-// 128 rows 125 and 74.
-constexpr int FEW = 32;
 int unit_rows_of(int dp) { return 32 * (dp <= 128 ? waves<128>() : waves<256>()); }
 // Calls whose units of 16 rows, by what the host knows, are few and short: the rows' kernel alone.  Two units (or a few of three) per workgroup of it are done before a tiles' workgroup has gone
 // through the serial part of its first one: 36 new tokens behind 1093 others of six sequences (32 heads of 128, 576 units, 10000 tiles in all) 47 us, not 64; 256 new tokens of one (64 / 8 heads, 1024

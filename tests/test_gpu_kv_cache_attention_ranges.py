@@ -29,10 +29,10 @@ def attend(ctx, lib, cache, starts, lens, pages, q, **kw):
     return out
 
 
-@pytest.mark.parametrize("shape", [s for s in SHAPES if sum(s[3]) * s[1] <= 64] + [(2, 4, 128, [1, 1], [3000, 6001], 0, 64, 1), (1, 8, 64, [2], [5000], 700, 16, 16)],
+@pytest.mark.parametrize("shape", [s for s in SHAPES if max(s[3]) * s[1] <= 32] + [(2, 4, 128, [1, 1], [3000, 6001], 0, 64, 1), (1, 8, 64, [2], [5000], 700, 16, 16)],
                          ids=lambda s: "-".join(str(x).replace(" ", "") for x in s))
 def test_probabilities_of_few_rows(ctx, lib, shape):
-    """bf16 queries: probabilities have the 22 bits that those of fp32 queries have."""
+    """bf16 queries of sequences of up to 32 rows: probabilities have the 22 bits that those of fp32 queries have."""
     heads, rep, dh, new, lens, window, pt, st = shape
     starts, pages, cache, _, q = case(lib, heads, rep, dh, new, lens, pt, st, torch.bfloat16, 3 * dh + len(new))
     got = attend(ctx, lib, cache, starts, lens, pages, q, window=window)
