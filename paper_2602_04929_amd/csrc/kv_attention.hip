@@ -3,7 +3,7 @@
 // One pass over the cache with the running maximum and sum of the softmax.  Levels minus their zero are whole numbers up to 255 and so exact in half; they are made in registers from the
 // cache's bytes (a byte beside 0x64 is 1024 + level as half; one packed addition takes 1024 + zero away), and the scales multiply scores and probabilities:
 //     x[t] = (scale s^K_t log2 e) q.(c^K_t - z^K_t),   p = 2^(x - max),   O += (p s^V_t 2^14 / ref) (c^V_t - z^V_t),   ref: a power of two above the scales seen so far
-// Queries become half times a power of two that brings the largest of a tile to 2^13 .. 2^14 (bf16 queries stay exact down to 2^-31 of it); fp32 queries are split into two half
+// A row's query becomes half times a power of two that brings its largest channel to 2^13 .. 2^14 (bf16 queries stay exact down to 2^-31 of it, whatever other rows hold); fp32 queries are split into two half
 // terms (2^-22 of them at most), and so is p s 2^14 / ref; but one half (2^-11 of it at most, an eighth of an output's rounding to bf16) for bf16 queries of sequences of more than FEW rows, in
 // either kernel, so that a row's bits do not hang on which one takes it: two prompts of 2048 tokens behind 4096, whose time is matrix instructions, would take 614 us, not 461.  Single tokens
 // wait for the cache's bytes and pay one per cent for the second half (32 sequences 78.1 us, not 77.1; one of 131000 tokens 70.1, not 69.0).
@@ -218,8 +218,7 @@ __global__ __launch_bounds__(256, resident<DP>()) void kv_attend_rows_kernel(Att
 #pragma unroll
                 for (int j = 0; j < 8; ++j) { const float m = fabsf(v[k][j]); most = m < __builtin_inff() ? fmaxf(most, m) : most; }
             }
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) most = fmaxf(most, __shfl_xor(most, o, 64));
+            most = fmaxf(most, from_xor<16>(most)); most = fmaxf(most, from_xor<32>(most));      // of the row
             const int e = most > 0.f ? min(14 - __builtin_amdgcn_frexp_expf(most), 100) : 0;
             unit = __builtin_amdgcn_ldexpf(a.scale2, -e);
 #pragma unroll
@@ -242,7 +241,7 @@ __global__ __launch_bounds__(256, resident<DP>()) void kv_attend_rows_kernel(Att
 #pragma unroll
             for (int c = 0; c < CT; ++c) vr[c] = *(const u4*)(vb + c * 256);
             const bool there = held;
-            const float sk = gk.x * unit, zk = -1024.f - gk.y, gvx = gv.x, zv = -1024.f - gv.y;
+            const float sk = gk.x, zk = -1024.f - gk.y, gvx = gv.x, zv = -1024.f - gv.y;
             // scores
             f4 st[4];
 #pragma unroll
@@ -266,7 +265,7 @@ __global__ __launch_bounds__(256, resident<DP>()) void kv_attend_rows_kernel(Att
                 pk_next = page_of(t0 + 8 * TILE + 16 * (col >> 2)); pv_next = page_of(t0 + 8 * TILE + 16 * grp);
             }
             float p[16];
-            unroll<16>([&](auto I) { constexpr int i = I; p[i] = st[i >> 2][i & 3] * row_lane<i>(sk); });
+            unroll<16>([&](auto I) { constexpr int i = I; p[i] = st[i >> 2][i & 3] * (row_lane<i>(sk) * unit); });
             const bool all = t0 + TILE - 1 <= s.len - s.n + r0 / a.rep && t0 + TILE <= end && t0 >= (a.window ? span.lo + (n_rows - 1) / a.rep + 1 : 0) && __all(there);
             unsigned hidden = 0;
             if (!all) {
@@ -469,6 +468,14 @@ __device__ __forceinline__ float across_halves(float v) {      // maximum of lan
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
+template <typename F>
+__device__ __forceinline__ int over_rows(int v, F&& f) {      // of the 32 rows of a wavefront, where lanes l and l ^ 32 hold the same
+    v = f(v, __builtin_amdgcn_mov_dpp(v, 0xB1, 0xf, 0xf, true)); v = f(v, __builtin_amdgcn_mov_dpp(v, 0x4E, 0xf, 0xf, true));       // the others of four
+    v = f(v, __builtin_amdgcn_mov_dpp(v, 0x141, 0xf, 0xf, true)); v = f(v, __builtin_amdgcn_mov_dpp(v, 0x140, 0xf, 0xf, true));     // of eight, of sixteen
+    return f(__builtin_amdgcn_readlane(v, 0), __builtin_amdgcn_readlane(v, 16));
+}
+__device__ __forceinline__ int least(int a, int b) { return min(a, b); }
+__device__ __forceinline__ int greatest(int a, int b) { return max(a, b); }
 __device__ __forceinline__ void run_ends() {      // everything before it is before, what was written to LDS is there
     __builtin_amdgcn_sched_barrier(0);
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -637,7 +644,7 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
         if (later) { fetch_v(0, here); if (n_tiles > 1) fetch_k(1, next); }
     }
     h8 qf[KS];
-    float unit;
+    float unit, own;      // what multiplies a score: of the wavefront, of the row
     {
         const bf16* const q = (const bf16*)a.Q + (long long)(s.start + tok) * a.ldq + (long long)(h * a.rep + r - tok * a.rep) * a.g.dh;
         float most = 0.f;
@@ -658,10 +665,13 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
             for (int j = 0; j < 8; ++j) { const float m = fabsf(to_f32(in.e[j])); most = m < __builtin_inff() ? fmaxf(most, m) : most; }
             qf[k] = in.v;
         }
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) most = fmaxf(most, __shfl_xor(most, o, 64));
-        const int e = most > 0.f ? min(14 - __builtin_amdgcn_frexp_expf(most), 100) : 0;
-        unit = __builtin_amdgcn_ldexpf(a.scale2, -e);
+        most = across_halves(most);
+        // the row's own power of two; what multiplies scores on the way is the same for all rows (one that leaves 2^100 between it and the smallest exponent), the rest a power of two
+        const bool some = most > 0.f;
+        const int e = some ? min(14 - __builtin_amdgcn_frexp_expf(most), 100) : 0;
+        const int e0 = over_rows(some ? e : 128, least), e1 = over_rows(some ? e : -128, greatest), shared = e0 > e1 ? 0 : min(e1, e0 + 100);
+        unit = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(__builtin_amdgcn_ldexpf(a.scale2, -shared))));
+        own = some ? __builtin_amdgcn_ldexpf(1.f, shared - e) : 1.f;
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
             union { bf16 e[8]; h8 v; } in;
@@ -723,7 +733,7 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
             }
             const float sk[2] = {gk[0] * unit, gk[1] * unit};
             float p[32], part[4] = {0.f, 0.f, 0.f, 0.f};
-            unroll<32>([&](auto I) { constexpr int i = I; sc[i >> 4][i & 15] *= row_lane<i & 15>(sk[i >> 4]); p[i] = ex2(sc[i >> 4][i & 15] - m); part[i & 3] += p[i]; });
+            unroll<32>([&](auto I) { constexpr int i = I; sc[i >> 4][i & 15] *= row_lane<i & 15>(sk[i >> 4]); p[i] = ex2(fmaf(sc[i >> 4][i & 15], own, -m)); part[i & 3] += p[i]; });
             float sum = (part[0] + part[1]) + (part[2] + part[3]);
             const float s_most = fmaxf(gv[0], gv[1]);
             const bool all = t0 >= all0 && t0 + TILE - 1 <= all1 && there == 15u;
@@ -737,7 +747,7 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
                     if ((unsigned)(32 * (i >> 4) + 16 * (i >> 3 & 1) + (i & 7) - first_seen) >= seen || (gone >> (i >> 3) & 1)) sc[i >> 4][i & 15] = -__builtin_inff();
                     top = fmaxf(top, sc[i >> 4][i & 15]);
                 }
-                const float to = fmaxf(m, across_halves(top));      // (-inf where nothing has been seen)
+                const float to = fmaxf(m, across_halves(top) * own);      // (-inf where nothing has been seen)
                 float turn = m == -__builtin_inff() ? 0.f : ex2(m - to), s_top = s_most;
                 m = to; l *= turn;
 #pragma unroll
@@ -752,7 +762,7 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
                 const float base = m == -__builtin_inff() ? 0.f : m;
                 sum = 0.f;
 #pragma unroll
-                for (int i = 0; i < 32; ++i) { p[i] = ex2(sc[i >> 4][i & 15] - base); sum += p[i]; }
+                for (int i = 0; i < 32; ++i) { p[i] = ex2(fmaf(sc[i >> 4][i & 15], own, -base)); sum += p[i]; }
             }
             l += sum;
             const float sv[2] = {__builtin_amdgcn_ldexpf(gv[0], up), __builtin_amdgcn_ldexpf(gv[1], up)};
