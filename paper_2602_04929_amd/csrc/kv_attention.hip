@@ -2,11 +2,13 @@
 //
 // One pass over the cache with the running maximum and sum of the softmax.  Levels minus their zero are whole numbers up to 255 and so exact in half; they are made in registers from the
 // cache's bytes (a byte beside 0x64 is 1024 + level as half; one packed addition takes 1024 + zero away), and the scales multiply scores and probabilities:
-//     x[t] = (scale s^K_t log2 e) q.(c^K_t - z^K_t),   p = 2^(x - max),   O += (p s^V_t 2^14 / ref) (c^V_t - z^V_t),   ref: a power of two above the scales seen so far
+//     x[t] = (scale s^K_t log2 e) q.(c^K_t - z^K_t),   p = 2^(x - max),   O += (2^up p s^V_t) (c^V_t - z^V_t)
 // A row's query becomes half times a power of two that brings its largest channel to 2^13 .. 2^14 (bf16 queries stay exact down to 2^-31 of it, whatever other rows hold); fp32 queries are split into two half
-// terms (2^-22 of them at most), and so is p s 2^14 / ref; but one half (2^-11 of it at most, an eighth of an output's rounding to bf16) for bf16 queries of sequences of more than FEW rows, in
+// terms (2^-22 of them at most), and so is 2^up p s; but one half (2^-11 of it at most, an eighth of an output's rounding to bf16) for bf16 queries of sequences of more than FEW rows, in
 // either kernel, so that a row's bits do not hang on which one takes it: two prompts of 2048 tokens behind 4096, whose time is matrix instructions, would take 614 us, not 461.  Single tokens
 // wait for the cache's bytes and pay one per cent for the second half (32 sequences 78.1 us, not 77.1; one of 131000 tokens 70.1, not 69.0).
+// `up` goes by the largest p s among the tokens that the row itself has seen so far, and falls and rises with it as the maximum moves: neither a token that is hidden from the row nor one of a huge
+// scale and next to no probability takes bits from the others.
 #include "kv_cache.h"
 #include <math.h>
 #include <algorithm>
@@ -83,7 +85,8 @@ __device__ __forceinline__ void store4(bf16* out, int c, const AttendArgs& a, f4
     for (int j = 0; j < 4; ++j) if (c + j < a.g.dh) out[c + j] = from_f32<bf16>(v[j]);
 }
 
-constexpr int HALF_TOP = 14;      // a probability of 1 with the largest scale becomes 2^14 as half, at most: parts of 2^-28 of it are still normal numbers
+constexpr float MOST_FLOAT = 0x1.fffffep127f;
+constexpr int HALF_TOP = 14;      // a row's largest probability times scale becomes 2^14 .. 2^15 as half: parts of 2^-28 of it are still normal numbers
 constexpr int ROWS = 16, TILE = 64;      // rows (query token, head of the group) of a unit, tokens a wavefront takes at a time
 // workgroups that a compute unit holds at once (registers): the shares that the work is cut into are 256 times as many
 template <int DP> constexpr int resident() { return DP <= 64 ? 3 : DP <= 128 ? 2 : 1; }
@@ -232,7 +235,8 @@ __global__ __launch_bounds__(256, resident<DP>()) void kv_attend_rows_kernel(Att
                 }
         }
 
-        float m = -__builtin_inff(), l = 0.f, ref = 0x1p-126f;
+        float m = -__builtin_inff(), l = 0.f, most_w = 0.f;      // most_w: largest probability times scale
+        int up = HALF_TOP + 1 + 126;                             // brings it to 2^14 .. 2^15
         f4 o[CT];
 #pragma unroll
         for (int c = 0; c < CT; ++c) o[c] = f4{0.f, 0.f, 0.f, 0.f};
@@ -286,23 +290,25 @@ __global__ __launch_bounds__(256, resident<DP>()) void kv_attend_rows_kernel(Att
             l *= turn;
 #pragma unroll
             for (int i = 0; i < 16; ++i) { p[i] = ex2(p[i] - base); l += p[i]; }
-            float s_top = gvx;
+            unroll<16>([&](auto I) { constexpr int i = I; p[i] *= row_lane<i>(gvx); });
+            if (!all) {      // whatever their scale is
 #pragma unroll
-            for (int k = 1; k < 64; k <<= 1) s_top = fmaxf(s_top, __shfl_xor(s_top, k, 64));
-            if (s_top >= ref && s_top < __builtin_inff()) {
-                const float now = __builtin_amdgcn_ldexpf(1.f, min(__builtin_amdgcn_frexp_expf(s_top), 127));
-                turn *= ref / now; ref = now;
+                for (int i = 0; i < 16; ++i) if (hidden >> i & 1) p[i] = 0.f;
             }
+            float w_top = p[0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) w_top = fmaxf(w_top, p[i]);
+            w_top = fmaxf(w_top, from_xor<16>(w_top)); w_top = fmaxf(w_top, from_xor<32>(w_top));
+            most_w = fmaxf(most_w * turn, fminf(w_top, MOST_FLOAT));
+            const int up_was = up;
+            if (most_w > 0.f) up = HALF_TOP + 1 - max(__builtin_amdgcn_frexp_expf(most_w), -126);
+            turn = __builtin_amdgcn_ldexpf(turn, up - up_was);      // (up rises only as most_w falls with turn: 2 at most)
             if (__any(turn != 1.f)) {
 #pragma unroll
                 for (int c = 0; c < CT; ++c) o[c] *= turn;
             }
-            const float sv = __builtin_amdgcn_ldexpf(gvx, HALF_TOP + 1 - __builtin_amdgcn_frexp_expf(ref));
-            unroll<16>([&](auto I) { constexpr int i = I; p[i] *= row_lane<i>(sv); });
-            if (!all) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) if (hidden >> i & 1) p[i] = 0.f;
-            }
+            for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_ldexpf(p[i], up);
             h8 ph[2][2];
 #pragma unroll
             for (int k = 0; k < 2; ++k)
@@ -324,7 +330,7 @@ __global__ __launch_bounds__(256, resident<DP>()) void kv_attend_rows_kernel(Att
             for (int c = 0; c < CT; ++c) {
                 const h8 v0 = levels8(vr[c][0], vr[c][1], zo[0], zo[1], zo[2], zo[3]), v1 = levels8(vr[c][2], vr[c][3], zo[4], zo[5], zo[6], zo[7]);
                 o[c] = mma16(v0, ph[0][0], o[c]); o[c] = mma16(v1, ph[0][1], o[c]);
-                if (two) { o[c] = mma16(v0, ph[1][0], o[c]); o[c] = mma16(v1, ph[1][1], o[c]); }
+                if (NT == 2 || two) { o[c] = mma16(v0, ph[1][0], o[c]); o[c] = mma16(v1, ph[1][1], o[c]); }
             }
         }
         l += from_xor<16>(l); l += from_xor<32>(l);
@@ -335,9 +341,8 @@ __global__ __launch_bounds__(256, resident<DP>()) void kv_attend_rows_kernel(Att
 #pragma unroll
         for (int w = 1; w < 4; ++w) top = fmaxf(top, ends[w][col].x);
         const float f = m == -__builtin_inff() ? 0.f : ex2(m - top);
-        const int back = __builtin_amdgcn_frexp_expf(ref) - 1 - HALF_TOP;
 #pragma unroll
-        for (int c = 0; c < CT; ++c) *(f4*)&joined[wave][col][c * 16 + grp * 4] = m == -__builtin_inff() ? f4{0.f, 0.f, 0.f, 0.f} : by_power(o[c] * f, back);
+        for (int c = 0; c < CT; ++c) *(f4*)&joined[wave][col][c * 16 + grp * 4] = m == -__builtin_inff() ? f4{0.f, 0.f, 0.f, 0.f} : by_power(o[c] * f, -up);
         __syncthreads();
         const bool whole = k0 == 0 && k1 == tiles;
         const long long piece = (2LL * blockIdx.x + (k0 == 0)) * ROWS;
@@ -425,7 +430,9 @@ __global__ __launch_bounds__(256) void kv_attend_join_kernel(AttendArgs a) {
 // within half); no maximum is formed then.
 // Two sequences of up to 2048 new tokens behind up to 4096, 64 / 8 heads of 128 (367 GFLOP): 469 us, 780 TFLOP/s of the 1423 that a large product of half matrices reaches.
 constexpr float MOST = 0x1p7f;
-constexpr int TILE_TOP = 8;      // as HALF_TOP
+constexpr int TILE_TOP = 8;      // halves are below 2^(TILE_TOP + 7): probabilities are up to MOST, scales below the row's bound
+constexpr int SPARE = 8;         // a row's bound of scales is so many powers of two above its largest probability times scale: larger scales (the bound is then raised) are rare, and parts of 2^-13 of
+                                 // that largest product are still normal halves, each off by 2^-24 of it at most
 template <int DP> constexpr int waves() { return DP <= 128 ? 8 : 4; }      // (wider heads need twice the registers)
 template <int DP> constexpr int permuted() { return DP % 128 == 0 ? 15 : DP % 64 == 0 ? 7 : 3; }      // bits of a piece's number that K's rows are XORed into
 template <int DP> constexpr int tiles_lds() { return 2 * 2 * TILE * DP * 2; }
@@ -478,7 +485,8 @@ __device__ __forceinline__ int least(int a, int b) { return min(a, b); }
 __device__ __forceinline__ int greatest(int a, int b) { return max(a, b); }
 __device__ __forceinline__ void run_ends() {      // everything before it is before, what was written to LDS is there
     __builtin_amdgcn_sched_barrier(0);
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xc07f);      // lgkmcnt(0), as an instruction that the compiler counts with
+    asm volatile("s_barrier" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
 }
 
@@ -516,7 +524,7 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
     // this lane's row; the wavefront's rows
     const int w0 = wave * 32, w_rows = min(max(n_rows - w0, 0), 32);
     const bool row_live = col < w_rows;
-    const int r = r0 + w0 + (row_live ? col : 0), tok = r / a.rep, pos = row_live ? s.len - s.n + tok : -1, low = a.window ? pos - a.window + 1 : 0;
+    const int r = r0 + w0 + (row_live ? col : 0), tok = r / a.rep, pos = row_live ? s.len - s.n + tok : -1;
     // tiles that the wavefront's rows see anything of, and places that all of them see
     int see0 = 0, see1 = 0, all0 = 0, all1 = -1;
     if (w_rows) {
@@ -686,8 +694,11 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
 #pragma unroll
         for (int j = 0; j < 16; ++j) o[c][j] = 0.f;
     h8 pf[4];
-    float m = -__builtin_inff(), l = 0.f, ref = 0x1p-126f;
-    int up = TILE_TOP + 126;      // 2^up ref = 2^TILE_TOP
+    float m = -__builtin_inff(), l = 0.f, most_w = 0.f;      // most_w: largest probability times scale that the row had when its bound was last set
+    // A half is 2^(TILE_TOP - e_wave) scale, the same for all rows, times 2^d probability: 2^(e_wave - d) is the row's bound of scales, 2^SPARE above most_w.  Rows of 2^200 between them have that
+    // (e_wave is at most 2^100 below the largest bound, and never falls); what lies further below, if anything does, loses bits
+    int e_wave = -126 + SPARE, d = 0;
+    float limit = 0.f;                     // the least bound of a row
     // operands in LDS
     constexpr int M = permuted<DP>();
     auto k_piece = [&](int buf, int k, int c) {
@@ -733,14 +744,16 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
             }
             const float sk[2] = {gk[0] * unit, gk[1] * unit};
             float p[32], part[4] = {0.f, 0.f, 0.f, 0.f};
-            unroll<32>([&](auto I) { constexpr int i = I; sc[i >> 4][i & 15] *= row_lane<i & 15>(sk[i >> 4]); p[i] = ex2(fmaf(sc[i >> 4][i & 15], own, -m)); part[i & 3] += p[i]; });
-            float sum = (part[0] + part[1]) + (part[2] + part[3]);
+            unroll<32>([&](auto I) { constexpr int i = I; sc[i >> 4][i & 15] *= row_lane<i & 15>(sk[i >> 4]); p[i] = ex2(fmaf(sc[i >> 4][i & 15], own, (float)d - m)); part[i & 3] += p[i]; });
+            float sum = __builtin_amdgcn_ldexpf((part[0] + part[1]) + (part[2] + part[3]), -d);
             const float s_most = fmaxf(gv[0], gv[1]);
             const bool all = t0 >= all0 && t0 + TILE - 1 <= all1 && there == 15u;
-            if (!all || __any(sum > MOST || s_most >= ref)) {
+            if (!all || __any(sum > MOST || s_most >= limit)) {
                 // places 32 k + 16 (i / 8) + i % 8 from first_seen on, seen of them, are seen by this row
-                const int first_seen = low - t0 - 8 * half;
-                const unsigned seen = (unsigned)max(min(pos, end - 1) - low + 1, 0), gone = ~there;
+                int at = pos;
+                asm("" : "+v"(at));      // (what follows from it is not kept in registers from the start on)
+                const int low = a.window ? at - a.window + 1 : 0, first_seen = low - t0 - 8 * half;
+                const unsigned seen = (unsigned)max(min(at, end - 1) - low + 1, 0), gone = ~there;
                 float top = -__builtin_inff();
 #pragma unroll
                 for (int i = 0; i < 32; ++i) {
@@ -748,31 +761,39 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
                     top = fmaxf(top, sc[i >> 4][i & 15]);
                 }
                 const float to = fmaxf(m, across_halves(top) * own);      // (-inf where nothing has been seen)
-                float turn = m == -__builtin_inff() ? 0.f : ex2(m - to), s_top = s_most;
+                __builtin_amdgcn_sched_barrier(0);      // (maximum, probabilities and bounds one after the other: mixed they took 2 % longer with heads of 32 and 64)
+                float turn = m == -__builtin_inff() ? 0.f : ex2(m - to), w_top = 0.f;
                 m = to; l *= turn;
-#pragma unroll
-                for (int k = 1; k < 64; k <<= 1) s_top = fmaxf(s_top, __shfl_xor(s_top, k, 64));
-                if (s_top >= ref && s_top < __builtin_inff()) {
-                    const int e = min(__builtin_amdgcn_frexp_expf(s_top), 127);
-                    const float now = __builtin_amdgcn_ldexpf(1.f, e);
-                    turn *= ref / now; ref = now; up = TILE_TOP - e;
-                }
-#pragma unroll
-                for (int c = 0; c < CT; ++c) o[c] *= turn;
                 const float base = m == -__builtin_inff() ? 0.f : m;
                 sum = 0.f;
+                asm("" : "+v"(gv[0]), "+v"(gv[1]));      // (nor are scales, spread over a row's lanes, in 32 registers)
+                unroll<32>([&](auto I) { constexpr int i = I; p[i] = ex2(fmaf(sc[i >> 4][i & 15], own, -base)); sum += p[i]; w_top = fmaxf(w_top, p[i] * row_lane<i & 15>(gv[i >> 4])); });
+                most_w = fmaxf(most_w * turn, fminf(across_halves(w_top), MOST_FLOAT));
+                const bool some = m != -__builtin_inff();
+                __builtin_amdgcn_sched_barrier(0);
+                const int e_was = e_wave - d, e_row = (most_w > 0.f ? max(__builtin_amdgcn_frexp_expf(most_w), -126) : -126) + SPARE;
+                const int e_least = over_rows(some ? e_row : 128, least), e_most = over_rows(some ? e_row : -126 + SPARE, greatest);
+                const float s_top = across_halves(fminf(fmaxf(gv[0], gv[1]), MOST_FLOAT));      // (seen or not: below, scales by themselves stay finite)
+                e_wave = max(max(e_wave, min(e_least, e_most)), max(e_most - 100, __builtin_amdgcn_frexp_expf(__int_as_float(over_rows(__float_as_int(s_top), greatest))) - 118));
+                limit = __uint_as_float((unsigned)(min(e_least, 128) + 127) << 23);
+                d = min(e_wave - e_row, 100);
+                turn = __builtin_amdgcn_ldexpf(turn, e_was - (e_wave - d));      // (a row's bound falls only as most_w does with turn: 2 at most)
 #pragma unroll
-                for (int i = 0; i < 32; ++i) { p[i] = ex2(fmaf(sc[i >> 4][i & 15], own, -base)); sum += p[i]; }
+                for (int c = 0; c < CT; ++c) o[c] *= turn;
+#pragma unroll
+                for (int i = 0; i < 32; ++i) p[i] = __builtin_amdgcn_ldexpf(p[i], d);
             }
             l += sum;
-            const float sv[2] = {__builtin_amdgcn_ldexpf(gv[0], up), __builtin_amdgcn_ldexpf(gv[1], up)};
+            const float sv[2] = {__builtin_amdgcn_ldexpf(gv[0], TILE_TOP - e_wave), __builtin_amdgcn_ldexpf(gv[1], TILE_TOP - e_wave)};
             unroll<32>([&](auto I) { constexpr int i = I; p[i] *= row_lane<i & 15>(sv[i >> 4]); });
-            if (!all) {
-                const int first_seen = low - t0 - 8 * half;
-                const unsigned seen = (unsigned)max(min(pos, end - 1) - low + 1, 0), gone = ~there;
+            if (!all && __any(sv[0] * 0.f + sv[1] * 0.f != 0.f)) {      // scales that are no numbers: what is not seen counts for nothing whatever its scale is
+                int at = pos;
+                asm("" : "+v"(at));
+                const int low = a.window ? at - a.window + 1 : 0, first_seen = low - t0 - 8 * half;
+                const unsigned seen = (unsigned)max(min(at, end - 1) - low + 1, 0), gone = ~there;
 #pragma unroll
                 for (int i = 0; i < 32; ++i)
-                    if ((unsigned)(32 * (i >> 4) + 16 * (i >> 3 & 1) + (i & 7) - first_seen) >= seen || (gone >> (i >> 3) & 1)) p[i] = 0.f;      // (whatever its scale is)
+                    if ((unsigned)(32 * (i >> 4) + 16 * (i >> 3 & 1) + (i & 7) - first_seen) >= seen || (gone >> (i >> 3) & 1)) p[i] = 0.f;
             }
 #pragma unroll
             for (int k = 0; k < 4; ++k)
@@ -785,6 +806,7 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
         run_ends();
     }
     if (W > 4 && !later) run_ends();      // as many as the others
+    const int up = TILE_TOP - e_wave + d;
     l += from_xor<32>(l);
     if (l != l) m = fmaxf(m, 0.f);      // scores that are all NaN leave the maximum where it was
     const bool none = m == -__builtin_inff();

@@ -46,6 +46,69 @@ def test_probabilities_of_few_rows(ctx, lib, shape):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("factor", [1e7, 1e12, 1e30])
+@pytest.mark.parametrize("new,window,many", [(1, 40, False), (7, 0, False), (7, 30, False), (50, 0, False), (50, 0, True), (70, 33, True), (200, 150, True)])
+def test_scales_of_tokens_that_are_not_seen(ctx, lib, dtype, factor, new, window, many):
+    """A scale of V far above the others, behind a row's own place or before its window, changes nothing in the row."""
+    if many and dtype == torch.float32:
+        pytest.skip("fp32 has one kernel")
+    length, dh, rep = 300, 64, 2
+    starts, pages, cache, _, q = case(lib, 2, rep, dh, [new], [length], 16, 1, dtype, 40 + new)
+    last = length - 1 - (new - 1) // 2      # seen by the last half of the rows; the row before it does not
+    spots = [last] if new > 1 else []
+    if window:
+        spots += [length - new - window, length - new - window + new // 2]      # out of the first row's window; leaves it half way
+    for t in spots:
+        cache.vg[pages[0, t // 16], :, t % 16, 0] *= factor
+    if many:
+        pages = wide(pages, 16)
+    got = attend(ctx, lib, cache, starts, [length], pages, q, window=window)
+    check(got, cache, starts, [length], pages, q, 1 / 8, window, many=many)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("new,many", [(1, False), (5, False), (40, False), (40, True), (300, True)])
+def test_scales_of_tokens_that_hardly_count(ctx, lib, dtype, new, many):
+    """Scales of V that grow as the scores fall: large ones with probabilities next to nothing, met first, in between and last."""
+    if many and dtype == torch.float32:
+        pytest.skip("fp32 has one kernel")
+    length, dh = 700, 64
+    starts, pages, cache, _, q = case(lib, 1, 1, dh, [new], [length], 64, 1, dtype, 60 + new)
+    q[:] = (torch.randn(dh, generator=torch.Generator().manual_seed(1)).to(dtype) / 8).cuda()      # every row asks the same
+    sign = np.sign(q[0, 0].float().cpu().numpy()).astype(int)
+    for t, (low, factor) in {3: (40, 1e10), 100: (80, 1e25), 250: (25, 1e5), 390: (60, 1e16), 398: (127, 1e30)}.items():      # all rows see them
+        at = pages[0, t // 64]
+        cache.k[at, 0, t % 64, :dh], cache.kg[at, 0, t % 64] = 128 - sign * low, (1.0, 128)      # a score of -low / 8 sum |q|
+        cache.vg[at, 0, t % 64, 0] *= factor
+    if many:
+        pages = wide(pages, 64)
+    got = attend(ctx, lib, cache, starts, [length], pages, q)
+    check(got, cache, starts, [length], pages, q, 1 / 8, 0, many=many)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("new,many", [(4, False), (60, False), (60, True)])
+def test_scales_as_far_apart_as_an_append_makes_them(ctx, lib, dtype, new, many):
+    """Beside scales of 1e-14, the largest there is: behind the rows' place, and in a token that they see with a probability of 2^-126 or less."""
+    if many and dtype == torch.float32:
+        pytest.skip("fp32 has one kernel")
+    length, dh = 200, 64
+    starts, pages, cache, _, q = case(lib, 1, 1, dh, [new], [length], 64, 1, dtype, 70 + new)
+    q[:] = (torch.randn(dh, generator=torch.Generator().manual_seed(1)).to(dtype)).cuda()
+    cache.vg[..., 0] *= 1e-12
+    sign = np.sign(q[0, 0].float().cpu().numpy()).astype(int)
+    for t in (5, 120):
+        at = pages[0, t // 64]
+        cache.k[at, 0, t % 64, :dh], cache.kg[at, 0, t % 64] = 128 - sign * 127, (4.0, 128)      # a score of -63 sum |q|, some -3000
+        cache.vg[at, 0, t % 64, 0] = 2.0 ** 121
+    cache.vg[pages[0, (length - 1) // 64], 0, (length - 1) % 64, 0] = 2.0 ** 121      # the last row alone sees it
+    if many:
+        pages = wide(pages, 64)
+    got = attend(ctx, lib, cache, starts, [length], pages, q)
+    check(got, cache, starts, [length], pages, q, 1 / 8, 0, many=many)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("factor", [1e9, 1e15, 1e30, 3e36])
 @pytest.mark.parametrize("new,many", [(3, False), (40, False), (40, True), (200, True)])
 def test_queries_of_other_rows(ctx, lib, dtype, factor, new, many):
@@ -75,3 +138,25 @@ def test_queries_of_other_rows(ctx, lib, dtype, factor, new, many):
         page, off = pages[0, t // 16], t % 16
         v = (torch.tensor(cache.v[page, 0, off // 16, :dh, off % 16], dtype=torch.float64) - float(cache.vg[page, 0, off, 1])) * float(cache.vg[page, 0, off, 0])
         assert ((got[1, 0].double().cpu() - v).abs() <= (torch.finfo(dtype).eps / 2 + 2.0 ** (-11 if many else -21)) * v.abs() + 2.0 ** -24 * 255 * float(cache.vg[page, 0, off, 0])).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_special_values_to_the_bound_of_each_sequence(ctx, lib, dtype):
+    """Two sequences, one with scales of V from 1e-8 to 1e4 and a NaN: the other one's rows, with a NaN query, queries of 1e-20 and of 1e-3 among them, to their own bound; both kernels."""
+    for new, many in ((1, False), (50, False), (50, True)):
+        if many and dtype == torch.float32:
+            continue
+        starts, pages, cache, _, q = case(lib, 1, 2, 64, [new, new], [150, 150], 16, 1, dtype, 5)
+        cache.vg[pages[1, 145 // 16], 0, 145 % 16, 0] = np.nan
+        cache.vg[pages[1, 2], 0, :, 0] *= 1e-6
+        cache.vg[pages[1, 1], 0, :, 0] *= 1e6
+        q[0] *= 1e-20
+        rows = torch.ones(len(q), 2, dtype=torch.bool)
+        if new > 1:
+            q[3, 0, 0] = float("nan")
+            q[5] *= 1e-3
+            rows[3, 0] = False
+        table = wide(pages, 16) if many else pages
+        got = attend(ctx, lib, cache, starts, [150, 150], table, q)
+        assert new == 1 or torch.isnan(got[3, 0]).all()
+        check(got, cache, starts, [150, 150], table, q, 1 / 8, 0, many=many, rows=rows)
