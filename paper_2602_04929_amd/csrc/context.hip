@@ -53,7 +53,7 @@ int tboa_ws_reserve_either(tboa_ctx* ctx, size_t full, size_t plain, bool& take_
     if (full <= ctx->ws_bytes) return 0;
     if (full < ctx->no_room || full <= plain) {
         const int rc = tboa_ws_reserve(ctx, full);
-        if (rc != TBOA_ENOMEM || full <= plain) return rc;
+        if (rc != TBOA_ENOMEM || full <= plain || capturing(ctx)) return rc;      // (a graph is not recorded in the smaller form because nobody reserved the larger one)
     }
     take_full = false;
     return tboa_ws_reserve(ctx, plain);

@@ -1,0 +1,53 @@
+"""A context's workspace and the graphs that hold its address (GPU)."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+MORE_THAN_ANY = 1 << 46
+
+
+def refused(lib, call):
+    with pytest.raises(lib.TurboBoAError) as e:
+        call()
+    assert e.value.code == -3
+    return str(e.value)
+
+
+def test_a_captured_call_without_room_is_refused(lib):
+    """A call that has a smaller form than the one it would take: not recorded in it without a word."""
+    d, hq, hkv, dh, length = 8192, 64, 8, 128, 256
+    g = torch.Generator(device="cuda").manual_seed(1)
+    X = torch.randn(1, length, d, generator=g, device="cuda").bfloat16()
+    Wq, Wo = ((0.02 * torch.randn(d, d, generator=g, device="cuda")).bfloat16() for _ in "qo")
+    Wk, Wv = ((0.02 * torch.randn(hkv * dh, d, generator=g, device="cuda")).bfloat16() for _ in "kv")
+    call = lambda c: c.build_hessians(X, None, Wq, Wk, Wv, Wo, hq, hkv, dh, with_R_v=False, parts="qk")  # noqa: E731
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    ctx, roomy = lib.Context(stream=stream), lib.Context()
+    try:
+        want = call(roomy)
+        torch.cuda.synchronize()
+        refused(lib, lambda: ctx.reserve_workspace(MORE_THAN_ANY))
+        ctx.reserve_workspace(256)      # the caller settles for little: the call takes its smaller form
+        with torch.cuda.stream(stream):
+            call(ctx)
+        stream.synchronize()
+        least = ctx.workspace_bytes()
+        assert least < roomy.workspace_bytes()
+        ctx.reserve_workspace(least + 256)      # there is room again, as far as the context knows
+        mark = torch.zeros(1, device="cuda")
+
+        def record():
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=stream):
+                mark.zero_()
+                call(ctx)
+        assert "captured" in refused(lib, record)
+        with torch.cuda.stream(stream):
+            got = call(ctx)
+        torch.cuda.synchronize()
+        assert ctx.workspace_bytes() == roomy.workspace_bytes() and torch.equal(got["Hout_q"], want["Hout_q"])
+    finally:
+        ctx.close()
+        roomy.close()
