@@ -28,9 +28,19 @@ int tboa_ws_reserve(tboa_ctx* ctx, size_t bytes) {
     if (bytes <= ctx->ws_bytes) return 0;
     if (capturing(ctx)) return tboa_fail(ctx, TBOA_ENOMEM, "workspace of %zu bytes: nothing can be allocated while the stream is captured, reserve it before", bytes);
     TB_HIP(ctx, hipStreamSynchronize(ctx->stream));
-    if (ctx->ws && ctx->ws_in_graph) {
-        try { ctx->ws_kept.push_back(ctx->ws); } catch (const std::bad_alloc&) { return tboa_fail(ctx, TBOA_ENOMEM, "out of host memory"); }
-        ctx->ws = nullptr; ctx->ws_bytes = 0; ctx->ws_in_graph = false;
+    if (ctx->ws && ctx->ws_in_graph) {      // it stays where it is: a new one beside it, or none
+        try { ctx->ws_kept.reserve(ctx->ws_kept.size() + 1); } catch (const std::bad_alloc&) { return tboa_fail(ctx, TBOA_ENOMEM, "out of host memory"); }
+        void* more = nullptr;
+        const hipError_t e = hipMalloc(&more, bytes);
+        if (e != hipSuccess) {
+            (void)hipGetLastError();
+            if (bytes < ctx->no_room) ctx->no_room = bytes;
+            return tboa_fail(ctx, TBOA_ENOMEM, "workspace of %zu bytes beside one that a graph holds: %s", bytes, hipGetErrorString(e));
+        }
+        ctx->ws_kept.push_back(ctx->ws);
+        ctx->ws = more; ctx->ws_bytes = bytes; ctx->ws_in_graph = false;
+        if (bytes >= ctx->no_room) ctx->no_room = (size_t)-1;
+        return 0;
     }
     const size_t had = ctx->ws_bytes;
     if (ctx->ws) { TB_HIP(ctx, hipFree(ctx->ws)); ctx->ws = nullptr; ctx->ws_bytes = 0; }

@@ -1,6 +1,10 @@
 """A context's workspace and the graphs that hold its address (GPU)."""
+import numpy as np
 import pytest
 import torch
+
+from tests.test_gpu_kv_cache_append import layout
+from tests.test_gpu_serving import Step, captured
 
 pytestmark = pytest.mark.gpu
 
@@ -51,3 +55,37 @@ def test_a_captured_call_without_room_is_refused(lib):
     finally:
         ctx.close()
         roomy.close()
+
+
+def test_a_refused_growth_leaves_the_workspace_of_a_graph(lib):
+    heads, rep, dh, pt = 2, 4, 128, 64
+    lens = np.array([5, 300, 64])
+    total, pages = layout(lens + 40, pt, 4)
+    stream = torch.cuda.Stream()
+    own, other = lib.Context(stream=stream), lib.Context()
+    try:
+        step = Step(lib, [1, 1, 1], lens, pages, total, heads, rep, dh, pt, 1, torch.bfloat16, 1)
+        own.reserve_workspace(step.need(own))
+        held = own.workspace_bytes()
+        shadow = step.data.clone()
+        torch.cuda.synchronize()
+        graph = captured(lib, step, own, stream)
+        refused(lib, lambda: own.reserve_workspace(MORE_THAN_ANY))
+        assert own.workspace_bytes() == held
+        for turn in range(3):
+            lens = lens + 1
+            step.fill(lens, turn)
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            got = step.out.clone()
+            want = step.run(other, data=shadow, out=torch.empty_like(step.out), turned=torch.empty_like(step.turned))
+            torch.cuda.synchronize()
+            assert torch.equal(got, want) and torch.equal(step.data, shadow)
+            with torch.cuda.stream(stream):
+                again = step.run(own, data=shadow, out=torch.empty_like(step.out), turned=torch.empty_like(step.turned))
+            torch.cuda.synchronize()
+            assert torch.equal(again, want) and own.workspace_bytes() == held
+    finally:
+        own.close()
+        other.close()
