@@ -13,7 +13,8 @@
  *   - Every tensor pointer is DEVICE memory owned by the caller unless marked "host".  Inputs are never
  *     modified; the library keeps no pointer after a call returns.  Temporary storage belongs to the
  *     context: one workspace, grown on demand (a growth frees and reallocates it after synchronising the stream) and
- *     released by tboa_destroy.  tboa_hessian_workspace_bytes / tboa_quantize_workspace_bytes tell what a call will need
+ *     released by tboa_destroy.  While the stream is captured it does not grow (TBOA_ENOMEM: reserve it before), and one that a
+ *     captured call uses is kept until tboa_destroy, whatever the context grows to later.  tboa_hessian_workspace_bytes / tboa_quantize_workspace_bytes tell what a call will need
  *     and tboa_reserve_workspace obtains it ahead, so that no call allocates afterwards.
  *     A context also holds 64 MiB from tboa_create on, for the partial sums of fp64 products.
  *   - Matrices are dense row-major.  Activations are token-major: X[t, c] is channel c of token t, so the

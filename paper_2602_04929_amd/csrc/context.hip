@@ -18,14 +18,12 @@ static bool capturing(tboa_ctx* ctx) {
     return st == hipStreamCaptureStatusActive;
 }
 
-int tboa_ws_in_graph(tboa_ctx* ctx) {
-    if (ctx->ws && !ctx->ws_in_graph && capturing(ctx)) ctx->ws_in_graph = true;
-    return 0;
-}
-
 int tboa_ws_reserve(tboa_ctx* ctx, size_t bytes) {
     if (ctx->plan_only) { if (bytes > ctx->plan_bytes) ctx->plan_bytes = bytes; if (bytes > ctx->plan_plain) ctx->plan_plain = bytes; return TB_PLAN_STOP; }
-    if (bytes <= ctx->ws_bytes) return 0;
+    if (bytes <= ctx->ws_bytes) {
+        if (ctx->ws && !ctx->ws_in_graph && capturing(ctx)) ctx->ws_in_graph = true;      // whatever call this is: its graph will hold the address
+        return 0;
+    }
     if (capturing(ctx)) return tboa_fail(ctx, TBOA_ENOMEM, "workspace of %zu bytes: nothing can be allocated while the stream is captured, reserve it before", bytes);
     TB_HIP(ctx, hipStreamSynchronize(ctx->stream));
     if (ctx->ws && ctx->ws_in_graph) {      // it stays where it is: a new one beside it, or none
@@ -60,7 +58,7 @@ int tboa_ws_reserve(tboa_ctx* ctx, size_t bytes) {
 int tboa_ws_reserve_either(tboa_ctx* ctx, size_t full, size_t plain, bool& take_full) {
     take_full = true;
     if (ctx->plan_only) { if (plain > ctx->plan_plain) ctx->plan_plain = plain; if (full > ctx->plan_bytes) ctx->plan_bytes = full; return TB_PLAN_STOP; }
-    if (full <= ctx->ws_bytes) return 0;
+    if (full <= ctx->ws_bytes) return tboa_ws_reserve(ctx, full);
     if (full < ctx->no_room || full <= plain) {
         const int rc = tboa_ws_reserve(ctx, full);
         if (rc != TBOA_ENOMEM || full <= plain || capturing(ctx)) return rc;      // (a graph is not recorded in the smaller form because nobody reserved the larger one)

@@ -75,9 +75,8 @@ struct Arena {
 };
 // returns TB_PLAN_STOP (not an error) on a plan-only context, after recording `bytes`
 #define TB_PLAN_STOP 1000
+// While the stream is captured nothing is allocated (TBOA_ENOMEM), and the workspace that is there outlives a later growth
 int tboa_ws_reserve(tboa_ctx* ctx, size_t bytes);
-// to be called by what may be captured, once it has its workspace: the workspace then outlives a later growth
-int tboa_ws_in_graph(tboa_ctx* ctx);
 // for a call that has a form with residues (`full` bytes) and one without (`plain`): the first unless it is known or found not to fit
 int tboa_ws_reserve_either(tboa_ctx* ctx, size_t full, size_t plain, bool& take_full);
 

@@ -981,7 +981,6 @@ extern "C" int tboa_kv_cache_attention(tboa_ctx* ctx, const tboa_kv_cache_desc* 
     const long long units = tiles ? most_units(g, batch->n_seqs, batch->n_tokens, rep) : 0;
     if (units > 2147483647LL) return tboa_fail(ctx, TBOA_EINVAL, "kv_cache_attention: too many rows");
     TB_TRY(tboa_ws_reserve(ctx, room(g, tiles, units, nullptr, nullptr)));
-    TB_TRY(tboa_ws_in_graph(ctx));
     AttendArgs a;
     a.g = g;
     a.q = KvBatch{batch->n_seqs, batch->pages_per_seq, (int)batch->n_tokens, batch->pages_per_seq * desc->page_tokens, batch->starts, batch->lens, batch->pages};

@@ -89,3 +89,33 @@ def test_a_refused_growth_leaves_the_workspace_of_a_graph(lib):
     finally:
         own.close()
         other.close()
+
+
+def test_any_captured_call_keeps_its_workspace(lib):
+    """A graph of a call that is no attention, replayed after the context's workspace has grown and what was free has been overwritten."""
+    g = torch.Generator(device="cuda").manual_seed(2)
+    X, W = torch.randn(70, 256, generator=g, device="cuda"), torch.randn(96, 256, generator=g, device="cuda")
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    own, other = lib.Context(stream=stream), lib.Context()
+    try:
+        with torch.cuda.stream(stream):
+            own.linear_forward(X, W)
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            out = own.linear_forward(X, W)
+        held = own.workspace_bytes()
+        for turn in range(3):
+            own.reserve_workspace(held + ((turn + 1) << 20))
+            filler = torch.full((held + (turn << 20),), 255, dtype=torch.uint8, device="cuda")
+            X.normal_(generator=g)
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            want = other.linear_forward(X, W)
+            torch.cuda.synchronize()
+            assert torch.equal(out, want) and (filler == 255).all()
+    finally:
+        own.close()
+        other.close()
