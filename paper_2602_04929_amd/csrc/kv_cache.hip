@@ -37,7 +37,7 @@ __device__ __forceinline__ void store8(bf16* p, const float (&v)[8]) {
 struct Rotation { int dim, adjacent; long long positions; const float* table; };      // dim 0: none
 
 template <typename T> struct RotateSide { const T* x; T* y; const float* w; long long ldx, ldy; int heads; };
-template <typename T> struct RotateArgs { RotateSide<T> side[2]; long long tokens; int dh; float eps; Rotation rot; const int* positions; };
+template <typename T> struct RotateArgs { RotateSide<T> side[2]; long long tokens; int dh; float eps; Rotation rot; const int* positions; long long first; };      // first: head vector of this launch
 
 // 1 / sqrt(mean of squares + eps), the sum in fp64: squares of 3e38 are within its range
 __device__ __forceinline__ float norm_factor(double sum, int dh, float eps) { return (float)(1.0 / sqrt(sum / (double)dh + (double)eps)); }
@@ -47,7 +47,7 @@ __device__ __forceinline__ float norm_factor(double sum, int dh, float eps) { re
 template <typename T>
 __global__ __launch_bounds__(256) void head_norm_rotate_kernel(RotateArgs<T> a, int lpr) {
     const int heads = a.side[0].heads + a.side[1].heads;
-    const long long row = ((long long)blockIdx.x * 256 + threadIdx.x) / lpr;
+    const long long row = a.first + ((long long)blockIdx.x * 256 + threadIdx.x) / lpr;
     const int s = threadIdx.x & (lpr - 1);
     const bool live = row < a.tokens * heads;
     const long long t = live ? row / heads : 0;
@@ -109,7 +109,7 @@ __device__ __forceinline__ int partner(int c, const Rotation& r, int& pair, bool
 template <typename T>
 __global__ __launch_bounds__(256) void head_norm_rotate_any_kernel(RotateArgs<T> a) {
     const int heads = a.side[0].heads + a.side[1].heads, lane = threadIdx.x & 63;
-    const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const long long row = a.first + (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (row >= a.tokens * heads) return;
     const long long t = row / heads;
     int h = (int)(row % heads);
@@ -495,7 +495,7 @@ __global__ __launch_bounds__(FORM ? 256 : 64 * MOST_WAVES, 2) void kv_append_ker
 template <typename T>
 int head_norm_rotate(tboa_ctx* ctx, long long n_tokens, int dh, int nq, const void* Q, long long ldq, const float* wq, int nk, const void* K, long long ldk, const float* wk, double eps,
                      const Rotation& rot, const int* positions, void* Qo, long long ldqo, void* Ko, long long ldko) {
-    RotateArgs<T> a{{{(const T*)Q, (T*)Qo, wq, ldq, ldqo, nq}, {(const T*)K, (T*)Ko, wk, ldk, ldko, nk}}, n_tokens, dh, (float)eps, rot, positions};
+    RotateArgs<T> a{{{(const T*)Q, (T*)Qo, wq, ldq, ldqo, nq}, {(const T*)K, (T*)Ko, wk, ldk, ldko, nk}}, n_tokens, dh, (float)eps, rot, positions, 0};
     const long long rows = n_tokens * (nq + nk);
     // 16-byte pieces where every head vector and table row starts on a 16-byte boundary and the pairs of 16 channels are whole pieces
     const int e = 16 / (int)sizeof(T);
@@ -503,11 +503,14 @@ int head_norm_rotate(tboa_ctx* ctx, long long n_tokens, int dh, int nq, const vo
     for (const auto& d : a.side) vec &= !d.heads || ((((uintptr_t)d.x | (uintptr_t)d.y) & 15) == 0 && d.ldx % e == 0 && d.ldy % e == 0);
     int lpr = 1;
     while (16 * lpr < dh) lpr *= 2;
-    const long long blocks = vec ? cdiv64(rows, 256 / lpr) : cdiv64(rows, 4);
-    if (blocks > 2147483647LL) return tboa_fail(ctx, TBOA_EINVAL, "head_norm_rotate: too many head vectors");
-    if (vec) hipLaunchKernelGGL((head_norm_rotate_kernel<T>), dim3((unsigned)blocks), dim3(256), 0, ctx->stream, a, lpr);
-    else hipLaunchKernelGGL((head_norm_rotate_any_kernel<T>), dim3((unsigned)blocks), dim3(256), 0, ctx->stream, a);
-    TB_KERNEL_CHECK(ctx);
+    const int per = vec ? 256 / lpr : 4;      // of a workgroup
+    constexpr long long MOST_BLOCKS = 1 << 23;      // of a launch: of 2^32 work items and more the runtime starts what is left modulo 2^32
+    for (; a.first < rows; a.first += MOST_BLOCKS * per) {
+        const dim3 grid((unsigned)std::min<long long>(cdiv64(rows - a.first, per), MOST_BLOCKS));
+        if (vec) hipLaunchKernelGGL((head_norm_rotate_kernel<T>), grid, dim3(256), 0, ctx->stream, a, lpr);
+        else hipLaunchKernelGGL((head_norm_rotate_any_kernel<T>), grid, dim3(256), 0, ctx->stream, a);
+        TB_KERNEL_CHECK(ctx);
+    }
     return 0;
 }
 
