@@ -976,10 +976,11 @@ extern "C" int tboa_kv_cache_attention(tboa_ctx* ctx, const tboa_kv_cache_desc* 
     KvDevice dev(ctx->device);
     // sequences of more than FEW rows go to the tiles' kernel (16-bit inputs), the others to the rows'; what the caller says of the batch may spare one of the two launches
     const long long most = batch->max_new > 0 ? std::min<long long>(batch->max_new, batch->n_tokens) : batch->n_tokens;
-    const bool tiles = dtype == TBOA_BF16 && most * rep > FEW && !is_small(g, *batch, rep, window);
+    // (of 2^32 work items and more the runtime would start what is left modulo 2^32: such calls are the rows' kernel's, whose grid does not grow)
+    const long long might = most_units(g, batch->n_seqs, batch->n_tokens, rep);
+    const bool tiles = dtype == TBOA_BF16 && most * rep > FEW && !is_small(g, *batch, rep, window) && might < (1LL << 32) / (2 * unit_rows_of(g.dp));
     const bool rows = !tiles || batch->n_seqs > 1 || batch->n_tokens * rep <= FEW;
-    const long long units = tiles ? most_units(g, batch->n_seqs, batch->n_tokens, rep) : 0;
-    if (units > 2147483647LL) return tboa_fail(ctx, TBOA_EINVAL, "kv_cache_attention: too many rows");
+    const long long units = tiles ? might : 0;
     TB_TRY(tboa_ws_reserve(ctx, room(g, tiles, units, nullptr, nullptr)));
     AttendArgs a;
     a.g = g;
