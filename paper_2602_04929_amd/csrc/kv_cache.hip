@@ -37,10 +37,16 @@ __device__ __forceinline__ void store8(bf16* p, const float (&v)[8]) {
 struct Rotation { int dim, adjacent; long long positions; const float* table; };      // dim 0: none
 
 template <typename T> struct RotateSide { const T* x; T* y; const float* w; long long ldx, ldy; int heads; };
-template <typename T> struct RotateArgs { RotateSide<T> side[2]; long long tokens; int dh; float eps; Rotation rot; const int* positions; long long first; };      // first: head vector of this launch
+template <typename T> struct RotateArgs { RotateSide<T> side[2]; long long tokens; int dh; double eps; Rotation rot; const int* positions; long long first; };      // first: head vector of this launch
 
-// 1 / sqrt(mean of squares + eps), the sum in fp64: squares of 3e38 are within its range
-__device__ __forceinline__ float norm_factor(double sum, int dh, float eps) { return (float)(1.0 / sqrt(sum / (double)dh + (double)eps)); }
+// 1 / sqrt(mean of squares + eps) as 2^shift r, the sum in fp64: squares of 3e38 are within its range.  Values below 2^-64 or above 2^64 are moved there first (exactly, or where they would vanish
+// beside the others anyway): fp32 holds the factor of 1e-39 not at all, that of 3e38 with fewer bits.
+struct NormFactor { float r; int shift; };
+__device__ __forceinline__ NormFactor norm_factor(double sum, int dh, double eps) {
+    const double f = 1.0 / sqrt(sum / (double)dh + eps);
+    const int shift = f > 0x1p64 ? 64 : f < 0x1p-64 ? -64 : 0;
+    return NormFactor{(float)(shift ? ldexp(f, -shift) : f), shift};
+}
 
 // One lane per 16 channels, both halves of their pairs (channels 8 s .. and rot/2 + 8 s .., or 16 s .. where pairs are adjacent), `lpr` lanes per head vector.
 // Every element is read and written once, in pieces of 16 bytes, and that is what bounds it: 16384 tokens, 64 + 8 heads of 128, bf16 (612 MB): 117 us, 5.2 TB/s; 16 tokens: 3.8 us.
@@ -65,10 +71,14 @@ __global__ __launch_bounds__(256) void head_norm_rotate_kernel(RotateArgs<T> a, 
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum += (double)u[i] * u[i] + (double)v[i] * v[i];
         for (int o = 1; o < lpr; o <<= 1) sum += __shfl_xor(sum, o, 64);
-        const float r = norm_factor(sum, a.dh, a.eps);
+        const NormFactor f = norm_factor(sum, a.dh, a.eps);
+        if (f.shift) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) { u[i] = __builtin_amdgcn_ldexpf(u[i], f.shift); v[i] = __builtin_amdgcn_ldexpf(v[i], f.shift); }
+        }
         if (mine) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) { u[i] = u[i] * r * d.w[c0 + i]; v[i] = v[i] * r * d.w[c1 + i]; }
+            for (int i = 0; i < 8; ++i) { u[i] = u[i] * f.r * d.w[c0 + i]; v[i] = v[i] * f.r * d.w[c1 + i]; }
         }
     }
     if (!mine) return;
@@ -131,13 +141,17 @@ __global__ __launch_bounds__(256) void head_norm_rotate_any_kernel(RotateArgs<T>
     }
     if (d.w) {
         for (int k = 1; k < 64; k <<= 1) sum += __shfl_xor(sum, k, 64);
-        const float r = norm_factor(sum, a.dh, a.eps);
+        const NormFactor f = norm_factor(sum, a.dh, a.eps);
+        if (f.shift) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { v[i] = __builtin_amdgcn_ldexpf(v[i], f.shift); o[i] = __builtin_amdgcn_ldexpf(o[i], f.shift); }
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int c = lane + 64 * i;
             if (c < a.dh) {
-                v[i] = v[i] * r * d.w[c];
-                if (c < a.rot.dim) { int pair; bool second; o[i] = o[i] * r * d.w[partner(c, a.rot, pair, second)]; }
+                v[i] = v[i] * f.r * d.w[c];
+                if (c < a.rot.dim) { int pair; bool second; o[i] = o[i] * f.r * d.w[partner(c, a.rot, pair, second)]; }
             }
         }
     }
@@ -495,7 +509,7 @@ __global__ __launch_bounds__(FORM ? 256 : 64 * MOST_WAVES, 2) void kv_append_ker
 template <typename T>
 int head_norm_rotate(tboa_ctx* ctx, long long n_tokens, int dh, int nq, const void* Q, long long ldq, const float* wq, int nk, const void* K, long long ldk, const float* wk, double eps,
                      const Rotation& rot, const int* positions, void* Qo, long long ldqo, void* Ko, long long ldko) {
-    RotateArgs<T> a{{{(const T*)Q, (T*)Qo, wq, ldq, ldqo, nq}, {(const T*)K, (T*)Ko, wk, ldk, ldko, nk}}, n_tokens, dh, (float)eps, rot, positions, 0};
+    RotateArgs<T> a{{{(const T*)Q, (T*)Qo, wq, ldq, ldqo, nq}, {(const T*)K, (T*)Ko, wk, ldk, ldko, nk}}, n_tokens, dh, eps, rot, positions, 0};
     const long long rows = n_tokens * (nq + nk);
     // 16-byte pieces where every head vector and table row starts on a 16-byte boundary and the pairs of 16 channels are whole pieces
     const int e = 16 / (int)sizeof(T);
