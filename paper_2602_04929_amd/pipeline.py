@@ -230,7 +230,7 @@ def serve_attention_block(ctx, weights, X, cache, batch, n_q_heads, rotation=Non
 
     weights: dict with Wqkv = [W_Q; W_K; W_V] and Wo, as quantize_attention_block's dequantized matrices; rotation by int32 positions [tokens]; norm_q, norm_k: fp32 [head_dim] weights of the
     norms of every head's query and key.  Keys without a norm are rotated by the append itself, on unrounded values.  Returns a dict: Y [tokens, d_model], and q, k, v, o on the way
-    (k as it goes to the append)."""
+    (k as it goes to the append).  Rows of X behind the last sequence go along: o is 0 there, and Y the residual."""
     Hq, Hkv, dh = n_q_heads, cache.desc.n_kv_heads, cache.desc.head_dim
     qkv = ctx.linear_forward(X, weights["Wqkv"]).view(X.shape[0], Hq + 2 * Hkv, dh)
     q, k, v = qkv[:, :Hq], qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:]
@@ -238,6 +238,9 @@ def serve_attention_block(ctx, weights, X, cache, batch, n_q_heads, rotation=Non
     if rotation is not None or norm_q is not None or norm_k is not None:
         ctx.head_norm_rotate(q, None if in_append else k, norm_q, norm_k, eps, rotation, positions, out_q=q, out_k=None if in_append else k)
     ctx.kv_cache_append(cache, batch, k, v, *((rotation, positions) if in_append else ()))
-    o = ctx.kv_cache_attention(cache, batch, q, scale=scale, window=window)
+    o = torch.empty(X.shape[0], Hq, dh, dtype=X.dtype, device=X.device)
+    with torch.cuda.stream(ctx._stream):
+        o.zero_()      # (attention does not write rows of no sequence)
+    ctx.kv_cache_attention(cache, batch, q, scale=scale, window=window, out=o)
     Y = ctx.linear_forward(o.view(-1, Hq * dh), weights["Wo"], residual=residual)
     return dict(Y=Y, q=q, k=k, v=v, o=o)
