@@ -334,7 +334,8 @@ int tboa_kv_cache_append(tboa_ctx* ctx, const tboa_kv_cache_desc* desc, const tb
  * (and, with window > 0, the last `window` of them, its own included).  Rows that see nothing get 0.
  *   Q, O [n_tokens][n_q_heads * head_dim] in `dtype`, rows ldq, ldo elements apart; scale 0: 1/sqrt(head_dim).  n_tokens * (n_q_heads / n_kv_heads) < 2^27
  * O overlaps neither Q nor the cache.  Levels enter the products exactly.  fp32 sums.  TBOA_F32: q and probabilities times scale as pairs of 11 bits.
- * TBOA_BF16: q as it is, probabilities times scale as pairs of 11 bits in sequences of up to 32 rows (new tokens times n_q_heads / n_kv_heads), rounded to 11 bits in longer ones.
+ * TBOA_BF16: q as it is, probabilities times scale as pairs of 11 bits in sequences of up to 32 rows (new tokens times n_q_heads / n_kv_heads; n_tokens where n_seqs is
+ * 1), rounded to 11 bits in longer ones.
  * Both are held against the row's own largest query channel and largest probability times scale: neither tokens that a row does not see nor other rows take bits from it (longer sequences: as long as
  * those products of 32 neighbouring rows lie within 2^200 of each other). */
 size_t tboa_kv_cache_attention_workspace_bytes(const tboa_kv_cache_desc* desc, int n_q_heads, int n_seqs, int64_t n_tokens);

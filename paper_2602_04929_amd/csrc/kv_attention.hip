@@ -148,7 +148,7 @@ __global__ __launch_bounds__(256, resident<DP>()) void kv_attend_rows_kernel(Att
         if (x >> 31) { k0 = (int)(x % tiles); x /= tiles; h = (int)(x % a.g.heads); tile = (int)(x / a.g.heads); }
         else { const unsigned u = (unsigned)x / tiles; k0 = (unsigned)x - u * tiles; tile = u / a.g.heads; h = u - tile * a.g.heads; }
         h = __builtin_amdgcn_readfirstlane(h); k0 = __builtin_amdgcn_readfirstlane(k0); tile = __builtin_amdgcn_readfirstlane(tile);
-        const bool two = NT == 2 || s.n * a.rep <= FEW;      // half terms of probabilities
+        const bool two = NT == 2 || (a.q.n_seqs > 1 ? s.n : a.q.n_tokens) * a.rep <= FEW;      // half terms of probabilities (one sequence alone: as the host, which has only n_tokens, chooses its kernel)
         const int k1 = (int)min((long long)tiles, k0 + (at_end - at));      // tiles k0 .. k1 - 1 of the unit
         const int r0 = tile * ROWS, n_rows = (int)min((long long)ROWS, (long long)s.n * a.rep - r0);
         const Span span = row_span(s, a, r0, n_rows);

@@ -5,12 +5,12 @@ import torch
 F64 = torch.float64
 
 
-def attention(cache, starts, lens, pages, q, scale, window, dtype=torch.float32, many=False):
+def attention(cache, starts, lens, pages, q, scale, window, dtype=torch.float32, many=False, rows_of_call=None):
     """Output (NaN for rows of no sequence and those that see a scale that is no number) and the bound of an output's error, per element.  With A the probabilities, x the scores and, of a token,
     X = scale sum |q| |k|; many: the kernel for many rows:
       scores          dh + 4 fp32 operations on terms that add up to X (and fp32 queries in two half terms, 2^-22 of them): (dh + 4 + [8 for fp32]) 2^-24 X, and 2 * 2^-24 |x - max x| for the
                       difference to the maximum, whose own error numerator and sum share; the exponential 2^-22.  Of every token, in the numerator and in the sum
-      probabilities   times scale, in two halves 2^-22; in one 2^-11 (bf16 sequences of more than 32 rows)
+      probabilities   times scale, in two halves 2^-22; in one 2^-11 (bf16 sequences of more than 32 rows; rows_of_call: of one sequence alone, the call's)
       sums            (n + 8) 2^-24, twice, n tokens
       next to nothing a half below 2^-14 is off by 2^-25 whatever it is.  The largest probability times scale of the row is at least 2^14 as half (2^-1 for many rows): 2^-39 (2^-24) of it for every
                       token, times at most 255 levels
@@ -23,7 +23,7 @@ def attention(cache, starts, lens, pages, q, scale, window, dtype=torch.float32,
         n, end = int(starts[b + 1] - starts[b]), min(int(lens[b]), pages.shape[1] * pt)
         if n == 0:
             continue
-        halves = 2.0 ** (-11 if dtype == torch.bfloat16 and n * rep > 32 else -22)
+        halves = 2.0 ** (-11 if dtype == torch.bfloat16 and (rows_of_call or n * rep) > 32 else -22)
         p = np.arange(end)
         page = np.asarray(pages[b])[p // pt]
         there = (page >= 0) & (page < len(cache.data))
@@ -60,9 +60,9 @@ def attention(cache, starts, lens, pages, q, scale, window, dtype=torch.float32,
     return out, lim
 
 
-def check(got, cache, starts, lens, pages, q, scale, window, many=False, rows=None, telling=0.9):
+def check(got, cache, starts, lens, pages, q, scale, window, many=False, rows=None, telling=0.9, rows_of_call=None):
     """rows: a mask [rows, heads] of what is compared (all that belong to sequences).  `telling`: at least this share of the compared outputs is larger than the bound, so that zeros would fail."""
-    want, lim = attention(cache, starts, lens, pages, q, scale, window, got.dtype, many)
+    want, lim = attention(cache, starts, lens, pages, q, scale, window, got.dtype, many, rows_of_call)
     g = got.double().cpu()
     use = torch.zeros(g.shape[:2], dtype=torch.bool)
     use[:int(starts[-1])] = True

@@ -160,3 +160,16 @@ def test_special_values_to_the_bound_of_each_sequence(ctx, lib, dtype):
         got = attend(ctx, lib, cache, starts, [150, 150], table, q)
         assert new == 1 or torch.isnan(got[3, 0]).all()
         check(got, cache, starts, [150, 150], table, q, 1 / 8, 0, many=many, rows=rows)
+
+
+@pytest.mark.parametrize("new,spare", [(4, 60), (16, 1), (3, 13)])
+def test_probabilities_of_one_padded_sequence(ctx, lib, new, spare):
+    """Up to 32 rows alone in a call of more: by its n_tokens a long one, in either kernel."""
+    starts, pages, cache, _, q = case(lib, 4, 2, 64, [new], [300], 16, 1, torch.bfloat16, 90 + new, spare_rows=spare)
+    want = attention(cache, starts, [300], pages, q, 1 / 8, 0)[0][:new].to(torch.bfloat16)
+    for p, many in ((pages, False), (wide(pages, 16), True)):
+        got = attend(ctx, lib, cache, starts, [300], p, q)
+        check(got, cache, starts, [300], p, q, 1 / 8, 0, many=many, rows_of_call=len(q) * 2)
+        other = (got[:new].cpu() != want).double().mean().item()
+        print("outputs that are not the nearest: %.5f" % other)
+        assert (other > 0.02) == (len(q) * 2 > 32)
