@@ -64,7 +64,7 @@ struct AttendArgs {
     int few;                      // sequences of more rows are kv_attend_tiles_kernel's
     int4* info;                   // per workgroup: the unit that begins in its share and ends in another: workgroups, first row of the sequence, row of the first | rows << 27, head
     float* tile_part; float2* tile_stat;      // kv_attend_tiles_kernel: per piece, its rows
-    float* part; float2* stat;    // per workgroup two pieces of 16 rows (of a unit that began before its share, of one that begins in it): unscaled outputs; maximum, sum
+    float* part; float2* stat;    // per workgroup two pieces of 16 rows (of a unit that began before its share, of one that begins in it): averages; maximum, sum
 };
 
 // channels c .. c + 3 of a row of the outputs
@@ -340,7 +340,10 @@ __global__ __launch_bounds__(256, resident<DP>()) void kv_attend_rows_kernel(Att
         float top = ends[0][col].x;
 #pragma unroll
         for (int w = 1; w < 4; ++w) top = fmaxf(top, ends[w][col].x);
-        const float f = m == -__builtin_inff() ? 0.f : ex2(m - top);
+        float sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) if (ends[w][col].x != -__builtin_inff()) sum += ends[w][col].y * ex2(ends[w][col].x - top);
+        const float f = m == -__builtin_inff() ? 0.f : ex2(m - top) / sum;      // (averages from here on: weighted sums of the largest values leave fp32)
 #pragma unroll
         for (int c = 0; c < CT; ++c) *(f4*)&joined[wave][col][c * 16 + grp * 4] = m == -__builtin_inff() ? f4{0.f, 0.f, 0.f, 0.f} : by_power(o[c] * f, -up);
         __syncthreads();
@@ -349,30 +352,22 @@ __global__ __launch_bounds__(256, resident<DP>()) void kv_attend_rows_kernel(Att
         if (threadIdx.x == 0 && k0 == 0 && !whole) a.info[blockIdx.x] = make_int4((int)((at + tiles - 1) / share) - (int)blockIdx.x + 1, s.start, r0 | (n_rows - 1) << 27, h);
         for (int i = threadIdx.x; i < n_rows * (DP / 4); i += 256) {
             const int rr = i / (DP / 4), c = i % (DP / 4) * 4;
-            float tp = ends[0][rr].x, sum = 0.f;
             f4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int w = 1; w < 4; ++w) tp = fmaxf(tp, ends[w][rr].x);
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                if (ends[w][rr].x != -__builtin_inff()) sum += ends[w][rr].y * ex2(ends[w][rr].x - tp);
-                v += *(const f4*)&joined[w][rr][c];
-            }
+            for (int w = 0; w < 4; ++w) v += *(const f4*)&joined[w][rr][c];
             if (whole) {
                 const int row = r0 + rr, tk = row / a.rep;
                 T* out = (T*)a.O + (long long)(s.start + tk) * a.ldo + (long long)(h * a.rep + row - tk * a.rep) * a.g.dh;
-                store4(out, c, a, sum == 0.f ? f4{0.f, 0.f, 0.f, 0.f} : v / sum);
-            } else {
-                *(f4*)(a.part + (piece + rr) * DP + c) = v;
-                if (c == 0) a.stat[piece + rr] = make_float2(tp, sum);
-            }
+                store4(out, c, a, v);
+            } else *(f4*)(a.part + (piece + rr) * DP + c) = v;
         }
+        if (!whole && threadIdx.x < n_rows) a.stat[piece + threadIdx.x] = make_float2(top, sum);      // (lane col of the first wavefront: its row's)
         at += k1 - k0;
         if (at < at_end) __syncthreads();      // (what is in LDS has been read)
     }
 }
 
-// Rows of a unit that lies in several shares: sum of 2^(max_i - max) O_i over that of the sums, a wavefront per row of the unit that begins in share blockIdx.x.  DP / 4 lanes hold a row;
+// Rows of a unit that lies in several shares: averages O_i weighted with 2^(max_i - max) sum_i, over the weights' sum; a wavefront per row of the unit that begins in share blockIdx.x.  DP / 4 lanes hold a row;
 // the first pieces are on their way before their weights are known.
 template <typename T, int DP>
 __global__ __launch_bounds__(256) void kv_attend_join_kernel(AttendArgs a) {
@@ -394,8 +389,14 @@ __global__ __launch_bounds__(256) void kv_attend_join_kernel(AttendArgs a) {
         float now = fmaxf(st.x, top);
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) now = fmaxf(now, __shfl_xor(now, o, 64));
-        const float turn = top == now ? 1.f : ex2(top - now), f = st.x == -__builtin_inff() ? 0.f : ex2(st.x - now);
-        v *= turn; sum = sum * turn + (st.x == -__builtin_inff() ? 0.f : f * st.y);
+        const float turn = top == now ? 1.f : ex2(top - now);
+        float f = st.x == -__builtin_inff() ? 0.f : ex2(st.x - now) * st.y, more = f;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) more += __shfl_xor(more, o, 64);
+        const float had = sum * turn;
+        sum = had + more;
+        const float part_of = sum == 0.f ? 0.f : 1.f / sum;
+        v *= had * part_of; f *= part_of;
         top = now;
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) v += ahead[k] * __shfl(f, min(group + k * GROUPS, 63), 64);
@@ -406,8 +407,6 @@ __global__ __launch_bounds__(256) void kv_attend_join_kernel(AttendArgs a) {
             for (int k = 0; k < AHEAD; ++k) v += ahead[k] * __shfl(f, min(k0 + group + k * GROUPS, 63), 64);
         }
     }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o, 64);
     f4 all = v;
 #pragma unroll
     for (int g = 1; g < GROUPS; ++g)
@@ -416,7 +415,7 @@ __global__ __launch_bounds__(256) void kv_attend_join_kernel(AttendArgs a) {
     if (group == 0) {
         const int row = r0 + rr, tk = row / a.rep;
         T* out = (T*)a.O + (long long)(info.y + tk) * a.ldo + (long long)(h * a.rep + row - tk * a.rep) * a.g.dh;
-        store4(out, 4 * c, a, sum == 0.f ? f4{0.f, 0.f, 0.f, 0.f} : all / sum);
+        store4(out, 4 * c, a, all);
     }
 }
 
@@ -809,17 +808,17 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
     const int up = TILE_TOP - e_wave + d;
     l += from_xor<32>(l);
     if (l != l) m = fmaxf(m, 0.f);      // scores that are all NaN leave the maximum where it was
-    const bool none = m == -__builtin_inff();
+    const bool none = m == -__builtin_inff() || l == 0.f;
+    const float f = none ? 0.f : 1.f / l;
     if (u.n_cuts == 1) {
         bf16* const out = (bf16*)a.O + (long long)(s.start + tok) * a.ldo + (long long)(h * a.rep + r - tok * a.rep) * a.g.dh;
-        const float f = none || l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
         for (int c = 0; c < CT; ++c) {
             f4 v[4];      // channels 32 c + 8 g + 4 half ..
 #pragma unroll
             for (int g = 0; g < 4; ++g)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) v[g][k] = none || l == 0.f ? 0.f : __builtin_amdgcn_ldexpf(o[c][4 * g + k] * f, -up);
+                for (int k = 0; k < 4; ++k) v[g][k] = none ? 0.f : __builtin_amdgcn_ldexpf(o[c][4 * g + k] * f, -up);
             if (a.out_piece == 8) {      // the two halves of the wavefront exchange theirs for whole 16-byte pieces
 #pragma unroll
                 for (int g = 0; g < 4; g += 2) {
@@ -841,7 +840,7 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
         for (int c = 0; c < CT; ++c)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                *(f4*)(a.tile_part + at * DP + 32 * c + 8 * i + 4 * half) = none ? f4{0.f, 0.f, 0.f, 0.f} : by_power(f4{o[c][4 * i], o[c][4 * i + 1], o[c][4 * i + 2], o[c][4 * i + 3]}, -up);
+                *(f4*)(a.tile_part + at * DP + 32 * c + 8 * i + 4 * half) = none ? f4{0.f, 0.f, 0.f, 0.f} : by_power(f4{o[c][4 * i], o[c][4 * i + 1], o[c][4 * i + 2], o[c][4 * i + 3]} * f, -up);
     }
 }
 
@@ -868,18 +867,19 @@ __global__ __launch_bounds__(256) void kv_attend_tiles_join_kernel(AttendArgs a)
         float top = -__builtin_inff(), sum = 0.f;
 #pragma unroll 4
         for (int i = 0; i < u.n_cuts; ++i) top = fmaxf(top, a.tile_stat[(long long)(u.cut + i) * RT + rr].x);
+        auto weight = [&](long long at) { const float2 st = a.tile_stat[at]; return st.x == -__builtin_inff() ? 0.f : ex2(st.x - top) * st.y; };
+#pragma unroll 4
+        for (int i = 0; i < u.n_cuts; ++i) sum += weight((long long)(u.cut + i) * RT + rr);
+        const float part_of = sum == 0.f ? 0.f : 1.f / sum;
         f4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
         for (int i = 0; i < u.n_cuts; ++i) {
             const long long at = (long long)(u.cut + i) * RT + rr;
-            const float2 st = a.tile_stat[at];
-            const float f = st.x == -__builtin_inff() ? 0.f : ex2(st.x - top);
-            sum += st.x == -__builtin_inff() ? 0.f : f * st.y;
-            v += f * *(const f4*)(a.tile_part + at * DP + c);
+            v += weight(at) * part_of * *(const f4*)(a.tile_part + at * DP + c);
         }
         const int row = r0 + rr, tk = row / a.rep;
         bf16* const out = (bf16*)a.O + (long long)(u.s.start + tk) * a.ldo + (long long)(u.h * a.rep + row - tk * a.rep) * a.g.dh;
-        store4(out, c, a, sum == 0.f ? f4{0.f, 0.f, 0.f, 0.f} : v / sum);
+        store4(out, c, a, v);
     }
 }
 
