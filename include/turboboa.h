@@ -272,9 +272,9 @@ int tboa_dequant_gemv(tboa_ctx* ctx, int d_out, int d_in, int bits, int group, c
                       const float* scales, const float* zeros, const float* x, float* y);
 
 /* ------------------------------------------------------------------------------------------------
- * Serving with a quantized key/value cache: the setting that tboa_build_hout_q_kv_cache prepares W_Q for.  Forward only; everything is enqueued on the context's stream and nothing
- * synchronises, so the three calls can be captured into a HIP graph (reserve tboa_kv_cache_attention_workspace_bytes before; a workspace that a captured graph uses is kept until
- * tboa_destroy even if the context's grows later).  A context's calls and the graphs captured from it share its workspace: they run one after the other, on one stream.
+ * Serving with a quantized key/value cache of 8 bits.  (tboa_build_hout_q_kv_cache prepares W_Q for such a cache, of 2 .. 8 bits and of keys as the projection gives them; here they
+ * may be normalised and rotated first.)  Forward only; everything is enqueued on the context's stream and nothing
+ * synchronises, so the three calls can be captured into a HIP graph (reserve tboa_kv_cache_attention_workspace_bytes before).  A context's calls and the graphs captured from it share its workspace: they run one after the other, on one stream.
  *
  * The cache is one buffer of n_pages pages of tboa_kv_cache_page_bytes(desc) bytes, 16-byte aligned (sizes and offsets of 64 bits).  A page holds page_tokens consecutive tokens of one
  * sequence for all heads, in this order:

@@ -91,8 +91,11 @@ constexpr int ROWS = 16, TILE = 64;      // rows (query token, head of the group
 // workgroups that a compute unit holds at once (registers): the shares that the work is cut into are 256 times as many
 template <int DP> constexpr int resident() { return DP <= 64 ? 3 : DP <= 128 ? 2 : 1; }
 
-// Rows of a sequence up to which kv_attend_rows_kernel takes it in any call (32 sequences behind 2000 others): 32 rows 155 us, not 247 (32 heads); 64 rows 270 and 267, or 67 and 70
-// (64 / 8 heads); 128 rows 125 and 74.
+// Rows of a sequence up to which kv_attend_rows_kernel takes it in any call.  Both kernels, 32 sequences behind 2000 others, us, this kernel and the one for many rows:
+//     heads (of dh)        32 of 32      64 / 8 of 32    32 of 64     64 / 8 of 64    32 of 128    64 / 8 of 128    8 of 256     16 / 2 of 256
+//     32 rows              89   218      37   55         117  230     45   59         156  252     44   70          118  210     42   42
+//     64 rows              145  233      53   57         198  246     68   60         283  270     76   73          227  224     61   61
+// (heads of 32 would gain at 64 too)
 constexpr int FEW = 32;
 
 // how a sequence is cut: row tiles, tiles of tokens that its rows see
@@ -114,7 +117,8 @@ __device__ __forceinline__ Span row_span(const KvSeq& s, const AttendArgs& a, in
 // share of that list, wherever units begin and end; its four wavefronts take every fourth tile and are joined through LDS.  A unit that lies in one share is finished there, pieces of the others go to
 // kv_attend_join_kernel.  S^T = K Q^T with tile i's row 4 g + j of the matrix instruction being token 16 g + 4 i + j: lane group g then holds the probabilities of tokens 16 g .. 16 g + 15
 // for row lane % 16, which are the right operand of O^T += V^T P^T as they stand.  The loads of V's tile are in flight while its scores are formed, those of K's next one while it is multiplied.
-// Bound by the cache's bytes: 32 sequences of 1000 to 8000 tokens, 64 / 8 heads of 128 (319 MB): 67 us and 5 us for the pieces, 4.4 TB/s; one of 131000 tokens (285 MB): 50 + 9 us.
+// Bound by the cache's bytes: 32 sequences of 1000 to 8000 tokens, 64 / 8 heads of 128 (319 MB): 69 us and 5 us for the pieces, 4.3 TB/s where a large copy reaches 4.7; one of 131000 tokens (285 MB):
+// 53 + 9 us, repeated passes over so little finding part of it in the last cache.
 template <typename T, int DP>
 __global__ __launch_bounds__(256, resident<DP>()) void kv_attend_rows_kernel(AttendArgs a) {
     constexpr int NT = sizeof(T) == 2 ? 1 : 2;      // half terms of queries
@@ -427,7 +431,9 @@ __global__ __launch_bounds__(256) void kv_attend_join_kernel(AttendArgs a) {
 // the next tile.  Runs end at a barrier; of the two wavefronts of a SIMD one is a run behind the other, so that one multiplies while the other exponentiates.
 // A row's maximum is only followed where it has to be: as long as the sum of a lane's 32 probabilities stays below MOST, so does each of them, and they simply exceed 1 (MOST 2^TILE_TOP = 2^15 is
 // within half); no maximum is formed then.
-// Two sequences of up to 2048 new tokens behind up to 4096, 64 / 8 heads of 128 (367 GFLOP): 469 us, 780 TFLOP/s of the 1423 that a large product of half matrices reaches.
+// Two sequences of up to 2048 new tokens behind up to 4096, 64 / 8 heads of 128 (367 GFLOP): 460 us, 800 TFLOP/s of the 1423 that a large product of half matrices reaches.
+// What bounds it: a wavefront spends 30 % of its cycles issuing vector and matrix instructions (32 of the latter a tile, beside about 310 vector and 165 scalar ones), 28 % waiting to issue and 26 % at
+// counters and barriers; and the units are uneven, the busiest compute unit having 194 tiles where the mean is 173.
 constexpr float MOST = 0x1p7f;
 constexpr int TILE_TOP = 8;      // halves are below 2^(TILE_TOP + 7): probabilities are up to MOST, scales below the row's bound
 constexpr int SPARE = 8;         // a row's bound of scales is so many powers of two above its largest probability times scale: larger scales (the bound is then raised) are rare, and parts of 2^-13 of
@@ -435,8 +441,8 @@ constexpr int SPARE = 8;         // a row's bound of scales is so many powers of
 template <int DP> constexpr int waves() { return DP <= 128 ? 8 : 4; }      // (wider heads need twice the registers)
 template <int DP> constexpr int permuted() { return DP % 128 == 0 ? 15 : DP % 64 == 0 ? 7 : 3; }      // bits of a piece's number that K's rows are XORed into
 template <int DP> constexpr int tiles_lds() { return 2 * 2 * TILE * DP * 2; }
-constexpr int TILES_TARGET = 256;                    // pieces that the units of a call are cut into where they are fewer: one for each compute unit, which holds one workgroup at a time (512: 79 us for 1000 tokens
-                                                     // of 64 / 8 heads, not 50)
+constexpr int TILES_TARGET = 256;                    // pieces that the units of a call are cut into where they are fewer: one for each compute unit, which holds one workgroup at a time.  1000 tokens of 64 / 8
+                                                     // heads of 32, 64, 128, of 16 / 2 of 256: 39, 42, 53, 82 us; with 512: 50, 58, 77, 93 (1100 tokens of 256: 119 and 94)
 
 struct TilesUnit { int b, h, tile, cut, n_cuts; KvSeq s; };
 template <int RT>
@@ -887,7 +893,9 @@ int shares(int dp) { return 256 * (dp == 32 ? resident<32>() : dp == 64 ? reside
 int unit_rows_of(int dp) { return 32 * (dp <= 128 ? waves<128>() : waves<256>()); }
 // Calls whose units of 16 rows, by what the host knows, are few and short: the rows' kernel alone.  Two units (or a few of three) per workgroup of it are done before a tiles' workgroup has gone
 // through the serial part of its first one: 36 new tokens behind 1093 others of six sequences (32 heads of 128, 576 units, 10000 tiles in all) 47 us, not 64; 256 new tokens of one (64 / 8 heads, 1024
-// units) 25, not 30; 64 behind 4000 others (256 units, 16000 tiles) 43 and 39, 16 behind 31000 (64 units, 31000 tiles) 96 and 52; 16 sequences of 250 (8192 units) 158 and 62.
+// units) 28, not 33, with heads of 256 (16 / 2) 21, not 56, but of 64 32, not 26, and of 32 28, not 24; 64 behind 4000 others (256 units, 16000 tiles) 43 and 39, heads of 256 37 and 61; 16 behind 31000
+// (64 units, 31000 tiles) 96 and 52, heads of 256 73 and 120; 16 sequences of 250 (8192 units) 158 and 62.  The host knows no lengths: a row of pages counts as if it were full, and one much wider than its
+// sequences sends short calls to the other kernel.
 bool is_small(const KvGeometry& g, const tboa_kv_batch& b, int rep, int window) {
     const long long room = ((long long)b.pages_per_seq << g.pt_log) + TILE, units = (b.n_tokens * rep / ROWS + std::min<long long>(b.n_seqs, b.n_tokens)) * g.heads;
     return units <= 9 * shares(g.dp) / 4 && units * ((window ? std::min<long long>(room, (long long)window + b.n_tokens + 2 * TILE) : room) / TILE) <= 16384;

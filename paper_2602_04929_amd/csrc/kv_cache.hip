@@ -224,9 +224,11 @@ __device__ __forceinline__ void load_piece(const T* p, bool vec, int n, float (&
 
 // What a wavefront does with TOKENS tokens of a head.  LPT lanes per token, NP pieces of 8 channels in each (piece q + LPT i of a token is lane q's): the ends of a token are found in its lanes,
 // whose grid is then theirs, and a token's levels leave as whole pieces; those of V turn by way of LDS into the tokens of a channel.
-// Bound by its instructions, not by its bytes (prompts of four sequences, 32 heads of 128: 147 MB would take 31 us): a key's value costs about ten operations in fp64, which is what the grid is
-// decided in, and 18 in fp32.  As many lanes per token as it has pieces, up to 16: four with up to eight pieces each took 14.5 us instead of 4.8 for a token of each of 64 sequences, 50 instead
-// of 42 for four prompts of 2000 (8 heads, a grid per token) and spilled registers.
+// Prompts of four sequences, 32 heads of 128, a grid per 16 tokens (147 MB): 89 us, three times what the bytes take at a copy's rate.  Half of the wavefronts' time is waiting for loads, which start
+// tile after tile (two wavefronts per SIMD: FORM 4 for bf16 takes all 256 registers and spills 66, addresses of the branch for unaligned rows); 29 % is vector instructions, 36 a
+// value on average (those of keys partly in fp64, which is what the grid is decided in).
+// As many lanes per token as it has pieces, up to 16 (timed in graphs of 20 calls): four with up to eight pieces each took 14.4 us instead of 5.0 for a token of each of 64 sequences, 50 instead
+// of 42 for four prompts of 2000 (8 heads, a grid per token).
 // ROT: keys, rotated in fp64 (products of 24 bits are exact there); a piece's partners are read once more.  Else the inputs themselves, in fp32.  Levels come from fp32 products, and a piece with such
 // a product within 2^-21 of a border from the fp64 quotients (three roundings are off by 3 * 2^-24 of it).
 template <typename T, int LPT, int NP, bool ROT>

@@ -230,7 +230,8 @@ def serve_attention_block(ctx, weights, X, cache, batch, n_q_heads, rotation=Non
 
     weights: dict with Wqkv = [W_Q; W_K; W_V] and Wo, as quantize_attention_block's dequantized matrices; rotation by int32 positions [tokens]; norm_q, norm_k: fp32 [head_dim] weights of the
     norms of every head's query and key.  Keys without a norm are rotated by the append itself, on unrounded values.  Returns a dict: Y [tokens, d_model], and q, k, v, o on the way
-    (k as it goes to the append).  Rows of X behind the last sequence go along: o is 0 there, and Y the residual."""
+    (k as it goes to the append).  Rows of X behind the last sequence go along: o is 0 there, and Y the residual.
+    The three serving calls can be captured into a graph; this block cannot where weights are fp32 and activations bf16 (linear_forward then waits for the host to learn the weights' form)."""
     Hq, Hkv, dh = n_q_heads, cache.desc.n_kv_heads, cache.desc.head_dim
     qkv = ctx.linear_forward(X, weights["Wqkv"]).view(X.shape[0], Hq + 2 * Hkv, dh)
     q, k, v = qkv[:, :Hq], qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:]
