@@ -5,7 +5,7 @@ import torch
 
 from tests.attention_bounds import check
 from tests.test_gpu_kv_cache_attention import case
-from tests.test_gpu_kv_cache_attention_ranges import attend, wide
+from tests.test_gpu_kv_cache_attention_ranges import attend, kinds, wide
 
 pytestmark = pytest.mark.gpu
 
@@ -17,11 +17,9 @@ def ctx(lib):
     c.close()
 
 
-@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
-@pytest.mark.parametrize("heads,new,length,many", [(1, 1, 60, False), (1, 1, 250, False), (1, 3, 6000, False), (700, 1, 200, False), (1, 50, 400, False), (1, 50, 400, True), (1, 70, 5000, True), (300, 20, 100, True)])
+@pytest.mark.parametrize("dtype,heads,new,length,many", kinds((1, 1, 60, False), (1, 1, 250, False), (1, 3, 6000, False), (700, 1, 200, False), (1, 50, 400, False), (1, 50, 400, True), (1, 70, 5000, True),
+                                                              (300, 20, 100, True)))
 def test_averages_of_large_values(ctx, lib, dtype, heads, new, length, many):
-    if many and dtype == torch.float32:
-        pytest.skip("fp32 has one kernel")
     starts, pages, cache, _, q = case(lib, heads, 2, 32, [new], [length], 64, 1, dtype, new + length)
     rng = np.random.default_rng(1)
     cache.vg[..., 0] = 2.0 ** 119 * (0.5 + 0.5 * rng.random(cache.vg.shape[:-1]))

@@ -10,6 +10,11 @@ from tests.test_gpu_kv_cache_attention import SHAPES, case
 pytestmark = pytest.mark.gpu
 
 
+def kinds(*cases):
+    """The cases, whose last entry says whether they are the kernel's for many rows, in both types; fp32 has no such kernel."""
+    return [(dtype, *c) for dtype in (torch.bfloat16, torch.float32) for c in cases if not (c[-1] and dtype == torch.float32)]
+
+
 @pytest.fixture(scope="module")
 def ctx(lib):
     c = lib.Context()
@@ -45,13 +50,10 @@ def test_probabilities_of_few_rows(ctx, lib, shape):
     assert other < 0.01 + 3 / got.numel()
 
 
-@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("factor", [1e7, 1e12, 1e30])
-@pytest.mark.parametrize("new,window,many", [(1, 40, False), (7, 0, False), (7, 30, False), (50, 0, False), (50, 0, True), (70, 33, True), (200, 150, True)])
+@pytest.mark.parametrize("dtype,new,window,many", kinds((1, 40, False), (7, 0, False), (7, 30, False), (50, 0, False), (50, 0, True), (70, 33, True), (200, 150, True)))
 def test_scales_of_tokens_that_are_not_seen(ctx, lib, dtype, factor, new, window, many):
     """A scale of V far above the others, behind a row's own place or before its window, changes nothing in the row."""
-    if many and dtype == torch.float32:
-        pytest.skip("fp32 has one kernel")
     length, dh, rep = 300, 64, 2
     starts, pages, cache, _, q = case(lib, 2, rep, dh, [new], [length], 16, 1, dtype, 40 + new)
     last = length - 1 - (new - 1) // 2      # seen by the last half of the rows; the row before it does not
@@ -66,12 +68,9 @@ def test_scales_of_tokens_that_are_not_seen(ctx, lib, dtype, factor, new, window
     check(got, cache, starts, [length], pages, q, 1 / 8, window, many=many)
 
 
-@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
-@pytest.mark.parametrize("new,many", [(1, False), (5, False), (40, False), (40, True), (300, True)])
+@pytest.mark.parametrize("dtype,new,many", kinds((1, False), (5, False), (40, False), (40, True), (300, True)))
 def test_scales_of_tokens_that_hardly_count(ctx, lib, dtype, new, many):
     """Scales of V that grow as the scores fall: large ones with probabilities next to nothing, met first, in between and last."""
-    if many and dtype == torch.float32:
-        pytest.skip("fp32 has one kernel")
     length, dh = 700, 64
     starts, pages, cache, _, q = case(lib, 1, 1, dh, [new], [length], 64, 1, dtype, 60 + new)
     q[:] = (torch.randn(dh, generator=torch.Generator().manual_seed(1)).to(dtype) / 8).cuda()      # every row asks the same
@@ -86,12 +85,9 @@ def test_scales_of_tokens_that_hardly_count(ctx, lib, dtype, new, many):
     check(got, cache, starts, [length], pages, q, 1 / 8, 0, many=many)
 
 
-@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
-@pytest.mark.parametrize("new,many", [(4, False), (60, False), (60, True)])
+@pytest.mark.parametrize("dtype,new,many", kinds((4, False), (60, False), (60, True)))
 def test_scales_as_far_apart_as_an_append_makes_them(ctx, lib, dtype, new, many):
     """Beside scales of 1e-14, the largest there is: behind the rows' place, and in a token that they see with a probability of 2^-126 or less."""
-    if many and dtype == torch.float32:
-        pytest.skip("fp32 has one kernel")
     length, dh = 200, 64
     starts, pages, cache, _, q = case(lib, 1, 1, dh, [new], [length], 64, 1, dtype, 70 + new)
     q[:] = (torch.randn(dh, generator=torch.Generator().manual_seed(1)).to(dtype)).cuda()
@@ -108,13 +104,10 @@ def test_scales_as_far_apart_as_an_append_makes_them(ctx, lib, dtype, new, many)
     check(got, cache, starts, [length], pages, q, 1 / 8, 0, many=many)
 
 
-@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("factor", [1e9, 1e15, 1e30, 3e36])
-@pytest.mark.parametrize("new,many", [(3, False), (40, False), (40, True), (200, True)])
+@pytest.mark.parametrize("dtype,new,many", kinds((3, False), (40, False), (40, True), (200, True)))
 def test_queries_of_other_rows(ctx, lib, dtype, factor, new, many):
     """One finite row far above the others, and one far below: the others are what they are without them, to the bound of their own values."""
-    if many and dtype == torch.float32:
-        pytest.skip("fp32 has one kernel")
     length, dh, rep = 260, 64, 2
     starts, pages, cache, _, q = case(lib, 1, rep, dh, [new], [length], 16, 1, dtype, 80 + new)
     q[1, 0] *= factor
