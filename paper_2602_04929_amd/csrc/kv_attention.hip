@@ -305,8 +305,8 @@ __global__ __launch_bounds__(256, resident<DP>()) void kv_attend_rows_kernel(Att
             w_top = fmaxf(w_top, from_xor<16>(w_top)); w_top = fmaxf(w_top, from_xor<32>(w_top));
             most_w = fmaxf(most_w * turn, fminf(w_top, MOST_FLOAT));
             const int up_was = up;
-            if (most_w > 0.f) up = HALF_TOP + 1 - max(__builtin_amdgcn_frexp_expf(most_w), -126);
-            turn = __builtin_amdgcn_ldexpf(turn, up - up_was);      // (up rises only as most_w falls with turn: 2 at most)
+            up = HALF_TOP + 1 - (most_w > 0.f ? max(__builtin_amdgcn_frexp_expf(most_w), -126) : -126);
+            turn = __builtin_amdgcn_ldexpf(turn, up - up_was);      // (up rises only as most_w falls with turn, to nothing at last: 2 at most)
             if (__any(turn != 1.f)) {
 #pragma unroll
                 for (int c = 0; c < CT; ++c) o[c] *= turn;

@@ -166,3 +166,22 @@ def test_probabilities_of_one_padded_sequence(ctx, lib, new, spare):
         other = (got[:new].cpu() != want).double().mean().item()
         print("outputs that are not the nearest: %.5f" % other)
         assert (other > 0.02) == (len(q) * 2 > 32)
+
+
+@pytest.mark.parametrize("dtype,heads,new,many", kinds((800, 1, False), (1, 5, False), (150, 40, False), (1, 40, True), (150, 40, True)))
+def test_scales_that_vanish_in_between(ctx, lib, dtype, heads, new, many):
+    """Large scales first, then scores so much higher that those count for nothing, of tokens whose scale is 0, then small scales at the same height.  (Many units: a wavefront goes through all three.)"""
+    length, dh = 1700, 32
+    starts, pages, cache, _, q = case(lib, heads, 1, dh, [new], [length], 64, 1, dtype, 110 + new)
+    q[:] = (torch.randn(dh, generator=torch.Generator().manual_seed(1)).to(dtype)).cuda()
+    sign = np.sign(q[0, 0].float().cpu().numpy()).astype(int)
+    for t in range(length):
+        at, off = pages[0, t // 64], t % 64
+        if t < 256:
+            cache.k[at, :, off, :dh], cache.kg[at, :, off] = 128 - sign * 127, (4.0, 128)      # a score of -90 sum |q|, some -2000
+        cache.vg[at, :, off, 0] = 2.0 ** 115 if t < 256 else 0.0 if t < 512 else 2.0 ** -100
+    if many:
+        pages = wide(pages, 64)
+    got = attend(ctx, lib, cache, starts, [length], pages, q)
+    assert torch.isfinite(got).all()
+    check(got, cache, starts, [length], pages, q, 1 / np.sqrt(dh), 0, many=many)
