@@ -701,7 +701,7 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
     h8 pf[4];
     float m = -__builtin_inff(), l = 0.f, most_w = 0.f;      // most_w: largest probability times scale that the row had when its bound was last set
     // A half is 2^(TILE_TOP - e_wave) scale, the same for all rows, times 2^d probability: 2^(e_wave - d) is the row's bound of scales, 2^SPARE above most_w.  Rows of 2^200 between them have that
-    // (e_wave is at most 2^100 below the largest bound, and never falls); what lies further below, if anything does, loses bits
+    // (e_wave is at most 2^100 below the largest bound); what lies further below, if anything does, loses bits
     int e_wave = -126 + SPARE, d = 0;
     float limit = 0.f;                     // the least bound of a row
     // operands in LDS
@@ -779,12 +779,19 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
                 const int e_was = e_wave - d, e_row = (most_w > 0.f ? max(__builtin_amdgcn_frexp_expf(most_w), -126) : -126) + SPARE;
                 const int e_least = over_rows(some ? e_row : 128, least), e_most = over_rows(some ? e_row : -126 + SPARE, greatest);
                 const float s_top = across_halves(fminf(fmaxf(gv[0], gv[1]), MOST_FLOAT));      // (seen or not: below, scales by themselves stay finite)
-                e_wave = max(max(e_wave, min(e_least, e_most)), max(e_most - 100, __builtin_amdgcn_frexp_expf(__int_as_float(over_rows(__float_as_int(s_top), greatest))) - 118));
+                e_wave = max(min(e_least, e_most), max(e_most - 100, __builtin_amdgcn_frexp_expf(__int_as_float(over_rows(__float_as_int(s_top), greatest))) - 118));
                 limit = __uint_as_float((unsigned)(min(e_least, 128) + 127) << 23);
                 d = min(e_wave - e_row, 100);
-                turn = __builtin_amdgcn_ldexpf(turn, e_was - (e_wave - d));      // (a row's bound falls only as most_w does with turn: 2 at most)
+                const int rise = e_was - (e_wave - d), first = min(rise, 100);
+                turn = __builtin_amdgcn_ldexpf(turn, first);
 #pragma unroll
                 for (int c = 0; c < CT; ++c) o[c] *= turn;
+                if (__any(rise > first)) {      // (2^rise itself may be no number)
+#pragma unroll
+                    for (int c = 0; c < CT; ++c)
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) o[c][j] = __builtin_amdgcn_ldexpf(o[c][j], rise - first);
+                }
 #pragma unroll
                 for (int i = 0; i < 32; ++i) p[i] = __builtin_amdgcn_ldexpf(p[i], d);
             }
