@@ -117,8 +117,8 @@ __device__ __forceinline__ Span row_span(const KvSeq& s, const AttendArgs& a, in
 // share of that list, wherever units begin and end; its four wavefronts take every fourth tile and are joined through LDS.  A unit that lies in one share is finished there, pieces of the others go to
 // kv_attend_join_kernel.  S^T = K Q^T with tile i's row 4 g + j of the matrix instruction being token 16 g + 4 i + j: lane group g then holds the probabilities of tokens 16 g .. 16 g + 15
 // for row lane % 16, which are the right operand of O^T += V^T P^T as they stand.  The loads of V's tile are in flight while its scores are formed, those of K's next one while it is multiplied.
-// Bound by the cache's bytes: 32 sequences of 1000 to 8000 tokens, 64 / 8 heads of 128 (319 MB): 69 us and 5 us for the pieces, 4.3 TB/s where a large copy reaches 4.7; one of 131000 tokens (285 MB):
-// 53 + 9 us, repeated passes over so little finding part of it in the last cache.
+// Bound by the cache's bytes: 32 sequences of 1000 to 8000 tokens, 64 / 8 heads of 128 (319 MB): 68 us and 5 us for the pieces, 4.4 TB/s where a large copy reaches 4.7; one of 131000 tokens (285 MB):
+// 52 + 9 us, repeated passes over so little finding part of it in the last cache.
 template <typename T, int DP>
 __global__ __launch_bounds__(256, resident<DP>()) void kv_attend_rows_kernel(AttendArgs a) {
     constexpr int NT = sizeof(T) == 2 ? 1 : 2;      // half terms of queries
@@ -431,7 +431,7 @@ __global__ __launch_bounds__(256) void kv_attend_join_kernel(AttendArgs a) {
 // the next tile.  Runs end at a barrier; of the two wavefronts of a SIMD one is a run behind the other, so that one multiplies while the other exponentiates.
 // A row's maximum is only followed where it has to be: as long as the sum of a lane's 32 probabilities stays below MOST, so does each of them, and they simply exceed 1 (MOST 2^TILE_TOP = 2^15 is
 // within half); no maximum is formed then.
-// Two sequences of up to 2048 new tokens behind up to 4096, 64 / 8 heads of 128 (367 GFLOP): 460 us, 800 TFLOP/s of the 1423 that a large product of half matrices reaches.
+// Two sequences of up to 2048 new tokens behind up to 4096, 64 / 8 heads of 128 (367 GFLOP): 460 to 484 us, card by card, 760 to 800 TFLOP/s of the 1423 that a large product of half matrices reaches.
 // What bounds it: a wavefront spends 30 % of its cycles issuing vector and matrix instructions (32 of the latter a tile, beside about 310 vector and 165 scalar ones), 28 % waiting to issue and 26 % at
 // counters and barriers; and the units are uneven, the busiest compute unit having 194 tiles where the mean is 173.
 constexpr float MOST = 0x1p7f;
