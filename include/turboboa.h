@@ -272,6 +272,27 @@ int tboa_dequant_gemv(tboa_ctx* ctx, int d_out, int d_in, int bits, int group, c
                       const float* scales, const float* zeros, const float* x, float* y);
 
 /* ------------------------------------------------------------------------------------------------
+ * Linear layers on packed weights, for one token or many: the codes are what is read, no dequantized matrix exists.  Enqueued on the context's stream, nothing synchronises: the calls can be captured
+ * into a HIP graph (reserve tboa_packed_workspace_bytes before). */
+typedef struct {
+    int d_out, d_in;                /* at most 2^24 each */
+    int bits, group;                /* bits 2, 3, 4 or 8; group = 0: a grid per row, else per `group` consecutive channels, group | d_in */
+    const uint32_t* packed;         /* device [d_out][tboa_packed_words_per_row(d_in, bits)], as tboa_pack_codes writes it */
+    const float *scales, *zeros;    /* device [d_out][n_groups], n_groups = 1 or d_in / group; zeros hold whole numbers 0 .. 2^bits - 1 */
+} tboa_packed_weight;
+/* Y = X W^T (+ Res), W[n, c] = scales[n, c / g] (code[n, c] - zeros[n, c / g]).
+ *   X [n_tokens][d_in], Res (or NULL) and Y [n_tokens][d_out] in `dtype` (TBOA_F32 or TBOA_BF16), rows ldx, ldr, ldy elements apart; Y may be Res (with the same pitch) and overlaps nothing else.
+ *   n_tokens at most 2^24
+ * Codes less zeros enter the products exactly; fp32 sums and one rounding at the end.  bf16 X exactly, down to 2^-31 of the row's largest channel; fp32 X with 22 bits or more.  An infinity or NaN in a
+ * row of X makes that row of Y no finite numbers, and touches no other. */
+int tboa_packed_linear(tboa_ctx* ctx, const tboa_packed_weight* weight, int64_t n_tokens, int dtype, const void* X, int64_t ldx, const void* Res, int64_t ldr, void* Y, int64_t ldy);
+/* The gated half of an MLP: Act = silu(X Wg^T) * (X Wu^T), silu(g) = g / (1 + exp(-g)), as tboa_swiglu_forward, from two packed matrices of the same rows, channels, bits and group.  X and the products
+ * as in tboa_packed_linear; Act [n_tokens][d_out], rows lda elements apart. */
+int tboa_packed_swiglu(tboa_ctx* ctx, const tboa_packed_weight* gate, const tboa_packed_weight* up, int64_t n_tokens, int dtype, const void* X, int64_t ldx, void* Act, int64_t lda);
+/* Workspace that either call needs for a matrix of this shape (host value: the pointers are not read); 0 for an invalid descriptor, and where none is needed. */
+size_t tboa_packed_workspace_bytes(const tboa_packed_weight* weight, int64_t n_tokens, int dtype);
+
+/* ------------------------------------------------------------------------------------------------
  * Serving with a quantized key/value cache of 8 bits.  (tboa_build_hout_q_kv_cache prepares W_Q for such a cache, of 2 .. 8 bits and of keys as the projection gives them; here they
  * may be normalised and rotated first.)  Forward only; everything is enqueued on the context's stream and nothing
  * synchronises, so the three calls can be captured into a HIP graph (reserve tboa_kv_cache_attention_workspace_bytes before).  A context's calls and the graphs captured from it share its workspace: they run one after the other, on one stream.
@@ -341,6 +362,17 @@ int tboa_kv_cache_append(tboa_ctx* ctx, const tboa_kv_cache_desc* desc, const tb
 size_t tboa_kv_cache_attention_workspace_bytes(const tboa_kv_cache_desc* desc, int n_q_heads, int n_seqs, int64_t n_tokens);
 int tboa_kv_cache_attention(tboa_ctx* ctx, const tboa_kv_cache_desc* desc, const tboa_kv_batch* batch, int n_q_heads, int dtype, const void* Q, int64_t ldq,
                             const void* cache, double scale, int window, void* O, int64_t ldo);
+
+/* Attention of a tree of drafted tokens: tboa_kv_cache_attention whose rows see, of their sequence's new tokens, those that a mask names instead of the ones up to themselves.
+ *   tree  device [n_tokens][tree_words]: bit j % 32 of word j / 32 of a row says whether it sees the j-th new token of its sequence (its own is one of them); bits from the number of new tokens on count
+ *         for nothing, new tokens beyond 32 tree_words are seen by none.  tree_words 1 .. 1024, and at least max_new / 32 where the batch tells it.
+ * All places before the sequence's new tokens are seen, or with window > 0 those greater than p - window, where the row stands at p = places before the new tokens + bits of its mask - 1: as far behind
+ * them as it has ancestors.  (The mask alone decides on new tokens, a window as short as a path is the caller's to cut.)  Rows that see nothing get 0, and so do those whose own place is before 0.
+ * Keys are appended as those of any new tokens, rotated by the positions that the caller gives for them; of the tokens that are kept in the end the caller appends keys and values again, with the
+ * length that this leaves.  Types, precision, the other arguments and what is checked are as in tboa_kv_cache_attention; TBOA_BF16: sequences of up to 32 rows have probabilities of 22 bits. */
+size_t tboa_kv_cache_tree_attention_workspace_bytes(const tboa_kv_cache_desc* desc, int n_q_heads, int n_seqs, int64_t n_tokens);
+int tboa_kv_cache_tree_attention(tboa_ctx* ctx, const tboa_kv_cache_desc* desc, const tboa_kv_batch* batch, int n_q_heads, int dtype, const void* Q, int64_t ldq,
+                                 const uint32_t* tree, int tree_words, const void* cache, double scale, int window, void* O, int64_t ldo);
 
 /* ------------------------------------------------------------------------------------------------
  * Building blocks, exported for stage-isolated checks and for roofline measurement.

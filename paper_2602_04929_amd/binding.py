@@ -49,6 +49,10 @@ class KVBatchDesc(C.Structure):
                 ("max_new", C.c_int)]
 
 
+class PackedWeightDesc(C.Structure):
+    _fields_ = [("d_out", C.c_int), ("d_in", C.c_int), ("bits", C.c_int), ("group", C.c_int), ("packed", C.c_void_p), ("scales", C.c_void_p), ("zeros", C.c_void_p)]
+
+
 class RotationDesc(C.Structure):
     _fields_ = [("rot_dim", C.c_int), ("adjacent", C.c_int), ("n_positions", C.c_int64), ("cos_sin", C.c_void_p)]
 
@@ -95,6 +99,11 @@ def _load():
         "tboa_kv_cache_append": ([vp, C.POINTER(KVCacheDesc), C.POINTER(KVBatchDesc), i32, vp, i64, vp, i64, C.POINTER(RotationDesc), vp, vp], i32),
         "tboa_kv_cache_attention_workspace_bytes": ([C.POINTER(KVCacheDesc), i32, i32, i64], C.c_size_t),
         "tboa_kv_cache_attention": ([vp, C.POINTER(KVCacheDesc), C.POINTER(KVBatchDesc), i32, i32, vp, i64, vp, f64, i32, vp, i64], i32),
+        "tboa_kv_cache_tree_attention_workspace_bytes": ([C.POINTER(KVCacheDesc), i32, i32, i64], C.c_size_t),
+        "tboa_kv_cache_tree_attention": ([vp, C.POINTER(KVCacheDesc), C.POINTER(KVBatchDesc), i32, i32, vp, i64, vp, i32, vp, f64, i32, vp, i64], i32),
+        "tboa_packed_linear": ([vp, C.POINTER(PackedWeightDesc), i64, i32, vp, i64, vp, i64, vp, i64], i32),
+        "tboa_packed_swiglu": ([vp, C.POINTER(PackedWeightDesc), C.POINTER(PackedWeightDesc), i64, i32, vp, i64, vp, i64], i32),
+        "tboa_packed_workspace_bytes": ([C.POINTER(PackedWeightDesc), i64, i32], C.c_size_t),
         "tboa_counter": ([vp, i32], i64),
         "tboa_profile_enable": ([vp, i32], i32),
         "tboa_profile_reset": ([vp], i32),
@@ -135,6 +144,60 @@ def _rows(t, heads, head_dim, dtype):
     assert t.is_cuda and t.dtype is dtype and h == heads and d == head_dim, "expected %s [tokens, %d, %d], got %s %s" % (dtype, heads, head_dim, t.dtype, tuple(t.shape))
     assert (sd == 1 or d == 1) and (sh == d or h == 1), "a token's heads and a head's channels must be contiguous"
     return pitch if n > 1 else h * d
+
+
+def _pitch(t, dtype):
+    """Row pitch of a tensor [.., channels] whose rows are equally far apart."""
+    assert t.is_cuda and t.dtype is dtype, "expected a CUDA tensor of %s" % dtype
+    if t.is_contiguous():
+        return t.shape[-1]
+    assert t.stride(-1) == 1 or t.shape[-1] == 1, "a row's channels must be contiguous"
+    pitch, rows = None, 1
+    for n, step in reversed(list(zip(t.shape[:-1], t.stride()[:-1]))):
+        if n > 1:
+            pitch = step if pitch is None else pitch
+            assert step == pitch * rows, "rows are not equally far apart"
+            rows *= n
+    return t.shape[-1] if pitch is None else pitch
+
+
+def tree_masks(parents, counts, words=0):
+    """Masks of trees for Context.kv_cache_tree_attention, on the host: parents[i] is the place of token i's parent among the new tokens of its sequence, before its own, or -1; counts: new tokens of
+    every sequence.  Returns int32 [tokens, words] and the depth of every token, int32 [tokens] (its place behind the tokens that the cache had, from 0)."""
+    words = max(words, -(-max([*counts, 1]) // 32))
+    seen, depth, at = [], [], 0
+    for n in counts:
+        for i, p in enumerate(parents[at:at + n]):
+            assert -1 <= p < i, "token %d of a sequence has parent %d" % (i, p)
+            seen.append((1 << i) | (seen[at + p] if p >= 0 else 0))
+            depth.append(1 + depth[at + p] if p >= 0 else 0)
+        at += n
+    assert at == len(parents), "%d parents for %d tokens" % (len(parents), at)
+    tree = [[(m >> 32 * w) & 0xffffffff for w in range(words)] for m in seen]
+    tree = torch.tensor([[v - (1 << 32) if v >> 31 else v for v in row] for row in tree], dtype=torch.int64).reshape(-1, words).to(torch.int32)
+    return tree, torch.tensor(depth, dtype=torch.int32)
+
+
+class PackedWeight:
+    """A linear layer as packed codes (Context.pack_codes: int32 [d_out, words]) with fp32 scales and zeros [d_out, groups] (see tboa_packed_weight); what Context.packed_linear and packed_swiglu read."""
+
+    def __init__(self, packed, scales, zeros, d_in, bits, group=0):
+        for t, dtype in ((packed, torch.int32), (scales, torch.float32), (zeros, torch.float32)):
+            _dev(t, dtype)
+        words = int(_lib.tboa_packed_words_per_row(d_in, bits))
+        assert group >= 0 and bits in (2, 3, 4, 8) and d_in > 0 and (group == 0 or d_in % group == 0), "%d channels in groups of %d, %d bits" % (d_in, group, bits)
+        assert packed.dim() == 2 and packed.shape[0] > 0 and packed.shape[1] == words, "packed is %s, rows of %d codes of %d bits have %d words" % (tuple(packed.shape), d_in, bits, words)
+        grids = (packed.shape[0], d_in // group if group else 1)
+        assert scales.shape == zeros.shape and (scales.shape == grids or (grids[1] == 1 and scales.shape == grids[:1])), "scales %s, zeros %s, expected %s" % (tuple(scales.shape), tuple(zeros.shape), grids)
+        assert packed.device == scales.device == zeros.device, "packed, scales and zeros are on different devices"
+        self.packed, self.scales, self.zeros = packed, scales, zeros
+        self.desc = PackedWeightDesc(packed.shape[0], d_in, bits, group, packed.data_ptr(), scales.data_ptr(), zeros.data_ptr())
+        self._ref = C.byref(self.desc)
+
+    @classmethod
+    def of(cls, ctx, layer, bits, group=0):
+        """Of a layer as Context.quantize_layer returns it (codes, scales, zeros)."""
+        return cls(ctx.pack_codes(layer["codes"], bits), layer["scales"].contiguous(), layer["zeros"].contiguous(), layer["codes"].shape[1], bits, group)
 
 
 class Rotation:
@@ -499,6 +562,53 @@ class Context:
         self._used(cache.data, Q, out, batch.starts, batch.lens, batch.pages)
         self._check(_lib.tboa_kv_cache_attention(self._h, C.byref(d), C.byref(batch.desc(T)), Hq, _dtype_code(Q), _ptr(Q), ldq, _ptr(cache.data), scale, window,
                                                  _ptr(out), _rows(out, Hq, d.head_dim, Q.dtype)))
+        return out
+
+    @staticmethod
+    def kv_cache_tree_attention_workspace_bytes(cache, n_q_heads, n_seqs, n_tokens):
+        return int(_lib.tboa_kv_cache_tree_attention_workspace_bytes(C.byref(cache.desc), n_q_heads, n_seqs, n_tokens))
+
+    def kv_cache_tree_attention(self, cache, batch, Q, tree, scale=0.0, window=0, out=None):
+        """Attention of drafted tokens Q [tokens, n_q_heads, head_dim] that branch: a row sees what its sequence had before its new tokens and, of these, the ones that its mask names.
+        tree: int32 [tokens, words], bit j % 32 of word j / 32 for the j-th new token of the row's sequence (tree_masks makes it from parents).  Otherwise as kv_cache_attention."""
+        d, (T, Hq, _) = cache.desc, Q.shape
+        ldq = _rows(Q, Hq, d.head_dim, Q.dtype)
+        assert _dev(tree, torch.int32).dim() == 2 and tree.shape[0] == T, "tree: int32 [%d, words], not %s" % (T, tuple(tree.shape))
+        if out is None:
+            out = torch.empty(T, Hq, d.head_dim, dtype=Q.dtype, device=Q.device)
+        assert out.shape[0] == T
+        self._used(cache.data, Q, tree, out, batch.starts, batch.lens, batch.pages)
+        self._check(_lib.tboa_kv_cache_tree_attention(self._h, C.byref(d), C.byref(batch.desc(T)), Hq, _dtype_code(Q), _ptr(Q), ldq, _ptr(tree), tree.shape[1], _ptr(cache.data), scale, window,
+                                                      _ptr(out), _rows(out, Hq, d.head_dim, Q.dtype)))
+        return out
+
+    # ---- linear layers on packed weights
+    @staticmethod
+    def packed_workspace_bytes(weight, n_tokens, dtype):
+        return int(_lib.tboa_packed_workspace_bytes(weight._ref, n_tokens, {torch.float32: F32, torch.bfloat16: BF16}[dtype]))
+
+    def _packed(self, weight, X, more, out):
+        """Tokens, type and row pitches of X, `more` and the output (leading dimensions may be pitched as one)."""
+        d = weight.desc
+        assert X.dim() > 0 and X.shape[-1] == d.d_in, "X is %s, the weight has %d channels" % (tuple(X.shape), d.d_in)
+        shape = (*X.shape[:-1], d.d_out)
+        if out is None:
+            out = torch.empty(shape, dtype=X.dtype, device=X.device)
+        assert out.shape == shape and (more is None or more.shape == shape), "outputs and residuals are %s" % (shape,)
+        self._used(weight.packed, weight.scales, weight.zeros, X, more, out)
+        return out, X.numel() // d.d_in, _pitch(X, X.dtype), 0 if more is None else _pitch(more, X.dtype), _pitch(out, X.dtype)
+
+    def packed_linear(self, weight, X, residual=None, out=None):
+        """X W^T (+ residual) of a PackedWeight; X [.., d_in] bf16 or fp32, rows may be pitched.  out may be the residual."""
+        out, T, ldx, ldr, ldy = self._packed(weight, X, residual, out)
+        self._check(_lib.tboa_packed_linear(self._h, weight._ref, T, _dtype_code(X), X.data_ptr(), ldx, None if residual is None else residual.data_ptr(), ldr, out.data_ptr(), ldy))
+        return out
+
+    def packed_swiglu(self, gate, up, X, out=None):
+        """silu(X Wg^T) * (X Wu^T) of two PackedWeights of one shape."""
+        out, T, ldx, _, ldy = self._packed(gate, X, None, out)
+        self._used(up.packed, up.scales, up.zeros)
+        self._check(_lib.tboa_packed_swiglu(self._h, gate._ref, up._ref, T, _dtype_code(X), X.data_ptr(), ldx, out.data_ptr(), ldy))
         return out
 
     def pack_codes(self, codes, bits):

@@ -80,6 +80,13 @@ int tboa_ws_reserve(tboa_ctx* ctx, size_t bytes);
 // for a call that has a form with residues (`full` bytes) and one without (`plain`): the first unless it is known or found not to fit
 int tboa_ws_reserve_either(tboa_ctx* ctx, size_t full, size_t plain, bool& take_full);
 
+// the context's device is current while a call runs, and the caller's is again after it
+struct TbDevice {
+    int before = -1, now = -1;
+    explicit TbDevice(int device) { if (hipGetDevice(&before) == hipSuccess && before != device && hipSetDevice(device) == hipSuccess) now = device; }
+    ~TbDevice() { if (now >= 0) (void)hipSetDevice(before); }
+};
+
 static inline int64_t cdiv64(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // ---------------------------------------------------------------- gemm_f64.hip

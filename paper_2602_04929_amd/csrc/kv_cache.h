@@ -12,12 +12,7 @@ struct KvGeometry {
 static inline int kv_padded_head(int dh) { return dh <= 32 ? 32 : dh <= 64 ? 64 : dh <= 96 ? 96 : dh <= 128 ? 128 : dh <= 192 ? 192 : 256; }
 bool kv_geometry(const tboa_kv_cache_desc* d, KvGeometry& g);
 int kv_check(tboa_ctx* ctx, const char* who, const tboa_kv_cache_desc* d, const tboa_kv_batch* b, const void* cache, KvGeometry& g);
-// the context's device is current while a call runs, and the caller's is again after it
-struct KvDevice {
-    int before = -1, now = -1;
-    explicit KvDevice(int device) { if (hipGetDevice(&before) == hipSuccess && before != device && hipSetDevice(device) == hipSuccess) now = device; }
-    ~KvDevice() { if (now >= 0) (void)hipSetDevice(before); }
-};
+typedef TbDevice KvDevice;
 
 constexpr int KV_MOST_TOKENS = 1 << 30;      // of a sequence
 struct KvBatch { int n_seqs, per_seq, n_tokens, room; const int *starts, *lens, *pages; };      // room: tokens that a row of `pages` stands for
