@@ -17,7 +17,7 @@ struct PackedArgs {
     const void* Res; long long ldr;
     void* Y; long long ldy;
     int vec;      // rows of X may be read 16 bytes at a time
-    int runs_of_group, run_shift;      // packed_few_kernel: runs of channels that a group has, as a power of two or -1
+    unsigned piece_magic;      // packed_few_kernel: a group has 2^32 / piece_magic pieces of a run that share their scale (0: one; 1: all)
 };
 
 __device__ __forceinline__ float to_f32(float v) { return v; }
@@ -32,6 +32,8 @@ __device__ __forceinline__ void unroll(F&& f) {
     if constexpr (I < N) { f(std::integral_constant<int, I>{}); unroll<N, I + 1>(f); }
 }
 
+__device__ __forceinline__ unsigned low_halves(unsigned a, unsigned b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
+__device__ __forceinline__ unsigned high_halves(unsigned a, unsigned b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 // 24 bits as three terms of 8
 __device__ __forceinline__ void split(float v, __bf16& hi, __bf16& mid, __bf16& lo) {
     hi = (__bf16)v;
@@ -142,41 +144,48 @@ __global__ __launch_bounds__(256) void packed_any_kernel(PackedArgs a) {
 }
 
 // ------------------------------------------------------------------------------------------------ few tokens
-// Codes that a lane loads at a time, VW words of a row: CL of them, NF fragments of 8 for a 16 x 16 x 32 instruction.  Four lanes side by side hold CK = 4 CL consecutive channels of a row.
+// A run of CK = 128 VW / BITS consecutive channels of a row is 4 VW words, VW for each of the four lane groups of a 16 x 16 x 32 instruction, NF fragments of 8 codes for each lane.
 // Two codes become a pair of bf16 by a shift and an and-or: code c in the upper bits of the mantissa of 2^BITS is 2^BITS + c.  Pairs are codes that stand 16 bits apart in the stream (48 for 3 bits, as
 // 16 is no multiple of 3), and X takes the same order.
+struct Masks { unsigned codes, one; };
 template <int BITS, int VW>
 struct Codes {
     static constexpr int CL = VW * 32 / BITS, NF = CL / 8, CK = 4 * CL, OFFSET = BITS == 8 ? 0 : 1 << BITS;
-    // channels of pair p of fragment f
+    // 2 and 4 bits: word r of lane group g is the run's word 4 r + g, so that a fragment's channels lie together (and so may groups of 32 or 64); else VW words in a row
+    static constexpr bool TURNED = (BITS == 2 || BITS == 4) && VW == 4;
+    // channels of pair p of fragment f, among the lane's
     static constexpr int first(int f, int p) { return BITS == 8 ? 8 * f + 2 * p : BITS == 4 ? 8 * f + p : BITS == 2 ? f / 2 * 16 + f % 2 * 4 + p : 4 * f + p; }
     static constexpr int second(int f, int p) { return BITS == 8 ? 8 * f + 2 * p + 1 : first(f, p) + (BITS == 4 ? 4 : BITS == 2 ? 8 : 16); }
-    // the pair whose codes begin at bit `at` of either half of v
+    // the run's channel that is channel c of lane group g
+    static __device__ __forceinline__ int channel(int c, int g) { return TURNED ? c / (32 / BITS) * (128 / BITS) + g * (32 / BITS) + c % (32 / BITS) : g * CL + c; }
+    // the pair whose codes begin at bit AT of either half of v
     template <int AT>
-    static __device__ __forceinline__ unsigned pair(unsigned v) {
+    static __device__ __forceinline__ unsigned pair(unsigned v, const Masks& m) {
         constexpr int to = 7 - BITS;      // where a code begins in the mantissa
-        constexpr unsigned mask = ((1u << BITS) - 1) << to, one = (unsigned)(127 + BITS) << 7;
-        const unsigned u = AT < to ? v << (to - AT) : v >> (AT - to);
-        return (u & (mask | mask << 16)) | (one | one << 16);
+        return ((AT < to ? v << (to - AT) : v >> (AT - to)) & m.codes) | m.one;
     }
-    static __device__ __forceinline__ unsigned low_halves(unsigned a, unsigned b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
-    static __device__ __forceinline__ unsigned high_halves(unsigned a, unsigned b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
+    static __device__ __forceinline__ Masks masks() {
+        constexpr unsigned mask = BITS == 8 ? 0u : ((1u << BITS) - 1) << (7 - BITS), one = (unsigned)(127 + BITS) << 7;
+        Masks m{mask | mask << 16, one | one << 16};
+        asm("" : "+s"(m.codes), "+v"(m.one));      // (as literals they would be an instruction more for every pair)
+        return m;
+    }
     // fragment F of a lane's codes
     template <int F>
-    static __device__ __forceinline__ void fragment(const unsigned (&w)[VW], unsigned (&out)[4]) {
+    static __device__ __forceinline__ void fragment(const unsigned (&w)[VW], unsigned (&out)[4], const Masks& m) {
         if constexpr (BITS == 4) {
-            out[0] = pair<0>(w[F]); out[1] = pair<4>(w[F]); out[2] = pair<8>(w[F]); out[3] = pair<12>(w[F]);
+            out[0] = pair<0>(w[F], m); out[1] = pair<4>(w[F], m); out[2] = pair<8>(w[F], m); out[3] = pair<12>(w[F], m);
         } else if constexpr (BITS == 2) {
             constexpr int at = F % 2 * 8;
-            out[0] = pair<at>(w[F / 2]); out[1] = pair<at + 2>(w[F / 2]); out[2] = pair<at + 4>(w[F / 2]); out[3] = pair<at + 6>(w[F / 2]);
+            out[0] = pair<at>(w[F / 2], m); out[1] = pair<at + 2>(w[F / 2], m); out[2] = pair<at + 4>(w[F / 2], m); out[3] = pair<at + 6>(w[F / 2], m);
         } else if constexpr (BITS == 3) {
             const unsigned b = __builtin_amdgcn_alignbit(w[2], w[1], 16);      // the stream from bit 48 on
             // five codes of either half of the stream at a time, from bits 0, 15, 30 and 45 on
             auto five = [&](int k) {
                 return k == 0 ? low_halves(w[0], b) : k == 1 ? low_halves(w[0] >> 15, b >> 15) : k == 2 ? low_halves(__builtin_amdgcn_alignbit(w[1], w[0], 30), w[2] >> 14) : low_halves(w[1] >> 13, w[2] >> 29);
             };
-            out[0] = pair<4 * F % 5 * 3>(five(4 * F / 5)); out[1] = pair<(4 * F + 1) % 5 * 3>(five((4 * F + 1) / 5));
-            out[2] = pair<(4 * F + 2) % 5 * 3>(five((4 * F + 2) / 5)); out[3] = pair<(4 * F + 3) % 5 * 3>(five((4 * F + 3) / 5));
+            out[0] = pair<4 * F % 5 * 3>(five(4 * F / 5), m); out[1] = pair<(4 * F + 1) % 5 * 3>(five((4 * F + 1) / 5), m);
+            out[2] = pair<(4 * F + 2) % 5 * 3>(five((4 * F + 2) / 5), m); out[3] = pair<(4 * F + 3) % 5 * 3>(five((4 * F + 3) / 5), m);
         } else {
 #pragma unroll
             for (int p = 0; p < 4; ++p) {      // whole numbers up to 255 are bf16
@@ -187,98 +196,170 @@ struct Codes {
     }
 };
 
-// Up to 16 MT tokens per workgroup: bound by the codes' bytes.  A wavefront has 16 RT outputs (of either matrix) and every KW-th run of CK channels, which lie in one group; the wavefronts are joined through
-// LDS.  bf16 X: codes enter with their offset, and (offset + zero) sum x, by a product with ones that all outputs share, is taken out again with every run:
+constexpr int GRIDS = 16;      // groups whose scales and zeros a wavefront has in LDS
+// 16-byte piece p of row n of 16 rows of 64 bytes in LDS: pieces exchanged by row, so that neither four lanes beside each other (written) nor 16 rows (read) meet in a bank
+__device__ __forceinline__ int place16(int n, int p) { return n * 64 + ((p ^ (n >> 2 & 3)) << 4); }
+// bytes of LDS that a wavefront has: runs of X, of codes, scales and zeros
+template <typename T, int BITS, int VW, int MT, int NR>
+constexpr int few_bytes() { return MT * 16 * (Codes<BITS, VW>::CK) * (int)sizeof(T) + NR * 1024 + 2 * NR * 16 * GRIDS * 4; }
+template <int MT, int NR>
+constexpr int most_waves() { return MT == 1 && NR == 1 ? 16 : 8; }
+
+// Up to 16 MT tokens per workgroup: bound by the codes' bytes.  A wavefront has 16 RT outputs (of either matrix) and an equal part of the runs of channels; the wavefronts are joined through LDS.  FF
+// fragments of a run have one scale.  bf16 X: codes enter with their offset, and (offset + zero) sum x, by a product with ones that all outputs share, is taken out again with every scale:
 //     y += scale (sum (offset + code) x - (offset + zero) sum x)
 // fp32 X: codes less zeros, exact in bf16, times three bf16 terms.
-template <typename T, int BITS, int VW, int MT, int RT, bool GATED>
-__global__ __launch_bounds__(MT == 1 ? 1024 : 512) void packed_few_kernel(PackedArgs a) {
+// Rows of codes, of X and of scales are read by four lanes side by side, 64 bytes together, and handed to the lanes that multiply them through the wavefront's own part of LDS: read by those lanes
+// themselves, a row each, every 16 bytes are an access of their own to the first cache (16 tokens of 8192 x 28672: 37 million accesses, 143000 cycles of every compute unit's, 67 us).
+template <typename T, int BITS, int VW, int FF, int MT, int RT, bool GATED>
+__global__ __launch_bounds__((64 * most_waves<MT, (GATED ? 2 : 1) * RT>())) void packed_few_kernel(PackedArgs a) {
     typedef Codes<BITS, VW> C;
     constexpr bool EXACT = sizeof(T) == 4;
-    constexpr int NW = GATED ? 2 : 1, NR = NW * RT, CL = C::CL, NF = C::NF, XT = EXACT ? 3 : 1, XW = CL * (int)sizeof(T) / 16;
-    extern __shared__ float part[];      // [wavefronts][NR][16][17]
+    constexpr int NW = GATED ? 2 : 1, NR = NW * RT, CL = C::CL, NF = C::NF, NS = NF / FF, XT = EXACT ? 3 : 1, E = 16 / (int)sizeof(T), XB = C::CK * (int)sizeof(T) / 64;      // XB: 64-byte blocks of a row of X
+    constexpr int P = MT == 1 && XB <= 4 ? 2 : 1;      // runs whose loads are under way together
+    extern __shared__ __attribute__((aligned(16))) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, col = lane & 15, grp = lane >> 4;
+    const int row4 = lane >> 2, quarter = lane & 3;      // as a reader: row of 16, 16-byte piece of 64
+    char* const xs = lds + wave * few_bytes<T, BITS, VW, MT, NR>(), * const ws = xs + MT * 1024 * XB;
+    float* const grids = (float*)(ws + NR * 1024);      // [2][NR][16][GRIDS]
     const int n0 = blockIdx.x * (16 * RT);
     const long long m0 = (long long)blockIdx.y * (16 * MT);
-    const int runs = (a.d_in + C::CK - 1) / C::CK;
-    const uint32_t* words[NR];
-    const float *scale[NR], *zero[NR];
+    // places within the workgroup's rows of codes and of X (32 bits beside a base that all lanes share)
+    unsigned at_w[RT], at_x[MT];
 #pragma unroll
-    for (int r = 0; r < NR; ++r) {
-        const long long row = min(n0 + (r % RT) * 16 + col, a.d_out - 1);
-        words[r] = a.w[r / RT] + row * a.words;
-        scale[r] = a.scale[r / RT] + row * a.n_groups; zero[r] = a.zero[r / RT] + row * a.n_groups;
-    }
-    const T* x[MT];
+    for (int r = 0; r < RT; ++r) at_w[r] = ((unsigned)min(r * 16 + row4, a.d_out - 1 - n0) * a.words + quarter * VW) * 4;
 #pragma unroll
-    for (int t = 0; t < MT; ++t) x[t] = (const T*)a.X + min(m0 + 16 * t + col, a.tokens - 1) * a.ldx;
+    for (int t = 0; t < MT; ++t) at_x[t] = (unsigned)min((long long)(16 * t + row4), a.tokens - 1 - m0) * (unsigned)a.ldx * (unsigned)sizeof(T) + quarter * 16;
+    const char* const x = (const char*)((const T*)a.X + m0 * a.ldx);
+    const char* codes[NW];
+#pragma unroll
+    for (int w = 0; w < NW; ++w) codes[w] = (const char*)(a.w[w] + (long long)n0 * a.words);
 
-    struct Run { unsigned w[NR][VW]; float s[NR], z[NR]; };
-    auto load_weights = [&](int run, Run& o) {
-        const int at = (run * 4 + grp) * VW, g = a.n_groups == 1 ? 0 : a.run_shift >= 0 ? run >> a.run_shift : run / a.runs_of_group;
+    struct Run { unsigned w[NR][VW]; u4 x[MT][XB]; };
+    auto load = [&](int run, Run& o, auto WHOLE) {      // WHOLE: all of the run's channels are there, and X can be read 16 bytes at a time
+        const int k0 = run * C::CK;
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
-            if ((run + 1) * C::CK <= a.d_in) {
+            if constexpr (decltype(WHOLE)::value) {
                 struct __attribute__((packed, aligned(4))) Piece { unsigned u[VW]; };
-                const Piece p = *(const Piece*)(words[r] + at);
+                const Piece p = *(const Piece*)(codes[r / RT] + (long long)run * (16 * VW) + at_w[r % RT]);
 #pragma unroll
                 for (int i = 0; i < VW; ++i) o.w[r][i] = p.u[i];
             } else {
+                const uint32_t* const row = (const uint32_t*)(codes[r / RT] + (at_w[r % RT] - quarter * VW * 4));
 #pragma unroll
-                for (int i = 0; i < VW; ++i) o.w[r][i] = words[r][min(at + i, a.words - 1)];
+                for (int i = 0; i < VW; ++i) o.w[r][i] = row[min((run * 4 + quarter) * VW + i, a.words - 1)];
             }
-            o.s[r] = scale[r][g]; o.z[r] = zero[r][g];
+        }
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            if constexpr (decltype(WHOLE)::value) {
+#pragma unroll
+                for (int i = 0; i < XB; ++i) o.x[t][i] = *(const u4*)(x + (long long)k0 * sizeof(T) + i * 64 + at_x[t]);
+            } else {
+                const T* const row = (const T*)a.X + min(m0 + 16 * t + row4, a.tokens - 1) * a.ldx;
+#pragma unroll
+                for (int i = 0; i < XB; ++i) {
+                    union { u4 u; T e[E]; } v;
+                    v.u = u4{0, 0, 0, 0};
+#pragma unroll
+                    for (int j = 0; j < E; ++j) { const int k = k0 + i * 4 * E + quarter * E + j; if (k < a.d_in) v.e[j] = row[k]; }
+                    o.x[t][i] = v.u;
+                }
+            }
         }
     };
+    int grid0 = -GRIDS;      // first group whose scales are in LDS
+    auto group_of = [&](unsigned piece) { return min((int)(a.piece_magic ? __umulhi(piece, a.piece_magic) : piece), a.n_groups - 1); };
+    auto load_grids = [&](int g) {
+        grid0 = max(min(g, a.n_groups - GRIDS), 0);
+#pragma unroll
+        for (int r = 0; r < NR; ++r)
+#pragma unroll
+            for (int z = 0; z < 2; ++z) {
+                const float* const row = (z ? a.zero : a.scale)[r / RT] + (long long)min(n0 + r % RT * 16 + row4, a.d_out - 1) * a.n_groups;
+                struct __attribute__((packed, aligned(4))) Piece { float f[4]; };
+                Piece p;
+                if (a.n_groups >= GRIDS) p = *(const Piece*)(row + grid0 + quarter * 4);
+                else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) p.f[i] = row[min(quarter * 4 + i, a.n_groups - 1)];
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) grids[((z * NR + r) * 16 + row4) * GRIDS + ((quarter * 4 + i) ^ row4)] = p.f[i];
+            }
+    };
+    auto grid = [&](int z, int r, int g) { return grids[((z * NR + r) * 16 + col) * GRIDS + ((g - grid0) ^ col)]; };
     f4 acc[NR][MT];
 #pragma unroll
     for (int r = 0; r < NR; ++r)
 #pragma unroll
         for (int t = 0; t < MT; ++t) acc[r][t] = f4{0.f, 0.f, 0.f, 0.f};
+    const Masks masks = C::masks();
     b8 ones;
 #pragma unroll
     for (int j = 0; j < 8; ++j) ones[j] = (__bf16)1.f;
-    Run here, next;
-    if (wave < runs) load_weights(wave, next);
-    for (int run = wave; run < runs; run += waves) {
-        here = next;
-        const int k = run * C::CK + grp * CL;
-        union Raw { u4 u[XW]; unsigned w[4 * XW]; T e[CL]; } raw[MT];
+    auto in_order = [] { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); __builtin_amdgcn_wave_barrier(); };      // (a wavefront's own accesses to LDS)
+    auto multiply = [&](int run, const Run& o) {
+        in_order();
 #pragma unroll
-        for (int t = 0; t < MT; ++t) {
-            if (a.vec && (run + 1) * C::CK <= a.d_in) {
+        for (int r = 0; r < NR; ++r) {
+            struct __attribute__((aligned(16))) Piece { unsigned u[VW]; } p;
 #pragma unroll
-                for (int i = 0; i < XW; ++i) raw[t].u[i] = ((const u4*)(x[t] + k))[i];
-            } else {
-#pragma unroll
-                for (int i = 0; i < XW; ++i) raw[t].u[i] = u4{0, 0, 0, 0};
-#pragma unroll
-                for (int j = 0; j < CL; ++j) if (k + j < a.d_in) raw[t].e[j] = x[t][k + j];
-            }
+            for (int i = 0; i < VW; ++i) p.u[i] = o.w[r][i];
+            *(Piece*)(ws + r * 1024 + place16(row4, quarter)) = p;
         }
-        if (run + waves < runs) load_weights(run + waves, next);
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+            for (int i = 0; i < XB; ++i) *(u4*)(xs + (t * XB + i) * 1024 + place16(row4, quarter)) = o.x[t][i];
+        if (group_of(run * NS + NS - 1) >= grid0 + GRIDS) load_grids(group_of(run * NS));
+        in_order();
+        unsigned w[NR][VW];
+#pragma unroll
+        for (int r = 0; r < NR; ++r)
+#pragma unroll
+            for (int i = 0; i < VW; ++i) w[r][i] = *(const unsigned*)(ws + r * 1024 + (C::TURNED ? place16(col, i) + grp * 4 : place16(col, grp) + i * 4));
         f4 sum[MT], temp[NR][MT];
-#pragma unroll
-        for (int t = 0; t < MT; ++t) {
-            sum[t] = f4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int r = 0; r < NR; ++r) temp[r][t] = f4{0.f, 0.f, 0.f, 0.f};
-        }
         unroll<NF>([&](auto F) {
-            constexpr int f = F;
+            constexpr int f = F, s = f / FF;
+            if constexpr (f % FF == 0) {
+#pragma unroll
+                for (int t = 0; t < MT; ++t) {
+                    sum[t] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int r = 0; r < NR; ++r) temp[r][t] = f4{0.f, 0.f, 0.f, 0.f};
+                }
+            }
+            const int g = group_of(run * NS + s);
             union { unsigned u[4]; b8 v; } wf[NR];
 #pragma unroll
             for (int r = 0; r < NR; ++r) {
-                C::template fragment<f>(here.w[r], wf[r].u);
+                C::template fragment<f>(w[r], wf[r].u, masks);
                 if constexpr (EXACT) {
-                    const float off = C::OFFSET + here.z[r];
+                    const float off = C::OFFSET + grid(1, r, g);
 #pragma unroll
                     for (int p = 0; p < 4; ++p)
-                        wf[r].u[p] = C::high_halves(__float_as_uint(__uint_as_float(wf[r].u[p] << 16) - off), __float_as_uint(__uint_as_float(wf[r].u[p] & 0xffff0000u) - off));
+                        wf[r].u[p] = high_halves(__float_as_uint(__uint_as_float(wf[r].u[p] << 16) - off), __float_as_uint(__uint_as_float(wf[r].u[p] & 0xffff0000u) - off));
                 }
             }
+            // the pieces of X that hold the fragment's channels: those of the first codes of its pairs, and of the second ones
+            constexpr int c0 = C::first(f, 0), c1 = C::second(f, 0), B = BITS == 8 ? 8 : 4, H = BITS == 8 ? 1 : 2;      // B channels from c0 on, and from c1 on (H = 2)
 #pragma unroll
             for (int t = 0; t < MT; ++t) {
+                T e[H][B];
+#pragma unroll
+                for (int h = 0; h < H; ++h) {
+                    constexpr int N = B < E ? B : E;      // (a part of a piece, or pieces)
+#pragma unroll
+                    for (int i = 0; i < B; i += N) {
+                        const int at = C::channel((h ? c1 : c0) + i, grp) * (int)sizeof(T);
+                        struct __attribute__((aligned(N * sizeof(T)))) Part { T e[N]; };
+                        const Part p = *(const Part*)(xs + (t * XB + (at >> 6)) * 1024 + place16(col, at >> 4 & 3) + (at & 15));
+#pragma unroll
+                        for (int j = 0; j < N; ++j) e[h][i + j] = p.e[j];
+                    }
+                }
                 union { unsigned u[4]; b8 v; } xf[XT];
                 if constexpr (EXACT) {
 #pragma unroll
@@ -286,15 +367,17 @@ __global__ __launch_bounds__(MT == 1 ? 1024 : 512) void packed_few_kernel(Packed
 #pragma unroll
                         for (int j = 0; j < 2; ++j) {
                             __bf16 hi, mid, lo;
-                            split(to_f32(raw[t].e[j ? C::second(f, p) : C::first(f, p)]), hi, mid, lo);
+                            split(to_f32(BITS == 8 ? e[0][2 * p + j] : e[j * (H - 1)][p]), hi, mid, lo);
                             xf[0].v[2 * p + j] = hi; xf[XT / 2].v[2 * p + j] = mid; xf[XT - 1].v[2 * p + j] = lo;
                         }
                 } else {
+                    union { T e[H][B]; unsigned u[H][B / 2]; } in;
 #pragma unroll
-                    for (int p = 0; p < 4; ++p) {
-                        const int i = C::first(f, p), j = C::second(f, p);
-                        xf[0].u[p] = BITS == 8 ? raw[t].w[i / 2] : i % 2 ? C::high_halves(raw[t].w[i / 2], raw[t].w[j / 2]) : C::low_halves(raw[t].w[i / 2], raw[t].w[j / 2]);
-                    }
+                    for (int h = 0; h < H; ++h)
+#pragma unroll
+                        for (int j = 0; j < B; ++j) in.e[h][j] = e[h][j];
+#pragma unroll
+                    for (int p = 0; p < 4; ++p) xf[0].u[p] = BITS == 8 ? in.u[0][p] : p % 2 ? high_halves(in.u[0][p / 2], in.u[H - 1][p / 2]) : low_halves(in.u[0][p / 2], in.u[H - 1][p / 2]);
                     sum[t] = mma16(xf[0].v, ones, sum[t]);
                 }
 #pragma unroll
@@ -302,19 +385,39 @@ __global__ __launch_bounds__(MT == 1 ? 1024 : 512) void packed_few_kernel(Packed
 #pragma unroll
                     for (int i = 0; i < XT; ++i) temp[r][t] = mma16(xf[i].v, wf[r].v, temp[r][t]);
             }
+            if constexpr (f % FF == FF - 1) {
+#pragma unroll
+                for (int r = 0; r < NR; ++r) {
+                    const float scale = grid(0, r, g), off = -(C::OFFSET + grid(1, r, g));
+#pragma unroll
+                    for (int t = 0; t < MT; ++t)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) acc[r][t][j] = fmaf(scale, EXACT ? temp[r][t][j] : fmaf(off, sum[t][j], temp[r][t][j]), acc[r][t][j]);
+                }
+            }
         });
+    };
+    // P runs' loads are issued together; the wavefronts of a SIMD take turns
+    const int runs = (a.d_in + C::CK - 1) / C::CK, whole = a.vec ? a.d_in / C::CK : 0, each = (runs + waves - 1) / waves;
+    const int end = min((wave + 1) * each, runs);
+    int run = wave * each;
+    for (; run + P <= min(whole, end); run += P) {
+        Run o[P];
 #pragma unroll
-        for (int r = 0; r < NR; ++r) {
-            const float off = -(C::OFFSET + here.z[r]);
+        for (int i = 0; i < P; ++i) load(run + i, o[i], std::true_type());
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int t = 0; t < MT; ++t)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[r][t][j] = fmaf(here.s[r], EXACT ? temp[r][t][j] : fmaf(off, sum[t][j], temp[r][t][j]), acc[r][t][j]);
-        }
+        for (int i = 0; i < P; ++i) multiply(run + i, o[i]);
     }
+    for (; run < end; ++run) {
+        Run o;
+        if (run < whole) load(run, o, std::true_type()); else load(run, o, std::false_type());
+        multiply(run, o);
+    }
+    float* const part = (float*)lds;      // [wavefronts][NR][16][17]
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
-        if (t) __syncthreads();
+        __syncthreads();
 #pragma unroll
         for (int r = 0; r < NR; ++r)
 #pragma unroll
@@ -338,38 +441,35 @@ __global__ __launch_bounds__(MT == 1 ? 1024 : 512) void packed_few_kernel(Packed
     }
 }
 
-template <typename T, int BITS, int VW, int MT, int RT, bool GATED>
+template <typename T, int BITS, int VW, int FF, int MT, int RT, bool GATED>
 int launch_few(tboa_ctx* ctx, PackedArgs a) {
     typedef Codes<BITS, VW> C;
-    constexpr int NR = GATED ? 2 * RT : RT;
-    const int runs = (a.d_in + C::CK - 1) / C::CK, most = MT == 1 ? 16 : 8;
+    constexpr int NR = GATED ? 2 * RT : RT, bytes = few_bytes<T, BITS, VW, MT, NR>();
+    const int runs = (a.d_in + C::CK - 1) / C::CK;
     int waves = 4;
-    while (waves < most && waves < runs) waves *= 2;
-    a.runs_of_group = a.group / C::CK;
-    a.run_shift = a.n_groups > 1 && (a.runs_of_group & (a.runs_of_group - 1)) == 0 ? __builtin_ctz(a.runs_of_group) : -1;
-    const int lds = waves * NR * 16 * 17 * 4;
-    if (lds > 65536) TB_HIP(ctx, hipFuncSetAttribute((const void*)packed_few_kernel<T, BITS, VW, MT, RT, GATED>, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
-    hipLaunchKernelGGL((packed_few_kernel<T, BITS, VW, MT, RT, GATED>), dim3((unsigned)cdiv64(a.d_out, 16 * RT), (unsigned)cdiv64(a.tokens, 16 * MT)), dim3(64 * waves), lds, ctx->stream, a);
+    while (waves < most_waves<MT, NR>() && waves * (MT == 1 ? 2 : 1) < runs && 2 * waves * bytes <= 160 * 1024) waves *= 2;
+    const int pieces = a.group / (32 * FF);
+    a.piece_magic = a.n_groups == 1 ? 1 : pieces == 1 ? 0 : (unsigned)(((1ull << 32) + pieces - 1) / pieces);
+    const auto kernel = packed_few_kernel<T, BITS, VW, FF, MT, RT, GATED>;
+    if (waves * bytes > 65536) TB_HIP(ctx, hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, waves * bytes));
+    hipLaunchKernelGGL(kernel, dim3((unsigned)cdiv64(a.d_out, 16 * RT), (unsigned)cdiv64(a.tokens, 16 * MT)), dim3(64 * waves), waves * bytes, ctx->stream, a);
     TB_KERNEL_CHECK(ctx);
     return 0;
 }
-template <typename T, int BITS, int VW, int MT, bool GATED>
+template <typename T, int BITS, int VW, int FF, int MT, bool GATED>
 int launch_few(tboa_ctx* ctx, const PackedArgs& a) {
-    if constexpr (!GATED) { if (a.d_out >= 16 * 2 * 256) return launch_few<T, BITS, VW, MT, 2, GATED>(ctx, a); }
-    return launch_few<T, BITS, VW, MT, 1, GATED>(ctx, a);
+    if constexpr (!GATED) { if (a.d_out >= 16 * 2 * 256) return launch_few<T, BITS, VW, FF, MT, 2, GATED>(ctx, a); }
+    return launch_few<T, BITS, VW, FF, MT, 1, GATED>(ctx, a);
 }
-template <typename T, int BITS, int VW, bool GATED>
+template <typename T, int BITS, int VW, int FF, bool GATED>
 int launch_few(tboa_ctx* ctx, const PackedArgs& a) {
-    constexpr int less = BITS == 2 && VW == 4 ? 2 : VW;      // (registers)
-    if (a.tokens <= 16) return launch_few<T, BITS, VW, 1, GATED>(ctx, a);
-    if constexpr (sizeof(T) == 2) { if (a.tokens > 32) return launch_few<T, BITS, less, 4, GATED>(ctx, a); }
-    return launch_few<T, BITS, less, 2, GATED>(ctx, a);
+    if (a.tokens <= 16) return launch_few<T, BITS, VW, FF, 1, GATED>(ctx, a);
+    if constexpr (sizeof(T) == 2) { if (a.tokens > 32) return launch_few<T, BITS, VW, FF, 4, GATED>(ctx, a); }
+    return launch_few<T, BITS, VW, FF, 2, GATED>(ctx, a);
 }
-// words that a lane may load at a time so that a run of channels lies in one group; 0: none
-template <int BITS>
-int words_of_run(const PackedArgs& a) {
-    if (BITS == 3) return a.n_groups == 1 || a.group % 128 == 0 ? 3 : 0;
-    for (int vw = 4; vw >= (BITS == 8 ? 2 : 1); vw /= 2) if (a.n_groups == 1 || a.group % (4 * vw * 32 / BITS) == 0) return vw;
+// fragments (of 32 channels in all) that a group has at least: as many as a run, or the most of which it has a whole number; 0: none
+int fragments_of_scale(const PackedArgs& a, int most, int least) {
+    for (int ff = most; ff >= least; ff /= 2) if (a.n_groups == 1 || a.group % (32 * ff) == 0) return ff;
     return 0;
 }
 
@@ -387,11 +487,19 @@ int launch_any(tboa_ctx* ctx, const PackedArgs& a) {
 }
 template <typename T, int BITS, bool GATED>
 int launch(tboa_ctx* ctx, const PackedArgs& a) {
-    if (cdiv64(a.tokens, 16) <= 65535) switch (words_of_run<BITS>(a)) {
-        case 4: if constexpr (BITS != 3) return launch_few<T, BITS, 4, GATED>(ctx, a); break;
-        case 3: if constexpr (BITS == 3) return launch_few<T, BITS, 3, GATED>(ctx, a); break;
-        case 2: if constexpr (BITS != 3) return launch_few<T, BITS, 2, GATED>(ctx, a); break;
-        case 1: if constexpr (BITS != 3 && BITS != 8) return launch_few<T, BITS, 1, GATED>(ctx, a); break;
+    if (cdiv64(a.tokens, 16) <= 65535) {
+        if constexpr (BITS == 2) {
+            const int ff = fragments_of_scale(a, 8, 2);
+            if (ff) return ff == 8 ? launch_few<T, 2, 4, 8, GATED>(ctx, a) : ff == 4 ? launch_few<T, 2, 4, 4, GATED>(ctx, a) : launch_few<T, 2, 4, 2, GATED>(ctx, a);
+        } else if constexpr (BITS == 3) {
+            if (fragments_of_scale(a, 4, 4)) return launch_few<T, 3, 3, 4, GATED>(ctx, a);
+        } else if constexpr (BITS == 4) {
+            const int ff = fragments_of_scale(a, 4, 1);
+            if (ff) return ff == 4 ? launch_few<T, 4, 4, 4, GATED>(ctx, a) : ff == 2 ? launch_few<T, 4, 4, 2, GATED>(ctx, a) : launch_few<T, 4, 4, 1, GATED>(ctx, a);
+        } else {
+            const int ff = fragments_of_scale(a, 2, 1);
+            if (ff) return ff == 2 ? launch_few<T, 8, 4, 2, GATED>(ctx, a) : launch_few<T, 8, 2, 1, GATED>(ctx, a);
+        }
     }
     if (a.group % 8 == 0 || a.n_groups == 1) return launch_any<T, BITS, 0, GATED>(ctx, a);
     return a.group >= 8 ? launch_any<T, BITS, 1, GATED>(ctx, a) : launch_any<T, BITS, 2, GATED>(ctx, a);
@@ -429,7 +537,7 @@ int run(tboa_ctx* ctx, const char* who, const tboa_packed_weight* weight, const 
     a.d_out = weight->d_out; a.d_in = weight->d_in; a.words = (int)tboa_packed_words_per_row(weight->d_in, weight->bits);
     a.group = weight->group ? weight->group : weight->d_in; a.n_groups = weight->d_in / a.group;
     a.tokens = n_tokens; a.X = X; a.ldx = ldx; a.Res = Res; a.ldr = ldr; a.Y = Y; a.ldy = ldy;
-    a.vec = (uintptr_t)X % 16 == 0 && ldx * size % 16 == 0;
+    a.vec = (uintptr_t)X % 16 == 0 && ldx * size % 16 == 0 && ldx < 1 << 24;      // (the rows of a workgroup within 32 bits)
     if (dtype == TBOA_F32) return up ? launch<float, true>(ctx, weight->bits, a) : launch<float, false>(ctx, weight->bits, a);
     return up ? launch<bf16, true>(ctx, weight->bits, a) : launch<bf16, false>(ctx, weight->bits, a);
 }
