@@ -196,46 +196,52 @@ struct Codes {
     }
 };
 
-constexpr int GRIDS = 16;      // groups whose scales and zeros a wavefront has in LDS
+constexpr int GRIDS = 8;      // groups whose scales and zeros a wavefront has in LDS
 // 16-byte piece p of row n of 16 rows of 64 bytes in LDS: pieces exchanged by row, so that neither four lanes beside each other (written) nor 16 rows (read) meet in a bank
 __device__ __forceinline__ int place16(int n, int p) { return n * 64 + ((p ^ (n >> 2 & 3)) << 4); }
-// bytes of LDS that a wavefront has: runs of X, of codes, scales and zeros
-template <typename T, int BITS, int VW, int MT, int NR>
-constexpr int few_bytes() { return MT * 16 * (Codes<BITS, VW>::CK) * (int)sizeof(T) + NR * 1024 + 2 * NR * 16 * GRIDS * 4; }
-template <int MT, int NR>
-constexpr int most_waves() { return MT == 1 && NR == 1 ? 16 : 8; }
+// bytes of LDS that a wavefront has: runs of X (XR rows of it), of codes, scales and zeros
+template <typename T, int BITS, int VW, int XR, int NR>
+constexpr int few_bytes() { return XR * (Codes<BITS, VW>::CK) * (int)sizeof(T) + NR * 1024 + 2 * NR * 16 * GRIDS * 4; }
+template <int XR, int NR>
+constexpr int most_waves() { return XR <= 16 && NR == 1 ? 16 : 8; }
 
-// Up to 16 MT tokens per workgroup: bound by the codes' bytes.  A wavefront has 16 RT outputs (of either matrix) and an equal part of the runs of channels; the wavefronts are joined through LDS.  FF
+// Up to XR tokens (4, or 16 MT) per workgroup: bound by the codes' bytes.  A wavefront has 16 RT outputs (of either matrix) and an equal part of the runs of channels; the wavefronts are joined through LDS.  FF
 // fragments of a run have one scale.  bf16 X: codes enter with their offset, and (offset + zero) sum x, by a product with ones that all outputs share, is taken out again with every scale:
 //     y += scale (sum (offset + code) x - (offset + zero) sum x)
 // fp32 X: codes less zeros, exact in bf16, times three bf16 terms.
 // Rows of codes, of X and of scales are read by four lanes side by side, 64 bytes together, and handed to the lanes that multiply them through the wavefront's own part of LDS: read by those lanes
 // themselves, a row each, every 16 bytes are an access of their own to the first cache (16 tokens of 8192 x 28672: 37 million accesses, 143000 cycles of every compute unit's, 67 us).
-template <typename T, int BITS, int VW, int FF, int MT, int RT, bool GATED>
-__global__ __launch_bounds__((64 * most_waves<MT, (GATED ? 2 : 1) * RT>())) void packed_few_kernel(PackedArgs a) {
+template <typename T, int BITS, int VW, int FF, int XR, int RT, bool GATED>
+__global__ __launch_bounds__((64 * most_waves<XR, (GATED ? 2 : 1) * RT>())) void packed_few_kernel(PackedArgs a) {
     typedef Codes<BITS, VW> C;
     constexpr bool EXACT = sizeof(T) == 4;
-    constexpr int NW = GATED ? 2 : 1, NR = NW * RT, CL = C::CL, NF = C::NF, NS = NF / FF, XT = EXACT ? 3 : 1, E = 16 / (int)sizeof(T), XB = C::CK * (int)sizeof(T) / 64;      // XB: 64-byte blocks of a row of X
-    constexpr int P = MT == 1 && XB <= 4 ? 2 : 1;      // runs whose loads are under way together
+    constexpr int MT = (XR + 15) / 16, NW = GATED ? 2 : 1, NR = NW * RT, NF = C::NF, NS = NF / FF, XT = EXACT ? 3 : 1, E = 16 / (int)sizeof(T), XB = C::CK * (int)sizeof(T) / 64;      // XB: 64-byte blocks of a row of X
+    constexpr int XI = XR == 4 ? (XB + 3) / 4 : XB;      // loads that a row of X takes: of four rows, 64 lanes read four blocks at a time
+    constexpr int P = XR == 4 ? 4 : MT == 1 && XB <= 4 ? 2 : 1;      // runs whose loads are under way together
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, col = lane & 15, grp = lane >> 4;
     const int row4 = lane >> 2, quarter = lane & 3;      // as a reader: row of 16, 16-byte piece of 64
-    char* const xs = lds + wave * few_bytes<T, BITS, VW, MT, NR>(), * const ws = xs + MT * 1024 * XB;
+    char* const xs = lds + wave * few_bytes<T, BITS, VW, XR, NR>(), * const ws = xs + XR * 64 * XB;
     float* const grids = (float*)(ws + NR * 1024);      // [2][NR][16][GRIDS]
     const int n0 = blockIdx.x * (16 * RT);
-    const long long m0 = (long long)blockIdx.y * (16 * MT);
+    const long long m0 = (long long)blockIdx.y * XR;
+    const int xrow = XR == 4 ? row4 & 3 : row4, xblock = XR == 4 ? lane >> 4 : 0;      // of X, as a reader
     // places within the workgroup's rows of codes and of X (32 bits beside a base that all lanes share)
     unsigned at_w[RT], at_x[MT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) at_w[r] = ((unsigned)min(r * 16 + row4, a.d_out - 1 - n0) * a.words + quarter * VW) * 4;
 #pragma unroll
-    for (int t = 0; t < MT; ++t) at_x[t] = (unsigned)min((long long)(16 * t + row4), a.tokens - 1 - m0) * (unsigned)a.ldx * (unsigned)sizeof(T) + quarter * 16;
+    for (int t = 0; t < MT; ++t) at_x[t] = (unsigned)min((long long)(16 * t + xrow), a.tokens - 1 - m0) * (unsigned)a.ldx * (unsigned)sizeof(T) + quarter * 16;
     const char* const x = (const char*)((const T*)a.X + m0 * a.ldx);
     const char* codes[NW];
 #pragma unroll
     for (int w = 0; w < NW; ++w) codes[w] = (const char*)(a.w[w] + (long long)n0 * a.words);
 
-    struct Run { unsigned w[NR][VW]; u4 x[MT][XB]; };
+    // block of X that this lane reads with load i; where that is in LDS; where a lane that multiplies finds byte `at` of its row of a run
+    auto block_of = [&](int i) { return XR == 4 ? (XB < 4 ? xblock % XB : i * 4 + xblock) : i; };
+    auto written = [&](int t, int i) { return (u4*)(xs + (XR == 4 ? block_of(i) * 256 + xrow * 64 + quarter * 16 : (t * XB + i) * 1024 + place16(row4, quarter))); };
+    auto read = [&](int t, int at) { return xs + (XR == 4 ? (at >> 6) * 256 + (col & 3) * 64 + (at & 63) : (t * XB + (at >> 6)) * 1024 + place16(col, at >> 4 & 3) + (at & 15)); };
+    struct Run { unsigned w[NR][VW]; u4 x[MT][XI]; };
     auto load = [&](int run, Run& o, auto WHOLE) {      // WHOLE: all of the run's channels are there, and X can be read 16 bytes at a time
         const int k0 = run * C::CK;
 #pragma unroll
@@ -255,15 +261,15 @@ __global__ __launch_bounds__((64 * most_waves<MT, (GATED ? 2 : 1) * RT>())) void
         for (int t = 0; t < MT; ++t) {
             if constexpr (decltype(WHOLE)::value) {
 #pragma unroll
-                for (int i = 0; i < XB; ++i) o.x[t][i] = *(const u4*)(x + (long long)k0 * sizeof(T) + i * 64 + at_x[t]);
+                for (int i = 0; i < XI; ++i) o.x[t][i] = *(const u4*)(x + (long long)k0 * sizeof(T) + (block_of(i) * 64 + at_x[t]));
             } else {
-                const T* const row = (const T*)a.X + min(m0 + 16 * t + row4, a.tokens - 1) * a.ldx;
+                const T* const row = (const T*)a.X + min(m0 + 16 * t + xrow, a.tokens - 1) * a.ldx;
 #pragma unroll
-                for (int i = 0; i < XB; ++i) {
+                for (int i = 0; i < XI; ++i) {
                     union { u4 u; T e[E]; } v;
                     v.u = u4{0, 0, 0, 0};
 #pragma unroll
-                    for (int j = 0; j < E; ++j) { const int k = k0 + i * 4 * E + quarter * E + j; if (k < a.d_in) v.e[j] = row[k]; }
+                    for (int j = 0; j < E; ++j) { const int k = k0 + block_of(i) * 4 * E + quarter * E + j; if (k < a.d_in) v.e[j] = row[k]; }
                     o.x[t][i] = v.u;
                 }
             }
@@ -271,25 +277,27 @@ __global__ __launch_bounds__((64 * most_waves<MT, (GATED ? 2 : 1) * RT>())) void
     };
     int grid0 = -GRIDS;      // first group whose scales are in LDS
     auto group_of = [&](unsigned piece) { return min((int)(a.piece_magic ? __umulhi(piece, a.piece_magic) : piece), a.n_groups - 1); };
-    auto load_grids = [&](int g) {
+    struct Grids { float f[2][NR][GRIDS / 4]; };
+    auto load_grids = [&](int g, Grids& o) {      // of groups g .. for this lane's row of every 16
         grid0 = max(min(g, a.n_groups - GRIDS), 0);
 #pragma unroll
         for (int r = 0; r < NR; ++r)
 #pragma unroll
             for (int z = 0; z < 2; ++z) {
                 const float* const row = (z ? a.zero : a.scale)[r / RT] + (long long)min(n0 + r % RT * 16 + row4, a.d_out - 1) * a.n_groups;
-                struct __attribute__((packed, aligned(4))) Piece { float f[4]; };
-                Piece p;
-                if (a.n_groups >= GRIDS) p = *(const Piece*)(row + grid0 + quarter * 4);
-                else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) p.f[i] = row[min(quarter * 4 + i, a.n_groups - 1)];
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) grids[((z * NR + r) * 16 + row4) * GRIDS + ((quarter * 4 + i) ^ row4)] = p.f[i];
+                const int first = min(grid0 + quarter * (GRIDS / 4), a.n_groups - 1), second = min(first + 1, a.n_groups - 1);
+                o.f[z][r][0] = row[first]; o.f[z][r][1] = row[second];
             }
     };
-    auto grid = [&](int z, int r, int g) { return grids[((z * NR + r) * 16 + col) * GRIDS + ((g - grid0) ^ col)]; };
+    auto keep_grids = [&](const Grids& o) {
+#pragma unroll
+        for (int r = 0; r < NR; ++r)
+#pragma unroll
+            for (int z = 0; z < 2; ++z)
+#pragma unroll
+                for (int i = 0; i < GRIDS / 4; ++i) grids[((z * NR + r) * 16 + row4) * GRIDS + ((quarter * (GRIDS / 4) + i) ^ (row4 >> 1))] = o.f[z][r][i];
+    };
+    auto grid = [&](int z, int r, int g) { return grids[((z * NR + r) * 16 + col) * GRIDS + ((g - grid0) ^ (col >> 1))]; };
     f4 acc[NR][MT];
 #pragma unroll
     for (int r = 0; r < NR; ++r)
@@ -312,8 +320,8 @@ __global__ __launch_bounds__((64 * most_waves<MT, (GATED ? 2 : 1) * RT>())) void
 #pragma unroll
         for (int t = 0; t < MT; ++t)
 #pragma unroll
-            for (int i = 0; i < XB; ++i) *(u4*)(xs + (t * XB + i) * 1024 + place16(row4, quarter)) = o.x[t][i];
-        if (group_of(run * NS + NS - 1) >= grid0 + GRIDS) load_grids(group_of(run * NS));
+            for (int i = 0; i < XI; ++i) *written(t, i) = o.x[t][i];
+        if (group_of(run * NS + NS - 1) >= grid0 + GRIDS) { Grids next; load_grids(group_of(run * NS), next); keep_grids(next); }
         in_order();
         unsigned w[NR][VW];
 #pragma unroll
@@ -355,7 +363,7 @@ __global__ __launch_bounds__((64 * most_waves<MT, (GATED ? 2 : 1) * RT>())) void
                     for (int i = 0; i < B; i += N) {
                         const int at = C::channel((h ? c1 : c0) + i, grp) * (int)sizeof(T);
                         struct __attribute__((aligned(N * sizeof(T)))) Part { T e[N]; };
-                        const Part p = *(const Part*)(xs + (t * XB + (at >> 6)) * 1024 + place16(col, at >> 4 & 3) + (at & 15));
+                        const Part p = *(const Part*)read(t, at);
 #pragma unroll
                         for (int j = 0; j < N; ++j) e[h][i + j] = p.e[j];
                     }
@@ -401,17 +409,26 @@ __global__ __launch_bounds__((64 * most_waves<MT, (GATED ? 2 : 1) * RT>())) void
     const int runs = (a.d_in + C::CK - 1) / C::CK, whole = a.vec ? a.d_in / C::CK : 0, each = (runs + waves - 1) / waves;
     const int end = min((wave + 1) * each, runs);
     int run = wave * each;
-    for (; run + P <= min(whole, end); run += P) {
-        Run o[P];
+    Grids first;
+    load_grids(group_of(run * NS), first);
+    auto several = [&](auto N) {
+        constexpr int n = decltype(N)::value;
+        for (; run + n <= min(whole, end); run += n) {
+            Run o[n];
 #pragma unroll
-        for (int i = 0; i < P; ++i) load(run + i, o[i], std::true_type());
-        __builtin_amdgcn_sched_barrier(0);
+            for (int i = 0; i < n; ++i) load(run + i, o[i], std::true_type());
+            __builtin_amdgcn_sched_barrier(0);
+            if (run == wave * each) keep_grids(first);
 #pragma unroll
-        for (int i = 0; i < P; ++i) multiply(run + i, o[i]);
-    }
+            for (int i = 0; i < n; ++i) multiply(run + i, o[i]);
+        }
+    };
+    several(std::integral_constant<int, P>());
+    if constexpr (P == 4) several(std::integral_constant<int, 2>());
     for (; run < end; ++run) {
         Run o;
         if (run < whole) load(run, o, std::true_type()); else load(run, o, std::false_type());
+        if (run == wave * each) keep_grids(first);
         multiply(run, o);
     }
     float* const part = (float*)lds;      // [wavefronts][NR][16][17]
@@ -441,31 +458,33 @@ __global__ __launch_bounds__((64 * most_waves<MT, (GATED ? 2 : 1) * RT>())) void
     }
 }
 
-template <typename T, int BITS, int VW, int FF, int MT, int RT, bool GATED>
+template <typename T, int BITS, int VW, int FF, int XR, int RT, bool GATED>
 int launch_few(tboa_ctx* ctx, PackedArgs a) {
     typedef Codes<BITS, VW> C;
-    constexpr int NR = GATED ? 2 * RT : RT, bytes = few_bytes<T, BITS, VW, MT, NR>();
+    constexpr int NR = GATED ? 2 * RT : RT, bytes = few_bytes<T, BITS, VW, XR, NR>();
     const int runs = (a.d_in + C::CK - 1) / C::CK;
+    const int most = a.d_out > 16 * RT * 512 ? 8 : most_waves<XR, NR>();      // (workgroups that all find room at once)
     int waves = 4;
-    while (waves < most_waves<MT, NR>() && waves * (MT == 1 ? 2 : 1) < runs && 2 * waves * bytes <= 160 * 1024) waves *= 2;
+    while (waves < most && waves * 2 < runs && 2 * waves * bytes <= 160 * 1024) waves *= 2;
     const int pieces = a.group / (32 * FF);
     a.piece_magic = a.n_groups == 1 ? 1 : pieces == 1 ? 0 : (unsigned)(((1ull << 32) + pieces - 1) / pieces);
-    const auto kernel = packed_few_kernel<T, BITS, VW, FF, MT, RT, GATED>;
+    const auto kernel = packed_few_kernel<T, BITS, VW, FF, XR, RT, GATED>;
     if (waves * bytes > 65536) TB_HIP(ctx, hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, waves * bytes));
-    hipLaunchKernelGGL(kernel, dim3((unsigned)cdiv64(a.d_out, 16 * RT), (unsigned)cdiv64(a.tokens, 16 * MT)), dim3(64 * waves), waves * bytes, ctx->stream, a);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)cdiv64(a.d_out, 16 * RT), (unsigned)cdiv64(a.tokens, XR)), dim3(64 * waves), std::max(waves * bytes, waves * NR * 16 * 17 * 4), ctx->stream, a);
     TB_KERNEL_CHECK(ctx);
     return 0;
 }
-template <typename T, int BITS, int VW, int FF, int MT, bool GATED>
+template <typename T, int BITS, int VW, int FF, int XR, bool GATED>
 int launch_few(tboa_ctx* ctx, const PackedArgs& a) {
-    if constexpr (!GATED) { if (a.d_out >= 16 * 2 * 256) return launch_few<T, BITS, VW, FF, MT, 2, GATED>(ctx, a); }
-    return launch_few<T, BITS, VW, FF, MT, 1, GATED>(ctx, a);
+    if constexpr (!GATED && XR > 4) { if (a.d_out >= 16 * 2 * 256) return launch_few<T, BITS, VW, FF, XR, 2, GATED>(ctx, a); }
+    return launch_few<T, BITS, VW, FF, XR, 1, GATED>(ctx, a);
 }
 template <typename T, int BITS, int VW, int FF, bool GATED>
 int launch_few(tboa_ctx* ctx, const PackedArgs& a) {
-    if (a.tokens <= 16) return launch_few<T, BITS, VW, FF, 1, GATED>(ctx, a);
-    if constexpr (sizeof(T) == 2) { if (a.tokens > 32) return launch_few<T, BITS, VW, FF, 4, GATED>(ctx, a); }
-    return launch_few<T, BITS, VW, FF, 2, GATED>(ctx, a);
+    if (a.tokens <= 4) return launch_few<T, BITS, VW, FF, 4, GATED>(ctx, a);
+    if (a.tokens <= 16) return launch_few<T, BITS, VW, FF, 16, GATED>(ctx, a);
+    if constexpr (sizeof(T) == 2) { if (a.tokens > 32) return launch_few<T, BITS, VW, FF, 64, GATED>(ctx, a); }
+    return launch_few<T, BITS, VW, FF, 32, GATED>(ctx, a);
 }
 // fragments (of 32 channels in all) that a group has at least: as many as a run, or the most of which it has a whole number; 0: none
 int fragments_of_scale(const PackedArgs& a, int most, int least) {
