@@ -16,8 +16,8 @@ struct PackedArgs {
     const void* X; long long ldx;
     const void* Res; long long ldr;
     void* Y; long long ldy;
-    int vec;      // rows of X may be read 16 bytes at a time
-    unsigned piece_magic;      // packed_few_kernel: a group has 2^32 / piece_magic pieces of a run that share their scale (0: one; 1: all)
+    int vec, out_vec;      // rows of X may be read 16 bytes at a time, of Y written four elements at a time
+    unsigned piece_magic, piece_all;      // packed_few_kernel: a group has 2^32 / piece_magic pieces of a run that share their scale (1: all), one where piece_all has all bits
 };
 
 __device__ __forceinline__ float to_f32(float v) { return v; }
@@ -26,6 +26,9 @@ __device__ __forceinline__ float from_f32(float v, float) { return v; }
 __device__ __forceinline__ bf16 from_f32(float v, bf16) { return __float2bfloat16(v); }
 __device__ __forceinline__ f4 mma16(b8 a, b8 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ float silu(float g) { return g / (1.f + expf(-g)); }
+
+// x / d = umulhi(x, m) + (x & all) for x d < 2^32 (a row has fewer than 2^32 / d pieces of d to a group), 0 for d = 0
+inline void magic(unsigned d, unsigned& m, unsigned& all) { m = d < 2 ? 0u : (unsigned)(((1ull << 32) + d - 1) / d); all = d == 1 ? ~0u : 0u; }
 
 template <int N, int I = 0, typename F>
 __device__ __forceinline__ void unroll(F&& f) {
@@ -276,7 +279,7 @@ __global__ __launch_bounds__((64 * most_waves<XR, (GATED ? 2 : 1) * RT>())) void
         }
     };
     int grid0 = -GRIDS;      // first group whose scales are in LDS
-    auto group_of = [&](unsigned piece) { return min((int)(a.piece_magic ? __umulhi(piece, a.piece_magic) : piece), a.n_groups - 1); };
+    auto group_of = [&](unsigned piece) { return min((int)(__umulhi(piece, a.piece_magic) + (piece & a.piece_all)), a.n_groups - 1); };
     struct Grids { float f[2][NR][GRIDS / 4]; };
     auto load_grids = [&](int g, Grids& o) {      // of groups g .. for this lane's row of every 16
         grid0 = max(min(g, a.n_groups - GRIDS), 0);
@@ -467,7 +470,7 @@ int launch_few(tboa_ctx* ctx, PackedArgs a) {
     int waves = 4;
     while (waves < most && waves * 2 < runs && 2 * waves * bytes <= 160 * 1024) waves *= 2;
     const int pieces = a.group / (32 * FF);
-    a.piece_magic = a.n_groups == 1 ? 1 : pieces == 1 ? 0 : (unsigned)(((1ull << 32) + pieces - 1) / pieces);
+    magic(a.n_groups == 1 ? 0 : pieces, a.piece_magic, a.piece_all);
     const auto kernel = packed_few_kernel<T, BITS, VW, FF, XR, RT, GATED>;
     if (waves * bytes > 65536) TB_HIP(ctx, hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, waves * bytes));
     hipLaunchKernelGGL(kernel, dim3((unsigned)cdiv64(a.d_out, 16 * RT), (unsigned)cdiv64(a.tokens, XR)), dim3(64 * waves), std::max(waves * bytes, waves * NR * 16 * 17 * 4), ctx->stream, a);
@@ -492,6 +495,404 @@ int fragments_of_scale(const PackedArgs& a, int most, int least) {
     return 0;
 }
 
+// ------------------------------------------------------------------------------------------------ many tokens
+// Bound by the matrix instructions.  packed_rows_kernel makes X into half (bf16: exactly, fp32: as two terms), every row times a power of two that brings its largest channel to 2^14 .. 2^15, in the blocks of
+// 16 rows x 32 channels that packed_many_kernel copies straight into LDS; and a table of the scales and zeros.  packed_many_kernel makes the codes into half on their way into LDS, once per tile of
+// 256 outputs and TM tokens.
+// One scale per row: codes less zeros, exactly, and the scale multiplies the result.  Groups: scale (code - zero) as half, scales first divided by the power of two of their row's largest.  That is two
+// roundings to 11 bits, 2^-12 each at most, random from weight to weight: about 2e-4 of a result's size, an eighth of what its rounding to bf16 is off by (keeping them exact costs a
+// multiplication of every result by every group's scale, half of the vector instructions' time).  fp32: two half terms of scale (code - zero), three products.
+struct ManyArgs {
+    PackedArgs p;
+    unsigned char* rows;          // X as half: [planes][token blocks of 16][kb][1 KB]
+    float* row_scale;             // [tokens] power of two that takes a row's own back out
+    uint2* table;                 // [matrices][d_out][n_groups]: bf16: .x half scale, half -(1024 + zero); fp32: scale, zero
+    float* out_scale;             // [matrices][d_out]
+    float* partial;               // [splits][tokens][matrices * d_out] where a tile's channels are split over workgroups
+    long long plane;              // bytes
+    int kb, blocks, splits;       // blocks of 32 channels; of 16 tokens
+    int tiles_m, tiles_n, segments, matrices;
+    unsigned unit_magic, unit_all;      // units of 16 channels that a group has, as PackedArgs::piece_magic
+};
+constexpr int KS = 32;      // channels of a stage
+
+// the places of a unit's 16 channels within their two 16-byte pieces: pairs of codes stand 16 (or 24) bits apart in the stream
+template <int BITS>
+constexpr int unit_channel(int i) { return BITS == 8 ? i : BITS == 4 ? i / 8 * 8 + i % 8 / 2 + i % 2 * 4 : i / 8 * 4 + i % 8 / 2 + i % 2 * 8; }
+
+template <typename T, int BITS>
+__global__ __launch_bounds__(1024) void packed_rows_kernel(ManyArgs a) {
+    const PackedArgs& p = a.p;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if ((int)blockIdx.x >= a.blocks) {      // a row of scales per wavefront
+        const long long row = (long long)(blockIdx.x - a.blocks) * 16 + wave;
+        const int which = row >= p.d_out;
+        const int n = (int)(row - (which ? p.d_out : 0));
+        if (row >= (long long)a.matrices * p.d_out) return;
+        const float* const scale = p.scale[which] + (long long)n * p.n_groups, * const zero = p.zero[which] + (long long)n * p.n_groups;
+        float most = 0.f;
+        for (int g = lane; g < p.n_groups; g += 64) { const float v = fabsf(scale[g]); most = v < __builtin_inff() ? fmaxf(most, v) : most; }
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) most = fmaxf(most, __shfl_xor(most, o, 64));
+        // the largest scale is 1 .. 2 times 2^-e
+        const int e = most > 0.f ? max(1 - __builtin_amdgcn_frexp_expf(most), -126) : 0;
+        for (int g = lane; g < p.n_groups; g += 64) {
+            const float s = p.n_groups == 1 ? 1.f : __builtin_amdgcn_ldexpf(scale[g], e), z = zero[g];
+            uint2 v;
+            if (sizeof(T) == 2) v = make_uint2((unsigned)__builtin_bit_cast(unsigned short, (_Float16)s) | (unsigned)__builtin_bit_cast(unsigned short, (_Float16)(-1024.f - z)) << 16, 0u);
+            else v = make_uint2(__float_as_uint(s), __float_as_uint(z));
+            a.table[row * p.n_groups + g] = v;
+        }
+        if (lane == 0) a.out_scale[row] = p.n_groups == 1 ? scale[0] : __builtin_amdgcn_ldexpf(1.f, -e);
+        return;
+    }
+    __shared__ int exps[16];
+    const long long m0 = (long long)blockIdx.x * 16;
+    {      // a row per wavefront
+        const T* const x = (const T*)p.X + min(m0 + wave, p.tokens - 1) * p.ldx;
+        float most = 0.f;
+        auto take = [&](float v) { v = fabsf(v); most = v < __builtin_inff() ? fmaxf(most, v) : most; };
+        if (p.vec) {
+            constexpr int E = 16 / (int)sizeof(T);
+            const int whole = p.d_in / E * E;
+            for (int k = lane * E; k < whole; k += 64 * E) {
+                union { u4 u; T e[E]; } v;
+                v.u = *(const u4*)(x + k);
+#pragma unroll
+                for (int j = 0; j < E; ++j) take(to_f32(v.e[j]));
+            }
+            for (int k = whole + lane; k < p.d_in; k += 64) take(to_f32(x[k]));
+        } else for (int k = lane; k < p.d_in; k += 64) take(to_f32(x[k]));
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) most = fmaxf(most, __shfl_xor(most, o, 64));
+        const int e = most > 0.f ? min(15 - __builtin_amdgcn_frexp_expf(most), 120) : 0;
+        if (lane == 0) { exps[wave] = e; if (m0 + wave < p.tokens) a.row_scale[m0 + wave] = __builtin_amdgcn_ldexpf(1.f, -e); }
+    }
+    __syncthreads();
+    const int row = threadIdx.x >> 1 & 15, half = threadIdx.x & 1, e = exps[row];      // a unit of 16 channels each: 32 lanes have a block
+    const T* const x = (const T*)p.X + min(m0 + row, p.tokens - 1) * p.ldx;
+    for (int kb = threadIdx.x >> 5; kb < a.kb; kb += 32) {
+        const int k = kb * KS + half * 16;
+        union { u4 u[sizeof(T)]; T e[16]; } in;
+        if (p.vec && k + 16 <= p.d_in) {
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T); ++i) in.u[i] = ((const u4*)(x + k))[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T); ++i) in.u[i] = u4{0, 0, 0, 0};
+#pragma unroll
+            for (int j = 0; j < 16; ++j) if (k + j < p.d_in) in.e[j] = x[k + j];
+        }
+        union { _Float16 e[16]; u4 u[2]; } hi, lo;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float v = __builtin_amdgcn_ldexpf(to_f32(in.e[unit_channel<BITS>(i)]), e);
+            hi.e[i] = (_Float16)v;
+            if constexpr (sizeof(T) == 4) lo.e[i] = (_Float16)(isfinite(v) ? v - (float)hi.e[i] : 0.f);
+        }
+        unsigned char* const out = a.rows + ((long long)blockIdx.x * a.kb + kb) * 1024 + row * 64;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int at = ((2 * half + i) ^ (row >> 2)) * 16;
+            *(u4*)(out + at) = hi.u[i];
+            if constexpr (sizeof(T) == 4) *(u4*)(out + a.plane + at) = lo.u[i];
+        }
+    }
+}
+
+// 16 codes of a row as they come from memory
+template <int BITS> struct Unit { unsigned w[BITS == 8 ? 4 : BITS == 2 ? 1 : 2]; };
+// codes as half 1024 + code, in pairs, two pieces of 16 bytes
+template <int BITS>
+__device__ __forceinline__ void unit_halves(const Unit<BITS>& in, int half, unsigned (&out)[8]) {
+    constexpr unsigned ONE = 0x64006400u;
+    if constexpr (BITS == 8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) out[i] = __builtin_amdgcn_perm(0x64646464u, in.w[i / 2], i % 2 ? 0x04030402u : 0x04010400u);
+    } else if constexpr (BITS == 4) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) out[i] = (in.w[i / 4] >> (i % 4 * 4) & 0x000f000fu) | ONE;
+    } else if constexpr (BITS == 2) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) out[i] = (in.w[0] >> (2 * i) & 0x00030003u) | ONE;
+    } else {
+        const unsigned long long v = (in.w[0] | (unsigned long long)in.w[1] << 32) >> (16 * half);      // 48 bits from here on
+        const unsigned a = (unsigned)v, b = (unsigned)(v >> 24);
+        const unsigned p = low_halves(a, b), q = low_halves(a >> 15, b >> 15);      // codes 0 .. 4 and 5 .. 7 of either eight
+#pragma unroll
+        for (int i = 0; i < 8; ++i) out[i] = ((i < 5 ? p >> (3 * i) : q >> (3 * i - 15)) & 0x00070007u) | ONE;
+    }
+}
+
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef float f16v __attribute__((ext_vector_type(16)));
+
+// A tile of TM tokens and 256 rows of codes (GATED: 128 of either matrix, 32 of one beside 32 of the other, so that a wavefront has both factors of its results); eight wavefronts, each TM / 2 tokens and 64 rows.
+// A ring of NS stages of 32 channels in LDS: X is copied there, NS - 1 stages ahead; codes are loaded two stages before that, made into half and written by all wavefronts, 16 codes a lane and stage.
+template <typename T, int BITS, int TM, bool GATED>
+__global__ __launch_bounds__(512) void packed_many_kernel(ManyArgs a) {
+    constexpr int NS = 4, TI = TM / 64, TJ = 2, LPW = TM / 128, A_BYTES = TM * 64, STAGE = A_BYTES + 256 * 64;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char ring[];
+    const PackedArgs& p = a.p;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, lh = lane >> 5;
+    // tiles of one band of outputs after each other, an XCD (every eighth workgroup) its own run of them
+    int tm, tn, split;
+    {
+        const int total = a.tiles_m * a.tiles_n * a.splits, per = (total + 7) / 8, w = blockIdx.x;
+        const int item = (w & 7) * per + (w >> 3);
+        if (w >> 3 >= per || item >= total) return;
+        split = item % a.splits;
+        const int t = item / a.splits, band = 4 * a.tiles_m, in = t % band, wide = min(4, a.tiles_n - t / band * 4);
+        tn = t / band * 4 + in % wide; tm = in / wide;
+    }
+    const long long m0 = (long long)tm * TM;
+    const int n0 = tn * (GATED ? 128 : 256);
+    const int stages = a.kb * a.segments, kt0 = (int)((long long)stages * split / a.splits), kt1 = (int)((long long)stages * (split + 1) / a.splits), nk = kt1 - kt0;
+
+    // this thread's row of codes, its half of a stage
+    const int r = threadIdx.x >> 1, half = threadIdx.x & 1;
+    const int which = GATED ? wave & 1 : 0, row_n = min(GATED ? n0 + 32 * (r >> 6) + (r & 31) : n0 + r, p.d_out - 1);
+    const auto codes = __builtin_amdgcn_make_buffer_rsrc((void*)(p.w[which] + (long long)n0 * p.words), 0, (int)(unsigned)min((long long)(p.d_out - n0) * p.words * 4, 0xfffffffcLL), 0x00020000);
+    const unsigned at_codes = (unsigned)(row_n - n0) * p.words * 4;
+    const uint2* const table = a.table + ((long long)which * p.d_out + row_n) * p.n_groups;
+    struct Load { Unit<BITS> u[NS]; uint2 g[NS]; };
+    int l_ks = kt0 % a.kb;      // of the next codes to be loaded
+    auto load = [&](Load& o, auto N) {      // of the next N stages: 2 N loads
+#pragma unroll
+        for (int i = 0; i < decltype(N)::value; ++i) {
+            const unsigned at = at_codes + (BITS == 3 ? 3 * l_ks + half : (l_ks * 2 + half) * (BITS / 2)) * 4;
+            Unit<BITS>& u = o.u[i];
+            if constexpr (BITS == 8) { const u4 v = __builtin_amdgcn_raw_buffer_load_b128(codes, at, 0, 0); u.w[0] = v[0]; u.w[1] = v[1]; u.w[2] = v[2]; u.w[3] = v[3]; }
+            else if constexpr (BITS == 2) u.w[0] = __builtin_amdgcn_raw_buffer_load_b32(codes, at, 0, 0);
+            else { const auto v = __builtin_amdgcn_raw_buffer_load_b64(codes, at, 0, 0); u.w[0] = v[0]; u.w[1] = v[1]; }
+            const unsigned unit = l_ks * 2 + half;
+            o.g[i] = table[min((int)(__umulhi(unit, a.unit_magic) + (unit & a.unit_all)), p.n_groups - 1)];
+            if (++l_ks == a.kb) l_ks = 0;
+        }
+    };
+    int b_seg = kt0 / a.kb, b_ks = kt0 - b_seg * a.kb;      // of the next codes to be written
+    unsigned char* const b_at = ring + A_BYTES + r * 64;
+    auto write = [&](const Unit<BITS>& u, uint2 g, int slot) {
+        unsigned v[8];
+        unit_halves<BITS>(u, half, v);
+        if constexpr (sizeof(T) == 2) {
+            const h2 both = __builtin_bit_cast(h2, g.x), s = {both[0], both[0]}, z = {both[1], both[1]};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = __builtin_bit_cast(unsigned, (__builtin_bit_cast(h2, v[i]) + z) * s);
+        } else {
+            const float s = __uint_as_float(g.x), z = -1024.f - __uint_as_float(g.y);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const h2 c = __builtin_bit_cast(h2, v[i]);
+                h2 w;
+#pragma unroll
+                for (int j = 0; j < 2; ++j) { const float f = ((float)c[j] + z) * s; w[j] = (_Float16)f; if (b_seg == 2) w[j] = (_Float16)(f - (float)w[j]); }
+                v[i] = __builtin_bit_cast(unsigned, w);
+            }
+        }
+        unsigned char* const to = b_at + slot * STAGE;
+        *(u4*)(to + (((2 * half) ^ (r >> 2 & 3)) << 4)) = u4{v[0], v[1], v[2], v[3]};
+        *(u4*)(to + (((2 * half + 1) ^ (r >> 2 & 3)) << 4)) = u4{v[4], v[5], v[6], v[7]};
+        if (++b_ks == a.kb) { b_ks = 0; ++b_seg; }
+    };
+    const unsigned ring_at = (unsigned)(unsigned long long)((__attribute__((address_space(3))) void*)ring);
+    long long block[LPW];
+#pragma unroll
+    for (int i = 0; i < LPW; ++i) block[i] = min(m0 / 16 + wave * LPW + i, (long long)a.blocks - 1) * a.kb * 1024;
+    int a_seg = kt0 / a.kb, a_ks = kt0 - a_seg * a.kb;      // of the next rows to be copied
+    auto copy = [&](int slot) {
+#pragma unroll
+        for (int i = 0; i < LPW; ++i)
+            lds_direct_16(lane * 16, (const char*)a.rows + (a_seg == 1 && a.segments > 1 ? a.plane : 0) + block[i] + (long long)a_ks * 1024, ring_at + slot * STAGE + (wave * LPW + i) * 1024);
+        if (++a_ks == a.kb) { a_ks = 0; ++a_seg; }
+    };
+    const int wm = wave / 4 * (TM / 2), wn = wave % 4 * 64;
+    auto x_piece = [&](int slot, int i, int ks) { const int row = wm + 32 * i + l32; return *(const h8*)(ring + slot * STAGE + row * 64 + (((2 * ks + lh) ^ (row >> 2 & 3)) << 4)); };
+    auto w_piece = [&](int slot, int j, int ks) { const int row = wn + 32 * j + l32; return *(const h8*)(ring + slot * STAGE + A_BYTES + row * 64 + (((2 * ks + lh) ^ (row >> 2 & 3)) << 4)); };
+    f16v acc[TI][TJ];
+#pragma unroll
+    for (int i = 0; i < TI; ++i)
+#pragma unroll
+        for (int j = 0; j < TJ; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+    h8 fx[2][TI], fw[2][TJ];
+    auto read = [&](int set, int slot, int ks) {
+#pragma unroll
+        for (int i = 0; i < TI; ++i) fx[set][i] = x_piece(slot, i, ks);
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) fw[set][j] = w_piece(slot, j, ks);
+    };
+    auto multiply = [&](int set) {
+#pragma unroll
+        for (int i = 0; i < TI; ++i)
+#pragma unroll
+            for (int j = 0; j < TJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fx[set][i], fw[set][j], acc[i][j], 0, 0, 0);
+    };
+    // As stage kt begins, stages kt .. kt + NS - 2 are in LDS or on their way there; `here` has the codes of the NS stages after those as kt is a multiple of NS
+    Load here, next;
+    load(here, std::integral_constant<int, NS - 1>());
+#pragma unroll
+    for (int s = 0; s < NS - 1; ++s) { copy(s); write(here.u[s], here.g[s], s); }
+    load(here, std::integral_constant<int, NS>());
+    wait_loads_but<0>();
+    __syncthreads();
+    read(0, 0, 0);
+    for (int kt = 0; kt < nk; kt += NS) {
+        unroll<NS>([&](auto S) {
+            constexpr int s = S, last = s == 0 ? NS - 1 : s - 1, after = s == NS - 1 ? 0 : s + 1;
+            if (kt + s >= nk) return;
+            read(1, s, 1);
+            if constexpr (s == 0) load(next, std::integral_constant<int, NS>());
+            copy(last);      // (the stage before this one has been read by everyone)
+            multiply(0);
+            write(here.u[s], here.g[s], last);
+            // what the next stage has was copied two stages ago: two stages' copies may still be on their way, and the loads beside them (older ones are awaited with them)
+            if constexpr (s < 2) wait_loads_but<2 * LPW + 2 * NS>(); else wait_loads_but<2 * LPW>();
+            __syncthreads();
+            read(0, after, 0);
+            multiply(1);
+        });
+        here = next;
+    }
+    // results through LDS, 32 tokens of a wavefront at a time: rows of 64 outputs
+    wait_loads_but<0>();
+    __syncthreads();
+    constexpr int WIDE = GATED ? 32 : 64, PITCH = WIDE + 4;
+    float* const mine = (float*)(ring + wave * 32 * 68 * 4);
+    const int c0 = GATED ? n0 + wn / 2 : n0 + wn;      // first output of the wavefront
+    const float* const os = a.out_scale;
+    const bool parts = a.splits > 1;
+#pragma unroll
+    for (int i = 0; i < TI; ++i) {
+        auto in_order = [] { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); __builtin_amdgcn_wave_barrier(); };
+        const int sides = GATED && parts ? 2 : 1;
+        for (int side = 0; side < sides; ++side) {      // (partial sums of a gated product: both factors, one after the other)
+            in_order();
+#pragma unroll
+            for (int j = 0; j < (GATED ? 1 : TJ); ++j)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    const int row = 8 * (v / 4) + 4 * lh + v % 4;
+                    float y = acc[i][j][v];
+                    if constexpr (GATED) {
+                        if (parts) y = side ? acc[i][1][v] : y;
+                        else {
+                            const long long m = min(m0 + wm + 32 * i + row, p.tokens - 1);
+                            const int n = min(c0 + l32, p.d_out - 1);
+                            const float rs = a.row_scale[m];
+                            y = silu(y * rs * os[n]) * (acc[i][1][v] * rs * os[p.d_out + n]);
+                        }
+                    }
+                    mine[row * PITCH + 32 * j + l32] = y;
+                }
+            in_order();
+            constexpr int LANES = WIDE / 4;      // that a row takes
+#pragma unroll
+            for (int q = 0; q < 32 * LANES / 64; ++q) {
+                const int row = q * (64 / LANES) + lane / LANES, c = lane % LANES * 4, n = c0 + c;
+                const long long m = m0 + wm + 32 * i + row;
+                if (m >= p.tokens || n >= p.d_out) continue;
+                f4 v = *(const f4*)(mine + row * PITCH + c);
+                if (parts) {
+                    float* const to = a.partial + ((long long)split * p.tokens + m) * ((GATED ? 2 : 1) * (long long)p.d_out) + side * (long long)p.d_out + n;
+                    if (n + 4 <= p.d_out && p.d_out % 4 == 0) *(f4*)to = v;
+                    else for (int k = 0; k < 4; ++k) if (n + k < p.d_out) to[k] = v[k];
+                    continue;
+                }
+                const float rs = GATED ? 1.f : a.row_scale[m];
+                T* const y = (T*)p.Y + m * p.ldy + n;
+                const T* const res = !GATED && p.Res ? (const T*)p.Res + m * p.ldr + n : nullptr;
+                union { T e[4]; } o;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (n + k >= p.d_out) break;
+                    float f = GATED ? v[k] : v[k] * rs * os[n + k];
+                    if (res) f += to_f32(res[k]);
+                    o.e[k] = from_f32(f, T());
+                }
+                struct __attribute__((aligned(4 * sizeof(T)))) Four { T e[4]; };
+                if (n + 4 <= p.d_out && p.out_vec) *(Four*)y = *(Four*)o.e;
+                else for (int k = 0; k < 4; ++k) if (n + k < p.d_out) y[k] = o.e[k];
+            }
+        }
+    }
+}
+
+// sums of the splits' partial results, scaled; one output per thread
+template <typename T, bool GATED>
+__global__ __launch_bounds__(256) void packed_join_kernel(ManyArgs a) {
+    const PackedArgs& p = a.p;
+    const long long wide = (GATED ? 2LL : 1LL) * p.d_out, all = p.tokens * p.d_out;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < all; i += (long long)gridDim.x * 256) {
+        const long long m = i / p.d_out;
+        const int n = (int)(i - m * p.d_out);
+        float y[2] = {0.f, 0.f};
+        const float* from = a.partial + m * wide + n;
+        for (int s = 0; s < a.splits; ++s, from += p.tokens * wide) { y[0] += from[0]; if (GATED) y[1] += from[p.d_out]; }
+        const float rs = a.row_scale[m];
+        float v = y[0] * rs * a.out_scale[n];
+        if (GATED) v = silu(v) * (y[1] * rs * a.out_scale[p.d_out + n]);
+        else if (p.Res) v += to_f32(((const T*)p.Res)[m * p.ldr + n]);
+        ((T*)p.Y)[m * p.ldy + n] = from_f32(v, T());
+    }
+}
+
+constexpr long long MOST_ROWS = 8192;      // tokens of one round: more are worked off round by round, in the same workspace
+// what a call of so many tokens is cut into, and the workspace for it
+size_t many_room(const PackedArgs& p, bool gated, int size, long long tokens, ManyArgs& a, void* ws) {
+    const int tm = tokens <= 128 ? 128 : 256;
+    a.kb = (int)cdiv64(p.d_in, KS); a.blocks = (int)cdiv64(tokens, 16);
+    a.segments = size == 2 ? 1 : p.n_groups == 1 ? 2 : 3;
+    a.tiles_m = (int)cdiv64(tokens, tm); a.tiles_n = (int)cdiv64(p.d_out, gated ? 128 : 256);
+    const long long tiles = (long long)a.tiles_m * a.tiles_n;
+    a.splits = (int)std::max<long long>(1, std::min<long long>(tiles >= 192 ? 1 : 256 / tiles, (long long)a.kb * a.segments / 16));
+    a.plane = (long long)a.blocks * a.kb * 1024;
+    const int matrices = a.matrices = gated ? 2 : 1;
+    Arena ar(ws);
+    a.rows = ar.get<unsigned char>((size_t)a.plane * (size == 2 ? 1 : 2));
+    a.row_scale = ar.get<float>((size_t)tokens);
+    a.table = ar.get<uint2>((size_t)matrices * p.d_out * p.n_groups);
+    a.out_scale = ar.get<float>((size_t)matrices * p.d_out);
+    a.partial = ar.get<float>(a.splits > 1 ? (size_t)a.splits * tokens * matrices * p.d_out : 0);
+    return ar.off;
+}
+bool many_takes(const PackedArgs& p) { return (p.n_groups == 1 || p.group % 16 == 0) && p.words <= 1 << 21; }
+
+template <typename T, int BITS, int TM, bool GATED>
+int launch_many(tboa_ctx* ctx, const ManyArgs& a) {
+    constexpr int LDS = 4 * (TM + 256) * 64;
+    const auto kernel = packed_many_kernel<T, BITS, TM, GATED>;
+    TB_HIP(ctx, hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(cdiv64((long long)a.tiles_m * a.tiles_n * a.splits, 8) * 8)), dim3(512), LDS, ctx->stream, a);
+    TB_KERNEL_CHECK(ctx);
+    return 0;
+}
+template <typename T, int BITS, bool GATED>
+int launch_many(tboa_ctx* ctx, const PackedArgs& p) {
+    ManyArgs a{};
+    TB_TRY(tboa_ws_reserve(ctx, many_room(p, GATED, sizeof(T), std::min(p.tokens, MOST_ROWS), a, nullptr)));
+    for (long long at = 0; at < p.tokens; at += MOST_ROWS) {
+        a.p = p;
+        a.p.tokens = std::min(p.tokens - at, MOST_ROWS);
+        a.p.X = (const T*)p.X + at * p.ldx; a.p.Y = (T*)p.Y + at * p.ldy;
+        if (p.Res) a.p.Res = (const T*)p.Res + at * p.ldr;
+        many_room(p, GATED, sizeof(T), a.p.tokens, a, ctx->ws);
+        const int units = p.group / 16;
+        magic(p.n_groups == 1 ? 0 : units, a.unit_magic, a.unit_all);
+        hipLaunchKernelGGL((packed_rows_kernel<T, BITS>), dim3((unsigned)(a.blocks + cdiv64((GATED ? 2LL : 1LL) * p.d_out, 16))), dim3(1024), 0, ctx->stream, a);
+        TB_KERNEL_CHECK(ctx);
+        if (a.p.tokens <= 128) TB_TRY((launch_many<T, BITS, 128, GATED>(ctx, a)));
+        else TB_TRY((launch_many<T, BITS, 256, GATED>(ctx, a)));
+        if (a.splits > 1) {
+            hipLaunchKernelGGL((packed_join_kernel<T, GATED>), dim3((unsigned)std::min<long long>(cdiv64(a.p.tokens * p.d_out, 256), 1 << 16)), dim3(256), 0, ctx->stream, a);
+            TB_KERNEL_CHECK(ctx);
+        }
+    }
+    return 0;
+}
+
 template <typename T, int BITS, int GROUPS, bool GATED>
 int launch_any(tboa_ctx* ctx, const PackedArgs& a) {
     const auto go = [&](auto MT) {
@@ -506,6 +907,7 @@ int launch_any(tboa_ctx* ctx, const PackedArgs& a) {
 }
 template <typename T, int BITS, bool GATED>
 int launch(tboa_ctx* ctx, const PackedArgs& a) {
+    if (a.tokens > 64 && many_takes(a)) return launch_many<T, BITS, GATED>(ctx, a);
     if (cdiv64(a.tokens, 16) <= 65535) {
         if constexpr (BITS == 2) {
             const int ff = fragments_of_scale(a, 8, 2);
@@ -538,6 +940,13 @@ bool good_weight(const tboa_packed_weight* w) {
            (w->group == 0 || w->d_in % w->group == 0);
 }
 
+PackedArgs shape_of(const tboa_packed_weight& w) {
+    PackedArgs a{};
+    a.d_out = w.d_out; a.d_in = w.d_in; a.words = (int)tboa_packed_words_per_row(w.d_in, w.bits);
+    a.group = w.group ? w.group : w.d_in; a.n_groups = w.d_in / a.group;
+    return a;
+}
+
 // what both calls check; up: the second matrix or NULL
 int run(tboa_ctx* ctx, const char* who, const tboa_packed_weight* weight, const tboa_packed_weight* up, int64_t n_tokens, int dtype, const void* X, int64_t ldx, const void* Res, int64_t ldr, void* Y,
         int64_t ldy) {
@@ -550,13 +959,12 @@ int run(tboa_ctx* ctx, const char* who, const tboa_packed_weight* weight, const 
     const int size = dtype == TBOA_F32 ? 4 : 2;
     if ((uintptr_t)X % size || (uintptr_t)Y % size || (uintptr_t)Res % size) return tboa_fail(ctx, TBOA_EINVAL, "%s: an address that is no multiple of its elements' size", who);
     const TbDevice dev(ctx->device);
-    PackedArgs a{};
+    PackedArgs a = shape_of(*weight);
     const tboa_packed_weight* both[2] = {weight, up ? up : weight};
     for (int i = 0; i < 2; ++i) { a.w[i] = both[i]->packed; a.scale[i] = both[i]->scales; a.zero[i] = both[i]->zeros; }
-    a.d_out = weight->d_out; a.d_in = weight->d_in; a.words = (int)tboa_packed_words_per_row(weight->d_in, weight->bits);
-    a.group = weight->group ? weight->group : weight->d_in; a.n_groups = weight->d_in / a.group;
     a.tokens = n_tokens; a.X = X; a.ldx = ldx; a.Res = Res; a.ldr = ldr; a.Y = Y; a.ldy = ldy;
     a.vec = (uintptr_t)X % 16 == 0 && ldx * size % 16 == 0 && ldx < 1 << 24;      // (the rows of a workgroup within 32 bits)
+    a.out_vec = (uintptr_t)Y % (4 * size) == 0 && ldy % 4 == 0;
     if (dtype == TBOA_F32) return up ? launch<float, true>(ctx, weight->bits, a) : launch<float, false>(ctx, weight->bits, a);
     return up ? launch<bf16, true>(ctx, weight->bits, a) : launch<bf16, false>(ctx, weight->bits, a);
 }
@@ -564,7 +972,12 @@ int run(tboa_ctx* ctx, const char* who, const tboa_packed_weight* weight, const 
 }  // namespace
 
 extern "C" size_t tboa_packed_workspace_bytes(const tboa_packed_weight* weight, int64_t n_tokens, int dtype) {
-    return 0;
+    if (!good_weight(weight) || (dtype != TBOA_F32 && dtype != TBOA_BF16) || n_tokens <= 64 || n_tokens > 1 << 24) return 0;
+    const PackedArgs p = shape_of(*weight);
+    if (!many_takes(p)) return 0;
+    ManyArgs a{};
+    return std::max(many_room(p, false, dtype == TBOA_F32 ? 4 : 2, std::min<long long>(n_tokens, MOST_ROWS), a, nullptr),
+                    many_room(p, true, dtype == TBOA_F32 ? 4 : 2, std::min<long long>(n_tokens, MOST_ROWS), a, nullptr));
 }
 
 extern "C" int tboa_packed_linear(tboa_ctx* ctx, const tboa_packed_weight* weight, int64_t n_tokens, int dtype, const void* X, int64_t ldx, const void* Res, int64_t ldr, void* Y, int64_t ldy) {

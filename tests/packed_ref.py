@@ -20,13 +20,17 @@ def bound(x, w, packed):
     """Of X W^T before its last rounding, per element.  With S = sum |x| |w| and R = sum |x| scale 2^(bits + 2):
       sums       a result is rounded at most d_in / 16 + 16 times (a matrix instruction adds 16 terms or more), each time by 2^-24 of what codes less zeros add up to, S at most.  Where codes enter
                  with an offset of up to 2^bits (bf16 X), its share is taken out again every 256 channels or fewer: 20 times 2^-24 of R more (codes, offset and zero are below 2^bits each)
-      operands   weights scale (code - zero) in fp32 2^-23 of S; fp32 X in two half terms 2^-22 of S, the smallest channels to 2^-39 of the row's largest"""
+      operands   weights scale (code - zero) in fp32 2^-23 of S; fp32 X in two half terms 2^-22 of S, the smallest channels to 2^-39 of the row's largest.  bf16 X of more
+                 than 64 tokens and several scales a row: scale (code - zero) as half, the product of a scale as half and a whole number up to 255, exact as half: (1 + 2^-11)^2 - 1 < 2^-10 + 2^-22 of
+                 S; scales down to 2^-13 of their row's largest (which is 1 .. 2) are normal halves, smaller ones off by 2^-25 at most, times 255"""
     d = packed.desc
     ng = packed.scales.numel() // d.d_out
     step = packed.scales.double().abs().view(d.d_out, ng).repeat_interleave(d.d_in // ng, 1)
     size = x.double().abs()
     s = size @ w.abs().T
     lim = (d.d_in / 16 + 16) * 2.0 ** -24 * s + 2.0 ** -21 * s + 2.0 ** -38 * size.amax(1, keepdim=True) * w.abs().sum(1)[None]
+    if x.dtype == torch.bfloat16 and len(x) > 64 and ng > 1:
+        lim = lim + (2.0 ** -10 + 2.0 ** -22) * s + 255 * 2.0 ** -24 * size.sum(1, keepdim=True) * (step.amax(1) * (step.amin(1) < 2.0 ** -13 * step.amax(1)))[None]
     return lim + 20 * 2.0 ** -24 * 2.0 ** (d.bits + 2) * (size @ step.T) if x.dtype == torch.bfloat16 else lim
 
 
