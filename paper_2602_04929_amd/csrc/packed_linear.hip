@@ -516,9 +516,9 @@ struct ManyArgs {
 };
 constexpr int KS = 32;      // channels of a stage
 
-// the places of a unit's 16 channels within their two 16-byte pieces: pairs of codes stand 16 (or 24) bits apart in the stream
+// the channels of a piece (8 of them, 16 bytes as half) in the order in which its codes are taken out of their word
 template <int BITS>
-constexpr int unit_channel(int i) { return BITS == 8 ? i : BITS == 4 ? i / 8 * 8 + i % 8 / 2 + i % 2 * 4 : i / 8 * 4 + i % 8 / 2 + i % 2 * 8; }
+constexpr int piece_channel(int i) { return BITS == 8 ? i : BITS == 4 ? i / 2 + i % 2 * 4 : BITS == 2 ? (i / 2) + i % 2 * 4 : i / 2 + i % 2 * 4; }
 
 template <typename T, int BITS>
 __global__ __launch_bounds__(1024) void packed_rows_kernel(ManyArgs a) {
@@ -586,7 +586,7 @@ __global__ __launch_bounds__(1024) void packed_rows_kernel(ManyArgs a) {
         union { _Float16 e[16]; u4 u[2]; } hi, lo;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            const float v = __builtin_amdgcn_ldexpf(to_f32(in.e[unit_channel<BITS>(i)]), e);
+            const float v = __builtin_amdgcn_ldexpf(to_f32(in.e[i / 8 * 8 + piece_channel<BITS>(i % 8)]), e);
             hi.e[i] = (_Float16)v;
             if constexpr (sizeof(T) == 4) lo.e[i] = (_Float16)(isfinite(v) ? v - (float)hi.e[i] : 0.f);
         }
@@ -600,27 +600,36 @@ __global__ __launch_bounds__(1024) void packed_rows_kernel(ManyArgs a) {
     }
 }
 
-// 16 codes of a row as they come from memory
-template <int BITS> struct Unit { unsigned w[BITS == 8 ? 4 : BITS == 2 ? 1 : 2]; };
-// codes as half 1024 + code, in pairs, two pieces of 16 bytes
-template <int BITS>
-__device__ __forceinline__ void unit_halves(const Unit<BITS>& in, int half, unsigned (&out)[8]) {
-    constexpr unsigned ONE = 0x64006400u;
+// Codes of 128 channels of a row, as the four lanes of a quad load them: lane q has the 32 channels of stage q (8 bits: 16 channels of stages 0 and 1, 16 of stages 2 and 3)
+template <int BITS> struct Codes128 { unsigned w[BITS == 8 ? 8 : BITS]; };
+template <int P>
+__device__ __forceinline__ unsigned quad(unsigned v) { return (unsigned)__builtin_amdgcn_mov_dpp((int)v, P, 0xf, 0xf, true); }
+// the 8 codes of stage S that are lane j's of its quad, as half 1024 + code in pairs
+template <int BITS, int S>
+__device__ __forceinline__ void piece_halves(const Codes128<BITS>& in, int j, unsigned (&out)[4]) {
+    constexpr unsigned ONE = 0x64006400u, OF = S * 0x55;      // quad_perm S S S S
     if constexpr (BITS == 8) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) out[i] = __builtin_amdgcn_perm(0x64646464u, in.w[i / 2], i % 2 ? 0x04030402u : 0x04010400u);
+        constexpr int a = S % 2 * 2, P = a | a << 2 | (a + 1) << 4 | (a + 1) << 6, at = S / 2 * 4;
+        const unsigned q0 = quad<P>(in.w[at]), q1 = quad<P>(in.w[at + 1]), q2 = quad<P>(in.w[at + 2]), q3 = quad<P>(in.w[at + 3]);      // (of all lanes: not under a condition)
+        const unsigned w0 = j & 1 ? q2 : q0, w1 = j & 1 ? q3 : q1;
+        out[0] = __builtin_amdgcn_perm(0x64646464u, w0, 0x04010400u); out[1] = __builtin_amdgcn_perm(0x64646464u, w0, 0x04030402u);
+        out[2] = __builtin_amdgcn_perm(0x64646464u, w1, 0x04010400u); out[3] = __builtin_amdgcn_perm(0x64646464u, w1, 0x04030402u);
     } else if constexpr (BITS == 4) {
+        const unsigned q0 = quad<OF>(in.w[0]), q1 = quad<OF>(in.w[1]), q2 = quad<OF>(in.w[2]), q3 = quad<OF>(in.w[3]), a = j & 1 ? q1 : q0, b = j & 1 ? q3 : q2, w = j & 2 ? b : a;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) out[i] = (in.w[i / 4] >> (i % 4 * 4) & 0x000f000fu) | ONE;
+        for (int i = 0; i < 4; ++i) out[i] = (w >> (4 * i) & 0x000f000fu) | ONE;
     } else if constexpr (BITS == 2) {
+        const unsigned q0 = quad<OF>(in.w[0]), q1 = quad<OF>(in.w[1]), w = (j & 2 ? q1 : q0) >> (16 * (j & 1));      // 8 codes in 16 bits: 0 .. 3 below, 4 .. 7 brought above
+        const unsigned v = (w & 0xffu) | (w & 0xff00u) << 8;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) out[i] = (in.w[0] >> (2 * i) & 0x00030003u) | ONE;
+        for (int i = 0; i < 4; ++i) out[i] = (v >> (2 * i) & 0x00030003u) | ONE;
     } else {
-        const unsigned long long v = (in.w[0] | (unsigned long long)in.w[1] << 32) >> (16 * half);      // 48 bits from here on
-        const unsigned a = (unsigned)v, b = (unsigned)(v >> 24);
-        const unsigned p = low_halves(a, b), q = low_halves(a >> 15, b >> 15);      // codes 0 .. 4 and 5 .. 7 of either eight
+        const unsigned w0 = quad<OF>(in.w[0]), w1 = quad<OF>(in.w[1]), w2 = quad<OF>(in.w[2]);
+        const unsigned lo = j & 2 ? (j & 1 ? w2 : w1) : w0, hi = j & 2 ? w2 : w1;
+        const unsigned w = __builtin_amdgcn_alignbit(hi, lo, j == 0 ? 0 : j == 1 ? 24 : j == 2 ? 16 : 8);      // 24 bits from 24 j on
+        const unsigned v = (w & 0xfffu) | (w & 0xfff000u) << 4;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) out[i] = ((i < 5 ? p >> (3 * i) : q >> (3 * i - 15)) & 0x00070007u) | ONE;
+        for (int i = 0; i < 4; ++i) out[i] = (v >> (3 * i) & 0x00070007u) | ONE;
     }
 }
 
@@ -630,7 +639,7 @@ typedef float f16v __attribute__((ext_vector_type(16)));
 
 // A tile of TM tokens and 256 rows of codes (GATED: 128 of either matrix, 32 of one beside 32 of the other, so that a wavefront has both factors of its results); eight wavefronts, each TM / 2 tokens and 64 rows.
 // A ring of NS stages of 32 channels in LDS: X is copied there, NS - 1 stages ahead; codes are loaded two stages before that, made into half and written by all wavefronts, 16 codes a lane and stage.
-template <typename T, int BITS, int TM, bool GATED>
+template <typename T, int BITS, bool ONE_SCALE, int TM, bool GATED>      // ONE_SCALE: whole groups of 128 channels
 __global__ __launch_bounds__(512) void packed_many_kernel(ManyArgs a) {
     constexpr int NS = 4, TI = TM / 64, TJ = 2, LPW = TM / 128, A_BYTES = TM * 64, STAGE = A_BYTES + 256 * 64;
     extern __shared__ __attribute__((aligned(1024))) unsigned char ring[];
@@ -648,54 +657,71 @@ __global__ __launch_bounds__(512) void packed_many_kernel(ManyArgs a) {
     }
     const long long m0 = (long long)tm * TM;
     const int n0 = tn * (GATED ? 128 : 256);
-    const int stages = a.kb * a.segments, kt0 = (int)((long long)stages * split / a.splits), kt1 = (int)((long long)stages * (split + 1) / a.splits), nk = kt1 - kt0;
+    const int turns = a.kb / NS * a.segments, kt0 = (int)((long long)turns * split / a.splits) * NS, nk = (int)((long long)turns * (split + 1) / a.splits) * NS - kt0;      // (whole turns of the ring)
 
-    // this thread's row of codes, its half of a stage
-    const int r = threadIdx.x >> 1, half = threadIdx.x & 1;
-    const int which = GATED ? wave & 1 : 0, row_n = min(GATED ? n0 + 32 * (r >> 6) + (r & 31) : n0 + r, p.d_out - 1);
-    const auto codes = __builtin_amdgcn_make_buffer_rsrc((void*)(p.w[which] + (long long)n0 * p.words), 0, (int)(unsigned)min((long long)(p.d_out - n0) * p.words * 4, 0xfffffffcLL), 0x00020000);
-    const unsigned at_codes = (unsigned)(row_n - n0) * p.words * 4;
-    const uint2* const table = a.table + ((long long)which * p.d_out + row_n) * p.n_groups;
-    struct Load { Unit<BITS> u[NS]; uint2 g[NS]; };
-    int l_ks = kt0 % a.kb;      // of the next codes to be loaded
-    auto load = [&](Load& o, auto N) {      // of the next N stages: 2 N loads
+    // This thread's two rows of codes, of 256: row r of the tile and row r + 128, piece j of each in every stage
+    const int r = threadIdx.x >> 2, j = threadIdx.x & 3;
+    const int which = GATED ? r >> 5 & 1 : 0;
+    int row_n[2];
+    unsigned at_codes[2];
+    const uint2* table[2];
 #pragma unroll
-        for (int i = 0; i < decltype(N)::value; ++i) {
-            const unsigned at = at_codes + (BITS == 3 ? 3 * l_ks + half : (l_ks * 2 + half) * (BITS / 2)) * 4;
-            Unit<BITS>& u = o.u[i];
-            if constexpr (BITS == 8) { const u4 v = __builtin_amdgcn_raw_buffer_load_b128(codes, at, 0, 0); u.w[0] = v[0]; u.w[1] = v[1]; u.w[2] = v[2]; u.w[3] = v[3]; }
-            else if constexpr (BITS == 2) u.w[0] = __builtin_amdgcn_raw_buffer_load_b32(codes, at, 0, 0);
-            else { const auto v = __builtin_amdgcn_raw_buffer_load_b64(codes, at, 0, 0); u.w[0] = v[0]; u.w[1] = v[1]; }
-            const unsigned unit = l_ks * 2 + half;
-            o.g[i] = table[min((int)(__umulhi(unit, a.unit_magic) + (unit & a.unit_all)), p.n_groups - 1)];
-            if (++l_ks == a.kb) l_ks = 0;
+    for (int h = 0; h < 2; ++h) {
+        const int row = r + 128 * h;
+        row_n[h] = min(GATED ? n0 + 32 * (row >> 6) + (row & 31) : n0 + row, p.d_out - 1);
+        at_codes[h] = (unsigned)(row_n[h] - n0) * p.words * 4 + j * (BITS == 8 ? 16 : 4 * BITS);
+        table[h] = a.table + ((long long)which * p.d_out + row_n[h]) * p.n_groups;
+    }
+    // (rows 32 .. 63 of every 64 are the second matrix's: the same for all of a wavefront's 16 rows)
+    const uint32_t* const base = __builtin_amdgcn_readfirstlane(which) ? p.w[1] : p.w[0];
+    const auto codes = __builtin_amdgcn_make_buffer_rsrc((void*)(base + (long long)n0 * p.words), 0, (int)(unsigned)min((long long)(p.d_out - n0) * p.words * 4, 0xfffffffcLL), 0x00020000);
+    constexpr int NG = ONE_SCALE ? 1 : NS, NL = 2 * ((BITS == 8 ? 2 : 1) + NG);      // scales of a row in NS stages; loads of `load`
+    struct Load { Codes128<BITS> u[2]; uint2 g[2][NG]; };
+    int l_ks = kt0 % a.kb;      // of the next codes to be loaded, a multiple of NS
+    auto load = [&](Load& o) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const unsigned at = at_codes[h] + l_ks * (BITS * 4);
+            Codes128<BITS>& u = o.u[h];
+            if constexpr (BITS == 8) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) { const u4 v = __builtin_amdgcn_raw_buffer_load_b128(codes, at + 64 * i, 0, 0); u.w[4 * i] = v[0]; u.w[4 * i + 1] = v[1]; u.w[4 * i + 2] = v[2]; u.w[4 * i + 3] = v[3]; }
+            } else if constexpr (BITS == 4) { const u4 v = __builtin_amdgcn_raw_buffer_load_b128(codes, at, 0, 0); u.w[0] = v[0]; u.w[1] = v[1]; u.w[2] = v[2]; u.w[3] = v[3]; }
+            else if constexpr (BITS == 2) { const auto v = __builtin_amdgcn_raw_buffer_load_b64(codes, at, 0, 0); u.w[0] = v[0]; u.w[1] = v[1]; }
+            else { const auto v = __builtin_amdgcn_raw_buffer_load_b96(codes, at, 0, 0); u.w[0] = v[0]; u.w[1] = v[1]; u.w[2] = v[2]; }
+#pragma unroll
+            for (int i = 0; i < NG; ++i) {
+                const unsigned unit = (l_ks + i) * 2 + (ONE_SCALE ? 0 : j >> 1);
+                o.g[h][i] = table[h][min((int)(__umulhi(unit, a.unit_magic) + (unit & a.unit_all)), p.n_groups - 1)];
+            }
         }
+        l_ks += NS;
+        if (l_ks >= a.kb) l_ks = 0;
     };
     int b_seg = kt0 / a.kb, b_ks = kt0 - b_seg * a.kb;      // of the next codes to be written
-    unsigned char* const b_at = ring + A_BYTES + r * 64;
-    auto write = [&](const Unit<BITS>& u, uint2 g, int slot) {
-        unsigned v[8];
-        unit_halves<BITS>(u, half, v);
+    unsigned char* const b_at = ring + A_BYTES + r * 64 + ((j ^ (r >> 2 & 3)) << 4);
+    auto halves = [&](const Load& o, auto H, auto S, u4& out) {      // piece j of row h in stage S
+        constexpr int h = decltype(H)::value, st = decltype(S)::value;
+        unsigned v[4];
+        piece_halves<BITS, st>(o.u[h], j, v);
+        const uint2 g = o.g[h][ONE_SCALE ? 0 : st];
         if constexpr (sizeof(T) == 2) {
             const h2 both = __builtin_bit_cast(h2, g.x), s = {both[0], both[0]}, z = {both[1], both[1]};
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = __builtin_bit_cast(unsigned, (__builtin_bit_cast(h2, v[i]) + z) * s);
+            for (int i = 0; i < 4; ++i) out[i] = __builtin_bit_cast(unsigned, (__builtin_bit_cast(h2, v[i]) + z) * s);
         } else {
             const float s = __uint_as_float(g.x), z = -1024.f - __uint_as_float(g.y);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < 4; ++i) {
                 const h2 c = __builtin_bit_cast(h2, v[i]);
                 h2 w;
 #pragma unroll
-                for (int j = 0; j < 2; ++j) { const float f = ((float)c[j] + z) * s; w[j] = (_Float16)f; if (b_seg == 2) w[j] = (_Float16)(f - (float)w[j]); }
-                v[i] = __builtin_bit_cast(unsigned, w);
+                for (int k = 0; k < 2; ++k) { const float f = ((float)c[k] + z) * s; w[k] = (_Float16)f; if (b_seg == 2) w[k] = (_Float16)(f - (float)w[k]); }
+                out[i] = __builtin_bit_cast(unsigned, w);
             }
         }
-        unsigned char* const to = b_at + slot * STAGE;
-        *(u4*)(to + (((2 * half) ^ (r >> 2 & 3)) << 4)) = u4{v[0], v[1], v[2], v[3]};
-        *(u4*)(to + (((2 * half + 1) ^ (r >> 2 & 3)) << 4)) = u4{v[4], v[5], v[6], v[7]};
-        if (++b_ks == a.kb) { b_ks = 0; ++b_seg; }
     };
+    auto written = [&] { if (++b_ks == a.kb) { b_ks = 0; ++b_seg; } };
     const unsigned ring_at = (unsigned)(unsigned long long)((__attribute__((address_space(3))) void*)ring);
     long long block[LPW];
 #pragma unroll
@@ -730,31 +756,51 @@ __global__ __launch_bounds__(512) void packed_many_kernel(ManyArgs a) {
 #pragma unroll
             for (int j = 0; j < TJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fx[set][i], fw[set][j], acc[i][j], 0, 0, 0);
     };
-    // As stage kt begins, stages kt .. kt + NS - 2 are in LDS or on their way there; `here` has the codes of the NS stages after those as kt is a multiple of NS
-    Load here, next;
-    load(here, std::integral_constant<int, NS - 1>());
+    // a run of matrix instructions: the next one's operands first, and vector instructions in the shadow of each
+    auto beside = [] {
+        __builtin_amdgcn_sched_group_barrier(0x100, TI + TJ, 0);
 #pragma unroll
-    for (int s = 0; s < NS - 1; ++s) { copy(s); write(here.u[s], here.g[s], s); }
-    load(here, std::integral_constant<int, NS>());
+        for (int i = 0; i < TI * TJ; ++i) { __builtin_amdgcn_sched_group_barrier(0x8, 1, 0); __builtin_amdgcn_sched_group_barrier(0x2, TI == 4 ? 5 : 9, 0); }
+        __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
+    };
+    // As stage kt begins, stages kt .. kt + NS - 2 are in LDS or on their way there.  Codes are loaded for NS stages at once (kt and a.kb are multiples of NS): those of the last loads are written from the
+    // stage on that is NS - 1 before theirs.
+    Load here, next;
+    load(here);
+    unroll<NS - 1>([&](auto S) {
+        copy(S);
+        unroll<2>([&](auto H) { u4 v; halves(here, H, S, v); *(u4*)(b_at + S * STAGE + H * 128 * 64) = v; });
+        written();
+    });
+    load(next);
     wait_loads_but<0>();
     __syncthreads();
     read(0, 0, 0);
     for (int kt = 0; kt < nk; kt += NS) {
-        unroll<NS>([&](auto S) {
-            constexpr int s = S, last = s == 0 ? NS - 1 : s - 1, after = s == NS - 1 ? 0 : s + 1;
-            if (kt + s >= nk) return;
-            read(1, s, 1);
-            if constexpr (s == 0) load(next, std::integral_constant<int, NS>());
+        unroll<NS>([&](auto SS) {
+            constexpr int s = SS, last = s == 0 ? NS - 1 : s - 1, after = s == NS - 1 ? 0 : s + 1;
+            constexpr std::integral_constant<int, last> S;      // the written stage's number among its NS
+            u4 v;
+            if constexpr (s == 1) { here = next; load(next); }
             copy(last);      // (the stage before this one has been read by everyone)
+            __builtin_amdgcn_sched_barrier(0);
+            read(1, s, 1);
+            halves(here, std::integral_constant<int, 0>(), S, v);
             multiply(0);
-            write(here.u[s], here.g[s], last);
+            *(u4*)(b_at + last * STAGE) = v;
+            beside();
             // what the next stage has was copied two stages ago: two stages' copies may still be on their way, and the loads beside them (older ones are awaited with them)
-            if constexpr (s < 2) wait_loads_but<2 * LPW + 2 * NS>(); else wait_loads_but<2 * LPW>();
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (s == 1 || s == 2) wait_loads_but<2 * LPW + NL>(); else wait_loads_but<2 * LPW>();
             __syncthreads();
+            __builtin_amdgcn_sched_barrier(0);
             read(0, after, 0);
+            halves(here, std::integral_constant<int, 1>(), S, v);
             multiply(1);
+            *(u4*)(b_at + last * STAGE + 128 * 64) = v;
+            beside();
+            written();
         });
-        here = next;
     }
     // results through LDS, 32 tokens of a wavefront at a time: rows of 64 outputs
     wait_loads_but<0>();
@@ -843,7 +889,7 @@ constexpr long long MOST_ROWS = 8192;      // tokens of one round: more are work
 // what a call of so many tokens is cut into, and the workspace for it
 size_t many_room(const PackedArgs& p, bool gated, int size, long long tokens, ManyArgs& a, void* ws) {
     const int tm = tokens <= 128 ? 128 : 256;
-    a.kb = (int)cdiv64(p.d_in, KS); a.blocks = (int)cdiv64(tokens, 16);
+    a.kb = (int)cdiv64(p.d_in, 4 * KS) * 4; a.blocks = (int)cdiv64(tokens, 16);
     a.segments = size == 2 ? 1 : p.n_groups == 1 ? 2 : 3;
     a.tiles_m = (int)cdiv64(tokens, tm); a.tiles_n = (int)cdiv64(p.d_out, gated ? 128 : 256);
     const long long tiles = (long long)a.tiles_m * a.tiles_n;
@@ -860,10 +906,10 @@ size_t many_room(const PackedArgs& p, bool gated, int size, long long tokens, Ma
 }
 bool many_takes(const PackedArgs& p) { return (p.n_groups == 1 || p.group % 16 == 0) && p.words <= 1 << 21; }
 
-template <typename T, int BITS, int TM, bool GATED>
+template <typename T, int BITS, bool ONE_SCALE, int TM, bool GATED>
 int launch_many(tboa_ctx* ctx, const ManyArgs& a) {
     constexpr int LDS = 4 * (TM + 256) * 64;
-    const auto kernel = packed_many_kernel<T, BITS, TM, GATED>;
+    const auto kernel = packed_many_kernel<T, BITS, ONE_SCALE, TM, GATED>;
     TB_HIP(ctx, hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
     hipLaunchKernelGGL(kernel, dim3((unsigned)(cdiv64((long long)a.tiles_m * a.tiles_n * a.splits, 8) * 8)), dim3(512), LDS, ctx->stream, a);
     TB_KERNEL_CHECK(ctx);
@@ -883,8 +929,9 @@ int launch_many(tboa_ctx* ctx, const PackedArgs& p) {
         magic(p.n_groups == 1 ? 0 : units, a.unit_magic, a.unit_all);
         hipLaunchKernelGGL((packed_rows_kernel<T, BITS>), dim3((unsigned)(a.blocks + cdiv64((GATED ? 2LL : 1LL) * p.d_out, 16))), dim3(1024), 0, ctx->stream, a);
         TB_KERNEL_CHECK(ctx);
-        if (a.p.tokens <= 128) TB_TRY((launch_many<T, BITS, 128, GATED>(ctx, a)));
-        else TB_TRY((launch_many<T, BITS, 256, GATED>(ctx, a)));
+        const bool one = p.n_groups == 1 || p.group % 128 == 0;
+        if (a.p.tokens <= 128) TB_TRY((one ? launch_many<T, BITS, true, 128, GATED>(ctx, a) : launch_many<T, BITS, false, 128, GATED>(ctx, a)));
+        else TB_TRY((one ? launch_many<T, BITS, true, 256, GATED>(ctx, a) : launch_many<T, BITS, false, 256, GATED>(ctx, a)));
         if (a.splits > 1) {
             hipLaunchKernelGGL((packed_join_kernel<T, GATED>), dim3((unsigned)std::min<long long>(cdiv64(a.p.tokens * p.d_out, 256), 1 << 16)), dim3(256), 0, ctx->stream, a);
             TB_KERNEL_CHECK(ctx);
