@@ -508,9 +508,10 @@ struct ManyArgs {
     float* row_scale;             // [tokens] power of two that takes a row's own back out
     uint2* table;                 // [matrices][d_out][n_groups]: bf16: .x half scale, half -(1024 + zero); fp32: scale, zero
     float* out_scale;             // [matrices][d_out]
-    float* partial;               // [splits][tokens][matrices * d_out] where a tile's channels are split over workgroups
+    float* partial;               // [splits][tiles that are split][TM][256]: their channels are split over workgroups
     long long plane;              // bytes
-    int kb, blocks, splits;       // blocks of 32 channels; of 16 tokens
+    int kb, blocks;               // blocks of 32 channels, a multiple of four; of 16 tokens
+    int full, splits;             // tiles that are not split (whole rounds of all compute units), how many ways the others are
     int tiles_m, tiles_n, segments, matrices;
     unsigned unit_magic, unit_all;      // units of 16 channels that a group has, as PackedArgs::piece_magic
 };
@@ -637,6 +638,12 @@ typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef float f16v __attribute__((ext_vector_type(16)));
 
+// tile t in the order in which tiles are worked off: bands of four columns of tiles
+__device__ __forceinline__ void tile_place(const ManyArgs& a, int t, int& tm, int& tn) {
+    const int band = 4 * a.tiles_m, in = t % band, wide = min(4, a.tiles_n - t / band * 4);
+    tn = t / band * 4 + in % wide; tm = in / wide;
+}
+
 // A tile of TM tokens and 256 rows of codes (GATED: 128 of either matrix, 32 of one beside 32 of the other, so that a wavefront has both factors of its results); eight wavefronts, each TM / 2 tokens and 64 rows.
 // A ring of NS stages of 32 channels in LDS: X is copied there, NS - 1 stages ahead; codes are loaded two stages before that, made into half and written by all wavefronts, 16 codes a lane and stage.
 template <typename T, int BITS, bool ONE_SCALE, int TM, bool GATED>      // ONE_SCALE: whole groups of 128 channels
@@ -645,19 +652,21 @@ __global__ __launch_bounds__(512) void packed_many_kernel(ManyArgs a) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char ring[];
     const PackedArgs& p = a.p;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, lh = lane >> 5;
-    // tiles of one band of outputs after each other, an XCD (every eighth workgroup) its own run of them
-    int tm, tn, split;
-    {
-        const int total = a.tiles_m * a.tiles_n * a.splits, per = (total + 7) / 8, w = blockIdx.x;
-        const int item = (w & 7) * per + (w >> 3);
-        if (w >> 3 >= per || item >= total) return;
+    // tiles of one band of outputs after each other, an XCD (every eighth workgroup) its own run of them; then those that are split
+    int tm, tn, split = 0, t;
+    const int w = blockIdx.x, cut = a.tiles_m * a.tiles_n - a.full;
+    if (w < a.full) t = (w & 7) * (a.full >> 3) + (w >> 3);
+    else {
+        const int total = cut * a.splits, per = (total + 7) / 8, v = w - a.full, item = (v & 7) * per + (v >> 3);
+        if (v >> 3 >= per || item >= total) return;
         split = item % a.splits;
-        const int t = item / a.splits, band = 4 * a.tiles_m, in = t % band, wide = min(4, a.tiles_n - t / band * 4);
-        tn = t / band * 4 + in % wide; tm = in / wide;
+        t = a.full + item / a.splits;
     }
+    const bool parts = w >= a.full && a.splits > 1;
+    tile_place(a, t, tm, tn);
     const long long m0 = (long long)tm * TM;
     const int n0 = tn * (GATED ? 128 : 256);
-    const int turns = a.kb / NS * a.segments, kt0 = (int)((long long)turns * split / a.splits) * NS, nk = (int)((long long)turns * (split + 1) / a.splits) * NS - kt0;      // (whole turns of the ring)
+    const int turns = a.kb / NS * a.segments, pieces = parts ? a.splits : 1, kt0 = (int)((long long)turns * split / pieces) * NS, nk = (int)((long long)turns * (split + 1) / pieces) * NS - kt0;      // (whole turns of the ring)
 
     // This thread's two rows of codes, of 256: row r of the tile and row r + 128, piece j of each in every stage
     const int r = threadIdx.x >> 2, j = threadIdx.x & 3;
@@ -756,6 +765,15 @@ __global__ __launch_bounds__(512) void packed_many_kernel(ManyArgs a) {
 #pragma unroll
             for (int j = 0; j < TJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fx[set][i], fw[set][j], acc[i][j], 0, 0, 0);
     };
+    auto arrived = [](Load& o) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (unsigned& w : o.u[h].w) asm volatile("" : "+v"(w));
+#pragma unroll
+            for (uint2& g : o.g[h]) { asm volatile("" : "+v"(g.x)); if (sizeof(T) == 4) asm volatile("" : "+v"(g.y)); }
+        }
+    };
     // a run of matrix instructions: the next one's operands first, and vector instructions in the shadow of each
     auto beside = [] {
         __builtin_amdgcn_sched_group_barrier(0x100, TI + TJ, 0);
@@ -763,9 +781,9 @@ __global__ __launch_bounds__(512) void packed_many_kernel(ManyArgs a) {
         for (int i = 0; i < TI * TJ; ++i) { __builtin_amdgcn_sched_group_barrier(0x8, 1, 0); __builtin_amdgcn_sched_group_barrier(0x2, TI == 4 ? 5 : 9, 0); }
         __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
     };
-    // As stage kt begins, stages kt .. kt + NS - 2 are in LDS or on their way there.  Codes are loaded for NS stages at once (kt and a.kb are multiples of NS): those of the last loads are written from the
-    // stage on that is NS - 1 before theirs.
-    Load here, next;
+    // As stage kt begins, stages kt .. kt + NS - 2 are in LDS or on their way there.  Codes are loaded for NS stages at once (kt and a.kb are multiples of NS) and written from the stage on that is NS - 1
+    // before theirs: `here` has those of stages kt .. kt + NS - 1, `next` those of the NS after them.
+    Load here, next, after_next;
     load(here);
     unroll<NS - 1>([&](auto S) {
         copy(S);
@@ -773,6 +791,7 @@ __global__ __launch_bounds__(512) void packed_many_kernel(ManyArgs a) {
         written();
     });
     load(next);
+    arrived(next);
     wait_loads_but<0>();
     __syncthreads();
     read(0, 0, 0);
@@ -780,27 +799,31 @@ __global__ __launch_bounds__(512) void packed_many_kernel(ManyArgs a) {
         unroll<NS>([&](auto SS) {
             constexpr int s = SS, last = s == 0 ? NS - 1 : s - 1, after = s == NS - 1 ? 0 : s + 1;
             constexpr std::integral_constant<int, last> S;      // the written stage's number among its NS
+            const Load& codes_of = s == 0 ? here : next;
             u4 v;
-            if constexpr (s == 1) { here = next; load(next); }
             copy(last);      // (the stage before this one has been read by everyone)
+            if constexpr (s == 1) load(after_next);
             __builtin_amdgcn_sched_barrier(0);
             read(1, s, 1);
-            halves(here, std::integral_constant<int, 0>(), S, v);
+            halves(codes_of, std::integral_constant<int, 0>(), S, v);
             multiply(0);
             *(u4*)(b_at + last * STAGE) = v;
             beside();
-            // what the next stage has was copied two stages ago: two stages' copies may still be on their way, and the loads beside them (older ones are awaited with them)
+            // what the next stage has was copied two stages ago: two stages' copies may still be on their way, and the loads after the first of them (older ones are awaited with them)
             __builtin_amdgcn_sched_barrier(0);
-            if constexpr (s == 1 || s == 2) wait_loads_but<2 * LPW + NL>(); else wait_loads_but<2 * LPW>();
+            if constexpr (s > 0) wait_loads_but<2 * LPW + NL>(); else wait_loads_but<2 * LPW>();
             __syncthreads();
             __builtin_amdgcn_sched_barrier(0);
             read(0, after, 0);
-            halves(here, std::integral_constant<int, 1>(), S, v);
+            halves(codes_of, std::integral_constant<int, 1>(), S, v);
             multiply(1);
             *(u4*)(b_at + last * STAGE + 128 * 64) = v;
             beside();
             written();
         });
+        __builtin_amdgcn_sched_barrier(0);
+        arrived(after_next);      // (here, where the newest copy is a stage old: the compiler, which does not know of the copies, waits for them too)
+        here = next; next = after_next;
     }
     // results through LDS, 32 tokens of a wavefront at a time: rows of 64 outputs
     wait_loads_but<0>();
@@ -809,7 +832,6 @@ __global__ __launch_bounds__(512) void packed_many_kernel(ManyArgs a) {
     float* const mine = (float*)(ring + wave * 32 * 68 * 4);
     const int c0 = GATED ? n0 + wn / 2 : n0 + wn;      // first output of the wavefront
     const float* const os = a.out_scale;
-    const bool parts = a.splits > 1;
 #pragma unroll
     for (int i = 0; i < TI; ++i) {
         auto in_order = [] { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); __builtin_amdgcn_wave_barrier(); };
@@ -842,9 +864,7 @@ __global__ __launch_bounds__(512) void packed_many_kernel(ManyArgs a) {
                 if (m >= p.tokens || n >= p.d_out) continue;
                 f4 v = *(const f4*)(mine + row * PITCH + c);
                 if (parts) {
-                    float* const to = a.partial + ((long long)split * p.tokens + m) * ((GATED ? 2 : 1) * (long long)p.d_out) + side * (long long)p.d_out + n;
-                    if (n + 4 <= p.d_out && p.d_out % 4 == 0) *(f4*)to = v;
-                    else for (int k = 0; k < 4; ++k) if (n + k < p.d_out) to[k] = v[k];
+                    *(f4*)(a.partial + (((long long)split * cut + (t - a.full)) * TM + (wm + 32 * i + row)) * 256 + (GATED ? side * 128 + wn / 2 : wn) + c) = v;
                     continue;
                 }
                 const float rs = GATED ? 1.f : a.row_scale[m];
@@ -866,17 +886,22 @@ __global__ __launch_bounds__(512) void packed_many_kernel(ManyArgs a) {
     }
 }
 
-// sums of the splits' partial results, scaled; one output per thread
-template <typename T, bool GATED>
+// sums of the splits' partial results of the tiles that are split, scaled; one output per thread
+template <typename T, int TM, bool GATED>
 __global__ __launch_bounds__(256) void packed_join_kernel(ManyArgs a) {
+    constexpr int WIDE = GATED ? 128 : 256;
     const PackedArgs& p = a.p;
-    const long long wide = (GATED ? 2LL : 1LL) * p.d_out, all = p.tokens * p.d_out;
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < all; i += (long long)gridDim.x * 256) {
-        const long long m = i / p.d_out;
-        const int n = (int)(i - m * p.d_out);
+    const int cut = a.tiles_m * a.tiles_n - a.full, c = threadIdx.x % WIDE, rows = 256 / WIDE;
+    for (int item = blockIdx.x; item < cut * (TM / rows); item += gridDim.x) {
+        const int at = item / (TM / rows), row = item % (TM / rows) * rows + threadIdx.x / WIDE;
+        int tm, tn;
+        tile_place(a, a.full + at, tm, tn);
+        const long long m = (long long)tm * TM + row;
+        const int n = tn * WIDE + c;
+        if (m >= p.tokens || n >= p.d_out) continue;
         float y[2] = {0.f, 0.f};
-        const float* from = a.partial + m * wide + n;
-        for (int s = 0; s < a.splits; ++s, from += p.tokens * wide) { y[0] += from[0]; if (GATED) y[1] += from[p.d_out]; }
+        const float* from = a.partial + ((long long)at * TM + row) * 256 + c;
+        for (int s = 0; s < a.splits; ++s, from += (long long)cut * TM * 256) { y[0] += from[0]; if (GATED) y[1] += from[128]; }
         const float rs = a.row_scale[m];
         float v = y[0] * rs * a.out_scale[n];
         if (GATED) v = silu(v) * (y[1] * rs * a.out_scale[p.d_out + n]);
@@ -885,6 +910,7 @@ __global__ __launch_bounds__(256) void packed_join_kernel(ManyArgs a) {
     }
 }
 
+constexpr int CUS = 256;
 constexpr long long MOST_ROWS = 8192;      // tokens of one round: more are worked off round by round, in the same workspace
 // what a call of so many tokens is cut into, and the workspace for it
 size_t many_room(const PackedArgs& p, bool gated, int size, long long tokens, ManyArgs& a, void* ws) {
@@ -892,8 +918,10 @@ size_t many_room(const PackedArgs& p, bool gated, int size, long long tokens, Ma
     a.kb = (int)cdiv64(p.d_in, 4 * KS) * 4; a.blocks = (int)cdiv64(tokens, 16);
     a.segments = size == 2 ? 1 : p.n_groups == 1 ? 2 : 3;
     a.tiles_m = (int)cdiv64(tokens, tm); a.tiles_n = (int)cdiv64(p.d_out, gated ? 128 : 256);
-    const long long tiles = (long long)a.tiles_m * a.tiles_n;
-    a.splits = (int)std::max<long long>(1, std::min<long long>(tiles >= 192 ? 1 : 256 / tiles, (long long)a.kb * a.segments / 16));
+    const int tiles = a.tiles_m * a.tiles_n, cut = tiles % CUS;
+    a.full = tiles - cut;
+    a.splits = cut ? std::max(1, std::min(CUS / cut, a.kb / 4 * a.segments / 2)) : 1;
+    if (a.splits == 1) a.full = tiles / 8 * 8;
     a.plane = (long long)a.blocks * a.kb * 1024;
     const int matrices = a.matrices = gated ? 2 : 1;
     Arena ar(ws);
@@ -901,7 +929,7 @@ size_t many_room(const PackedArgs& p, bool gated, int size, long long tokens, Ma
     a.row_scale = ar.get<float>((size_t)tokens);
     a.table = ar.get<uint2>((size_t)matrices * p.d_out * p.n_groups);
     a.out_scale = ar.get<float>((size_t)matrices * p.d_out);
-    a.partial = ar.get<float>(a.splits > 1 ? (size_t)a.splits * tokens * matrices * p.d_out : 0);
+    a.partial = ar.get<float>(a.splits > 1 ? (size_t)a.splits * cut * tm * 256 : 0);
     return ar.off;
 }
 bool many_takes(const PackedArgs& p) { return (p.n_groups == 1 || p.group % 16 == 0) && p.words <= 1 << 21; }
@@ -911,8 +939,13 @@ int launch_many(tboa_ctx* ctx, const ManyArgs& a) {
     constexpr int LDS = 4 * (TM + 256) * 64;
     const auto kernel = packed_many_kernel<T, BITS, ONE_SCALE, TM, GATED>;
     TB_HIP(ctx, hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(cdiv64((long long)a.tiles_m * a.tiles_n * a.splits, 8) * 8)), dim3(512), LDS, ctx->stream, a);
+    const int cut = a.tiles_m * a.tiles_n - a.full;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(a.full + cdiv64((a.tiles_m * a.tiles_n - a.full) * a.splits, 8) * 8)), dim3(512), LDS, ctx->stream, a);
     TB_KERNEL_CHECK(ctx);
+    if (a.splits > 1) {
+        hipLaunchKernelGGL((packed_join_kernel<T, TM, GATED>), dim3((unsigned)std::min(cut * TM, 1 << 16)), dim3(256), 0, ctx->stream, a);
+        TB_KERNEL_CHECK(ctx);
+    }
     return 0;
 }
 template <typename T, int BITS, bool GATED>
@@ -932,10 +965,6 @@ int launch_many(tboa_ctx* ctx, const PackedArgs& p) {
         const bool one = p.n_groups == 1 || p.group % 128 == 0;
         if (a.p.tokens <= 128) TB_TRY((one ? launch_many<T, BITS, true, 128, GATED>(ctx, a) : launch_many<T, BITS, false, 128, GATED>(ctx, a)));
         else TB_TRY((one ? launch_many<T, BITS, true, 256, GATED>(ctx, a) : launch_many<T, BITS, false, 256, GATED>(ctx, a)));
-        if (a.splits > 1) {
-            hipLaunchKernelGGL((packed_join_kernel<T, GATED>), dim3((unsigned)std::min<long long>(cdiv64(a.p.tokens * p.d_out, 256), 1 << 16)), dim3(256), 0, ctx->stream, a);
-            TB_KERNEL_CHECK(ctx);
-        }
     }
     return 0;
 }
