@@ -778,8 +778,10 @@ __global__ __launch_bounds__(512) void packed_many_kernel(ManyArgs a) {
     auto beside = [] {
         __builtin_amdgcn_sched_group_barrier(0x100, TI + TJ, 0);
 #pragma unroll
-        for (int i = 0; i < TI * TJ; ++i) { __builtin_amdgcn_sched_group_barrier(0x8, 1, 0); __builtin_amdgcn_sched_group_barrier(0x2, TI == 4 ? 5 : 9, 0); }
-        __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
+        for (int i = 0; i < TI * TJ; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0); __builtin_amdgcn_sched_group_barrier(0x2, TI == 4 ? 8 : 12, 0);
+            if (i == TI * TJ * 5 / 8) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);      // (what waits at the next barrier is then done)
+        }
     };
     // As stage kt begins, stages kt .. kt + NS - 2 are in LDS or on their way there.  Codes are loaded for NS stages at once (kt and a.kb are multiples of NS) and written from the stage on that is NS - 1
     // before theirs: `here` has those of stages kt .. kt + NS - 1, `next` those of the NS after them.
@@ -886,27 +888,37 @@ __global__ __launch_bounds__(512) void packed_many_kernel(ManyArgs a) {
     }
 }
 
-// sums of the splits' partial results of the tiles that are split, scaled; one output per thread
+// sums of the splits' partial results of the tiles that are split, scaled
 template <typename T, int TM, bool GATED>
 __global__ __launch_bounds__(256) void packed_join_kernel(ManyArgs a) {
-    constexpr int WIDE = GATED ? 128 : 256;
+    constexpr int WIDE = GATED ? 128 : 256, LANES = WIDE / 4, ROWS = 256 / LANES;      // four outputs a thread
     const PackedArgs& p = a.p;
-    const int cut = a.tiles_m * a.tiles_n - a.full, c = threadIdx.x % WIDE, rows = 256 / WIDE;
-    for (int item = blockIdx.x; item < cut * (TM / rows); item += gridDim.x) {
-        const int at = item / (TM / rows), row = item % (TM / rows) * rows + threadIdx.x / WIDE;
+    const int cut = a.tiles_m * a.tiles_n - a.full, c = threadIdx.x % LANES * 4;
+    for (int item = blockIdx.x; item < cut * (TM / ROWS); item += gridDim.x) {
+        const int at = item / (TM / ROWS), row = item % (TM / ROWS) * ROWS + threadIdx.x / LANES;
         int tm, tn;
         tile_place(a, a.full + at, tm, tn);
         const long long m = (long long)tm * TM + row;
         const int n = tn * WIDE + c;
         if (m >= p.tokens || n >= p.d_out) continue;
-        float y[2] = {0.f, 0.f};
+        f4 y[2] = {f4{0.f, 0.f, 0.f, 0.f}, f4{0.f, 0.f, 0.f, 0.f}};
         const float* from = a.partial + ((long long)at * TM + row) * 256 + c;
-        for (int s = 0; s < a.splits; ++s, from += (long long)cut * TM * 256) { y[0] += from[0]; if (GATED) y[1] += from[128]; }
+#pragma unroll 4
+        for (int s = 0; s < a.splits; ++s) { y[0] += *(const f4*)from; if (GATED) y[1] += *(const f4*)(from + 128); from += (long long)cut * TM * 256; }
         const float rs = a.row_scale[m];
-        float v = y[0] * rs * a.out_scale[n];
-        if (GATED) v = silu(v) * (y[1] * rs * a.out_scale[p.d_out + n]);
-        else if (p.Res) v += to_f32(((const T*)p.Res)[m * p.ldr + n]);
-        ((T*)p.Y)[m * p.ldy + n] = from_f32(v, T());
+        T* const to = (T*)p.Y + m * p.ldy + n;
+        const T* const res = !GATED && p.Res ? (const T*)p.Res + m * p.ldr + n : nullptr;
+        struct __attribute__((aligned(4 * sizeof(T)))) Four { T e[4]; } o;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (n + k >= p.d_out) break;
+            float v = y[0][k] * rs * a.out_scale[n + k];
+            if (GATED) v = silu(v) * (y[1][k] * rs * a.out_scale[p.d_out + n + k]);
+            if (res) v += to_f32(res[k]);
+            o.e[k] = from_f32(v, T());
+        }
+        if (n + 4 <= p.d_out && p.out_vec) *(Four*)to = o;
+        else for (int k = 0; k < 4; ++k) if (n + k < p.d_out) to[k] = o.e[k];
     }
 }
 
@@ -943,7 +955,7 @@ int launch_many(tboa_ctx* ctx, const ManyArgs& a) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)(a.full + cdiv64((a.tiles_m * a.tiles_n - a.full) * a.splits, 8) * 8)), dim3(512), LDS, ctx->stream, a);
     TB_KERNEL_CHECK(ctx);
     if (a.splits > 1) {
-        hipLaunchKernelGGL((packed_join_kernel<T, TM, GATED>), dim3((unsigned)std::min(cut * TM, 1 << 16)), dim3(256), 0, ctx->stream, a);
+        hipLaunchKernelGGL((packed_join_kernel<T, TM, GATED>), dim3((unsigned)std::min(cut * TM / (GATED ? 8 : 4), 1 << 16)), dim3(256), 0, ctx->stream, a);
         TB_KERNEL_CHECK(ctx);
     }
     return 0;
