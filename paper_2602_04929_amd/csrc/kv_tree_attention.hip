@@ -3,15 +3,15 @@
 //
 // The same products and the same running softmax as attention of a chain (kv_attention.hip): levels less their zero are exact in half, scales multiply scores and probabilities,
 //     x[t] = (scale s^K_t log2 e) q.(c^K_t - z^K_t),   p = 2^(x - max),   O += (2^up p s^V_t) (c^V_t - z^V_t)
-// with a power of two per row for its query and one, `up`, by the largest p s among the tokens that the row itself has seen.  fp32 queries are two half terms; 2^up p s is two half terms for fp32 and
-// for sequences of up to FEW rows, one (2^-12 of it) in longer ones.
+// with a power of two per row for its query and one, `up`, by the largest p s among the tokens that the row itself has seen.  fp32 queries are two half terms, and so is
+// 2^up p s; for bf16 queries it is one (off by 2^-11 of it at most, an eighth of an output's rounding to bf16).
 #include "kv_attention.h"
 
 namespace {
 
 constexpr float MOST_FLOAT = 0x1.fffffep127f;
 constexpr int HALF_TOP = 14;      // a row's largest probability times scale becomes 2^14 .. 2^15 as half
-constexpr int TILE = 64, FEW = 32;
+constexpr int TILE = 64;
 template <int DP> constexpr int resident() { return DP <= 128 ? 2 : 1; }      // workgroups that a compute unit holds at once (registers)
 constexpr int most_resident = 2;
 
@@ -44,7 +44,7 @@ __device__ __forceinline__ unsigned below(int n) { return n <= 0 ? 0u : n >= 16 
 // the right operand of O^T += V^T P^T as they stand.
 template <typename T, int DP, int U>
 __global__ __launch_bounds__(256, resident<DP>()) void kv_tree_kernel(AttendArgs a) {
-    constexpr int NT = sizeof(T) == 2 ? 1 : 2, RW = 16 * U;      // half terms of queries; rows of a wavefront
+    constexpr int NT = sizeof(T) == 2 ? 1 : 2, RW = 16 * U;      // half terms of queries and of probabilities; rows of a wavefront
     constexpr int K64 = DP / 64, K32 = (DP % 64) / 32, KS = DP / 32, CT = DP / 16;
     __shared__ float joined[4][RW][DP + 4];
     __shared__ float2 ends[4][RW];
@@ -74,7 +74,6 @@ __global__ __launch_bounds__(256, resident<DP>()) void kv_tree_kernel(AttendArgs
         const int h = __builtin_amdgcn_readfirstlane((int)(x % a.g.heads)), r0 = __builtin_amdgcn_readfirstlane((int)(x / a.g.heads) * (RW * c.wr));
         const int step1 = (int)min((long long)c.steps, step0 + (at_end - at));      // steps step0 .. step1 - 1 of the unit
         const int rows = s.n * a.rep, n_rows = min(RW * c.wr, rows - r0);
-        const bool two = NT == 2 || (a.q.n_seqs > 1 ? s.n : a.q.n_tokens) * a.rep <= FEW;      // half terms of probabilities
         const int before = s.len - s.n, end = min(s.len, a.q.room), group = wave / c.wr, rg = wave - group * c.wr;
         const int hi = min((c.first + step1 * c.wt) * TILE, end), stride = c.wt * TILE;
         // this lane's rows
@@ -209,15 +208,19 @@ __global__ __launch_bounds__(256, resident<DP>()) void kv_tree_kernel(AttendArgs
                         for (int n = 0; n < NT; ++n) st[u][i] = mma16(lv, qh[u][n][k], st[u][i]);
                 }
             }
-            if (t0 + stride < hi) {
-                pk = pk_next; pv = pv_next;
-                load_k(t0 + stride);
-                pk_next = page_of(t0 + 2 * stride + 16 * (col >> 2)); pv_next = page_of(t0 + 2 * stride + 16 * grp);
-            }
+            auto load_next = [&] {
+                if (t0 + stride < hi) {
+                    pk = pk_next; pv = pv_next;
+                    load_k(t0 + stride);
+                    pk_next = page_of(t0 + 2 * stride + 16 * (col >> 2)); pv_next = page_of(t0 + 2 * stride + 16 * grp);
+                }
+            };
+            if constexpr (U == 1) load_next();
             const bool all = t0 + TILE <= min(before, end) && (!a.window || t0 >= before + s.n - a.window) && __all(there);
-            h8 ph[U][2][2];
+            h8 ph[U][NT][2];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
+                if constexpr (U > 1) __builtin_amdgcn_sched_barrier(0);      // (one unit's softmax after the other: mixed they spill registers)
                 float p[16];
                 unroll<16>([&](auto I) { constexpr int i = I; p[i] = st[u][i >> 2][i & 3] * (row_lane<i>(sk) * unit[u]); });
                 unsigned seen = 0xffffu;
@@ -268,9 +271,10 @@ __global__ __launch_bounds__(256, resident<DP>()) void kv_tree_kernel(AttendArgs
                     for (int j = 0; j < 8; ++j) {
                         const _Float16 w = (_Float16)p[8 * k + j];
                         ph[u][0][k][j] = w;
-                        ph[u][1][k][j] = (_Float16)(p[8 * k + j] - (float)w);
+                        if constexpr (NT == 2) ph[u][1][k][j] = (_Float16)(p[8 * k + j] - (float)w);
                     }
             }
+            if constexpr (U > 1) { __builtin_amdgcn_sched_barrier(0); load_next(); }      // (beside the softmax of two units there are no registers for it)
             // zeros of V's 16 tokens as pairs
             h2 zo[8];
             {
@@ -284,8 +288,8 @@ __global__ __launch_bounds__(256, resident<DP>()) void kv_tree_kernel(AttendArgs
                 const h8 v0 = levels8(vr[ct][0], vr[ct][1], zo[0], zo[1], zo[2], zo[3]), v1 = levels8(vr[ct][2], vr[ct][3], zo[4], zo[5], zo[6], zo[7]);
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    o[u][ct] = mma16(v0, ph[u][0][0], o[u][ct]); o[u][ct] = mma16(v1, ph[u][0][1], o[u][ct]);
-                    if (NT == 2 || two) { o[u][ct] = mma16(v0, ph[u][1][0], o[u][ct]); o[u][ct] = mma16(v1, ph[u][1][1], o[u][ct]); }
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) { o[u][ct] = mma16(v0, ph[u][n][0], o[u][ct]); o[u][ct] = mma16(v1, ph[u][n][1], o[u][ct]); }
                 }
             }
         }

@@ -25,11 +25,11 @@ def as_words(bits):
     return torch.from_numpy((b << np.arange(32, dtype=np.uint64)).sum(-1).astype(np.uint32).view(np.int32))
 
 
-def attention(cache, starts, lens, pages, q, bits, scale, window, dtype, rows_of_call=None):
+def attention(cache, starts, lens, pages, q, bits, scale, window, dtype):
     """Output (NaN for rows of no sequence and those that see a value's scale that is no number) and its bound.  With A the probabilities, x the scores and, of a token, X = scale sum |q| |k|:
       scores          dh + 4 fp32 operations on terms that add up to X (and fp32 queries in two half terms, 2^-22 of them): (dh + 4 + [8 for fp32]) 2^-24 X, and 2 * 2^-24 |x - max x| for the
                       difference to the maximum; the exponential 2^-22.  Of every token, in the numerator and in the sum
-      probabilities   times scale, in two halves 2^-22; in one 2^-11 (bf16 sequences of more than 32 rows; rows_of_call: of one sequence alone, the call's)
+      probabilities   times scale, in two halves 2^-22; in one 2^-11 (bf16)
       sums            (n + 8) 2^-24, twice, n tokens
       next to nothing a half below 2^-14 is off by 2^-25 whatever it is; the largest probability times scale of the row is at least 2^14 as half: 2^-39 of it for every token, times at most 255 levels
       output          half a step of the type"""
@@ -42,7 +42,7 @@ def attention(cache, starts, lens, pages, q, bits, scale, window, dtype, rows_of
         end = min(length, pages.shape[1] * pt)
         if n == 0:
             continue
-        halves = 2.0 ** (-11 if dtype == torch.bfloat16 and (rows_of_call or n * rep) > 32 else -22)
+        halves = 2.0 ** (-11 if dtype == torch.bfloat16 else -22)
         r = slice(int(starts[b]), int(starts[b]) + n)
         if end <= 0:
             out[r] = 0
@@ -83,9 +83,9 @@ def attention(cache, starts, lens, pages, q, bits, scale, window, dtype, rows_of
     return out, lim
 
 
-def check(got, cache, starts, lens, pages, q, bits, scale, window=0, rows=None, telling=0.9, rows_of_call=None):
+def check(got, cache, starts, lens, pages, q, bits, scale, window=0, rows=None, telling=0.9):
     """rows: a mask [rows, heads] of what is compared.  `telling`: at least this share of the compared outputs is larger than the bound, so that zeros would fail."""
-    want, lim = attention(cache, starts, lens, pages, q, bits, scale, window, got.dtype, rows_of_call)
+    want, lim = attention(cache, starts, lens, pages, q, bits, scale, window, got.dtype)
     g = got.double().cpu()
     use = torch.zeros(g.shape[:2], dtype=torch.bool)
     use[:int(starts[-1])] = True
