@@ -4,6 +4,24 @@
 #include <math.h>
 #include <algorithm>
 
+struct AttendArgs {
+    KvGeometry g; KvBatch q;
+    const void* Q; long long ldq; void* O; long long ldo;
+    const unsigned char* cache;
+    float scale2;                 // scale log2 e
+    int rep, window;
+    int vec, out_piece;           // elements of Q that may be read together, 8, 4 or 0 (one by one); of O that may be written together: 8, 4 or 1
+    int few;                      // sequences of more rows are kv_attend_tiles_kernel's
+    const unsigned* tree; int tree_words, piece_rows;      // trees of drafted tokens (kv_tree_attention.hip): masks of a token's sequence's new tokens, rows of a piece
+    int4* info;                   // per workgroup: the unit that begins in its share and ends in another: workgroups, first row of the sequence, row of the first | rows << 27, head
+    float* tile_part; float2* tile_stat; int4* tile_info;      // kv_attend_tiles_kernel: per piece, its rows; of trees what the join needs
+    float* part; float2* stat;    // per workgroup two pieces of 16 rows (of a unit that began before its share, of one that begins in it): averages; maximum, sum
+};
+// trees of drafted tokens: bf16 sequences of more than `few` rows by the kernel for many rows (kv_attention.hip)
+size_t kv_tree_tiles_room(const KvGeometry& g, AttendArgs* a, void* ws);
+bool kv_tree_tiles_takes(const KvGeometry& g, int n_seqs, long long n_tokens, int rep);
+int kv_tree_tiles(tboa_ctx* ctx, const AttendArgs& a);
+
 namespace {
 
 typedef __hip_bfloat16 bf16;
@@ -45,19 +63,6 @@ __device__ __forceinline__ h8 levels8(unsigned a, unsigned b, h2 o0, h2 o1, h2 o
 }
 __device__ __forceinline__ f4 mma16(h8 a, h8 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
-struct AttendArgs {
-    KvGeometry g; KvBatch q;
-    const void* Q; long long ldq; void* O; long long ldo;
-    const unsigned char* cache;
-    float scale2;                 // scale log2 e
-    int rep, window;
-    int vec, out_piece;           // elements of Q that may be read together, 8, 4 or 0 (one by one); of O that may be written together: 8, 4 or 1
-    int few;                      // sequences of more rows are kv_attend_tiles_kernel's
-    const unsigned* tree; int tree_words, piece_rows;      // trees of drafted tokens (kv_tree_attention.hip): masks of a token's sequence's new tokens, rows of a piece
-    int4* info;                   // per workgroup: the unit that begins in its share and ends in another: workgroups, first row of the sequence, row of the first | rows << 27, head
-    float* tile_part; float2* tile_stat;      // kv_attend_tiles_kernel: per piece, its rows
-    float* part; float2* stat;    // per workgroup two pieces of 16 rows (of a unit that began before its share, of one that begins in it): averages; maximum, sum
-};
 
 // channels c .. c + 3 of a row of the outputs
 __device__ __forceinline__ void store4(float* out, int c, const AttendArgs& a, f4 v) {

@@ -402,6 +402,50 @@ __device__ __forceinline__ bool find_unit(const AttendArgs& a, int x, TilesUnit&
     return u.cut < u.n_cuts;
 }
 
+// Trees of drafted tokens: all rows of a sequence see as many tiles, and where units are fewer than compute units they are cut into pieces of at most `share` tiles, the least (in steps of an eighth) with which
+// there are no more pieces than compute units: a piece more would begin when the others end.  16 trees of 32 tokens behind 1000 to 8000 others, 64 / 8 heads: 197 us,
+// and 263 with some 340 pieces.
+constexpr int TREE_PIECES = TILES_TARGET;      // no call has more where units are cut
+__device__ __forceinline__ Span tree_span(const KvSeq& s, const AttendArgs& a) {
+    return Span{a.window ? max(s.len - s.n - a.window, 0) : 0, max(min(s.len, a.q.room), 0)};
+}
+__device__ __forceinline__ int tree_tiles(const KvSeq& s, const AttendArgs& a) { const Span p = tree_span(s, a); return max((p.hi + TILE - 1) / TILE - p.lo / TILE, 1); }
+template <int RT>
+__device__ __forceinline__ bool find_tree_unit(const AttendArgs& a, int x, TilesUnit& u) {
+    const int lane = threadIdx.x & 63;
+    KvSeq head{0, 0, 0};
+    int units = 0;
+    long long tiles = 0;
+    for (int i = lane; i < a.q.n_seqs; i += 64) {
+        const KvSeq e = kv_sequence(a.q, i);
+        if (i < 64) head = e;
+        const int mine = unit_rows<RT>(e, a);
+        units += mine;
+        if (mine) tiles += (long long)mine * tree_tiles(e, a);
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) { units += __shfl_xor(units, o, 64); tiles += __shfl_xor(tiles, o, 64); }
+    const long long all = (long long)__builtin_amdgcn_readfirstlane(units) * a.g.heads;
+    if (all == 0) return false;
+    long long share = all >= TILES_TARGET ? 1LL << 40 : max((tiles * a.g.heads + TILES_TARGET - 1) / TILES_TARGET, 4LL);
+    auto cuts = [&](const KvSeq& e) { return (int)((tree_tiles(e, a) + share - 1) / share); };
+    while (all < TILES_TARGET) {      // (with a share of the longest sequence's tiles there are as many pieces as units: it ends)
+        long long pieces = 0;
+        for (int i = lane; i < a.q.n_seqs; i += 64) { const KvSeq e = i < 64 ? head : kv_sequence(a.q, i); const int mine = unit_rows<RT>(e, a); if (mine) pieces += (long long)mine * cuts(e); }
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) pieces += __shfl_xor(pieces, o, 64);
+        if (pieces * a.g.heads <= TILES_TARGET) break;
+        share += share / 8 + 1;
+    }
+    long long at = x;
+    if (!kv_find(a.q, head, [&](const KvSeq& e) { const int mine = unit_rows<RT>(e, a); return mine ? (long long)mine * a.g.heads * cuts(e) : 0LL; }, at, u.b, u.s)) return false;
+    u.n_cuts = __builtin_amdgcn_readfirstlane(cuts(u.s));
+    const int item = __builtin_amdgcn_readfirstlane((int)at), unit = item / u.n_cuts;
+    u.cut = item - unit * u.n_cuts;
+    u.h = unit % a.g.heads; u.tile = unit / a.g.heads;
+    return true;
+}
+
 __device__ __forceinline__ f16v mma32(h8 a, h8 b, f16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 
 __device__ __forceinline__ float across_halves(float v) {      // maximum of lanes l and l ^ 32
@@ -432,7 +476,7 @@ __device__ __forceinline__ void operands_ahead() {
     __builtin_amdgcn_sched_group_barrier(0x8, AHEAD, 0);
 }
 
-template <int DP, bool WIDE>      // WIDE: pages of 64 tokens and more, a tile lies in one
+template <int DP, bool WIDE, bool TREE>      // WIDE: pages of 64 tokens and more, a tile lies in one; TREE: a row sees of its sequence's new tokens those that its mask names
 __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_tiles_kernel(AttendArgs a) {
     constexpr int W = waves<DP>(), RT = 32 * W, KS = DP / 16, CT = DP / 32, PIECES = 4 * DP, PP = (PIECES + 64 * W - 1) / (64 * W);      // 16-byte pieces of a tile of K (and of V), per thread
     constexpr bool EVEN = PIECES % (64 * W) == 0;
@@ -442,10 +486,15 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
     unsigned char* const vbuf = lds + 2 * TILE * KROW;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5, i16 = lane & 15;
     TilesUnit u;
-    if (!find_unit<RT>(a, blockIdx.x, u)) return;
+    const bool any = TREE ? find_tree_unit<RT>(a, blockIdx.x, u) : find_unit<RT>(a, blockIdx.x, u);
+    if constexpr (TREE) {      // for the join: pieces of the unit that this is the first one of, where its rows are
+        if (tid == 0 && blockIdx.x < TREE_PIECES)
+            a.tile_info[blockIdx.x] = any && u.cut == 0 ? make_int4(u.n_cuts, u.s.start, u.tile * RT, u.h | (min(RT, u.s.n * a.rep - u.tile * RT) - 1) << 16) : make_int4(0, 0, 0, 0);
+    }
+    if (!any) return;
     const KvSeq s = u.s;
     const int h = u.h, r0 = u.tile * RT, n_rows = min(RT, s.n * a.rep - r0);
-    const Span span = row_span(s, a, r0, n_rows);
+    const Span span = TREE ? tree_span(s, a) : row_span(s, a, r0, n_rows);
     const int end = min(s.len, a.q.room);
     int lo, hi;      // tokens of this piece: whole tiles, the last one up to hi
     {
@@ -458,12 +507,14 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
     const int w0 = wave * 32, w_rows = min(max(n_rows - w0, 0), 32);
     const bool row_live = col < w_rows;
     const int r = r0 + w0 + (row_live ? col : 0), tok = r / a.rep, pos = row_live ? s.len - s.n + tok : -1;
+    const unsigned* const mask = TREE ? a.tree + (long long)(s.start + tok) * a.tree_words : nullptr;
     // tiles that the wavefront's rows see anything of, and places that all of them see
     int see0 = 0, see1 = 0, all0 = 0, all1 = -1;
     if (w_rows) {
-        const Span mine = row_span(s, a, r0 + w0, w_rows);
+        const Span mine = TREE ? span : row_span(s, a, r0 + w0, w_rows);
         see0 = max(mine.lo - lo, 0) / TILE; see1 = min((mine.hi - lo + TILE - 1) / TILE, n_tiles);
         all0 = a.window ? s.len - s.n + (r0 + w0 + w_rows - 1) / a.rep - a.window + 1 : 0; all1 = min(s.len - s.n + (r0 + w0) / a.rep, end - 1);
+        if constexpr (TREE) { all0 = a.window ? s.len - a.window : 0; all1 = min(s.len - s.n, end) - 1; }
         if (w_rows < 32) all1 = -1;
     }
     see0 = __builtin_amdgcn_readfirstlane(see0); see1 = __builtin_amdgcn_readfirstlane(see1); all0 = __builtin_amdgcn_readfirstlane(all0); all1 = __builtin_amdgcn_readfirstlane(all1);
@@ -632,6 +683,31 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
     // (e_wave is at most 2^100 below the largest bound); what lies further below, if anything does, loses bits
     int e_wave = -126 + SPARE, d = 0;
     float limit = 0.f;                     // the least bound of a row
+    // places 32 k + 16 (i / 8) + i % 8 + 8 half of the tile at t0 that this row of a tree sees, a bit each
+    auto tree_sees = [&](int t0) {
+        const int before = s.len - s.n;
+        unsigned seen = 0;
+        if (pos < 0) return seen;
+        int low = 0;
+        if (a.window) {
+            int bits = 0;
+            for (int i = 0; i < a.tree_words && 32 * i < s.n; ++i) bits += __popc(mask[i] & (s.n - 32 * i >= 32 ? ~0u : (1u << (s.n - 32 * i)) - 1));
+            low = before + bits - a.window;
+        }
+        auto below = [](int n) { return n <= 0 ? 0u : n >= 8 ? 0xffu : (1u << n) - 1; };
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int t = t0 + 32 * (g >> 1) + 16 * (g & 1) + 8 * half, j = t - before;
+            unsigned b = below(min(before, end) - t) & ~below(low - t);
+            if (j > -8 && j < s.n) {
+                auto word = [&](int i) { return i >= 0 && i < a.tree_words ? mask[i] : 0u; };
+                const unsigned long long two = word(j >> 5) | (unsigned long long)word((j >> 5) + 1) << 32;
+                b |= (unsigned)(two >> (j & 31)) & below(end - t) & ~below(-j);
+            }
+            seen |= b << 8 * g;
+        }
+        return seen;
+    };
     // operands in LDS
     constexpr int M = permuted<DP>();
     auto k_piece = [&](int buf, int k, int c) {
@@ -680,6 +756,7 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
             unroll<32>([&](auto I) { constexpr int i = I; sc[i >> 4][i & 15] *= row_lane<i & 15>(sk[i >> 4]); p[i] = ex2(fmaf(sc[i >> 4][i & 15], own, (float)d - m)); part[i & 3] += p[i]; });
             float sum = __builtin_amdgcn_ldexpf((part[0] + part[1]) + (part[2] + part[3]), -d);
             const float s_most = fmaxf(gv[0], gv[1]);
+            unsigned tree_bits = ~0u;
             const bool all = t0 >= all0 && t0 + TILE - 1 <= all1 && there == 15u;
             if (!all || __any(sum > MOST || s_most >= limit)) {
                 // places 32 k + 16 (i / 8) + i % 8 from first_seen on, seen of them, are seen by this row
@@ -687,10 +764,11 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
                 asm("" : "+v"(at));      // (what follows from it is not kept in registers from the start on)
                 const int low = a.window ? at - a.window + 1 : 0, first_seen = low - t0 - 8 * half;
                 const unsigned seen = (unsigned)max(min(at, end - 1) - low + 1, 0), gone = ~there;
+                if constexpr (TREE) tree_bits = all && row_live ? ~0u : tree_sees(t0);
                 float top = -__builtin_inff();
 #pragma unroll
                 for (int i = 0; i < 32; ++i) {
-                    if ((unsigned)(32 * (i >> 4) + 16 * (i >> 3 & 1) + (i & 7) - first_seen) >= seen || (gone >> (i >> 3) & 1)) sc[i >> 4][i & 15] = -__builtin_inff();
+                    if ((TREE ? !(tree_bits >> i & 1) : (unsigned)(32 * (i >> 4) + 16 * (i >> 3 & 1) + (i & 7) - first_seen) >= seen) || (gone >> (i >> 3) & 1)) sc[i >> 4][i & 15] = -__builtin_inff();
                     top = fmaxf(top, sc[i >> 4][i & 15]);
                 }
                 const float to = fmaxf(m, across_halves(top) * own);      // (-inf where nothing has been seen)
@@ -733,7 +811,7 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
                 const unsigned seen = (unsigned)max(min(at, end - 1) - low + 1, 0), gone = ~there;
 #pragma unroll
                 for (int i = 0; i < 32; ++i)
-                    if ((unsigned)(32 * (i >> 4) + 16 * (i >> 3 & 1) + (i & 7) - first_seen) >= seen || (gone >> (i >> 3) & 1)) p[i] = 0.f;
+                    if ((TREE ? !(tree_bits >> i & 1) : (unsigned)(32 * (i >> 4) + 16 * (i >> 3 & 1) + (i & 7) - first_seen) >= seen) || (gone >> (i >> 3) & 1)) p[i] = 0.f;
             }
 #pragma unroll
             for (int k = 0; k < 4; ++k)
@@ -824,6 +902,35 @@ __global__ __launch_bounds__(256) void kv_attend_tiles_join_kernel(AttendArgs a)
     }
 }
 
+// the same for trees: a lane group per row of the unit whose first piece this is
+template <int DP, int RT>
+__global__ __launch_bounds__(256) void kv_tree_tiles_join_kernel(AttendArgs a) {
+    constexpr int LANES = DP / 4, GROUPS = 64 / LANES;
+    const int4 info = a.tile_info[blockIdx.x];
+    const int n_cuts = info.x, n_rows = (info.w >> 16) + 1, h = info.w & 0xffff, lane = threadIdx.x & 63, c = 4 * (lane % LANES), group = lane / LANES;
+    if (n_cuts < 2 || group >= GROUPS || c >= a.g.dh) return;
+    for (int rr = (blockIdx.y * 4 + (threadIdx.x >> 6)) * GROUPS + group; rr < n_rows; rr += 4 * gridDim.y * GROUPS) {
+        const long long first = (long long)blockIdx.x * RT + rr;
+        float top = -__builtin_inff(), sum = 0.f;
+#pragma unroll 4
+        for (int i = 0; i < n_cuts; ++i) top = fmaxf(top, a.tile_stat[first + (long long)i * RT].x);
+        f4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int i = 0; i < n_cuts; ++i) {
+            const long long at = first + (long long)i * RT;
+            const float2 st = a.tile_stat[at];
+            const f4 part = *(const f4*)(a.tile_part + at * DP + c);
+            const float w = st.x == -__builtin_inff() ? 0.f : ex2(st.x - top) * st.y, more = sum + w;      // (averages all the way: the weighted sums of the largest values leave fp32)
+            const float of = more == 0.f ? 0.f : 1.f / more;
+            v = v * (sum * of) + part * (w * of);
+            sum = more;
+        }
+        const int row = info.z + rr, tk = row / a.rep;
+        bf16* const out = (bf16*)a.O + (long long)(info.y + tk) * a.ldo + (long long)(h * a.rep + row - tk * a.rep) * a.g.dh;
+        store4(out, c, a, v);
+    }
+}
+
 int shares(int dp) { return 256 * (dp == 32 ? resident<32>() : dp == 64 ? resident<64>() : dp <= 128 ? resident<128>() : resident<256>()); }
 int unit_rows_of(int dp) { return 32 * (dp <= 128 ? waves<128>() : waves<256>()); }
 // Calls whose units of 16 rows, by what the host knows, are few and short: the rows' kernel alone.  Two units (or a few of three) per workgroup of it are done before a tiles' workgroup has gone
@@ -866,11 +973,11 @@ int attend_tiles(tboa_ctx* ctx, const AttendArgs& a, long long units) {
     const dim3 grid((unsigned)std::max<long long>(units, TILES_TARGET)), block(64 * waves<DP>());
     const unsigned cut = (unsigned)std::min<long long>(units, TILES_TARGET / 2);      // units that may be cut
     if (a.g.pt_log >= 6) {
-        TB_HIP(ctx, hipFuncSetAttribute((const void*)kv_attend_tiles_kernel<DP, true>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
-        hipLaunchKernelGGL((kv_attend_tiles_kernel<DP, true>), grid, block, LDS, ctx->stream, a);
+        TB_HIP(ctx, hipFuncSetAttribute((const void*)kv_attend_tiles_kernel<DP, true, false>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
+        hipLaunchKernelGGL((kv_attend_tiles_kernel<DP, true, false>), grid, block, LDS, ctx->stream, a);
     } else {
-        TB_HIP(ctx, hipFuncSetAttribute((const void*)kv_attend_tiles_kernel<DP, false>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
-        hipLaunchKernelGGL((kv_attend_tiles_kernel<DP, false>), grid, block, LDS, ctx->stream, a);
+        TB_HIP(ctx, hipFuncSetAttribute((const void*)kv_attend_tiles_kernel<DP, false, false>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
+        hipLaunchKernelGGL((kv_attend_tiles_kernel<DP, false, false>), grid, block, LDS, ctx->stream, a);
     }
     TB_KERNEL_CHECK(ctx);
     hipLaunchKernelGGL((kv_attend_tiles_join_kernel<DP, 32 * waves<DP>()>), dim3(cut, (unsigned)std::min<long long>(std::max(2048u / cut, 1u), 8 * waves<DP>())), dim3(256), 0, ctx->stream, a);
@@ -894,7 +1001,46 @@ int attend(tboa_ctx* ctx, const AttendArgs& a, bool rows, long long units) {
     }
 }
 
+template <int DP>
+int attend_tree_tiles(tboa_ctx* ctx, const AttendArgs& a, long long units) {
+    constexpr int LDS = tiles_lds<DP>(), RT = 32 * waves<DP>();
+    const dim3 grid((unsigned)std::max<long long>(units, TREE_PIECES)), block(64 * waves<DP>());
+    if (a.g.pt_log >= 6) {
+        TB_HIP(ctx, hipFuncSetAttribute((const void*)kv_attend_tiles_kernel<DP, true, true>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
+        hipLaunchKernelGGL((kv_attend_tiles_kernel<DP, true, true>), grid, block, LDS, ctx->stream, a);
+    } else {
+        TB_HIP(ctx, hipFuncSetAttribute((const void*)kv_attend_tiles_kernel<DP, false, true>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
+        hipLaunchKernelGGL((kv_attend_tiles_kernel<DP, false, true>), grid, block, LDS, ctx->stream, a);
+    }
+    TB_KERNEL_CHECK(ctx);
+    hipLaunchKernelGGL((kv_tree_tiles_join_kernel<DP, RT>), dim3(TREE_PIECES, 16), dim3(256), 0, ctx->stream, a);      // (pieces behind those are of units that are not cut)
+    TB_KERNEL_CHECK(ctx);
+    return 0;
+}
+
 }  // namespace
+
+size_t kv_tree_tiles_room(const KvGeometry& g, AttendArgs* a, void* ws) {
+    const size_t rows = (size_t)TREE_PIECES * unit_rows_of(g.dp);
+    Arena ar(ws);
+    float* part = ar.get<float>(rows * g.dp);
+    float2* stat = ar.get<float2>(rows);
+    int4* info = ar.get<int4>(TREE_PIECES);
+    if (a) { a->tile_part = part; a->tile_stat = stat; a->tile_info = info; }
+    return ar.off;
+}
+bool kv_tree_tiles_takes(const KvGeometry& g, int n_seqs, long long n_tokens, int rep) { return most_units(g, n_seqs, n_tokens, rep) < (1LL << 32) / (2 * unit_rows_of(g.dp)); }
+int kv_tree_tiles(tboa_ctx* ctx, const AttendArgs& a) {
+    const long long units = most_units(a.g, a.q.n_seqs, a.q.n_tokens, a.rep);
+    switch (a.g.dp) {
+        case 32: return attend_tree_tiles<32>(ctx, a, units);
+        case 64: return attend_tree_tiles<64>(ctx, a, units);
+        case 96: return attend_tree_tiles<96>(ctx, a, units);
+        case 128: return attend_tree_tiles<128>(ctx, a, units);
+        case 192: return attend_tree_tiles<192>(ctx, a, units);
+        default: return attend_tree_tiles<256>(ctx, a, units);
+    }
+}
 
 extern "C" size_t tboa_kv_cache_attention_workspace_bytes(const tboa_kv_cache_desc* desc, int n_q_heads, int n_seqs, int64_t n_tokens) {
     KvGeometry g;

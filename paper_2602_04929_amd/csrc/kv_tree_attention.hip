@@ -32,7 +32,7 @@ __device__ __forceinline__ Cut cut_of(const KvSeq& s, const AttendArgs& a) {
 }
 template <int RW>
 __device__ __forceinline__ long long steps_of(const KvSeq& s, const AttendArgs& a) {
-    if (s.n == 0) return 0;
+    if (s.n == 0 || s.n * a.rep > a.few) return 0;
     const Cut c = cut_of<RW>(s, a);
     return (long long)c.blocks * a.g.heads * c.steps;
 }
@@ -42,6 +42,8 @@ __device__ __forceinline__ unsigned below(int n) { return n <= 0 ? 0u : n >= 16 
 // that list; pieces of units that lie in several shares go to kv_tree_join_kernel.  A wavefront has U times 16 rows: levels are made into half once for all of them.
 // S^T = K Q^T with tile i's row 4 g + j of the matrix instruction being token 16 g + 4 i + j: lane group g then holds the probabilities of tokens 16 g .. 16 g + 15 for row lane % 16, which are
 // the right operand of O^T += V^T P^T as they stand.
+// Bound by the vector instructions that make levels into half and the softmax, with too few wavefronts (registers) to hide them: 8 trees of up to 64 tokens behind up to 4000 others, 32 heads of 128, a row a token:
+// 114 us and 10 for the join; the levels take 24 at the rate of memory.
 template <typename T, int DP, int U>
 __global__ __launch_bounds__(256, resident<DP>()) void kv_tree_kernel(AttendArgs a) {
     constexpr int NT = sizeof(T) == 2 ? 1 : 2, RW = 16 * U;      // half terms of queries and of probabilities; rows of a wavefront
@@ -380,21 +382,24 @@ __global__ __launch_bounds__(256) void kv_tree_join_kernel(AttendArgs a) {
 int wave_units(const KvGeometry& g, int dtype, long long rows) { return dtype == TBOA_BF16 && g.dp <= 128 && rows > 16 ? 2 : 1; }
 int piece_rows(int units, long long rows) { const int rw = 16 * units; return rows <= rw ? rw : rows <= 2 * rw ? 2 * rw : 4 * rw; }
 int shares(const KvGeometry& g) { return 256 * (g.dp <= 128 ? 2 : 1); }
-size_t room(const KvGeometry& g, int rows_of_piece, AttendArgs* a, void* ws) {
+// Rows of a bf16 sequence up to which it is this kernel's; with more the kernel for many rows of kv_attention.hip takes it, whose eight wavefronts share the levels that it makes into half.
+// Both kernels, joins included, 64 / 8 heads of 128: one tree of 16 tokens (128 rows) behind 500 others 35 us here and 27 there, 16 trees of up to 32 behind up to 8000 337 and 219.
+constexpr int FEW = 64;
+size_t room(const KvGeometry& g, int rows_of_piece, bool tiles, AttendArgs* a, void* ws) {
     const size_t n = (size_t)shares(g);
     Arena ar(ws);
     float* part = ar.get<float>(2 * n * rows_of_piece * g.dp);
     float2* stat = ar.get<float2>(2 * n * rows_of_piece);
     int4* info = ar.get<int4>(n);
     if (a) { a->part = part; a->stat = stat; a->info = info; a->piece_rows = rows_of_piece; }
-    return ar.off;
+    return ar.off + (tiles ? kv_tree_tiles_room(g, a, a ? (char*)ws + ar.off : nullptr) : 0);
 }
 
 template <typename T, int DP, int U>
 int launch(tboa_ctx* ctx, const AttendArgs& a) {
     hipLaunchKernelGGL((kv_tree_kernel<T, DP, U>), dim3(256 * resident<DP>()), dim3(256), 0, ctx->stream, a);
     TB_KERNEL_CHECK(ctx);
-    hipLaunchKernelGGL((kv_tree_join_kernel<T, DP>), dim3(256 * resident<DP>(), std::min(a.piece_rows / 4, 8)), dim3(256), 0, ctx->stream, a);
+    hipLaunchKernelGGL((kv_tree_join_kernel<T, DP>), dim3(256 * resident<DP>(), std::min(a.piece_rows / 4, 16)), dim3(256), 0, ctx->stream, a);
     TB_KERNEL_CHECK(ctx);
     return 0;
 }
@@ -422,7 +427,7 @@ extern "C" size_t tboa_kv_cache_tree_attention_workspace_bytes(const tboa_kv_cac
     if (!kv_geometry(desc, g) || n_q_heads <= 0 || n_q_heads > 65535 || n_q_heads % g.heads || n_seqs < 0 || n_seqs > 1 << 20 || n_tokens < 0 || n_tokens > 1 << 24) return 0;
     if (n_seqs == 0 || n_tokens == 0) return 0;
     const long long rows = n_tokens * (n_q_heads / g.heads);
-    return room(g, piece_rows(wave_units(g, TBOA_BF16, rows), rows), nullptr, nullptr);
+    return std::max(room(g, piece_rows(wave_units(g, TBOA_F32, rows), rows), false, nullptr, nullptr), room(g, piece_rows(wave_units(g, TBOA_BF16, rows), rows), rows > FEW, nullptr, nullptr));
 }
 
 extern "C" int tboa_kv_cache_tree_attention(tboa_ctx* ctx, const tboa_kv_cache_desc* desc, const tboa_kv_batch* batch, int n_q_heads, int dtype, const void* Q, int64_t ldq,
@@ -444,7 +449,8 @@ extern "C" int tboa_kv_cache_tree_attention(tboa_ctx* ctx, const tboa_kv_cache_d
     KvDevice dev(ctx->device);
     const long long rows = (batch->max_new > 0 ? std::min<long long>(batch->max_new, batch->n_tokens) : batch->n_tokens) * rep;
     const int units = wave_units(g, dtype, rows), of_piece = piece_rows(units, rows);
-    TB_TRY(tboa_ws_reserve(ctx, room(g, of_piece, nullptr, nullptr)));
+    const bool tiles = dtype == TBOA_BF16 && rows > FEW && kv_tree_tiles_takes(g, batch->n_seqs, batch->n_tokens, rep);
+    TB_TRY(tboa_ws_reserve(ctx, room(g, of_piece, tiles, nullptr, nullptr)));
     AttendArgs a{};
     a.g = g;
     a.q = KvBatch{batch->n_seqs, batch->pages_per_seq, (int)batch->n_tokens, batch->pages_per_seq * desc->page_tokens, batch->starts, batch->lens, batch->pages};
@@ -454,6 +460,10 @@ extern "C" int tboa_kv_cache_tree_attention(tboa_ctx* ctx, const tboa_kv_cache_d
     a.vec = g.dh % 8 == 0 && ((uintptr_t)Q & 15) == 0 && ldq * size % 16 == 0 ? 8 : g.dh % 4 == 0 && ldq % 4 == 0 && ((uintptr_t)Q & (4 * size - 1)) == 0 ? 4 : 0;
     a.out_piece = g.dh % 8 == 0 && ldo % 8 == 0 && ((uintptr_t)O & 15) == 0 ? 8 : g.dh % 4 == 0 && ldo % 4 == 0 && ((uintptr_t)O & (4 * size - 1)) == 0 ? 4 : 1;
     a.tree = tree; a.tree_words = tree_words;
-    room(g, of_piece, &a, ctx->ws);
+    const bool all = tiles && batch->n_seqs == 1;      // one sequence: whatever its rows, one kernel
+    a.few = all ? 0 : tiles ? FEW : 1 << 30;
+    room(g, of_piece, tiles, &a, ctx->ws);
+    if (tiles) TB_TRY(kv_tree_tiles(ctx, a));
+    if (all) return 0;
     return dtype == TBOA_F32 ? launch<float>(ctx, a, units) : launch<bf16>(ctx, a, units);
 }

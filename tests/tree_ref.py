@@ -31,7 +31,8 @@ def attention(cache, starts, lens, pages, q, bits, scale, window, dtype):
                       difference to the maximum; the exponential 2^-22.  Of every token, in the numerator and in the sum
       probabilities   times scale, in two halves 2^-22; in one 2^-11 (bf16)
       sums            (n + 8) 2^-24, twice, n tokens
-      next to nothing a half below 2^-14 is off by 2^-25 whatever it is; the largest probability times scale of the row is at least 2^14 as half: 2^-39 of it for every token, times at most 255 levels
+      next to nothing a half below 2^-14 is off by 2^-25 whatever it is; the largest probability times scale of the row is at least 2^14 as half (2^-1 for bf16
+                      sequences, or a call for one sequence, of more than 64 rows, the kernel for many rows): 2^-39 (2^-24) of it for every token, times at most 255 levels
       output          half a step of the type"""
     q = q.double().cpu()
     rows, hq, dh = q.shape
@@ -78,7 +79,7 @@ def attention(cache, starts, lens, pages, q, bits, scale, window, dtype):
             apart = torch.where(a > 0, (x - x.masked_fill(~seen, -torch.inf).amax(1, keepdim=True)).abs(), 0.0)
             e = a * ((dh + 4 + 8 * (dtype == torch.float32)) * 2.0 ** -24 * big + 2 * 2.0 ** -24 * apart + 2.0 ** -22)
             e = torch.where(seen, e, 0.0)
-            low = count * 255 * 2.0 ** -39 * (a * s[None]).amax(1, keepdim=True)
+            low = count * 255 * 2.0 ** (-24 if dtype == torch.bfloat16 and (n * rep > 64 or (len(lens) == 1 and rows * rep > 64)) else -39) * (a * s[None]).amax(1, keepdim=True)
             lim[r, h] = torch.finfo(dtype).eps / 2 * o.abs() + 1.01 * (e @ v.abs() + e.sum(1, keepdim=True) * o.abs() + (halves + 2 * (count + 8) * 2.0 ** -24) * (a @ v.abs()) + low) + 2.0 ** -133
     return out, lim
 
