@@ -43,7 +43,7 @@ __device__ __forceinline__ unsigned below(int n) { return n <= 0 ? 0u : n >= 16 
 // S^T = K Q^T with tile i's row 4 g + j of the matrix instruction being token 16 g + 4 i + j: lane group g then holds the probabilities of tokens 16 g .. 16 g + 15 for row lane % 16, which are
 // the right operand of O^T += V^T P^T as they stand.
 // Bound by the vector instructions that make levels into half and the softmax, with too few wavefronts (registers) to hide them: 8 trees of up to 64 tokens behind up to 4000 others, 32 heads of 128, a row a token:
-// 114 us and 10 for the join; the levels take 24 at the rate of memory.
+// 114 us and 10 for the join; the levels take 37 at the rate of memory.
 template <typename T, int DP, int U>
 __global__ __launch_bounds__(256, resident<DP>()) void kv_tree_kernel(AttendArgs a) {
     constexpr int NT = sizeof(T) == 2 ? 1 : 2, RW = 16 * U;      // half terms of queries and of probabilities; rows of a wavefront

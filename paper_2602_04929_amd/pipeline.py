@@ -6,6 +6,8 @@ import time
 
 import torch
 
+from .binding import PackedWeight
+
 
 def make_side_contexts(n=2):
     """Contexts on fresh streams (default priority) for layers that may run beside the main context's work."""
@@ -224,16 +226,44 @@ def quantize_mlp(ctx, mlp, cfg, alpha=0.25, use_R=True, cd_iters=1, adaptive_gri
     return out
 
 
-def serve_attention_block(ctx, weights, X, cache, batch, n_q_heads, rotation=None, positions=None, norm_q=None, norm_k=None, eps=1e-6, scale=0.0, window=0, residual=None):
+def pack_attention_block(ctx, quantized, bits, group=0):
+    """Wqkv and Wo of a result of quantize_attention_block as PackedWeights, for serve_attention_block."""
+    qkv = {n: torch.cat([quantized[l][n] for l in "qkv"]) for n in ("codes", "scales", "zeros")}
+    return dict(Wqkv=PackedWeight.of(ctx, qkv, bits, group), Wo=PackedWeight.of(ctx, quantized["o"], bits, group))
+
+
+def pack_mlp(ctx, quantized, bits, group=0):
+    """Wg, Wu and Wd of a result of quantize_mlp as PackedWeights, for serve_mlp."""
+    return {w: PackedWeight.of(ctx, quantized[n], bits, group) for w, n in (("Wg", "gate"), ("Wu", "up"), ("Wd", "down"))}
+
+
+def _product(ctx, X, W, residual=None):
+    return ctx.packed_linear(W, X, residual=residual) if isinstance(W, PackedWeight) else ctx.linear_forward(X, W, residual=residual)
+
+
+def serve_mlp(ctx, weights, X, residual=None):
+    """The gated MLP for X [tokens, d_model]: act = silu(X Wg^T) * (X Wu^T), Y = act Wd^T (+ residual).
+
+    weights: dict with Wg, Wu and Wd, PackedWeights (pack_mlp) or quantize_mlp's dequantized matrices.  Returns a dict: Y and act.  With PackedWeights it can be captured into a graph."""
+    gate, up = weights["Wg"], weights["Wu"]
+    act = ctx.packed_swiglu(gate, up, X) if isinstance(gate, PackedWeight) else ctx.swiglu_forward(X, gate, up)
+    return dict(Y=_product(ctx, act, weights["Wd"], residual), act=act)
+
+
+def serve_attention_block(ctx, weights, X, cache, batch, n_q_heads, rotation=None, positions=None, norm_q=None, norm_k=None, eps=1e-6, scale=0.0, window=0, residual=None, tree=None):
     """The attention block with its weights quantized and its keys and values in a quantized cache, for the new tokens X [tokens, d_model] of a ragged batch (prompts, single tokens or both):
     projections -> norms and rotation -> append -> attention over the cache -> output projection (+ residual).
 
-    weights: dict with Wqkv = [W_Q; W_K; W_V] and Wo, as quantize_attention_block's dequantized matrices; rotation by int32 positions [tokens]; norm_q, norm_k: fp32 [head_dim] weights of the
+    weights: dict with Wqkv = [W_Q; W_K; W_V] and Wo, PackedWeights (pack_attention_block) or quantize_attention_block's dequantized matrices; rotation by int32 positions [tokens]; norm_q, norm_k: fp32 [head_dim] weights of the
     norms of every head's query and key.  Keys without a norm are rotated by the append itself, on unrounded values.  Returns a dict: Y [tokens, d_model], and q, k, v, o on the way
     (k as it goes to the append).  Rows of X behind the last sequence go along: o is 0 there, and Y the residual.
-    The three serving calls can be captured into a graph; this block cannot where weights are fp32 and activations bf16 (linear_forward then waits for the host to learn the weights' form)."""
+    tree: int32 [tokens, words], for drafted tokens that branch (tree_masks; Context.kv_cache_tree_attention).  positions are then the depths behind what the cache had, not the places; the k and v
+    of the tokens that are accepted go to kv_cache_append once more, as the only new tokens, with lens that end behind them, and what the cache holds behind those is overwritten by the next step
+    (a grid of several tokens keeps what it grew to for tokens that were not accepted).
+    The serving calls can be captured into a graph, with PackedWeights this whole block; it cannot where weights are fp32 matrices and activations bf16 (linear_forward then waits for the host to
+    learn the weights' form)."""
     Hq, Hkv, dh = n_q_heads, cache.desc.n_kv_heads, cache.desc.head_dim
-    qkv = ctx.linear_forward(X, weights["Wqkv"]).view(X.shape[0], Hq + 2 * Hkv, dh)
+    qkv = _product(ctx, X, weights["Wqkv"]).view(X.shape[0], Hq + 2 * Hkv, dh)
     q, k, v = qkv[:, :Hq], qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:]
     in_append = rotation is not None and norm_k is None
     if rotation is not None or norm_q is not None or norm_k is not None:
@@ -242,6 +272,9 @@ def serve_attention_block(ctx, weights, X, cache, batch, n_q_heads, rotation=Non
     o = torch.empty(X.shape[0], Hq, dh, dtype=X.dtype, device=X.device)
     with torch.cuda.stream(ctx._stream):
         o.zero_()      # (attention does not write rows of no sequence)
-    ctx.kv_cache_attention(cache, batch, q, scale=scale, window=window, out=o)
-    Y = ctx.linear_forward(o.view(-1, Hq * dh), weights["Wo"], residual=residual)
+    if tree is None:
+        ctx.kv_cache_attention(cache, batch, q, scale=scale, window=window, out=o)
+    else:
+        ctx.kv_cache_tree_attention(cache, batch, q, tree, scale=scale, window=window, out=o)
+    Y = _product(ctx, o.view(-1, Hq * dh), weights["Wo"], residual)
     return dict(Y=Y, q=q, k=k, v=v, o=o)
