@@ -11,12 +11,13 @@ typedef unsigned u4 __attribute__((ext_vector_type(4)));
 
 struct PackedArgs {
     const uint32_t* w[2]; const float* scale[2]; const float* zero[2];      // two: gate and up
-    int d_out, d_in, words, group, n_groups;      // words of a row; channels of a group
+    int d_out, d_in, bits, words, group, n_groups;      // words of a row; channels of a group
     long long tokens;
     const void* X; long long ldx;
     const void* Res; long long ldr;
     void* Y; long long ldy;
     int vec, out_vec;      // rows of X may be read 16 bytes at a time, of Y written four elements at a time
+    float* partial; int splits;      // packed_few_kernel: parts of the channels that workgroups of their own have, and their sums [splits][tokens][d_out] (splits > 1)
     unsigned piece_magic, piece_all;      // packed_few_kernel: a group has 2^32 / piece_magic pieces of a run that share their scale (1: all), one where piece_all has all bits
 };
 
@@ -213,7 +214,7 @@ constexpr int most_waves() { return XR <= 16 && NR == 1 ? 16 : 8; }
 //     y += scale (sum (offset + code) x - (offset + zero) sum x)
 // fp32 X: codes less zeros, exact in bf16, times three bf16 terms.
 // Rows of codes, of X and of scales are read by four lanes side by side, 64 bytes together, and handed to the lanes that multiply them through the wavefront's own part of LDS: read by those lanes
-// themselves, a row each, every 16 bytes are an access of their own to the first cache (16 tokens of 8192 x 28672: 37 million accesses, 143000 cycles of every compute unit's, 67 us).
+// themselves, a row each, every 16 bytes are an access of their own to the first cache (16 tokens of 8192 x 28672: 37 million accesses, 143000 cycles of every compute unit's, 67 us and not 34).
 template <typename T, int BITS, int VW, int FF, int XR, int RT, bool GATED>
 __global__ __launch_bounds__((64 * most_waves<XR, (GATED ? 2 : 1) * RT>())) void packed_few_kernel(PackedArgs a) {
     typedef Codes<BITS, VW> C;
@@ -409,9 +410,9 @@ __global__ __launch_bounds__((64 * most_waves<XR, (GATED ? 2 : 1) * RT>())) void
         });
     };
     // P runs' loads are issued together; the wavefronts of a SIMD take turns
-    const int runs = (a.d_in + C::CK - 1) / C::CK, whole = a.vec ? a.d_in / C::CK : 0, each = (runs + waves - 1) / waves;
-    const int end = min((wave + 1) * each, runs);
-    int run = wave * each;
+    const int runs = (a.d_in + C::CK - 1) / C::CK, whole = a.vec ? a.d_in / C::CK : 0, each = (runs + waves * a.splits - 1) / (waves * a.splits), begin = min((blockIdx.z * waves + wave) * each, runs);
+    const int end = min(begin + each, runs);
+    int run = begin;
     Grids first;
     load_grids(group_of(run * NS), first);
     auto several = [&](auto N) {
@@ -421,7 +422,7 @@ __global__ __launch_bounds__((64 * most_waves<XR, (GATED ? 2 : 1) * RT>())) void
 #pragma unroll
             for (int i = 0; i < n; ++i) load(run + i, o[i], std::true_type());
             __builtin_amdgcn_sched_barrier(0);
-            if (run == wave * each) keep_grids(first);
+            if (run == begin) keep_grids(first);
 #pragma unroll
             for (int i = 0; i < n; ++i) multiply(run + i, o[i]);
         }
@@ -431,7 +432,7 @@ __global__ __launch_bounds__((64 * most_waves<XR, (GATED ? 2 : 1) * RT>())) void
     for (; run < end; ++run) {
         Run o;
         if (run < whole) load(run, o, std::true_type()); else load(run, o, std::false_type());
-        if (run == wave * each) keep_grids(first);
+        if (run == begin) keep_grids(first);
         multiply(run, o);
     }
     float* const part = (float*)lds;      // [wavefronts][NR][16][17]
@@ -453,6 +454,7 @@ __global__ __launch_bounds__((64 * most_waves<XR, (GATED ? 2 : 1) * RT>())) void
                     y[w] = 0.f;
                     for (int v = 0; v < waves; ++v) y[w] += part[((v * NR + w * RT + r) * 16 + row) * 17 + c];
                 }
+                if (!GATED && a.splits > 1) { a.partial[(blockIdx.z * a.tokens + m) * a.d_out + n] = y[0]; continue; }
                 float v = GATED ? silu(y[0]) * y[NW - 1] : y[0];
                 if (!GATED && a.Res) v += to_f32(((const T*)a.Res)[m * a.ldr + n]);
                 ((T*)a.Y)[m * a.ldy + n] = from_f32(v, T());
@@ -461,11 +463,43 @@ __global__ __launch_bounds__((64 * most_waves<XR, (GATED ? 2 : 1) * RT>())) void
     }
 }
 
+// sums of the splits' partial results, an output a thread
+template <typename T>
+__global__ __launch_bounds__(256) void packed_few_join_kernel(PackedArgs a) {
+    const int n = blockIdx.x * 256 + threadIdx.x;
+    const long long m = blockIdx.y;
+    if (n >= a.d_out) return;
+    float v = 0.f;
+#pragma unroll 4
+    for (int s = 0; s < a.splits; ++s) v += a.partial[(s * a.tokens + m) * a.d_out + n];
+    if (a.Res) v += to_f32(((const T*)a.Res)[m * a.ldr + n]);
+    ((T*)a.Y)[m * a.ldy + n] = from_f32(v, T());
+}
+
+// Parts of the channels for 33 to 64 tokens of bf16, whose X (64 rows of it go through every workgroup) allows a compute unit one workgroup of eight wavefronts at a time: the fewest with which rounds of
+// workgroups times runs of a wavefront is least, more of them for a fifth less (they are joined), each of at least 1024 channels.  64 tokens of 5120 x 13824, three bits: 320 workgroups of 16 outputs 61 us, 480 of 32
+// outputs and a third of the channels 34, and 4 for the join.
+int few_splits(const PackedArgs& a) {
+    if (a.tokens > 64) return 1;
+    const long long groups = cdiv64(a.d_out, 32), runs = cdiv64(a.d_in, a.bits == 2 ? 256 : 128);
+    const auto cost = [&](int s) { return cdiv64(groups * s, 256) * cdiv64(runs, 8 * s); };
+    int best = 1;
+    for (int s = 2; s <= 8 && s <= a.d_in / 1024; ++s)
+        if (cost(s) * 5 <= cost(best) * 4) best = s;
+    return best;
+}
+size_t few_room(const PackedArgs& a) { const int splits = few_splits(a); return splits > 1 ? (size_t)splits * a.tokens * a.d_out * sizeof(float) : 0; }
+
 template <typename T, int BITS, int VW, int FF, int XR, int RT, bool GATED>
 int launch_few(tboa_ctx* ctx, PackedArgs a) {
     typedef Codes<BITS, VW> C;
     constexpr int NR = GATED ? 2 * RT : RT, bytes = few_bytes<T, BITS, VW, XR, NR>();
-    const int runs = (a.d_in + C::CK - 1) / C::CK;
+    a.splits = XR == 64 && !GATED ? few_splits(a) : 1;
+    if (a.splits > 1) {
+        TB_TRY(tboa_ws_reserve(ctx, few_room(a)));
+        a.partial = (float*)ctx->ws;
+    }
+    const int runs = (a.d_in + C::CK - 1) / C::CK / a.splits + (a.splits > 1);      // (parts: eight wavefronts with a run each too)
     const int most = a.d_out > 16 * RT * 512 ? 8 : most_waves<XR, NR>();      // (workgroups that all find room at once)
     int waves = 4;
     while (waves < most && waves * 2 < runs && 2 * waves * bytes <= 160 * 1024) waves *= 2;
@@ -473,13 +507,18 @@ int launch_few(tboa_ctx* ctx, PackedArgs a) {
     magic(a.n_groups == 1 ? 0 : pieces, a.piece_magic, a.piece_all);
     const auto kernel = packed_few_kernel<T, BITS, VW, FF, XR, RT, GATED>;
     if (waves * bytes > 65536) TB_HIP(ctx, hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, waves * bytes));
-    hipLaunchKernelGGL(kernel, dim3((unsigned)cdiv64(a.d_out, 16 * RT), (unsigned)cdiv64(a.tokens, XR)), dim3(64 * waves), std::max(waves * bytes, waves * NR * 16 * 17 * 4), ctx->stream, a);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)cdiv64(a.d_out, 16 * RT), (unsigned)cdiv64(a.tokens, XR), a.splits), dim3(64 * waves), std::max(waves * bytes, waves * NR * 16 * 17 * 4), ctx->stream, a);
     TB_KERNEL_CHECK(ctx);
+    if (a.splits > 1) {
+        hipLaunchKernelGGL((packed_few_join_kernel<T>), dim3((unsigned)cdiv64(a.d_out, 256), (unsigned)a.tokens), dim3(256), 0, ctx->stream, a);
+        TB_KERNEL_CHECK(ctx);
+    }
     return 0;
 }
 template <typename T, int BITS, int VW, int FF, int XR, bool GATED>
 int launch_few(tboa_ctx* ctx, const PackedArgs& a) {
-    if constexpr (!GATED && XR > 4) { if (a.d_out >= 16 * 2 * 256) return launch_few<T, BITS, VW, FF, XR, 2, GATED>(ctx, a); }
+    if constexpr (!GATED && XR == 64) return launch_few<T, BITS, VW, FF, XR, 2, GATED>(ctx, a);
+    else if constexpr (!GATED && XR > 4) { if (a.d_out >= 16 * 2 * 256) return launch_few<T, BITS, VW, FF, XR, 2, GATED>(ctx, a); }
     return launch_few<T, BITS, VW, FF, XR, 1, GATED>(ctx, a);
 }
 template <typename T, int BITS, int VW, int FF, bool GATED>
@@ -1030,7 +1069,7 @@ bool good_weight(const tboa_packed_weight* w) {
 
 PackedArgs shape_of(const tboa_packed_weight& w) {
     PackedArgs a{};
-    a.d_out = w.d_out; a.d_in = w.d_in; a.words = (int)tboa_packed_words_per_row(w.d_in, w.bits);
+    a.d_out = w.d_out; a.d_in = w.d_in; a.bits = w.bits; a.words = (int)tboa_packed_words_per_row(w.d_in, w.bits);
     a.group = w.group ? w.group : w.d_in; a.n_groups = w.d_in / a.group;
     return a;
 }
@@ -1060,8 +1099,10 @@ int run(tboa_ctx* ctx, const char* who, const tboa_packed_weight* weight, const 
 }  // namespace
 
 extern "C" size_t tboa_packed_workspace_bytes(const tboa_packed_weight* weight, int64_t n_tokens, int dtype) {
-    if (!good_weight(weight) || (dtype != TBOA_F32 && dtype != TBOA_BF16) || n_tokens <= 64 || n_tokens > 1 << 24) return 0;
-    const PackedArgs p = shape_of(*weight);
+    if (!good_weight(weight) || (dtype != TBOA_F32 && dtype != TBOA_BF16) || n_tokens <= 32 || n_tokens > 1 << 24) return 0;
+    PackedArgs p = shape_of(*weight);
+    p.tokens = n_tokens;
+    if (n_tokens <= 64) return dtype == TBOA_BF16 ? few_room(p) : 0;
     if (!many_takes(p)) return 0;
     ManyArgs a{};
     return std::max(many_room(p, false, dtype == TBOA_F32 ? 4 : 2, std::min<long long>(n_tokens, MOST_ROWS), a, nullptr),

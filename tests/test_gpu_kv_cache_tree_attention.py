@@ -257,3 +257,50 @@ def test_refusals(ctx, lib):
         with pytest.raises(AssertionError):
             ctx.kv_cache_tree_attention(dev, batch, q, bad)
     assert ctx.kv_cache_tree_attention(dev, batch, q[:0], tree[:0]).shape == (0, 4, 64)
+
+
+@pytest.mark.parametrize("heads,rep,new,lens", [(1, 2, [40, 33, 70], [100, 90, 80]), (2, 8, [30], [79]), (3, 4, [25, 2, 0], [90, 60, 30])])
+def test_many_rows_whose_pages_are_not_there(ctx, lib, heads, rep, new, lens):
+    """bf16 trees of more rows than one workgroup of the kernel for few rows takes: pages outside the cache, and places beyond the row of pages, are invisible; a sequence without pages gets 0."""
+    starts, pages, cache, dev, q, bits = drafted(lib, heads, rep, 64, new, lens, 16, 1, torch.bfloat16, 22)
+    pages = pages[:, :5].copy()      # 80 places
+    pages[0, 1] = -1
+    if len(new) > 1:
+        pages[1, 0], pages[2, :] = len(cache.data), [-5, 1 << 30, -1, -1, -1]
+    got = ctx.kv_cache_tree_attention(dev, lib.KVBatch(i32(starts), i32(lens), i32(pages)), q, ref.as_words(bits).cuda())
+    torch.cuda.synchronize()
+    ref.check(got, cache, starts, lens, pages, q, bits, 1 / 8)
+    assert len(new) == 1 or (got[starts[2]:] == 0).all()
+
+
+def test_many_rows_strides_streams_and_offsets(ctx, lib):
+    """The same calls with queries inside a fused projection, outputs inside a wider tensor, a context on a stream of its own, pages beyond 2^32 bytes, and rows of no sequence left as they were."""
+    heads, rep, dh, pt = 4, 4, 128, 64
+    new, lens = [30, 2, 70], [470, 300, 3000]
+    starts, pages, cache, dev, q, bits = drafted(lib, heads, rep, dh, new, lens, pt, 1, torch.bfloat16, 33, spare_rows=4)
+    tree = ref.as_words(bits).cuda()
+    base = ctx.kv_cache_tree_attention(dev, lib.KVBatch(i32(starts), i32(lens), i32(pages)), q, tree, out=torch.full_like(q, 7))
+    torch.cuda.synchronize()
+    ref.check(base, cache, starts, lens, pages, q, bits, 1 / np.sqrt(dh))
+    assert (base[102:] == 7).all()
+    for shift in (0, 1, 4):
+        wide = torch.randn(106 * (heads * (rep + 2) + 1) * dh + shift, device="cuda").bfloat16()[shift:].view(106, heads * (rep + 2) + 1, dh)
+        wide[:, 1:1 + heads * rep] = q
+        out = torch.full((106 * (heads * rep + 5) * dh + shift,), 7.0, device="cuda", dtype=torch.bfloat16)[shift:].view(106, heads * rep + 5, dh)
+        ctx.kv_cache_tree_attention(dev, lib.KVBatch(i32(starts), i32(lens), i32(pages)), wide[:, 1:1 + heads * rep], tree, out=out[:, 2:2 + heads * rep])
+        torch.cuda.synchronize()
+        assert torch.equal(out[:, 2:2 + heads * rep], base) and (out[:, :2] == 7).all() and (out[:, 2 + heads * rep:] == 7).all()
+    per = dev.data.shape[1]
+    far = (1 << 32) // per + 50
+    big = torch.zeros(far + len(cache.data), per, dtype=torch.uint8, device="cuda")
+    big[far:] = dev.data
+    side = torch.cuda.Stream()
+    other = lib.Context(stream=side)
+    try:
+        side.wait_stream(torch.cuda.current_stream())
+        got = other.kv_cache_tree_attention(lib.KVCache(big, heads, dh, pt, 1), lib.KVBatch(i32(starts), i32(lens), i32(pages + far)), q, tree)
+        torch.cuda.current_stream().wait_stream(side)
+        torch.cuda.synchronize()
+        assert torch.equal(got[:102], base[:102])
+    finally:
+        other.close()

@@ -245,3 +245,24 @@ def test_refusals(ctx, lib):
         ctx.packed_linear(packed, x[:1].expand(3, 64))      # rows that overlap
     assert e.value.code == -1
     assert ctx.packed_linear(packed, x[:0]).shape == (0, 20) and ctx.packed_swiglu(packed, packed, x[:0]).shape == (0, 20)
+
+
+@pytest.mark.parametrize("tokens", [33, 64])
+@pytest.mark.parametrize("bits,group,d_in,d_out", [(4, 128, 8192, 100), (3, 128, 13824, 33), (2, 0, 9000, 4100), (8, 64, 2048, 8200), (4, 32, 3200, 640)])
+def test_channels_shared_by_workgroups(ctx, lib, bits, group, d_in, d_out, tokens):
+    """33 to 64 tokens, whose channels are split: results, the residual in its place, and no workspace beyond what is said to be needed."""
+    packed, w = ref.weight(lib, ctx, d_out, d_in, bits, group, 12)
+    x, res = rows(tokens, d_in, torch.bfloat16, 13), rows(tokens, d_out, torch.bfloat16, 14)
+    want, lim = x.double() @ w.T + res.double(), ref.bound(x, w, packed)
+    own = lib.Context()
+    try:
+        got = own.packed_linear(packed, x, residual=res)
+        torch.cuda.synchronize()
+        assert own.workspace_bytes() <= max(2 * own.packed_workspace_bytes(packed, tokens, torch.bfloat16), 1 << 20)
+        ref.check(got, want, lim + 2.0 ** -24 * (want.abs() + 2 * res.double().abs()))
+        out = res.clone()
+        own.packed_linear(packed, x, residual=out, out=out)
+        torch.cuda.synchronize()
+        assert torch.equal(out, got)
+    finally:
+        own.close()
