@@ -21,7 +21,8 @@ template <int RW>
 __device__ __forceinline__ Cut cut_of(const KvSeq& s, const AttendArgs& a) {
     Cut c;
     const int rows = s.n * a.rep;
-    c.wr = rows <= RW ? 1 : rows <= 2 * RW ? 2 : 4;
+    const int most = min(rows, a.piece_rows);      // (a caller's max_new that is too small leaves room for fewer: then there are more blocks)
+    c.wr = most <= RW ? 1 : most <= 2 * RW ? 2 : 4;
     c.wt = 4 / c.wr;
     c.blocks = (rows + RW * c.wr - 1) / (RW * c.wr);
     const int before = s.len - s.n, hi = min(s.len, a.q.room);

@@ -304,3 +304,14 @@ def test_many_rows_strides_streams_and_offsets(ctx, lib):
         assert torch.equal(got[:102], base[:102])
     finally:
         other.close()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("max_new", [1, 3, 9, 17])
+def test_sequences_of_more_new_tokens_than_told(ctx, lib, dtype, max_new):
+    """max_new chooses between kernels only: sequences of more new tokens get the same, within the workspace that was made for fewer."""
+    new, lens = [100, 3, 31, 0, 9], [900, 2000, 31, 50, 700]
+    starts, pages, cache, dev, q, bits = drafted(lib, 2, 4, 64, new, lens, 64, 1, dtype, 17)
+    got = ctx.kv_cache_tree_attention(dev, lib.KVBatch(i32(starts), i32(lens), i32(pages), max_new=max_new), q, ref.as_words(bits).cuda())
+    torch.cuda.synchronize()
+    ref.check(got, cache, starts, lens, pages, q, bits, 1 / 8)
