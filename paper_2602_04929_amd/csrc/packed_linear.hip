@@ -985,6 +985,12 @@ size_t many_room(const PackedArgs& p, bool gated, int size, long long tokens, Ma
     a.partial = ar.get<float>(a.splits > 1 ? (size_t)a.splits * cut * tm * 256 : 0);
     return ar.off;
 }
+// of all rounds of a call: the last one has fewer tokens and may still need more, where its tiles are split and those of a whole round are not
+size_t rounds_room(const PackedArgs& p, bool gated, int size, long long tokens) {
+    ManyArgs a{};
+    const size_t first = many_room(p, gated, size, std::min(tokens, MOST_ROWS), a, nullptr), last = tokens % MOST_ROWS;
+    return last ? std::max(first, many_room(p, gated, size, (long long)last, a, nullptr)) : first;
+}
 bool many_takes(const PackedArgs& p) { return (p.n_groups == 1 || p.group % 16 == 0) && p.words <= 1 << 21; }
 
 template <typename T, int BITS, bool ONE_SCALE, int TM, bool GATED>
@@ -1004,13 +1010,13 @@ int launch_many(tboa_ctx* ctx, const ManyArgs& a) {
 template <typename T, int BITS, bool GATED>
 int launch_many(tboa_ctx* ctx, const PackedArgs& p) {
     ManyArgs a{};
-    TB_TRY(tboa_ws_reserve(ctx, many_room(p, GATED, sizeof(T), std::min(p.tokens, MOST_ROWS), a, nullptr)));
+    TB_TRY(tboa_ws_reserve(ctx, rounds_room(p, GATED, sizeof(T), p.tokens)));
     for (long long at = 0; at < p.tokens; at += MOST_ROWS) {
         a.p = p;
         a.p.tokens = std::min(p.tokens - at, MOST_ROWS);
         a.p.X = (const T*)p.X + at * p.ldx; a.p.Y = (T*)p.Y + at * p.ldy;
         if (p.Res) a.p.Res = (const T*)p.Res + at * p.ldr;
-        many_room(p, GATED, sizeof(T), a.p.tokens, a, ctx->ws);
+        if (many_room(p, GATED, sizeof(T), a.p.tokens, a, ctx->ws) > ctx->ws_bytes) return tboa_fail(ctx, TBOA_ENOMEM, "a workspace of %zu bytes is too small", ctx->ws_bytes);
         const int units = p.group / 16;
         magic(p.n_groups == 1 ? 0 : units, a.unit_magic, a.unit_all);
         hipLaunchKernelGGL((packed_rows_kernel<T, BITS>), dim3((unsigned)(a.blocks + cdiv64((GATED ? 2LL : 1LL) * p.d_out, 16))), dim3(1024), 0, ctx->stream, a);
@@ -1106,9 +1112,8 @@ extern "C" size_t tboa_packed_workspace_bytes(const tboa_packed_weight* weight, 
     p.tokens = n_tokens;
     if (n_tokens <= 64) return dtype == TBOA_BF16 ? few_room(p) : 0;
     if (!many_takes(p)) return 0;
-    ManyArgs a{};
-    return std::max(many_room(p, false, dtype == TBOA_F32 ? 4 : 2, std::min<long long>(n_tokens, MOST_ROWS), a, nullptr),
-                    many_room(p, true, dtype == TBOA_F32 ? 4 : 2, std::min<long long>(n_tokens, MOST_ROWS), a, nullptr));
+    const int size = dtype == TBOA_F32 ? 4 : 2;
+    return std::max(rounds_room(p, false, size, n_tokens), rounds_room(p, true, size, n_tokens));
 }
 
 extern "C" int tboa_packed_linear(tboa_ctx* ctx, const tboa_packed_weight* weight, int64_t n_tokens, int dtype, const void* X, int64_t ldx, const void* Res, int64_t ldr, void* Y, int64_t ldy) {

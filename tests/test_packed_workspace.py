@@ -1,0 +1,22 @@
+"""Workspace of tboa_packed_linear and tboa_packed_swiglu as the library reports it (CPU: host arithmetic)."""
+import ctypes
+
+import pytest
+
+import paper_2602_04929_amd as tb
+
+MOST = 8192      # tokens of one round; more go round by round through one workspace
+SHAPES = [(4096, 4096, 4, 128), (2048, 2048, 4, 128), (10240, 8192, 4, 128), (8192, 8192, 4, 128), (4096, 11008, 4, 128), (11008, 4096, 4, 128), (13824, 5120, 3, 128), (4096, 4096, 8, 0),
+          (1003, 1024, 2, 64), (300, 320, 3, 32)]
+
+
+def room(shape, tokens, dtype):
+    return int(tb.binding._lib.tboa_packed_workspace_bytes(ctypes.byref(tb.binding.PackedWeightDesc(*shape, None, None, None)), tokens, dtype))
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_no_round_needs_more_than_the_call(shape, dtype):
+    """The last round of a call of more than 8192 tokens has fewer of them, and may need more."""
+    for tokens in [MOST + n for n in (1, 65, 300, 1000, 2000, 2048, 3000, 4096, 5000, 6000, 7000, 8000)] + [2 * MOST, 2 * MOST + 2048, 1 << 24]:
+        assert room(shape, tokens, dtype) >= max(room(shape, MOST, dtype), room(shape, tokens % MOST, dtype)), tokens
