@@ -290,7 +290,8 @@ int tboa_packed_linear(tboa_ctx* ctx, const tboa_packed_weight* weight, int64_t 
 /* The gated half of an MLP: Act = silu(X Wg^T) * (X Wu^T), silu(g) = g / (1 + exp(-g)), as tboa_swiglu_forward, from two packed matrices of the same rows, channels, bits and group.  X and the products
  * as in tboa_packed_linear; Act [n_tokens][d_out], rows lda elements apart. */
 int tboa_packed_swiglu(tboa_ctx* ctx, const tboa_packed_weight* gate, const tboa_packed_weight* up, int64_t n_tokens, int dtype, const void* X, int64_t ldx, void* Act, int64_t lda);
-/* Workspace that either call needs for a matrix of this shape (host value: the pointers are not read); 0 for an invalid descriptor, and where none is needed. */
+/* Workspace that either call needs for a matrix of this shape and up to n_tokens tokens: who reserves it for the largest batch can capture any smaller one (host value: the pointers are not read).  0 for
+ * an invalid descriptor, and where none is needed. */
 size_t tboa_packed_workspace_bytes(const tboa_packed_weight* weight, int64_t n_tokens, int dtype);
 
 /* ------------------------------------------------------------------------------------------------

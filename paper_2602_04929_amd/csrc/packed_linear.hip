@@ -1109,11 +1109,16 @@ int run(tboa_ctx* ctx, const char* who, const tboa_packed_weight* weight, const 
 extern "C" size_t tboa_packed_workspace_bytes(const tboa_packed_weight* weight, int64_t n_tokens, int dtype) {
     if (!good_weight(weight) || (dtype != TBOA_F32 && dtype != TBOA_BF16) || n_tokens <= 32 || n_tokens > 1 << 24) return 0;
     PackedArgs p = shape_of(*weight);
-    p.tokens = n_tokens;
-    if (n_tokens <= 64) return dtype == TBOA_BF16 ? few_room(p) : 0;
-    if (!many_takes(p)) return 0;
-    const int size = dtype == TBOA_F32 ? 4 : 2;
-    return std::max(rounds_room(p, false, size, n_tokens), rounds_room(p, true, size, n_tokens));
+    size_t most = 0;
+    if (dtype == TBOA_BF16) { p.tokens = std::min<long long>(n_tokens, 64); most = few_room(p); }
+    if (n_tokens <= 64 || !many_takes(p)) return most;
+    // a call of fewer tokens may need more (its tiles are split): the largest of all up to n_tokens, each the last with its number of tiles
+    const long long last = std::min<long long>(n_tokens, MOST_ROWS);
+    for (long long n = std::min(last, 128LL);; n = std::min(last, n / 256 * 256 + 256)) {
+        ManyArgs a{};
+        for (const bool gated : {false, true}) most = std::max(most, many_room(p, gated, dtype == TBOA_F32 ? 4 : 2, n, a, nullptr));
+        if (n == last) return most;
+    }
 }
 
 extern "C" int tboa_packed_linear(tboa_ctx* ctx, const tboa_packed_weight* weight, int64_t n_tokens, int dtype, const void* X, int64_t ldx, const void* Res, int64_t ldr, void* Y, int64_t ldy) {
