@@ -7,6 +7,7 @@
 // terms (2^-22 of them at most), and so is 2^up p s; but one half (2^-11 of it at most, an eighth of an output's rounding to bf16) for bf16 queries of sequences of more than FEW rows, in
 // either kernel, so that a row's bits do not hang on which one takes it: two prompts of 2048 tokens behind 4096, whose time is matrix instructions, would take 614 us, not 461.  Single tokens
 // wait for the cache's bytes and pay one per cent for the second half (32 sequences 78.1 us, not 77.1; one of 131000 tokens 70.1, not 69.0).
+// Trees of drafted tokens have two half terms whatever their rows (16 trees of up to 32 tokens, 64 / 8 heads, behind up to 8000 others: 215 us, not 203).
 // `up` goes by the largest p s among the tokens that the row itself has seen so far, and falls and rises with it as the maximum moves: neither a token that is hidden from the row nor one of a huge
 // scale and next to no probability takes bits from the others.
 #include "kv_attention.h"
@@ -404,7 +405,7 @@ __device__ __forceinline__ bool find_unit(const AttendArgs& a, int x, TilesUnit&
 
 // Trees of drafted tokens: all rows of a sequence see as many tiles, and where units are fewer than compute units they are cut into pieces of at most `share` tiles, the least (in steps of an eighth) with which
 // there are no more pieces than compute units: a piece more would begin when the others end.  16 trees of 32 tokens behind 1000 to 8000 others, 64 / 8 heads: 197 us,
-// and 263 with some 340 pieces.
+// and 263 with some 340 pieces (either with one half term of probabilities).
 constexpr int TREE_PIECES = TILES_TARGET;      // no call has more where units are cut
 __device__ __forceinline__ Span tree_span(const KvSeq& s, const AttendArgs& a) {
     return Span{a.window ? max(s.len - s.n - a.window, 0) : 0, max(min(s.len, a.q.room), 0)};
@@ -467,13 +468,13 @@ __device__ __forceinline__ void run_ends() {      // everything before it is bef
     __builtin_amdgcn_sched_barrier(0);
 }
 
-// N matrix instructions with an LDS operand each: the operands' loads AHEAD of them, no more (the registers would not hold them)
-template <int N, int AHEAD>
+// N times EACH matrix instructions with an LDS operand for EACH: the operands' loads AHEAD of them, no more (the registers would not hold them)
+template <int N, int AHEAD, int EACH = 1>
 __device__ __forceinline__ void operands_ahead() {
     __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
 #pragma unroll
-    for (int i = 0; i < N - AHEAD; ++i) { __builtin_amdgcn_sched_group_barrier(0x8, 1, 0); __builtin_amdgcn_sched_group_barrier(0x100, 1, 0); }
-    __builtin_amdgcn_sched_group_barrier(0x8, AHEAD, 0);
+    for (int i = 0; i < N - AHEAD; ++i) { __builtin_amdgcn_sched_group_barrier(0x8, EACH, 0); __builtin_amdgcn_sched_group_barrier(0x100, 1, 0); }
+    __builtin_amdgcn_sched_group_barrier(0x8, EACH * AHEAD, 0);
 }
 
 template <int DP, bool WIDE, bool TREE>      // WIDE: pages of 64 tokens and more, a tile lies in one; TREE: a row sees of its sequence's new tokens those that its mask names
@@ -677,7 +678,7 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
     for (int c = 0; c < CT; ++c)
 #pragma unroll
         for (int j = 0; j < 16; ++j) o[c][j] = 0.f;
-    h8 pf[4];
+    h8 pf[4], pl[TREE ? 4 : 1];
     float m = -__builtin_inff(), l = 0.f, most_w = 0.f;      // most_w: largest probability times scale that the row had when its bound was last set
     // A half is 2^(TILE_TOP - e_wave) scale, the same for all rows, times 2^d probability: 2^(e_wave - d) is the row's bound of scales, 2^SPARE above most_w.  Rows of 2^200 between them have that
     // (e_wave is at most 2^100 below the largest bound); what lies further below, if anything does, loses bits
@@ -741,8 +742,12 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
         }
         if (pv) {
 #pragma unroll
-            for (int i = 0; i < 4 * CT; ++i) o[i % CT] = mma32(v_piece(buf, i / CT, i % CT), pf[i / CT], o[i % CT]);
-            operands_ahead<4 * CT, (AHEAD < 4 * CT ? AHEAD : 4 * CT)>();
+            for (int i = 0; i < 4 * CT; ++i) {
+                const h8 v = v_piece(buf, i / CT, i % CT);
+                o[i % CT] = mma32(v, pf[i / CT], o[i % CT]);
+                if constexpr (TREE) o[i % CT] = mma32(v, pl[i / CT], o[i % CT]);
+            }
+            operands_ahead<4 * CT, (TREE ? 2 : AHEAD < 4 * CT ? AHEAD : 4 * CT), TREE ? 2 : 1>();      // (trees: registers; 215 us as it is, 227 with 3 or 6, 222 unordered, for the 16 trees at the top)
         }
         run_ends();
         const int t0 = lo + n * TILE;
@@ -816,7 +821,10 @@ __global__ __launch_bounds__(64 * waves<DP>(), waves<DP>() / 4) void kv_attend_t
 #pragma unroll
             for (int k = 0; k < 4; ++k)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) pf[k][j] = (_Float16)p[8 * k + j];
+                for (int j = 0; j < 8; ++j) {
+                    pf[k][j] = (_Float16)p[8 * k + j];
+                    if constexpr (TREE) pl[k][j] = (_Float16)(p[8 * k + j] - (float)pf[k][j]);
+                }
         }
         if (slot <= n_tiles) store_v(slot & 1);
         if (slot < n_tiles) store_k(slot & 1);

@@ -4,7 +4,7 @@
 // The same products and the same running softmax as attention of a chain (kv_attention.hip): levels less their zero are exact in half, scales multiply scores and probabilities,
 //     x[t] = (scale s^K_t log2 e) q.(c^K_t - z^K_t),   p = 2^(x - max),   O += (2^up p s^V_t) (c^V_t - z^V_t)
 // with a power of two per row for its query and one, `up`, by the largest p s among the tokens that the row itself has seen.  fp32 queries are two half terms, and so is
-// 2^up p s; for bf16 queries it is one (off by 2^-11 of it at most, an eighth of an output's rounding to bf16).
+// 2^up p s, for bf16 queries too (2^-22 of it at most; as one half term 8 trees of up to 64 rows took 142 us, not 147).
 #include "kv_attention.h"
 
 namespace {
@@ -47,7 +47,7 @@ __device__ __forceinline__ unsigned below(int n) { return n <= 0 ? 0u : n >= 16 
 // 114 us and 10 for the join; the levels take 37 at the rate of memory.
 template <typename T, int DP, int U>
 __global__ __launch_bounds__(256, resident<DP>()) void kv_tree_kernel(AttendArgs a) {
-    constexpr int NT = sizeof(T) == 2 ? 1 : 2, RW = 16 * U;      // half terms of queries and of probabilities; rows of a wavefront
+    constexpr int NT = sizeof(T) == 2 ? 1 : 2, RW = 16 * U;      // half terms of queries; rows of a wavefront
     constexpr int K64 = DP / 64, K32 = (DP % 64) / 32, KS = DP / 32, CT = DP / 16;
     __shared__ float joined[4][RW][DP + 4];
     __shared__ float2 ends[4][RW];
@@ -220,7 +220,7 @@ __global__ __launch_bounds__(256, resident<DP>()) void kv_tree_kernel(AttendArgs
             };
             if constexpr (U == 1) load_next();
             const bool all = t0 + TILE <= min(before, end) && (!a.window || t0 >= before + s.n - a.window) && __all(there);
-            h8 ph[U][NT][2];
+            h8 ph[U][2][2];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 if constexpr (U > 1) __builtin_amdgcn_sched_barrier(0);      // (one unit's softmax after the other: mixed they spill registers)
@@ -274,7 +274,7 @@ __global__ __launch_bounds__(256, resident<DP>()) void kv_tree_kernel(AttendArgs
                     for (int j = 0; j < 8; ++j) {
                         const _Float16 w = (_Float16)p[8 * k + j];
                         ph[u][0][k][j] = w;
-                        if constexpr (NT == 2) ph[u][1][k][j] = (_Float16)(p[8 * k + j] - (float)w);
+                        ph[u][1][k][j] = (_Float16)(p[8 * k + j] - (float)w);
                     }
             }
             if constexpr (U > 1) { __builtin_amdgcn_sched_barrier(0); load_next(); }      // (beside the softmax of two units there are no registers for it)
@@ -291,8 +291,8 @@ __global__ __launch_bounds__(256, resident<DP>()) void kv_tree_kernel(AttendArgs
                 const h8 v0 = levels8(vr[ct][0], vr[ct][1], zo[0], zo[1], zo[2], zo[3]), v1 = levels8(vr[ct][2], vr[ct][3], zo[4], zo[5], zo[6], zo[7]);
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) { o[u][ct] = mma16(v0, ph[u][n][0], o[u][ct]); o[u][ct] = mma16(v1, ph[u][n][1], o[u][ct]); }
+                    o[u][ct] = mma16(v0, ph[u][0][0], o[u][ct]); o[u][ct] = mma16(v1, ph[u][0][1], o[u][ct]);
+                    o[u][ct] = mma16(v0, ph[u][1][0], o[u][ct]); o[u][ct] = mma16(v1, ph[u][1][1], o[u][ct]);
                 }
             }
         }
