@@ -6,6 +6,7 @@ library raises: there is no fallback path.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import functools
 import os
@@ -196,8 +197,11 @@ class PackedWeight:
 
     @classmethod
     def of(cls, ctx, layer, bits, group=0):
-        """Of a layer as Context.quantize_layer returns it (codes, scales, zeros)."""
-        return cls(ctx.pack_codes(layer["codes"], bits), layer["scales"].contiguous(), layer["zeros"].contiguous(), layer["codes"].shape[1], bits, group)
+        """Of a layer as Context.quantize_layer returns it (codes, scales, zeros), or of several of the same channels, one below the other.  Made on the context's stream, behind what the current one has to do."""
+        layers = layer if isinstance(layer, (list, tuple)) else [layer]
+        with ctx._behind_current(*[t for l in layers for t in (l["codes"], l["scales"], l["zeros"])]):
+            codes, scales, zeros = ((torch.cat([l[n] for l in layers]) if len(layers) > 1 else layers[0][n].contiguous()) for n in ("codes", "scales", "zeros"))
+            return cls(ctx.pack_codes(codes, bits), scales, zeros, codes.shape[1], bits, group)
 
 
 class Rotation:
@@ -515,6 +519,16 @@ class Context:
                 if t is not None:
                     t.record_stream(self._stream)
 
+    @contextlib.contextmanager
+    def _behind_current(self, *tensors):
+        """torch's own work on `tensors` on the context's stream, behind what the current stream has to do."""
+        self._used(*tensors)
+        current = torch.cuda.current_stream(self.device)
+        if current != self._stream:
+            self._stream.wait_stream(current)
+        with torch.cuda.stream(self._stream):
+            yield
+
     def head_norm_rotate(self, Q, K=None, wq=None, wk=None, eps=1e-6, rotation=None, positions=None, out_q=None, out_k=None):
         """Norms of head vectors (wq, wk: fp32 [head_dim] or None, not normalised) and their rotation at int32 positions [tokens]; Q [tokens, heads, head_dim], K likewise or None, rows
         may be pitched.  Returns (Q', K'); out_q, out_k may be the inputs."""
@@ -617,6 +631,7 @@ class Context:
         d_out, d_in = codes.shape
         wpr = int(_lib.tboa_packed_words_per_row(d_in, bits))
         packed = torch.empty(d_out, max(wpr, 1), dtype=torch.int32, device=codes.device)
+        self._used(codes, packed)
         self._check(_lib.tboa_pack_codes(self._h, d_out, d_in, bits, _ptr(codes), _ptr(packed)))
         return packed
 

@@ -228,8 +228,7 @@ def quantize_mlp(ctx, mlp, cfg, alpha=0.25, use_R=True, cd_iters=1, adaptive_gri
 
 def pack_attention_block(ctx, quantized, bits, group=0):
     """Wqkv and Wo of a result of quantize_attention_block as PackedWeights, for serve_attention_block."""
-    qkv = {n: torch.cat([quantized[l][n] for l in "qkv"]) for n in ("codes", "scales", "zeros")}
-    return dict(Wqkv=PackedWeight.of(ctx, qkv, bits, group), Wo=PackedWeight.of(ctx, quantized["o"], bits, group))
+    return dict(Wqkv=PackedWeight.of(ctx, [quantized[l] for l in "qkv"], bits, group), Wo=PackedWeight.of(ctx, quantized["o"], bits, group))
 
 
 def pack_mlp(ctx, quantized, bits, group=0):
