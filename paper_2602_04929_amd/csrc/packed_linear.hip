@@ -28,8 +28,10 @@ __device__ __forceinline__ bf16 from_f32(float v, bf16) { return __float2bfloat1
 __device__ __forceinline__ f4 mma16(b8 a, b8 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ float silu(float g) { return g / (1.f + expf(-g)); }
 
-// x / d = umulhi(x, m) + (x & all) for x d < 2^32 (a row has fewer than 2^32 / d pieces of d to a group), 0 for d = 0
+// x / d = umulhi(x, m) + (x & all) for x d < 2^32, 0 for d = 0
 inline void magic(unsigned d, unsigned& m, unsigned& all) { m = d < 2 ? 0u : (unsigned)(((1ull << 32) + d - 1) / d); all = d == 1 ? ~0u : 0u; }
+// whether that holds for all of a row's pieces of so many channels and those of its last, incomplete run (rows of millions of channels in a few groups: packed_any_kernel, which divides)
+inline bool divides(const PackedArgs& a, int channels) { return a.n_groups == 1 || (a.d_in / channels + 64LL) * (a.group / channels) < 1LL << 32; }
 
 template <int N, int I = 0, typename F>
 __device__ __forceinline__ void unroll(F&& f) {
@@ -530,7 +532,7 @@ int launch_few(tboa_ctx* ctx, const PackedArgs& a) {
 }
 // fragments (of 32 channels in all) that a group has at least: as many as a run, or the most of which it has a whole number; 0: none
 int fragments_of_scale(const PackedArgs& a, int most, int least) {
-    for (int ff = most; ff >= least; ff /= 2) if (a.n_groups == 1 || a.group % (32 * ff) == 0) return ff;
+    for (int ff = most; ff >= least; ff /= 2) if (a.n_groups == 1 || a.group % (32 * ff) == 0) return divides(a, 32 * ff) ? ff : 0;
     return 0;
 }
 
@@ -991,7 +993,7 @@ size_t rounds_room(const PackedArgs& p, bool gated, int size, long long tokens) 
     const size_t first = many_room(p, gated, size, std::min(tokens, MOST_ROWS), a, nullptr), last = tokens % MOST_ROWS;
     return last ? std::max(first, many_room(p, gated, size, (long long)last, a, nullptr)) : first;
 }
-bool many_takes(const PackedArgs& p) { return (p.n_groups == 1 || p.group % 16 == 0) && p.words <= 1 << 21; }
+bool many_takes(const PackedArgs& p) { return (p.n_groups == 1 || p.group % 16 == 0) && divides(p, 16) && p.words <= 1 << 21; }
 
 template <typename T, int BITS, bool ONE_SCALE, int TM, bool GATED>
 int launch_many(tboa_ctx* ctx, const ManyArgs& a) {

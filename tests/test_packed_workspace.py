@@ -31,3 +31,14 @@ def test_fewer_tokens_need_no_more(shape, dtype):
         need = room(shape, tokens, dtype)
         assert need >= most, tokens
         most = need
+
+
+@pytest.mark.parametrize("shape,many", [((300, 3 * 87381 * 16, 4, 87381 * 16), False), ((300, 8140704, 8, 208736), False), ((300, 1 << 20, 4, 1 << 19), True), ((300, 1 << 22, 4, 0), True), ((300, 1 << 21, 2, 1 << 14), True)])
+def test_rows_whose_groups_are_found_by_a_product_of_32_bits(shape, many):
+    """The kernel for many tokens, the only one of more than 64 that has a workspace, finds a channel's group by a reciprocal of 32 bits, exact while units of 16 channels times units of a group stay below 2^32."""
+    d_out, d_in, bits, group = shape
+    units = d_in // 16
+    g = group // 16
+    exact = g < 2 or all((x * ((2 ** 32 + g - 1) // g)) >> 32 == x // g for k in range(1, units // g + 1) for x in (k * g - 1, k * g))
+    assert many == exact
+    assert (room(shape, 1000, 0) > 0) == many      # (fp32: 64 tokens or fewer need none)
