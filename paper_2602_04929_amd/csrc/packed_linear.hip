@@ -895,7 +895,7 @@ __global__ __launch_bounds__(512) void packed_many_kernel(ManyArgs a) {
                             const long long m = min(m0 + wm + 32 * i + row, p.tokens - 1);
                             const int n = min(c0 + l32, p.d_out - 1);
                             const float rs = a.row_scale[m];
-                            y = silu(y * rs * os[n]) * (acc[i][1][v] * rs * os[p.d_out + n]);
+                            y = silu(y * os[n] * rs) * (acc[i][1][v] * os[p.d_out + n] * rs);      // (the row's power of two last: it alone may leave fp32, where the scale brings the product back)
                         }
                     }
                     mine[row * PITCH + 32 * j + l32] = y;
@@ -919,7 +919,7 @@ __global__ __launch_bounds__(512) void packed_many_kernel(ManyArgs a) {
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     if (n + k >= p.d_out) break;
-                    float f = GATED ? v[k] : v[k] * rs * os[n + k];
+                    float f = GATED ? v[k] : v[k] * os[n + k] * rs;
                     if (res) f += to_f32(res[k]);
                     o.e[k] = from_f32(f, T());
                 }
@@ -955,8 +955,8 @@ __global__ __launch_bounds__(256) void packed_join_kernel(ManyArgs a) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             if (n + k >= p.d_out) break;
-            float v = y[0][k] * rs * a.out_scale[n + k];
-            if (GATED) v = silu(v) * (y[1][k] * rs * a.out_scale[p.d_out + n + k]);
+            float v = y[0][k] * a.out_scale[n + k] * rs;
+            if (GATED) v = silu(v) * (y[1][k] * a.out_scale[p.d_out + n + k] * rs);
             if (res) v += to_f32(res[k]);
             o.e[k] = from_f32(v, T());
         }
