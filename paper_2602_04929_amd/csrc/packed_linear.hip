@@ -40,12 +40,13 @@ __device__ __forceinline__ void unroll(F&& f) {
 
 __device__ __forceinline__ unsigned low_halves(unsigned a, unsigned b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
 __device__ __forceinline__ unsigned high_halves(unsigned a, unsigned b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
-// 24 bits as three terms of 8
+// 24 bits as three terms of 8, cut off (rounded, the largest numbers would become infinite)
+__device__ __forceinline__ __bf16 upper(float v) { return __builtin_bit_cast(__bf16, (unsigned short)(__float_as_uint(v) >> 16)); }
 __device__ __forceinline__ void split(float v, __bf16& hi, __bf16& mid, __bf16& lo) {
-    hi = (__bf16)v;
+    hi = upper(v);
     const float r = v - (float)hi;
-    mid = (__bf16)r;
-    lo = (__bf16)(r - (float)mid);
+    mid = upper(r);
+    lo = upper(r - (float)mid);
 }
 
 // Any group, any size: weights scale (code - zero) in fp32, as three bf16 terms, times X (bf16: as it is; fp32: three terms, products down to 2^-24).  A workgroup has 16 outputs of 16 MT tokens, its
@@ -152,13 +153,14 @@ __global__ __launch_bounds__(256) void packed_any_kernel(PackedArgs a) {
 // ------------------------------------------------------------------------------------------------ few tokens
 // A run of CK = 128 VW / BITS consecutive channels of a row is 4 VW words, VW for each of the four lane groups of a 16 x 16 x 32 instruction, NF fragments of 8 codes for each lane.
 // Two codes become a pair of bf16 by a shift and an and-or: code c in the upper bits of the mantissa of 2^BITS is 2^BITS + c.  Pairs are codes that stand 16 bits apart in the stream (48 for 3 bits, as
-// 16 is no multiple of 3), and X takes the same order.
+// 16 is no multiple of 3), and X takes the same order.  All of it times 2^-DOWN, which the sum over all channels takes back: 256 channels of the largest X then add up to a number, offsets included.
 struct Masks { unsigned codes, one; };
 template <int BITS, int VW>
 struct Codes {
-    static constexpr int CL = VW * 32 / BITS, NF = CL / 8, CK = 4 * CL, OFFSET = BITS == 8 ? 0 : 1 << BITS;
+    static constexpr int CL = VW * 32 / BITS, NF = CL / 8, CK = 4 * CL, OFFSET = BITS == 8 ? 0 : 1 << BITS, DOWN = BITS + 10;
     // 2 and 4 bits: word r of lane group g is the run's word 4 r + g, so that a fragment's channels lie together (and so may groups of 32 or 64); else VW words in a row
     static constexpr bool TURNED = (BITS == 2 || BITS == 4) && VW == 4;
+    static constexpr float LESS = 1.f / (1u << DOWN), MORE = 1u << DOWN;
     // channels of pair p of fragment f, among the lane's
     static constexpr int first(int f, int p) { return BITS == 8 ? 8 * f + 2 * p : BITS == 4 ? 8 * f + p : BITS == 2 ? f / 2 * 16 + f % 2 * 4 + p : 4 * f + p; }
     static constexpr int second(int f, int p) { return BITS == 8 ? 8 * f + 2 * p + 1 : first(f, p) + (BITS == 4 ? 4 : BITS == 2 ? 8 : 16); }
@@ -171,7 +173,7 @@ struct Codes {
         return ((AT < to ? v << (to - AT) : v >> (AT - to)) & m.codes) | m.one;
     }
     static __device__ __forceinline__ Masks masks() {
-        constexpr unsigned mask = BITS == 8 ? 0u : ((1u << BITS) - 1) << (7 - BITS), one = (unsigned)(127 + BITS) << 7;
+        constexpr unsigned mask = BITS == 8 ? 0u : ((1u << BITS) - 1) << (7 - BITS), one = (unsigned)(127 + BITS - DOWN) << 7;
         Masks m{mask | mask << 16, one | one << 16};
         asm("" : "+s"(m.codes), "+v"(m.one));      // (as literals they would be an instruction more for every pair)
         return m;
@@ -196,7 +198,7 @@ struct Codes {
 #pragma unroll
             for (int p = 0; p < 4; ++p) {      // whole numbers up to 255 are bf16
                 const unsigned v = w[2 * F + p / 2] >> (p % 2 * 16);
-                out[p] = high_halves(__float_as_uint((float)(v & 255u)), __float_as_uint((float)(v >> 8 & 255u)));
+                out[p] = high_halves(__float_as_uint((float)(v & 255u) * LESS), __float_as_uint((float)(v >> 8 & 255u) * LESS));
             }
         }
     }
@@ -213,7 +215,7 @@ constexpr int most_waves() { return XR <= 16 && NR == 1 ? 16 : 8; }
 
 // Up to XR tokens (4, or 16 MT) per workgroup: bound by the codes' bytes.  A wavefront has 16 RT outputs (of either matrix) and an equal part of the runs of channels; the wavefronts are joined through LDS.  FF
 // fragments of a run have one scale.  bf16 X: codes enter with their offset, and (offset + zero) sum x, by a product with ones that all outputs share, is taken out again with every scale:
-//     y += scale (sum (offset + code) x - (offset + zero) sum x)
+//     y += scale (sum (offset + code) x - (offset + zero) sum x)      (all of it times 2^-DOWN)
 // fp32 X: codes less zeros, exact in bf16, times three bf16 terms.
 // Rows of codes, of X and of scales are read by four lanes side by side, 64 bytes together, and handed to the lanes that multiply them through the wavefront's own part of LDS: read by those lanes
 // themselves, a row each, every 16 bytes are an access of their own to the first cache (16 tokens of 8192 x 28672: 37 million accesses, 143000 cycles of every compute unit's, 67 us and not 34).
@@ -312,7 +314,7 @@ __global__ __launch_bounds__((64 * most_waves<XR, (GATED ? 2 : 1) * RT>())) void
     const Masks masks = C::masks();
     b8 ones;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) ones[j] = (__bf16)1.f;
+    for (int j = 0; j < 8; ++j) ones[j] = (__bf16)C::LESS;
     auto in_order = [] { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); __builtin_amdgcn_wave_barrier(); };      // (a wavefront's own accesses to LDS)
     auto multiply = [&](int run, const Run& o) {
         in_order();
@@ -351,7 +353,7 @@ __global__ __launch_bounds__((64 * most_waves<XR, (GATED ? 2 : 1) * RT>())) void
             for (int r = 0; r < NR; ++r) {
                 C::template fragment<f>(w[r], wf[r].u, masks);
                 if constexpr (EXACT) {
-                    const float off = C::OFFSET + grid(1, r, g);
+                    const float off = (C::OFFSET + grid(1, r, g)) * C::LESS;
 #pragma unroll
                     for (int p = 0; p < 4; ++p)
                         wf[r].u[p] = high_halves(__float_as_uint(__uint_as_float(wf[r].u[p] << 16) - off), __float_as_uint(__uint_as_float(wf[r].u[p] & 0xffff0000u) - off));
@@ -455,6 +457,7 @@ __global__ __launch_bounds__((64 * most_waves<XR, (GATED ? 2 : 1) * RT>())) void
                 for (int w = 0; w < NW; ++w) {
                     y[w] = 0.f;
                     for (int v = 0; v < waves; ++v) y[w] += part[((v * NR + w * RT + r) * 16 + row) * 17 + c];
+                    y[w] *= C::MORE;
                 }
                 if (!GATED && a.splits > 1) { a.partial[(blockIdx.z * a.tokens + m) * a.d_out + n] = y[0]; continue; }
                 float v = GATED ? silu(y[0]) * y[NW - 1] : y[0];
