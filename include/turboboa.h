@@ -283,8 +283,8 @@ typedef struct {
 /* Y = X W^T (+ Res), W[n, c] = scales[n, c / g] (code[n, c] - zeros[n, c / g]).
  *   X [n_tokens][d_in], Res (or NULL) and Y [n_tokens][d_out] in `dtype` (TBOA_F32 or TBOA_BF16), rows ldx, ldr, ldy elements apart; Y may be Res (with the same pitch) and overlaps nothing else.
  *   n_tokens at most 2^24
- * Codes less zeros enter the products exactly, but for more than 64 tokens of bf16 and several grids a row scale * (code - zero) does, as half (two roundings of 2^-11 at most, less than 2^-10 together;
- * scales below 2^-13 of their row's largest to 2^-25 of that); fp32 sums and one rounding at the end.  bf16 X exactly, down to 2^-31 of the row's largest channel (and to 2^-110 for up to 64 tokens); fp32 X with 22 bits or more.  An infinity or NaN in a
+ * Codes less zeros enter the products exactly and scales with all their bits (for more than 64 tokens those below 2^-60 of their row's largest count as that much); fp32 sums and one rounding at the end.
+ * bf16 X exactly, down to 2^-31 of the row's largest channel (and to 2^-110 for up to 64 tokens); fp32 X to 2^-22, and for more than 64 tokens to 2^-39 of the row's largest channel.  An infinity or NaN in a
  * row of X makes that row of Y no finite numbers, and touches no other. */
 int tboa_packed_linear(tboa_ctx* ctx, const tboa_packed_weight* weight, int64_t n_tokens, int dtype, const void* X, int64_t ldx, const void* Res, int64_t ldr, void* Y, int64_t ldy);
 /* The gated half of an MLP: Act = silu(X Wg^T) * (X Wu^T), silu(g) = g / (1 + exp(-g)), as tboa_swiglu_forward, from two packed matrices of the same rows, channels, bits and group.  X and the products

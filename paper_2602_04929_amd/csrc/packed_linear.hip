@@ -543,21 +543,22 @@ int fragments_of_scale(const PackedArgs& a, int most, int least) {
 // Bound by the matrix instructions.  packed_rows_kernel makes X into half (bf16: exactly, fp32: as two terms), every row times a power of two that brings its largest channel to 2^14 .. 2^15, in the blocks of
 // 16 rows x 32 channels that packed_many_kernel copies straight into LDS; and a table of the scales and zeros.  packed_many_kernel makes the codes into half on their way into LDS, once per tile of
 // 256 outputs and TM tokens.
-// One scale per row: codes less zeros, exactly, and the scale multiplies the result.  Groups: scale (code - zero) as half, scales first divided by the power of two of their row's largest.  That is two
-// roundings to 11 bits, 2^-12 each at most, random from weight to weight: about 2e-4 of a result's size, an eighth of what its rounding to bf16 is off by (keeping them exact costs a
-// multiplication of every result by every group's scale, half of the vector instructions' time).  fp32: two half terms of scale (code - zero), three products.
+// Codes less zeros are exact in half.  A result is kept in the unit of the scale s_g of the group that its channels have come to: where a group begins, it is multiplied by s_(g-1) / s_g, so that the
+// matrix instructions add to it what they add to any sum, and at the end by the last group's scale.  2048 tokens of 8192 x 4096, four bits, one scale a row 142 us, groups of 128 149, of 64 169, of 32 194, of 16
+// 280; scale times code less zero as half instead, which is rounded twice to 11 bits (2e-4 of a result's size), 162 to 168 in groups.
 struct ManyArgs {
     PackedArgs p;
     unsigned char* rows;          // X as half: [planes][token blocks of 16][kb][1 KB]
     float* row_scale;             // [tokens] power of two that takes a row's own back out
-    uint2* table;                 // [matrices][d_out][n_groups]: bf16: .x half scale, half -(1024 + zero); fp32: scale, zero
-    float* out_scale;             // [matrices][d_out]
+    unsigned* zeros;              // [n_groups][matrices][wide]: -(1024 + zero) as half, twice
+    float* scales;                // [n_groups][matrices][wide]
+    int wide, size;               // d_out rounded up to 256; bytes of an element of X and Y
     float* partial;               // [splits][tiles that are split][TM][256]: their channels are split over workgroups
     long long plane;              // bytes
     int kb, blocks;               // blocks of 32 channels, a multiple of four; of 16 tokens
     int full, splits;             // tiles that are not split (whole rounds of all compute units), how many ways the others are
     int tiles_m, tiles_n, segments, matrices;
-    unsigned unit_magic, unit_all;      // units of 16 channels that a group has, as PackedArgs::piece_magic
+    int units; unsigned unit_magic, unit_all;      // units of 16 channels that a group has, as PackedArgs::piece_magic
 };
 constexpr int KS = 32;      // channels of a stage
 
@@ -569,26 +570,24 @@ template <typename T, int BITS>
 __global__ __launch_bounds__(1024) void packed_rows_kernel(ManyArgs a) {
     const PackedArgs& p = a.p;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    if ((int)blockIdx.x >= a.blocks) {      // a row of scales per wavefront
-        const long long row = (long long)(blockIdx.x - a.blocks) * 16 + wave;
-        const int which = row >= p.d_out;
-        const int n = (int)(row - (which ? p.d_out : 0));
-        if (row >= (long long)a.matrices * p.d_out) return;
-        const float* const scale = p.scale[which] + (long long)n * p.n_groups, * const zero = p.zero[which] + (long long)n * p.n_groups;
+    if ((int)blockIdx.x >= a.blocks) {      // scales and zeros of 64 outputs, one a lane, a sixteenth of their groups a wavefront
+        __shared__ float tops[16][64];
+        const int b = blockIdx.x - a.blocks, per = a.wide / 64, which = b >= per, n = (b - which * per) * 64 + lane;
+        const long long row = (long long)min(n, p.d_out - 1) * p.n_groups, at = (long long)which * a.wide + n, step = (long long)a.matrices * a.wide;
+        const float* const scale = p.scale[which] + row, * const zero = p.zero[which] + row;
         float most = 0.f;
-        for (int g = lane; g < p.n_groups; g += 64) { const float v = fabsf(scale[g]); most = v < __builtin_inff() ? fmaxf(most, v) : most; }
+        for (int g = wave; g < p.n_groups; g += 16) { const float v = fabsf(scale[g]); most = v < __builtin_inff() ? fmaxf(most, v) : most; }
+        tops[wave][lane] = most;
+        __syncthreads();
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) most = fmaxf(most, __shfl_xor(most, o, 64));
-        // the largest scale is 1 .. 2 times 2^-e
-        const int e = most > 0.f ? max(1 - __builtin_amdgcn_frexp_expf(most), -126) : 0;
-        for (int g = lane; g < p.n_groups; g += 64) {
-            const float s = p.n_groups == 1 ? 1.f : __builtin_amdgcn_ldexpf(scale[g], e), z = zero[g];
-            uint2 v;
-            if (sizeof(T) == 2) v = make_uint2((unsigned)__builtin_bit_cast(unsigned short, (_Float16)s) | (unsigned)__builtin_bit_cast(unsigned short, (_Float16)(-1024.f - z)) << 16, 0u);
-            else v = make_uint2(__float_as_uint(s), __float_as_uint(z));
-            a.table[row * p.n_groups + g] = v;
+        for (int i = 0; i < 16; ++i) most = fmaxf(most, tops[i][lane]);
+        const float least = most > 0.f ? fmaxf(most * 0x1p-60f, 0x1p-149f) : 0.f;      // (quotients of scales stay numbers)
+        for (int g = wave; g < p.n_groups; g += 16) {
+            const unsigned z = __builtin_bit_cast(unsigned short, (_Float16)(-1024.f - zero[g]));
+            a.zeros[g * step + at] = z | z << 16;
+            const float v = scale[g];
+            a.scales[g * step + at] = fabsf(v) < least ? least : v;
         }
-        if (lane == 0) a.out_scale[row] = p.n_groups == 1 ? scale[0] : __builtin_amdgcn_ldexpf(1.f, -e);
         return;
     }
     __shared__ int exps[16];
@@ -688,14 +687,30 @@ __device__ __forceinline__ void tile_place(const ManyArgs& a, int t, int& tm, in
     tn = t / band * 4 + in % wide; tm = in / wide;
 }
 
+// results n .. n + 3 of token m
+template <typename T>
+__device__ __forceinline__ void put4(const PackedArgs& p, long long m, int n, f4 v, bool may_add) {
+    T* const y = (T*)p.Y + m * p.ldy + n;
+    const T* const res = may_add && p.Res ? (const T*)p.Res + m * p.ldr + n : nullptr;
+    struct __attribute__((aligned(4 * sizeof(T)))) Four { T e[4]; } o;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if (n + k >= p.d_out) break;
+        o.e[k] = from_f32(res ? v[k] + to_f32(res[k]) : v[k], T());
+    }
+    if (n + 4 <= p.d_out && p.out_vec) *(Four*)y = o;
+    else for (int k = 0; k < 4; ++k) if (n + k < p.d_out) y[k] = o.e[k];
+}
+
 // A tile of TM tokens and 256 rows of codes (GATED: 128 of either matrix, 32 of one beside 32 of the other, so that a wavefront has both factors of its results); eight wavefronts, each TM / 2 tokens and 64 rows.
 // A ring of NS stages of 32 channels in LDS: X is copied there, NS - 1 stages ahead; codes are loaded two stages before that, made into half and written by all wavefronts, 16 codes a lane and stage.
 // Bound by the matrix instructions and, half as long again, the vector instructions that make codes into half beside them: 4096 tokens of 10240 x 8192, four bits, 677 us (1015 TFLOP/s).  Each wavefront
 // making the codes of its own 64 rows 730 - 759 us, codes copied into LDS and made into half once for all 775.
-template <typename T, int BITS, bool ONE_SCALE, int TM, bool GATED>      // ONE_SCALE: whole groups of 128 channels
+// GRIDS_OF: 0: one scale a row; 1: groups of whole 128 channels, which begin where the ring does; 2: of whole 16, the depth of a matrix instruction, whose scales go through LDS.
+template <int BITS, int GRIDS_OF, int TM, bool GATED>
 __global__ __launch_bounds__(512) void packed_many_kernel(ManyArgs a) {
-    constexpr int NS = 4, TI = TM / 64, TJ = 2, LPW = TM / 128, A_BYTES = TM * 64, STAGE = A_BYTES + 256 * 64;
-    extern __shared__ __attribute__((aligned(1024))) unsigned char ring[];
+    constexpr int NS = 4, TI = TM / 64, TJ = 2, LPW = TM / 128, A_BYTES = TM * 64, STAGE = A_BYTES + 256 * 64, UNITS = 2 * NS;      // UNITS of 16 channels in a turn of the ring
+    extern __shared__ __attribute__((aligned(1024))) unsigned char ring[];      // [NS][STAGE]; GRIDS_OF == 2: scales [3][UNITS][256]
     const PackedArgs& p = a.p;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, lh = lane >> 5;
     // tiles of one band of outputs after each other, an XCD (every eighth workgroup) its own run of them; then those that are split
@@ -717,23 +732,30 @@ __global__ __launch_bounds__(512) void packed_many_kernel(ManyArgs a) {
     // This thread's two rows of codes, of 256: row r of the tile and row r + 128, piece j of each in every stage
     const int r = threadIdx.x >> 2, j = threadIdx.x & 3;
     const int which = GATED ? r >> 5 & 1 : 0;
-    int row_n[2];
+    auto output = [&](int row) { return GATED ? n0 + 32 * (row >> 6) + (row & 31) : n0 + row; };      // of a row of the tile (beyond the last one: tables go on, rows of codes do not)
     unsigned at_codes[2];
-    const uint2* table[2];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int row = r + 128 * h;
-        row_n[h] = min(GATED ? n0 + 32 * (row >> 6) + (row & 31) : n0 + row, p.d_out - 1);
-        at_codes[h] = (unsigned)(row_n[h] - n0) * p.words * 4 + j * (BITS == 8 ? 16 : 4 * BITS);
-        table[h] = a.table + ((long long)which * p.d_out + row_n[h]) * p.n_groups;
-    }
+    for (int h = 0; h < 2; ++h) at_codes[h] = (unsigned)(min(output(r + 128 * h), p.d_out - 1) - n0) * p.words * 4 + j * (BITS == 8 ? 16 : 4 * BITS);
     // (rows 32 .. 63 of every 64 are the second matrix's: the same for all of a wavefront's 16 rows)
     const uint32_t* const base = __builtin_amdgcn_readfirstlane(which) ? p.w[1] : p.w[0];
     const auto codes = __builtin_amdgcn_make_buffer_rsrc((void*)(base + (long long)n0 * p.words), 0, (int)(unsigned)min((long long)(p.d_out - n0) * p.words * 4, 0xfffffffcLL), 0x00020000);
-    constexpr int NG = ONE_SCALE ? 1 : NS, NL = 2 * ((BITS == 8 ? 2 : 1) + NG);      // scales of a row in NS stages; loads of `load`
-    struct Load { Codes128<BITS> u[2]; uint2 g[2][NG]; };
-    int l_ks = kt0 % a.kb;      // of the next codes to be loaded, a multiple of NS
+    const long long table_step = (long long)a.matrices * a.wide;
+    const unsigned at_zeros = which * a.wide + output(r);      // row r + 128: 128 outputs on, 64 of a gated tile
+    const int wm = wave / 4 * (TM / 2), wn = wave % 4 * 64;
+    const unsigned at_scales = output(wn) + l32;               // results: of the second 32 columns 32 outputs on, of a gated tile the other matrix's
+    const unsigned next_scale = GATED ? a.wide : 32;
+    constexpr int NG = GRIDS_OF == 2 ? NS : 1, NL = 2 * ((BITS == 8 ? 2 : 1) + (GRIDS_OF == 0 ? 0 : NG)) + (GRIDS_OF == 1 ? 2 : GRIDS_OF == 2);      // zeros of a row in NS stages; loads of `load`
+    struct Load { Codes128<BITS> u[2]; unsigned z[2][NG]; float s[TJ]; };
+    const unsigned ring_at = (unsigned)(unsigned long long)((__attribute__((address_space(3))) void*)ring);
+    auto group_of = [&](unsigned unit) { return min((int)(__umulhi(unit, a.unit_magic) + (unit & a.unit_all)), p.n_groups - 1); };
+    const unsigned row_zero[2] = {a.zeros[at_zeros], a.zeros[at_zeros + (GATED ? 64 : 128)]};      // GRIDS_OF == 0: the only ones
+    int l_ks = kt0 % a.kb, l_slot = 0;      // of the next codes to be loaded, a multiple of NS; where their scales go
     auto load = [&](Load& o) {
+        if constexpr (GRIDS_OF == 2) {      // a unit's scales a wavefront, four a lane
+            const int row = 4 * lane;
+            lds_direct_16(((GATED ? (row >> 5 & 1) * a.wide : 0) + output(row)) * 4, (const char*)(a.scales + group_of(l_ks * 2 + wave) * table_step), ring_at + NS * STAGE + (l_slot * UNITS + wave) * 1024);
+            l_slot = l_slot == 2 ? 0 : l_slot + 1;
+        }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const unsigned at = at_codes[h] + l_ks * (BITS * 4);
@@ -745,39 +767,24 @@ __global__ __launch_bounds__(512) void packed_many_kernel(ManyArgs a) {
             else if constexpr (BITS == 2) { const auto v = __builtin_amdgcn_raw_buffer_load_b64(codes, at, 0, 0); u.w[0] = v[0]; u.w[1] = v[1]; }
             else { const auto v = __builtin_amdgcn_raw_buffer_load_b96(codes, at, 0, 0); u.w[0] = v[0]; u.w[1] = v[1]; u.w[2] = v[2]; }
 #pragma unroll
-            for (int i = 0; i < NG; ++i) {
-                const unsigned unit = (l_ks + i) * 2 + (ONE_SCALE ? 0 : j >> 1);
-                o.g[h][i] = table[h][min((int)(__umulhi(unit, a.unit_magic) + (unit & a.unit_all)), p.n_groups - 1)];
-            }
+            for (int i = 0; i < NG; ++i) o.z[h][i] = GRIDS_OF == 0 ? row_zero[h] : a.zeros[group_of((l_ks + i) * 2 + (GRIDS_OF == 2 ? j >> 1 : 0)) * table_step + at_zeros + h * (GATED ? 64 : 128)];
+        }
+        if constexpr (GRIDS_OF == 1) {
+            const float* const s = a.scales + group_of(l_ks * 2) * table_step + at_scales;
+            o.s[0] = s[0]; o.s[1] = s[next_scale];
         }
         l_ks += NS;
         if (l_ks >= a.kb) l_ks = 0;
     };
-    int b_seg = kt0 / a.kb, b_ks = kt0 - b_seg * a.kb;      // of the next codes to be written
     unsigned char* const b_at = ring + A_BYTES + r * 64 + ((j ^ (r >> 2 & 3)) << 4);
-    auto halves = [&](const Load& o, auto H, auto S, u4& out) {      // piece j of row h in stage S
+    auto halves = [&](const Load& o, auto H, auto S, u4& out) {      // piece j of row h in stage S: codes less zeros
         constexpr int h = decltype(H)::value, st = decltype(S)::value;
         unsigned v[4];
         piece_halves<BITS, st>(o.u[h], j, v);
-        const uint2 g = o.g[h][ONE_SCALE ? 0 : st];
-        if constexpr (sizeof(T) == 2) {
-            const h2 both = __builtin_bit_cast(h2, g.x), s = {both[0], both[0]}, z = {both[1], both[1]};
+        const h2 z = __builtin_bit_cast(h2, o.z[h][GRIDS_OF == 2 ? st : 0]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) out[i] = __builtin_bit_cast(unsigned, (__builtin_bit_cast(h2, v[i]) + z) * s);
-        } else {
-            const float s = __uint_as_float(g.x), z = -1024.f - __uint_as_float(g.y);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const h2 c = __builtin_bit_cast(h2, v[i]);
-                h2 w;
-#pragma unroll
-                for (int k = 0; k < 2; ++k) { const float f = ((float)c[k] + z) * s; w[k] = (_Float16)f; if (b_seg == 2) w[k] = (_Float16)(f - (float)w[k]); }
-                out[i] = __builtin_bit_cast(unsigned, w);
-            }
-        }
+        for (int i = 0; i < 4; ++i) out[i] = __builtin_bit_cast(unsigned, __builtin_bit_cast(h2, v[i]) + z);
     };
-    auto written = [&] { if (++b_ks == a.kb) { b_ks = 0; ++b_seg; } };
-    const unsigned ring_at = (unsigned)(unsigned long long)((__attribute__((address_space(3))) void*)ring);
     long long block[LPW];
 #pragma unroll
     for (int i = 0; i < LPW; ++i) block[i] = min(m0 / 16 + wave * LPW + i, (long long)a.blocks - 1) * a.kb * 1024;
@@ -788,7 +795,6 @@ __global__ __launch_bounds__(512) void packed_many_kernel(ManyArgs a) {
             lds_direct_16(lane * 16, (const char*)a.rows + (a_seg == 1 && a.segments > 1 ? a.plane : 0) + block[i] + (long long)a_ks * 1024, ring_at + slot * STAGE + (wave * LPW + i) * 1024);
         if (++a_ks == a.kb) { a_ks = 0; ++a_seg; }
     };
-    const int wm = wave / 4 * (TM / 2), wn = wave % 4 * 64;
     auto x_piece = [&](int slot, int i, int ks) { const int row = wm + 32 * i + l32; return *(const h8*)(ring + slot * STAGE + row * 64 + (((2 * ks + lh) ^ (row >> 2 & 3)) << 4)); };
     auto w_piece = [&](int slot, int j, int ks) { const int row = wn + 32 * j + l32; return *(const h8*)(ring + slot * STAGE + A_BYTES + row * 64 + (((2 * ks + lh) ^ (row >> 2 & 3)) << 4)); };
     f16v acc[TI][TJ];
@@ -805,11 +811,20 @@ __global__ __launch_bounds__(512) void packed_many_kernel(ManyArgs a) {
 #pragma unroll
         for (int j = 0; j < TJ; ++j) fw[set][j] = w_piece(slot, j, ks);
     };
-    auto multiply = [&](int set) {
+    float turn[TJ];      // from the unit of the results to that of the products that come
+    auto multiply = [&](int set, auto TURNED) {
 #pragma unroll
         for (int i = 0; i < TI; ++i)
 #pragma unroll
-            for (int j = 0; j < TJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fx[set][i], fw[set][j], acc[i][j], 0, 0, 0);
+            for (int j = 0; j < TJ; ++j) {
+                if constexpr (decltype(TURNED)::value) acc[i][j] *= turn[j];
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fx[set][i], fw[set][j], acc[i][j], 0, 0, 0);
+            }
+    };
+    float scale[TJ];     // the unit of the results
+    auto turn_to = [&](const float (&next)[TJ]) {
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) { turn[j] = scale[j] == next[j] ? 1.f : scale[j] / next[j]; scale[j] = next[j]; }
     };
     auto arrived = [](Load& o) {
 #pragma unroll
@@ -817,69 +832,93 @@ __global__ __launch_bounds__(512) void packed_many_kernel(ManyArgs a) {
 #pragma unroll
             for (unsigned& w : o.u[h].w) asm volatile("" : "+v"(w));
 #pragma unroll
-            for (uint2& g : o.g[h]) { asm volatile("" : "+v"(g.x)); if (sizeof(T) == 4) asm volatile("" : "+v"(g.y)); }
+            for (unsigned& z : o.z[h]) asm volatile("" : "+v"(z));
         }
+        if constexpr (GRIDS_OF == 1) { asm volatile("" : "+v"(o.s[0])); asm volatile("" : "+v"(o.s[1])); }
     };
     // a run of matrix instructions: the next one's operands first, and vector instructions in the shadow of each
-    auto beside = [] {
+    auto beside = [](auto TURNED) {
+        constexpr bool turned = decltype(TURNED)::value;
         __builtin_amdgcn_sched_group_barrier(0x100, TI + TJ, 0);
 #pragma unroll
         for (int i = 0; i < TI * TJ; ++i) {
+            if constexpr (turned) __builtin_amdgcn_sched_group_barrier(0x2, 16, 0);
             __builtin_amdgcn_sched_group_barrier(0x8, 1, 0); __builtin_amdgcn_sched_group_barrier(0x2, TI == 4 ? 8 : 12, 0);
             if (i == TI * TJ * 5 / 8) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);      // (what waits at the next barrier is then done)
         }
     };
     // As stage kt begins, stages kt .. kt + NS - 2 are in LDS or on their way there.  Codes are loaded for NS stages at once (kt and a.kb are multiples of NS) and written from the stage on that is NS - 1
-    // before theirs: `here` has those of stages kt .. kt + NS - 1, `next` those of the NS after them.
+    // before theirs: `here` has those of stages kt .. kt + NS - 1, `next` those of the NS after them.  Scales of GRIDS_OF == 2 are copied two turns ahead, the second of three slots being the next turn's.
     Load here, next, after_next;
     load(here);
     unroll<NS - 1>([&](auto S) {
         copy(S);
         unroll<2>([&](auto H) { u4 v; halves(here, H, S, v); *(u4*)(b_at + S * STAGE + H * 128 * 64) = v; });
-        written();
     });
     load(next);
     arrived(next);
     wait_loads_but<0>();
     __syncthreads();
+    const float* const scales_at = (const float*)(ring + NS * STAGE) + wn + l32;      // [slot][unit][256]
+#pragma unroll
+    for (int j = 0; j < TJ; ++j) scale[j] = GRIDS_OF == 2 ? scales_at[32 * j] : GRIDS_OF == 1 ? here.s[j] : 1.f;
     read(0, 0, 0);
+    int slot = 0, unit = kt0 % a.kb * 2;      // GRIDS_OF == 2: of this turn's scales; of the row, its first unit
     for (int kt = 0; kt < nk; kt += NS) {
+        if constexpr (GRIDS_OF == 1) turn_to(here.s);
         unroll<NS>([&](auto SS) {
             constexpr int s = SS, last = s == 0 ? NS - 1 : s - 1, after = s == NS - 1 ? 0 : s + 1;
             constexpr std::integral_constant<int, last> S;      // the written stage's number among its NS
             const Load& codes_of = s == 0 ? here : next;
-            u4 v;
+            auto run = [&](auto H, auto TURNED) {
+                constexpr int h = decltype(H)::value;
+                u4 v;
+                if constexpr (h == 0) read(1, s, 1); else read(0, after, 0);
+                halves(codes_of, H, S, v);
+                multiply(h, TURNED);
+                *(u4*)(b_at + last * STAGE + h * 128 * 64) = v;
+                beside(TURNED);
+            };
+            auto half_stage = [&](auto H) {
+                constexpr int h = decltype(H)::value, u = 2 * s + h;
+                if constexpr (GRIDS_OF == 2) {
+                    const unsigned at = unit + u;
+                    if ((__umulhi(at, a.unit_magic) + (at & a.unit_all)) * (unsigned)a.units == at) {      // a group begins
+                        const float* const from = scales_at + (slot * UNITS + u) * 256;
+                        const float more[TJ] = {from[0], from[32]};
+                        turn_to(more);
+#pragma unroll
+                        for (int i = 0; i < TI; ++i)
+#pragma unroll
+                            for (int j = 0; j < TJ; ++j) acc[i][j] *= turn[j];
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                run(H, std::integral_constant<bool, GRIDS_OF == 1 && u == 0>());
+            };
             copy(last);      // (the stage before this one has been read by everyone)
             if constexpr (s == 1) load(after_next);
             __builtin_amdgcn_sched_barrier(0);
-            read(1, s, 1);
-            halves(codes_of, std::integral_constant<int, 0>(), S, v);
-            multiply(0);
-            *(u4*)(b_at + last * STAGE) = v;
-            beside();
+            half_stage(std::integral_constant<int, 0>());
             // what the next stage has was copied two stages ago: two stages' copies may still be on their way, and the loads after the first of them (older ones are awaited with them)
             __builtin_amdgcn_sched_barrier(0);
             if constexpr (s > 0) wait_loads_but<2 * LPW + NL>(); else wait_loads_but<2 * LPW>();
             __syncthreads();
             __builtin_amdgcn_sched_barrier(0);
-            read(0, after, 0);
-            halves(codes_of, std::integral_constant<int, 1>(), S, v);
-            multiply(1);
-            *(u4*)(b_at + last * STAGE + 128 * 64) = v;
-            beside();
-            written();
+            half_stage(std::integral_constant<int, 1>());
         });
         __builtin_amdgcn_sched_barrier(0);
         arrived(after_next);      // (here, where the newest copy is a stage old: the compiler, which does not know of the copies, waits for them too)
         here = next; next = after_next;
+        if constexpr (GRIDS_OF == 2) { slot = slot == 2 ? 0 : slot + 1; unit += UNITS; if (unit == 2 * a.kb) unit = 0; }
     }
     // results through LDS, 32 tokens of a wavefront at a time: rows of 64 outputs
+    if constexpr (GRIDS_OF == 0) { scale[0] = a.scales[at_scales]; scale[1] = a.scales[at_scales + next_scale]; }
     wait_loads_but<0>();
     __syncthreads();
     constexpr int WIDE = GATED ? 32 : 64, PITCH = WIDE + 4;
     float* const mine = (float*)(ring + wave * 32 * 68 * 4);
     const int c0 = GATED ? n0 + wn / 2 : n0 + wn;      // first output of the wavefront
-    const float* const os = a.out_scale;
 #pragma unroll
     for (int i = 0; i < TI; ++i) {
         auto in_order = [] { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); __builtin_amdgcn_wave_barrier(); };
@@ -891,14 +930,13 @@ __global__ __launch_bounds__(512) void packed_many_kernel(ManyArgs a) {
 #pragma unroll
                 for (int v = 0; v < 16; ++v) {
                     const int row = 8 * (v / 4) + 4 * lh + v % 4;
-                    float y = acc[i][j][v];
+                    float y = acc[i][j][v] * scale[j];
                     if constexpr (GATED) {
-                        if (parts) y = side ? acc[i][1][v] : y;
+                        const float up = acc[i][1][v] * scale[1];
+                        if (parts) y = side ? up : y;
                         else {
-                            const long long m = min(m0 + wm + 32 * i + row, p.tokens - 1);
-                            const int n = min(c0 + l32, p.d_out - 1);
-                            const float rs = a.row_scale[m];
-                            y = silu(y * os[n] * rs) * (acc[i][1][v] * os[p.d_out + n] * rs);      // (the row's power of two last: it alone may leave fp32, where the scale brings the product back)
+                            const float rs = a.row_scale[min(m0 + wm + 32 * i + row, p.tokens - 1)];
+                            y = silu(y * rs) * (up * rs);      // (the row's power of two last: it alone may leave fp32, where the scale brings the product back)
                         }
                     }
                     mine[row * PITCH + 32 * j + l32] = y;
@@ -916,25 +954,13 @@ __global__ __launch_bounds__(512) void packed_many_kernel(ManyArgs a) {
                     continue;
                 }
                 const float rs = GATED ? 1.f : a.row_scale[m];
-                T* const y = (T*)p.Y + m * p.ldy + n;
-                const T* const res = !GATED && p.Res ? (const T*)p.Res + m * p.ldr + n : nullptr;
-                union { T e[4]; } o;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    if (n + k >= p.d_out) break;
-                    float f = GATED ? v[k] : v[k] * os[n + k] * rs;
-                    if (res) f += to_f32(res[k]);
-                    o.e[k] = from_f32(f, T());
-                }
-                struct __attribute__((aligned(4 * sizeof(T)))) Four { T e[4]; };
-                if (n + 4 <= p.d_out && p.out_vec) *(Four*)y = *(Four*)o.e;
-                else for (int k = 0; k < 4; ++k) if (n + k < p.d_out) y[k] = o.e[k];
+                if (a.size == 2) put4<bf16>(p, m, n, v * rs, !GATED); else put4<float>(p, m, n, v * rs, !GATED);
             }
         }
     }
 }
 
-// sums of the splits' partial results of the tiles that are split, scaled
+// sums of the splits' partial results of the tiles that are split
 template <typename T, int TM, bool GATED>
 __global__ __launch_bounds__(256) void packed_join_kernel(ManyArgs a) {
     constexpr int WIDE = GATED ? 128 : 256, LANES = WIDE / 4, ROWS = 256 / LANES;      // four outputs a thread
@@ -952,19 +978,13 @@ __global__ __launch_bounds__(256) void packed_join_kernel(ManyArgs a) {
 #pragma unroll 4
         for (int s = 0; s < a.splits; ++s) { y[0] += *(const f4*)from; if (GATED) y[1] += *(const f4*)(from + 128); from += (long long)cut * TM * 256; }
         const float rs = a.row_scale[m];
-        T* const to = (T*)p.Y + m * p.ldy + n;
-        const T* const res = !GATED && p.Res ? (const T*)p.Res + m * p.ldr + n : nullptr;
-        struct __attribute__((aligned(4 * sizeof(T)))) Four { T e[4]; } o;
+        y[0] *= rs;
+        if constexpr (GATED) {
+            y[1] *= rs;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            if (n + k >= p.d_out) break;
-            float v = y[0][k] * a.out_scale[n + k] * rs;
-            if (GATED) v = silu(v) * (y[1][k] * a.out_scale[p.d_out + n + k] * rs);
-            if (res) v += to_f32(res[k]);
-            o.e[k] = from_f32(v, T());
+            for (int k = 0; k < 4; ++k) y[0][k] = silu(y[0][k]) * y[1][k];
         }
-        if (n + 4 <= p.d_out && p.out_vec) *(Four*)to = o;
-        else for (int k = 0; k < 4; ++k) if (n + k < p.d_out) to[k] = o.e[k];
+        put4<T>(p, m, n, y[0], !GATED);
     }
 }
 
@@ -974,7 +994,8 @@ constexpr long long MOST_ROWS = 8192;      // tokens of one round: more are work
 size_t many_room(const PackedArgs& p, bool gated, int size, long long tokens, ManyArgs& a, void* ws) {
     const int tm = tokens <= 128 ? 128 : 256;
     a.kb = (int)cdiv64(p.d_in, 4 * KS) * 4; a.blocks = (int)cdiv64(tokens, 16);
-    a.segments = size == 2 ? 1 : p.n_groups == 1 ? 2 : 3;
+    a.segments = size == 2 ? 1 : 2; a.size = size;
+    a.wide = (int)cdiv64(p.d_out, 256) * 256;
     a.tiles_m = (int)cdiv64(tokens, tm); a.tiles_n = (int)cdiv64(p.d_out, gated ? 128 : 256);
     const int tiles = a.tiles_m * a.tiles_n, cut = tiles % CUS;
     a.full = tiles - cut;
@@ -985,8 +1006,8 @@ size_t many_room(const PackedArgs& p, bool gated, int size, long long tokens, Ma
     Arena ar(ws);
     a.rows = ar.get<unsigned char>((size_t)a.plane * (size == 2 ? 1 : 2));
     a.row_scale = ar.get<float>((size_t)tokens);
-    a.table = ar.get<uint2>((size_t)matrices * p.d_out * p.n_groups);
-    a.out_scale = ar.get<float>((size_t)matrices * p.d_out);
+    a.zeros = ar.get<unsigned>((size_t)matrices * a.wide * p.n_groups);
+    a.scales = ar.get<float>((size_t)matrices * a.wide * p.n_groups);
     a.partial = ar.get<float>(a.splits > 1 ? (size_t)a.splits * cut * tm * 256 : 0);
     return ar.off;
 }
@@ -998,19 +1019,25 @@ size_t rounds_room(const PackedArgs& p, bool gated, int size, long long tokens) 
 }
 bool many_takes(const PackedArgs& p) { return (p.n_groups == 1 || p.group % 16 == 0) && divides(p, 16) && p.words <= 1 << 21; }
 
-template <typename T, int BITS, bool ONE_SCALE, int TM, bool GATED>
+template <int BITS, int GRIDS_OF, int TM, bool GATED>
 int launch_many(tboa_ctx* ctx, const ManyArgs& a) {
-    constexpr int LDS = 4 * (TM + 256) * 64;
-    const auto kernel = packed_many_kernel<T, BITS, ONE_SCALE, TM, GATED>;
+    constexpr int LDS = 4 * (TM + 256) * 64 + (GRIDS_OF == 2 ? 3 * 8 * 1024 : 0);
+    const auto kernel = packed_many_kernel<BITS, GRIDS_OF, TM, GATED>;
     TB_HIP(ctx, hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
     const int cut = a.tiles_m * a.tiles_n - a.full;
     hipLaunchKernelGGL(kernel, dim3((unsigned)(a.full + cdiv64((a.tiles_m * a.tiles_n - a.full) * a.splits, 8) * 8)), dim3(512), LDS, ctx->stream, a);
     TB_KERNEL_CHECK(ctx);
     if (a.splits > 1) {
-        hipLaunchKernelGGL((packed_join_kernel<T, TM, GATED>), dim3((unsigned)std::min(cut * TM / (GATED ? 8 : 4), 1 << 16)), dim3(256), 0, ctx->stream, a);
+        const auto join = a.size == 2 ? packed_join_kernel<bf16, TM, GATED> : packed_join_kernel<float, TM, GATED>;
+        hipLaunchKernelGGL(join, dim3((unsigned)std::min(cut * TM / (GATED ? 8 : 4), 1 << 16)), dim3(256), 0, ctx->stream, a);
         TB_KERNEL_CHECK(ctx);
     }
     return 0;
+}
+template <int BITS, int TM, bool GATED>
+int launch_many(tboa_ctx* ctx, const ManyArgs& a) {
+    if (a.p.n_groups == 1) return launch_many<BITS, 0, TM, GATED>(ctx, a);
+    return a.p.group % 128 == 0 ? launch_many<BITS, 1, TM, GATED>(ctx, a) : launch_many<BITS, 2, TM, GATED>(ctx, a);
 }
 template <typename T, int BITS, bool GATED>
 int launch_many(tboa_ctx* ctx, const PackedArgs& p) {
@@ -1022,13 +1049,11 @@ int launch_many(tboa_ctx* ctx, const PackedArgs& p) {
         a.p.X = (const T*)p.X + at * p.ldx; a.p.Y = (T*)p.Y + at * p.ldy;
         if (p.Res) a.p.Res = (const T*)p.Res + at * p.ldr;
         if (many_room(p, GATED, sizeof(T), a.p.tokens, a, ctx->ws) > ctx->ws_bytes) return tboa_fail(ctx, TBOA_ENOMEM, "a workspace of %zu bytes is too small", ctx->ws_bytes);
-        const int units = p.group / 16;
-        magic(p.n_groups == 1 ? 0 : units, a.unit_magic, a.unit_all);
-        hipLaunchKernelGGL((packed_rows_kernel<T, BITS>), dim3((unsigned)(a.blocks + cdiv64((GATED ? 2LL : 1LL) * p.d_out, 16))), dim3(1024), 0, ctx->stream, a);
+        a.units = p.group / 16;
+        magic(p.n_groups == 1 ? 0 : a.units, a.unit_magic, a.unit_all);
+        hipLaunchKernelGGL((packed_rows_kernel<T, BITS>), dim3((unsigned)(a.blocks + a.matrices * (a.wide / 64))), dim3(1024), 0, ctx->stream, a);
         TB_KERNEL_CHECK(ctx);
-        const bool one = p.n_groups == 1 || p.group % 128 == 0;
-        if (a.p.tokens <= 128) TB_TRY((one ? launch_many<T, BITS, true, 128, GATED>(ctx, a) : launch_many<T, BITS, false, 128, GATED>(ctx, a)));
-        else TB_TRY((one ? launch_many<T, BITS, true, 256, GATED>(ctx, a) : launch_many<T, BITS, false, 256, GATED>(ctx, a)));
+        TB_TRY((a.p.tokens <= 128 ? launch_many<BITS, 128, GATED>(ctx, a) : launch_many<BITS, 256, GATED>(ctx, a)));
     }
     return 0;
 }
