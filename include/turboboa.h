@@ -372,7 +372,7 @@ int tboa_kv_cache_attention(tboa_ctx* ctx, const tboa_kv_cache_desc* desc, const
  * them as it has ancestors.  (The mask alone decides on new tokens, a window as short as a path is the caller's to cut.)  Rows that see nothing get 0, and so do those whose own place is before 0.
  * Keys are appended as those of any new tokens, rotated by the positions that the caller gives for them; of the tokens that are kept in the end the caller appends keys and values again, with the
  * length that this leaves.  Types, precision, the other arguments and what is checked are as in tboa_kv_cache_attention, but probabilities times scale are pairs of 11 bits for TBOA_BF16 too,
- * whatever the rows (in sequences, or a call for one sequence, of more than 64 rows to 2^-24 of the row's largest). */
+ * whatever the rows (in sequences, or a call for one sequence, of more than 512 rows to 2^-24 of the row's largest). */
 size_t tboa_kv_cache_tree_attention_workspace_bytes(const tboa_kv_cache_desc* desc, int n_q_heads, int n_seqs, int64_t n_tokens);
 int tboa_kv_cache_tree_attention(tboa_ctx* ctx, const tboa_kv_cache_desc* desc, const tboa_kv_batch* batch, int n_q_heads, int dtype, const void* Q, int64_t ldq,
                                  const uint32_t* tree, int tree_words, const void* cache, double scale, int window, void* O, int64_t ldo);

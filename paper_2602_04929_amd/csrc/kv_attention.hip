@@ -7,7 +7,7 @@
 // terms (2^-22 of them at most), and so is 2^up p s; but one half (2^-11 of it at most, an eighth of an output's rounding to bf16) for bf16 queries of sequences of more than FEW rows, in
 // either kernel, so that a row's bits do not hang on which one takes it: two prompts of 2048 tokens behind 4096, whose time is matrix instructions, would take 614 us, not 461.  Single tokens
 // wait for the cache's bytes and pay one per cent for the second half (32 sequences 78.1 us, not 77.1; one of 131000 tokens 70.1, not 69.0).
-// Trees of drafted tokens have two half terms whatever their rows (16 trees of up to 32 tokens, 64 / 8 heads, behind up to 8000 others: 215 us, not 203).
+// Trees of drafted tokens have two half terms whatever their rows (16 trees of up to 32 tokens, 64 / 8 heads, behind up to 8000 others, by the kernel for many rows: 215 us, not 203).
 // `up` goes by the largest p s among the tokens that the row itself has seen so far, and falls and rises with it as the maximum moves: neither a token that is hidden from the row nor one of a huge
 // scale and next to no probability takes bits from the others.
 #include "kv_attention.h"
@@ -405,7 +405,7 @@ __device__ __forceinline__ bool find_unit(const AttendArgs& a, int x, TilesUnit&
 
 // Trees of drafted tokens: all rows of a sequence see as many tiles, and where units are fewer than compute units they are cut into pieces of at most `share` tiles, the least (in steps of an eighth) with which
 // there are no more pieces than compute units: a piece more would begin when the others end.  16 trees of 32 tokens behind 1000 to 8000 others, 64 / 8 heads: 197 us,
-// and 263 with some 340 pieces (either with one half term of probabilities).
+// and 263 with some 340 pieces (either by this kernel, with one half term of probabilities).
 constexpr int TREE_PIECES = TILES_TARGET;      // no call has more where units are cut
 __device__ __forceinline__ Span tree_span(const KvSeq& s, const AttendArgs& a) {
     return Span{a.window ? max(s.len - s.n - a.window, 0) : 0, max(min(s.len, a.q.room), 0)};

@@ -4,20 +4,18 @@
 // The same products and the same running softmax as attention of a chain (kv_attention.hip): levels less their zero are exact in half, scales multiply scores and probabilities,
 //     x[t] = (scale s^K_t log2 e) q.(c^K_t - z^K_t),   p = 2^(x - max),   O += (2^up p s^V_t) (c^V_t - z^V_t)
 // with a power of two per row for its query and one, `up`, by the largest p s among the tokens that the row itself has seen.  fp32 queries are two half terms, and so is
-// 2^up p s, for bf16 queries too (2^-22 of it at most; as one half term 8 trees of up to 64 rows took 142 us, not 147).
+// 2^up p s, for bf16 queries too (2^-22 of it at most).
 #include "kv_attention.h"
 
 namespace {
 
 constexpr float MOST_FLOAT = 0x1.fffffep127f;
 constexpr int HALF_TOP = 14;      // a row's largest probability times scale becomes 2^14 .. 2^15 as half
-constexpr int TILE = 64;
+constexpr int TILE = 64, RW = 16;      // tokens a wavefront takes at a time, its rows
 template <int DP> constexpr int resident() { return DP <= 128 ? 2 : 1; }      // workgroups that a compute unit holds at once (registers)
-constexpr int most_resident = 2;
 
 // How a sequence is cut.  A workgroup's four wavefronts take `wr` blocks of RW rows side by side and 4 / wr tiles of 64 tokens at a time (a step).
 struct Cut { int wr, wt, blocks, first, tiles, steps; };
-template <int RW>
 __device__ __forceinline__ Cut cut_of(const KvSeq& s, const AttendArgs& a) {
     Cut c;
     const int rows = s.n * a.rep;
@@ -31,23 +29,23 @@ __device__ __forceinline__ Cut cut_of(const KvSeq& s, const AttendArgs& a) {
     c.steps = (c.tiles + c.wt - 1) / c.wt;
     return c;
 }
-template <int RW>
 __device__ __forceinline__ long long steps_of(const KvSeq& s, const AttendArgs& a) {
     if (s.n == 0 || s.n * a.rep > a.few) return 0;
-    const Cut c = cut_of<RW>(s, a);
+    const Cut c = cut_of(s, a);
     return (long long)c.blocks * a.g.heads * c.steps;
 }
 __device__ __forceinline__ unsigned below(int n) { return n <= 0 ? 0u : n >= 16 ? 0xffffu : (1u << n) - 1; }      // bits 0 .. n - 1 of 16
 
 // Units (up to 4 RW rows of a sequence's drafted tokens and the heads of a KV group, all places that they see) follow each other as a list of steps, and every workgroup takes an equal share of
-// that list; pieces of units that lie in several shares go to kv_tree_join_kernel.  A wavefront has U times 16 rows: levels are made into half once for all of them.
+// that list; pieces of units that lie in several shares go to kv_tree_join_kernel.
 // S^T = K Q^T with tile i's row 4 g + j of the matrix instruction being token 16 g + 4 i + j: lane group g then holds the probabilities of tokens 16 g .. 16 g + 15 for row lane % 16, which are
 // the right operand of O^T += V^T P^T as they stand.
-// Bound by the vector instructions that make levels into half and the softmax, with too few wavefronts (registers) to hide them: 8 trees of up to 64 tokens behind up to 4000 others, 32 heads of 128, a row a token:
-// 114 us and 10 for the join; the levels take 37 at the rate of memory.
-template <typename T, int DP, int U>
+// Bound by the vector instructions that make levels into half and the softmax: 8 trees of up to 64 tokens behind up to 4000 others, 32 heads of 128, a row a token: 88 us and 10 for the join, where vector
+// instructions are issued 59 % of the time and wavefronts wait 26 % of theirs (the levels take 37 at the rate of memory).  With two units of 16 rows a wavefront, which would make levels into half once for both,
+// registers spill: 121 us, 61 % of the time waiting.
+template <typename T, int DP>
 __global__ __launch_bounds__(256, resident<DP>()) void kv_tree_kernel(AttendArgs a) {
-    constexpr int NT = sizeof(T) == 2 ? 1 : 2, RW = 16 * U;      // half terms of queries; rows of a wavefront
+    constexpr int NT = sizeof(T) == 2 ? 1 : 2;      // half terms of queries
     constexpr int K64 = DP / 64, K32 = (DP % 64) / 32, KS = DP / 32, CT = DP / 16;
     __shared__ float joined[4][RW][DP + 4];
     __shared__ float2 ends[4][RW];
@@ -57,7 +55,7 @@ __global__ __launch_bounds__(256, resident<DP>()) void kv_tree_kernel(AttendArgs
     for (int i = lane; i < a.q.n_seqs; i += 64) {
         const KvSeq e = kv_sequence(a.q, i);
         if (i < 64) head = e;
-        total += steps_of<RW>(e, a);
+        total += steps_of(e, a);
     }
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) total += __shfl_xor(total, o, 64);
@@ -70,8 +68,8 @@ __global__ __launch_bounds__(256, resident<DP>()) void kv_tree_kernel(AttendArgs
         long long x = at;
         int b;
         KvSeq s;
-        if (!kv_find(a.q, head, [&](const KvSeq& e) { return steps_of<RW>(e, a); }, x, b, s)) return;
-        const Cut c = cut_of<RW>(s, a);
+        if (!kv_find(a.q, head, [&](const KvSeq& e) { return steps_of(e, a); }, x, b, s)) return;
+        const Cut c = cut_of(s, a);
         const int step0 = __builtin_amdgcn_readfirstlane((int)(x % c.steps));
         x /= c.steps;
         const int h = __builtin_amdgcn_readfirstlane((int)(x % a.g.heads)), r0 = __builtin_amdgcn_readfirstlane((int)(x / a.g.heads) * (RW * c.wr));
@@ -79,25 +77,18 @@ __global__ __launch_bounds__(256, resident<DP>()) void kv_tree_kernel(AttendArgs
         const int rows = s.n * a.rep, n_rows = min(RW * c.wr, rows - r0);
         const int before = s.len - s.n, end = min(s.len, a.q.room), group = wave / c.wr, rg = wave - group * c.wr;
         const int hi = min((c.first + step1 * c.wt) * TILE, end), stride = c.wt * TILE;
-        // this lane's rows
-        bool live[U];
-        int low[U];
-        const unsigned* mask[U];
-        const T* q[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int r = r0 + rg * RW + u * 16 + col;
-            live[u] = r < rows;
-            const int tok = live[u] ? r / a.rep : 0, hh = live[u] ? r - tok * a.rep : 0;
-            q[u] = (const T*)a.Q + (long long)(s.start + tok) * a.ldq + (long long)(h * a.rep + hh) * a.g.dh;
-            mask[u] = a.tree + (long long)(s.start + tok) * a.tree_words;
-            low[u] = 0;
-            if (a.window) {      // of the places before the new tokens, the last ones of the window that ends at the row's own, which is as far behind them as its mask has bits
-                int bits = 0;
-                for (int i = 0; i < a.tree_words && 32 * i < s.n; ++i) bits += __popc(mask[u][i] & (s.n - 32 * i >= 32 ? ~0u : (1u << (s.n - 32 * i)) - 1));
-                low[u] = before + bits - a.window;
-            }
-            if (before + tok < 0) live[u] = false;
+        // this lane's row
+        const int r = r0 + rg * RW + col;
+        const bool own = r < rows;
+        const int tok = own ? r / a.rep : 0, hh = own ? r - tok * a.rep : 0;
+        const bool live = own && before + tok >= 0;
+        const T* const q = (const T*)a.Q + (long long)(s.start + tok) * a.ldq + (long long)(h * a.rep + hh) * a.g.dh;
+        const unsigned* const mask = a.tree + (long long)(s.start + tok) * a.tree_words;
+        int low = 0;
+        if (a.window) {      // of the places before the new tokens, the last ones of the window that ends at the row's own, which is as far behind them as its mask has bits
+            int bits = 0;
+            for (int i = 0; i < a.tree_words && 32 * i < s.n; ++i) bits += __popc(mask[i] & (s.n - 32 * i >= 32 ? ~0u : (1u << (s.n - 32 * i)) - 1));
+            low = before + bits - a.window;
         }
         const long long head_levels = (long long)h * DP << a.g.pt_log, head_grids = (long long)h << (a.g.pt_log - a.g.st_log);
         const int in_page = (1 << a.g.pt_log) - 1;
@@ -136,10 +127,9 @@ __global__ __launch_bounds__(256, resident<DP>()) void kv_tree_kernel(AttendArgs
             pk_next = page_of(t0 + stride + 16 * (col >> 2)); pv_next = page_of(t0 + stride + 16 * grp);
         }
 
-        h8 qh[U][NT][KS];
-        float unit[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
+        h8 qh[NT][KS];
+        float unit;
+        {
             float v[KS][8], most = 0.f;
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
@@ -147,45 +137,41 @@ __global__ __launch_bounds__(256, resident<DP>()) void kv_tree_kernel(AttendArgs
                 if (a.vec == 4) {
                     union { typename Four<T>::type u[2]; T e[8]; } in;
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) in.u[j] = live[u] && ch + 4 * j < a.g.dh ? *(const typename Four<T>::type*)(q[u] + ch + 4 * j) : typename Four<T>::type{};
+                    for (int j = 0; j < 2; ++j) in.u[j] = live && ch + 4 * j < a.g.dh ? *(const typename Four<T>::type*)(q + ch + 4 * j) : typename Four<T>::type{};
 #pragma unroll
                     for (int j = 0; j < 8; ++j) v[k][j] = to_f32(in.e[j]);
                 } else if (a.vec) {
                     union { u4 u[sizeof(T) / 2]; T e[8]; } in;
 #pragma unroll
-                    for (int j = 0; j < (int)sizeof(T) / 2; ++j) in.u[j] = live[u] && ch < a.g.dh ? ((const u4*)(q[u] + ch))[j] : u4{0, 0, 0, 0};
+                    for (int j = 0; j < (int)sizeof(T) / 2; ++j) in.u[j] = live && ch < a.g.dh ? ((const u4*)(q + ch))[j] : u4{0, 0, 0, 0};
 #pragma unroll
                     for (int j = 0; j < 8; ++j) v[k][j] = to_f32(in.e[j]);
                 } else {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) v[k][j] = live[u] && ch + j < a.g.dh ? to_f32(q[u][ch + j]) : 0.f;
+                    for (int j = 0; j < 8; ++j) v[k][j] = live && ch + j < a.g.dh ? to_f32(q[ch + j]) : 0.f;
                 }
 #pragma unroll
                 for (int j = 0; j < 8; ++j) { const float m = fabsf(v[k][j]); most = m < __builtin_inff() ? fmaxf(most, m) : most; }
             }
             most = fmaxf(most, from_xor<16>(most)); most = fmaxf(most, from_xor<32>(most));      // of the row
             const int e = most > 0.f ? min(14 - __builtin_amdgcn_frexp_expf(most), 100) : 0;
-            unit[u] = __builtin_amdgcn_ldexpf(a.scale2, -e);
+            unit = __builtin_amdgcn_ldexpf(a.scale2, -e);
 #pragma unroll
             for (int k = 0; k < KS; ++k)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     const float w = __builtin_amdgcn_ldexpf(v[k][j], e);
                     const _Float16 hi16 = (_Float16)w;
-                    qh[u][0][k][j] = hi16;
-                    if constexpr (NT == 2) qh[u][1][k][j] = (_Float16)(isfinite(w) ? w - (float)hi16 : 0.f);
+                    qh[0][k][j] = hi16;
+                    if constexpr (NT == 2) qh[1][k][j] = (_Float16)(isfinite(w) ? w - (float)hi16 : 0.f);
                 }
         }
 
-        float m[U], l[U], most_w[U];      // maximum, sum, largest probability times scale
-        int up[U];                        // brings that to 2^14 .. 2^15
-        f4 o[U][CT];
+        float m = -__builtin_inff(), l = 0.f, most_w = 0.f;      // maximum, sum, largest probability times scale
+        int up = HALF_TOP + 1 + 126;                              // brings that to 2^14 .. 2^15
+        f4 o[CT];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            m[u] = -__builtin_inff(); l[u] = 0.f; most_w[u] = 0.f; up[u] = HALF_TOP + 1 + 126;
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct) o[u][ct] = f4{0.f, 0.f, 0.f, 0.f};
-        }
+        for (int ct = 0; ct < CT; ++ct) o[ct] = f4{0.f, 0.f, 0.f, 0.f};
         for (; t0 < hi; t0 += stride) {
             u4 vr[CT];
 #pragma unroll
@@ -193,91 +179,80 @@ __global__ __launch_bounds__(256, resident<DP>()) void kv_tree_kernel(AttendArgs
             const bool there = held;
             const float sk = gk.x, zk = -1024.f - gk.y, gvx = gv.x, zv = -1024.f - gv.y;
             // scores
-            f4 st[U][4];
+            f4 st[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const _Float16 zo = (_Float16)__shfl(zk, 16 * (col >> 2) + 4 * i + (col & 3), 64);
                 const h2 z = {zo, zo};
-#pragma unroll
-                for (int u = 0; u < U; ++u) st[u][i] = f4{0.f, 0.f, 0.f, 0.f};
+                st[i] = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int k = 0; k < KS; ++k) {
                     h8 lv;
                     if (k < 2 * K64) lv = levels8(kr[i][k >> 1][(k & 1) * 2], kr[i][k >> 1][(k & 1) * 2 + 1], z, z, z, z);
                     else lv = levels8(ks[i].x, ks[i].y, z, z, z, z);
 #pragma unroll
-                    for (int u = 0; u < U; ++u)
-#pragma unroll
-                        for (int n = 0; n < NT; ++n) st[u][i] = mma16(lv, qh[u][n][k], st[u][i]);
+                    for (int n = 0; n < NT; ++n) st[i] = mma16(lv, qh[n][k], st[i]);
                 }
             }
-            auto load_next = [&] {
-                if (t0 + stride < hi) {
-                    pk = pk_next; pv = pv_next;
-                    load_k(t0 + stride);
-                    pk_next = page_of(t0 + 2 * stride + 16 * (col >> 2)); pv_next = page_of(t0 + 2 * stride + 16 * grp);
-                }
-            };
-            if constexpr (U == 1) load_next();
+            if (t0 + stride < hi) {
+                pk = pk_next; pv = pv_next;
+                load_k(t0 + stride);
+                pk_next = page_of(t0 + 2 * stride + 16 * (col >> 2)); pv_next = page_of(t0 + 2 * stride + 16 * grp);
+            }
             const bool all = t0 + TILE <= min(before, end) && (!a.window || t0 >= before + s.n - a.window) && __all(there);
-            h8 ph[U][2][2];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if constexpr (U > 1) __builtin_amdgcn_sched_barrier(0);      // (one unit's softmax after the other: mixed they spill registers)
-                float p[16];
-                unroll<16>([&](auto I) { constexpr int i = I; p[i] = st[u][i >> 2][i & 3] * (row_lane<i>(sk) * unit[u]); });
-                unsigned seen = 0xffffu;
-                if (!all) {
-                    const int tv = t0 + 16 * grp, j0 = tv - before;      // places tv .. tv + 15: before the new tokens, or the new tokens from the j0-th on
-                    seen = below(min(before, end) - tv) & ~below(low[u] - tv);
-                    if (j0 > -16 && j0 < s.n) {
-                        auto word = [&](int i) { return i >= 0 && i < a.tree_words ? mask[u][i] : 0u; };
-                        const unsigned long long bits = word(j0 >> 5) | (unsigned long long)word((j0 >> 5) + 1) << 32;
-                        seen |= (unsigned)(bits >> (j0 & 31)) & below(end - tv) & ~below(-j0);
-                    }
-                    if (!live[u] || !there) seen = 0;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) if (!(seen >> i & 1)) p[i] = -__builtin_inff();
+            h8 ph[2][2];
+            float p[16];
+            unroll<16>([&](auto I) { constexpr int i = I; p[i] = st[i >> 2][i & 3] * (row_lane<i>(sk) * unit); });
+            unsigned seen = 0xffffu;
+            if (!all) {
+                const int tv = t0 + 16 * grp, j0 = tv - before;      // places tv .. tv + 15: before the new tokens, or the new tokens from the j0-th on
+                seen = below(min(before, end) - tv) & ~below(low - tv);
+                if (j0 > -16 && j0 < s.n) {
+                    auto word = [&](int i) { return i >= 0 && i < a.tree_words ? mask[i] : 0u; };
+                    const unsigned long long bits = word(j0 >> 5) | (unsigned long long)word((j0 >> 5) + 1) << 32;
+                    seen |= (unsigned)(bits >> (j0 & 31)) & below(end - tv) & ~below(-j0);
                 }
-                float top = p[0];
+                if (!live || !there) seen = 0;
 #pragma unroll
-                for (int i = 1; i < 16; ++i) top = fmaxf(top, p[i]);
-                top = fmaxf(top, from_xor<16>(top)); top = fmaxf(top, from_xor<32>(top));
-                const float m_new = fmaxf(m[u], top), base = m_new == -__builtin_inff() ? 0.f : m_new;
-                float turn = ex2(m[u] - base);
-                m[u] = m_new;
-                l[u] *= turn;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) { p[i] = ex2(p[i] - base); l[u] += p[i]; }
-                unroll<16>([&](auto I) { constexpr int i = I; p[i] *= row_lane<i>(gvx); });
-                if (!all) {      // whatever their scale is
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) if (!(seen >> i & 1)) p[i] = 0.f;
-                }
-                float w_top = p[0];
-#pragma unroll
-                for (int i = 1; i < 16; ++i) w_top = fmaxf(w_top, p[i]);
-                w_top = fmaxf(w_top, from_xor<16>(w_top)); w_top = fmaxf(w_top, from_xor<32>(w_top));
-                most_w[u] = fmaxf(most_w[u] * turn, fminf(w_top, MOST_FLOAT));
-                const int up_was = up[u];
-                up[u] = HALF_TOP + 1 - (most_w[u] > 0.f ? max(__builtin_amdgcn_frexp_expf(most_w[u]), -126) : -126);
-                turn = __builtin_amdgcn_ldexpf(turn, up[u] - up_was);      // (up rises only as most_w falls with turn, to nothing at last: 2 at most)
-                if (__any(turn != 1.f)) {
-#pragma unroll
-                    for (int ct = 0; ct < CT; ++ct) o[u][ct] *= turn;
-                }
-#pragma unroll
-                for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_ldexpf(p[i], up[u]);
-#pragma unroll
-                for (int k = 0; k < 2; ++k)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const _Float16 w = (_Float16)p[8 * k + j];
-                        ph[u][0][k][j] = w;
-                        ph[u][1][k][j] = (_Float16)(p[8 * k + j] - (float)w);
-                    }
+                for (int i = 0; i < 16; ++i) if (!(seen >> i & 1)) p[i] = -__builtin_inff();
             }
-            if constexpr (U > 1) { __builtin_amdgcn_sched_barrier(0); load_next(); }      // (beside the softmax of two units there are no registers for it)
+            float top = p[0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) top = fmaxf(top, p[i]);
+            top = fmaxf(top, from_xor<16>(top)); top = fmaxf(top, from_xor<32>(top));
+            const float m_new = fmaxf(m, top), base = m_new == -__builtin_inff() ? 0.f : m_new;
+            float turn = ex2(m - base);
+            m = m_new;
+            l *= turn;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) { p[i] = ex2(p[i] - base); l += p[i]; }
+            unroll<16>([&](auto I) { constexpr int i = I; p[i] *= row_lane<i>(gvx); });
+            if (!all) {      // whatever their scale is
+#pragma unroll
+                for (int i = 0; i < 16; ++i) if (!(seen >> i & 1)) p[i] = 0.f;
+            }
+            float w_top = p[0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) w_top = fmaxf(w_top, p[i]);
+            w_top = fmaxf(w_top, from_xor<16>(w_top)); w_top = fmaxf(w_top, from_xor<32>(w_top));
+            most_w = fmaxf(most_w * turn, fminf(w_top, MOST_FLOAT));
+            const int up_was = up;
+            up = HALF_TOP + 1 - (most_w > 0.f ? max(__builtin_amdgcn_frexp_expf(most_w), -126) : -126);
+            turn = __builtin_amdgcn_ldexpf(turn, up - up_was);      // (up rises only as most_w falls with turn, to nothing at last: 2 at most)
+            if (__any(turn != 1.f)) {
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) o[ct] *= turn;
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_ldexpf(p[i], up);
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const _Float16 w = (_Float16)p[8 * k + j];
+                    ph[0][k][j] = w;
+                    ph[1][k][j] = (_Float16)(p[8 * k + j] - (float)w);
+                }
             // zeros of V's 16 tokens as pairs
             h2 zo[8];
             {
@@ -289,32 +264,23 @@ __global__ __launch_bounds__(256, resident<DP>()) void kv_tree_kernel(AttendArgs
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) {
                 const h8 v0 = levels8(vr[ct][0], vr[ct][1], zo[0], zo[1], zo[2], zo[3]), v1 = levels8(vr[ct][2], vr[ct][3], zo[4], zo[5], zo[6], zo[7]);
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    o[u][ct] = mma16(v0, ph[u][0][0], o[u][ct]); o[u][ct] = mma16(v1, ph[u][0][1], o[u][ct]);
-                    o[u][ct] = mma16(v0, ph[u][1][0], o[u][ct]); o[u][ct] = mma16(v1, ph[u][1][1], o[u][ct]);
-                }
+                o[ct] = mma16(v0, ph[0][0], o[ct]); o[ct] = mma16(v1, ph[0][1], o[ct]);
+                o[ct] = mma16(v0, ph[1][0], o[ct]); o[ct] = mma16(v1, ph[1][1], o[ct]);
             }
         }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            l[u] += from_xor<16>(l[u]); l[u] += from_xor<32>(l[u]);
-            if (l[u] != l[u]) m[u] = fmaxf(m[u], 0.f);      // scores that are all NaN leave the maximum where it was: the row has seen something
-            if (grp == 0) ends[wave][u * 16 + col] = make_float2(m[u], l[u]);
-        }
+        l += from_xor<16>(l); l += from_xor<32>(l);
+        if (l != l) m = fmaxf(m, 0.f);      // scores that are all NaN leave the maximum where it was: the row has seen something
+        if (grp == 0) ends[wave][col] = make_float2(m, l);
         __syncthreads();
         const bool whole = step0 == 0 && step1 == c.steps;
         const long long piece = (2LL * blockIdx.x + (step0 == 0)) * a.piece_rows;
+        float top = -__builtin_inff(), sum = 0.f;
+        for (int w = rg; w < 4; w += c.wr) top = fmaxf(top, ends[w][col].x);
+        for (int w = rg; w < 4; w += c.wr) if (ends[w][col].x != -__builtin_inff()) sum += ends[w][col].y * ex2(ends[w][col].x - top);
+        const float f = m == -__builtin_inff() ? 0.f : ex2(m - top) / sum;      // (averages from here on: weighted sums of the largest values leave fp32)
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            float top = -__builtin_inff(), sum = 0.f;
-            for (int w = rg; w < 4; w += c.wr) top = fmaxf(top, ends[w][u * 16 + col].x);
-            for (int w = rg; w < 4; w += c.wr) if (ends[w][u * 16 + col].x != -__builtin_inff()) sum += ends[w][u * 16 + col].y * ex2(ends[w][u * 16 + col].x - top);
-            const float f = m[u] == -__builtin_inff() ? 0.f : ex2(m[u] - top) / sum;      // (averages from here on: weighted sums of the largest values leave fp32)
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct) *(f4*)&joined[wave][u * 16 + col][ct * 16 + grp * 4] = m[u] == -__builtin_inff() ? f4{0.f, 0.f, 0.f, 0.f} : by_power(o[u][ct] * f, -up[u]);
-            if (!whole && grp == 0 && group == 0 && rg * RW + u * 16 + col < n_rows) a.stat[piece + rg * RW + u * 16 + col] = make_float2(top, sum);
-        }
+        for (int ct = 0; ct < CT; ++ct) *(f4*)&joined[wave][col][ct * 16 + grp * 4] = m == -__builtin_inff() ? f4{0.f, 0.f, 0.f, 0.f} : by_power(o[ct] * f, -up);
+        if (!whole && grp == 0 && group == 0 && rg * RW + col < n_rows) a.stat[piece + rg * RW + col] = make_float2(top, sum);
         __syncthreads();
         if (threadIdx.x == 0 && step0 == 0 && !whole) a.info[blockIdx.x] = make_int4((int)((at + c.steps - 1) / share) - (int)blockIdx.x + 1, s.start, r0 / 16 | (n_rows - 1) << 23, h);
         for (int i = threadIdx.x; i < n_rows * (DP / 4); i += 256) {
@@ -379,13 +345,13 @@ __global__ __launch_bounds__(256) void kv_tree_join_kernel(AttendArgs a) {
     }
 }
 
-// 16-row units of a wavefront: two for bf16 heads of up to 128 channels (registers), one where no sequence has more than 16 rows
-int wave_units(const KvGeometry& g, int dtype, long long rows) { return dtype == TBOA_BF16 && g.dp <= 128 && rows > 16 ? 2 : 1; }
-int piece_rows(int units, long long rows) { const int rw = 16 * units; return rows <= rw ? rw : rows <= 2 * rw ? 2 * rw : 4 * rw; }
+int piece_rows(long long rows) { return rows <= RW ? RW : rows <= 2 * RW ? 2 * RW : 4 * RW; }
 int shares(const KvGeometry& g) { return 256 * (g.dp <= 128 ? 2 : 1); }
-// Rows of a bf16 sequence up to which it is this kernel's; with more the kernel for many rows of kv_attention.hip takes it, whose eight wavefronts share the levels that it makes into half.
-// Both kernels, joins included, 64 / 8 heads of 128: one tree of 16 tokens (128 rows) behind 500 others 35 us here and 27 there, 16 trees of up to 32 behind up to 8000 337 and 219.
-constexpr int FEW = 64;
+// Rows of a bf16 sequence up to which it is this kernel's; with more the kernel for many rows of kv_attention.hip takes it, whose eight wavefronts share the levels that it makes into half.  Both, joins and
+// launches included, us, this one and the one for many rows:
+//     one tree behind 8000, 64 / 8 heads of 128: 128 rows 44 73, 256 52 124, 512 73 93, 1024 133 110, 2048 229 143;   16 of up to: 128 148 192, 256 229 214, 512 411 471;   8 behind 4000 of up to 2048: 496 428
+//     16 trees behind 4000, 16 heads of 64: 100 rows 104 196, 128 114 196;   4 of up to 1000 behind 1000: 145 176;   4 behind 4000, 16 / 2 heads of 256: 256 rows 54 82
+constexpr int FEW = 512;
 size_t room(const KvGeometry& g, int rows_of_piece, bool tiles, AttendArgs* a, void* ws) {
     const size_t n = (size_t)shares(g);
     Arena ar(ws);
@@ -396,28 +362,23 @@ size_t room(const KvGeometry& g, int rows_of_piece, bool tiles, AttendArgs* a, v
     return ar.off + (tiles ? kv_tree_tiles_room(g, a, a ? (char*)ws + ar.off : nullptr) : 0);
 }
 
-template <typename T, int DP, int U>
-int launch(tboa_ctx* ctx, const AttendArgs& a) {
-    hipLaunchKernelGGL((kv_tree_kernel<T, DP, U>), dim3(256 * resident<DP>()), dim3(256), 0, ctx->stream, a);
+template <typename T, int DP>
+int launch_heads(tboa_ctx* ctx, const AttendArgs& a) {
+    hipLaunchKernelGGL((kv_tree_kernel<T, DP>), dim3(256 * resident<DP>()), dim3(256), 0, ctx->stream, a);
     TB_KERNEL_CHECK(ctx);
     hipLaunchKernelGGL((kv_tree_join_kernel<T, DP>), dim3(256 * resident<DP>(), std::min(a.piece_rows / 4, 16)), dim3(256), 0, ctx->stream, a);
     TB_KERNEL_CHECK(ctx);
     return 0;
 }
-template <typename T, int DP>
-int launch(tboa_ctx* ctx, const AttendArgs& a, int units) {
-    if constexpr (sizeof(T) == 2 && DP <= 128) { if (units == 2) return launch<T, DP, 2>(ctx, a); }
-    return launch<T, DP, 1>(ctx, a);
-}
 template <typename T>
-int launch(tboa_ctx* ctx, const AttendArgs& a, int units) {
+int launch(tboa_ctx* ctx, const AttendArgs& a) {
     switch (a.g.dp) {
-        case 32: return launch<T, 32>(ctx, a, units);
-        case 64: return launch<T, 64>(ctx, a, units);
-        case 96: return launch<T, 96>(ctx, a, units);
-        case 128: return launch<T, 128>(ctx, a, units);
-        case 192: return launch<T, 192>(ctx, a, units);
-        default: return launch<T, 256>(ctx, a, units);
+        case 32: return launch_heads<T, 32>(ctx, a);
+        case 64: return launch_heads<T, 64>(ctx, a);
+        case 96: return launch_heads<T, 96>(ctx, a);
+        case 128: return launch_heads<T, 128>(ctx, a);
+        case 192: return launch_heads<T, 192>(ctx, a);
+        default: return launch_heads<T, 256>(ctx, a);
     }
 }
 
@@ -428,7 +389,7 @@ extern "C" size_t tboa_kv_cache_tree_attention_workspace_bytes(const tboa_kv_cac
     if (!kv_geometry(desc, g) || n_q_heads <= 0 || n_q_heads > 65535 || n_q_heads % g.heads || n_seqs < 0 || n_seqs > 1 << 20 || n_tokens < 0 || n_tokens > 1 << 24) return 0;
     if (n_seqs == 0 || n_tokens == 0) return 0;
     const long long rows = n_tokens * (n_q_heads / g.heads);
-    return std::max(room(g, piece_rows(wave_units(g, TBOA_F32, rows), rows), false, nullptr, nullptr), room(g, piece_rows(wave_units(g, TBOA_BF16, rows), rows), rows > FEW, nullptr, nullptr));
+    return room(g, piece_rows(rows), rows > FEW, nullptr, nullptr);      // (fp32: without the second part)
 }
 
 extern "C" int tboa_kv_cache_tree_attention(tboa_ctx* ctx, const tboa_kv_cache_desc* desc, const tboa_kv_batch* batch, int n_q_heads, int dtype, const void* Q, int64_t ldq,
@@ -449,7 +410,7 @@ extern "C" int tboa_kv_cache_tree_attention(tboa_ctx* ctx, const tboa_kv_cache_d
     if (batch->n_tokens * rep >= 1LL << 27) return tboa_fail(ctx, TBOA_EINVAL, "kv_cache_tree_attention: too many rows");
     KvDevice dev(ctx->device);
     const long long rows = (batch->max_new > 0 ? std::min<long long>(batch->max_new, batch->n_tokens) : batch->n_tokens) * rep;
-    const int units = wave_units(g, dtype, rows), of_piece = piece_rows(units, rows);
+    const int of_piece = piece_rows(rows);
     const bool tiles = dtype == TBOA_BF16 && rows > FEW && kv_tree_tiles_takes(g, batch->n_seqs, batch->n_tokens, rep);
     TB_TRY(tboa_ws_reserve(ctx, room(g, of_piece, tiles, nullptr, nullptr)));
     AttendArgs a{};
@@ -466,5 +427,5 @@ extern "C" int tboa_kv_cache_tree_attention(tboa_ctx* ctx, const tboa_kv_cache_d
     room(g, of_piece, tiles, &a, ctx->ws);
     if (tiles) TB_TRY(kv_tree_tiles(ctx, a));
     if (all) return 0;
-    return dtype == TBOA_F32 ? launch<float>(ctx, a, units) : launch<bf16>(ctx, a, units);
+    return dtype == TBOA_F32 ? launch<float>(ctx, a) : launch<bf16>(ctx, a);
 }
