@@ -218,7 +218,7 @@ constexpr int most_waves() { return XR <= 16 && NR == 1 ? 16 : 8; }
 //     y += scale (sum (offset + code) x - (offset + zero) sum x)      (all of it times 2^-DOWN)
 // fp32 X: codes less zeros, exact in bf16, times three bf16 terms.
 // Rows of codes, of X and of scales are read by four lanes side by side, 64 bytes together, and handed to the lanes that multiply them through the wavefront's own part of LDS: read by those lanes
-// themselves, a row each, every 16 bytes are an access of their own to the first cache (16 tokens of 8192 x 28672: 37 million accesses, 143000 cycles of every compute unit's, 67 us and not 34).
+// themselves, a row each, every 16 bytes are an access of their own to the first cache (16 tokens of 8192 x 28672: 37 million accesses, not 9.7; 67 us and not 34, the same weights again and again, 42.6 from memory).
 template <typename T, int BITS, int VW, int FF, int XR, int RT, bool GATED>
 __global__ __launch_bounds__((64 * most_waves<XR, (GATED ? 2 : 1) * RT>())) void packed_few_kernel(PackedArgs a) {
     typedef Codes<BITS, VW> C;
@@ -704,8 +704,9 @@ __device__ __forceinline__ void put4(const PackedArgs& p, long long m, int n, f4
 
 // A tile of TM tokens and 256 rows of codes (GATED: 128 of either matrix, 32 of one beside 32 of the other, so that a wavefront has both factors of its results); eight wavefronts, each TM / 2 tokens and 64 rows.
 // A ring of NS stages of 32 channels in LDS: X is copied there, NS - 1 stages ahead; codes are loaded two stages before that, made into half and written by all wavefronts, 16 codes a lane and stage.
-// Bound by the matrix instructions and, half as long again, the vector instructions that make codes into half beside them: 4096 tokens of 10240 x 8192, four bits, 677 us (1015 TFLOP/s).  Each wavefront
-// making the codes of its own 64 rows 730 - 759 us, codes copied into LDS and made into half once for all 775.
+// Bound by the matrix instructions and the vector instructions that make codes into half beside them: 4096 tokens of 10240 x 8192, four bits in groups of 128, 651 us (1055 TFLOP/s), the matrix cores busy 51 %
+// of the cycles and vector instructions issued in 48 %, at 1.85 GHz.  An earlier form, 677 us, against each wavefront making the codes of its own 64 rows 730 - 759, codes copied into LDS and made into half once
+// for all 775.
 // GRIDS_OF: 0: one scale a row; 1: groups of whole 128 channels, which begin where the ring does; 2: of whole 16, the depth of a matrix instruction, whose scales go through LDS.
 template <int BITS, int GRIDS_OF, int TM, bool GATED>
 __global__ __launch_bounds__(512) void packed_many_kernel(ManyArgs a) {
