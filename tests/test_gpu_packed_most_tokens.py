@@ -33,3 +33,33 @@ def test_more_than_one_round(lib, d_out, d_in, bits, group, tokens, dtype):
             own.close()
     finally:
         ctx.close()
+
+
+def test_captured_with_what_is_said_to_be_needed(lib):
+    """Several rounds in one graph, with the workspace that the query tells and no more; and a batch of fewer tokens, whose tiles are split, in another graph on the same workspace."""
+    stream = torch.cuda.Stream()
+    ctx = lib.Context(stream=stream)
+    try:
+        with torch.cuda.stream(stream):
+            (gate, _), (up, _) = ref.weight(lib, ctx, 2048, 1024, 4, 128, 61), ref.weight(lib, ctx, 2048, 1024, 4, 128, 62)
+            sizes = (8192 + 2048, 2048)
+            ctx.reserve_workspace(ctx.packed_workspace_bytes(gate, sizes[0], torch.bfloat16))
+            held = ctx.workspace_bytes()
+            calls = []
+            for tokens in sizes:
+                x, act = rows(tokens, 1024, torch.bfloat16, 63), torch.empty(tokens, 2048, dtype=torch.bfloat16, device="cuda")
+                g = torch.cuda.CUDAGraph()
+                with torch.cuda.graph(g, stream=stream):
+                    ctx.packed_swiglu(gate, up, x, out=act)
+                calls.append((g, x, act))
+            for k in range(3):
+                for g, x, act in calls:
+                    x.copy_(rows(len(x), 1024, torch.bfloat16, 70 + k))
+                    want = ctx.packed_swiglu(gate, up, x).clone()
+                    act.fill_(7)
+                    g.replay()
+                    stream.synchronize()
+                    assert torch.equal(act, want), (k, len(x))
+            assert ctx.workspace_bytes() == held
+    finally:
+        ctx.close()
